@@ -86,7 +86,9 @@ typedef enum hg_dtype { HG_DTYPE_F16 = 0, HG_DTYPE_BF16 = 1 } hg_dtype;
 #define HG_DEV_BAD_PAGE 2     /* a block-table entry of a resident page was outside [0, num_pages): the page was not
                                  read and its tokens were left out of the partial, as if they were not resident */
 #define HG_DEV_RANGE 4        /* a slice reached past max_pages * page_size tokens, the end of its block-table row:
-                                 it was cut there (the partials cover [tok_begin, max_pages * page_size)) */
+                                 it was cut there (the partials cover [tok_begin, max_pages * page_size)).  Of the
+                                 page operations: a row number or a position outside the block table */
+#define HG_DEV_NO_PAGE 8      /* hg_kv_reserve ran out of free pages (n_ready says what it could serve) */
 
 /*
  * Problem description (host struct).
@@ -405,6 +407,57 @@ hg_status hg_kv_evict_copy(const void* k_cache, const void* v_cache, const int32
                            int32_t max_evict, void* k_out, void* v_out, void* stream, const hg_attn_desc* desc);
 hg_status hg_kv_evict_finish(const int32_t* src_begin, const int32_t* n_moved, int32_t* freed_pages, int32_t* n_freed,
                              int32_t max_freed, void* stream, const hg_attn_desc* desc);
+
+/*
+ * Page management: block-table rows that share pages.
+ *
+ * Section 4.8's paged cache with residency metadata needs somebody to hand out pages, and sequences that branch (beams,
+ * parallel samples, requests with a common prompt) should hold their common tokens once.  The state is one array,
+ *     ref_count  dev int32 [num_pages], 16-byte aligned: how many block-table entries (and other holders of the
+ *                caller's) use the page; 0 = free.
+ * All zero for a pool nobody uses yet; a caller who fills block tables by itself counts its entries.  Free pages are
+ * handed out lowest id first; every result depends on the arguments alone.  All calls work on desc->block_table (not
+ * NULL, updated in place) and are ordered by the stream like everything else; contents move only in hg_kv_copy_pages,
+ * which a caller with one table for several layers' pools calls once per layer.  Chunk fields of desc are unused.
+ *
+ *   hg_kv_fork      row b takes the pages of the row src_row[b] (dev int32 [B]), all rows at once as they were before
+ *                   the call: src_row[b] = b leaves the row alone, a negative one frees it (entries -1, lengths 0).
+ *                   Several rows may take the same one, and rows may take each other's (a beam step).  seq_lens,
+ *                   tok_begin and tok_end (the last two may be NULL) move with the rows; counts follow the entries.
+ *                   A value of B or more leaves the row alone and sets HG_DEV_RANGE.  Batches up to 40960.
+ *   hg_kv_reserve   makes positions [seq_lens[b], seq_lens[b] + n_new[b]) of every row writable (n_new: dev int32 [B],
+ *                   or NULL for one each; 0 or less: nothing): a slot without a page gets one, a page that others use
+ *                   too is replaced by a page of the row's own (copy on write).  Sequences are served as if one after
+ *                   the other, their slots in order; so of the rows that share a page and all write it, the last keeps
+ *                   it.  copy_src[b] / copy_dst[b] (dev int32 [B]): the page whose first copy_rows[b] token rows
+ *                   (copy_rows may be NULL) have to be copied before the sequence is read or appended to, or -1 - the
+ *                   list hg_kv_copy_pages takes.  n_ready[b] (may be NULL): how many of the n_new[b] positions are
+ *                   writable; fewer where the pool ran out of pages (HG_DEV_NO_PAGE; the slot stays as it was), where
+ *                   the block-table row ends (HG_DEV_RANGE) or meets an entry outside the pool (HG_DEV_BAD_PAGE), and
+ *                   beyond 262144 slots in one call.  Append no more than that.  Batches up to 16384.
+ *   hg_kv_release   takes one reference off every page of a list (dev int32 [n]; negative entries are skipped) whose
+ *                   block-table entries are gone already - the list hg_kv_evict leaves in freed_pages.  A page listed
+ *                   more often than it is held keeps the count 0 and sets HG_DEV_BAD_PAGE.
+ *   hg_kv_compact   moves the pages in use to the low end of the pool: with U pages in use, the k-th lowest free page
+ *                   below U takes the contents of the k-th highest page from U on, for at most max_moves pairs.  Counts
+ *                   and block table are renamed at once; the pairs are left in move_src / move_dst (dev int32
+ *                   [max_moves], -1 beyond), their number in *n_moves (dev), and remap[num_pages] (dev) holds every
+ *                   page's new id.  Before anything else reads the pool, pass the pairs to hg_kv_copy_pages.
+ *   hg_kv_copy_pages  copies token rows [0, rows[i]) (rows: dev int32 [n], NULL = whole pages) of page src[i] to page
+ *                   dst[i], all heads, K and V, for i < n and, where n_dev (dev) is given, i < *n_dev.  Pairs with a
+ *                   negative id are skipped, ids outside the pool too (HG_DEV_BAD_PAGE).  The pairs are copied side by
+ *                   side: no page may be a dst twice, or a dst and a src (the lists above never do that).
+ * n of hg_kv_release and hg_kv_copy_pages may be 0.
+ */
+hg_status hg_kv_fork(const int32_t* src_row, int32_t* ref_count, int32_t* seq_lens, int32_t* tok_begin, int32_t* tok_end,
+                     void* stream, const hg_attn_desc* desc);
+hg_status hg_kv_reserve(const int32_t* seq_lens, const int32_t* n_new, int32_t* ref_count, int32_t* copy_src, int32_t* copy_dst,
+                        int32_t* copy_rows, int32_t* n_ready, void* stream, const hg_attn_desc* desc);
+hg_status hg_kv_release(const int32_t* page_ids, int32_t n, int32_t* ref_count, void* stream, const hg_attn_desc* desc);
+hg_status hg_kv_compact(int32_t* ref_count, int32_t* remap, int32_t* move_src, int32_t* move_dst, int32_t max_moves,
+                        int32_t* n_moves, void* stream, const hg_attn_desc* desc);
+hg_status hg_kv_copy_pages(const int32_t* src, const int32_t* dst, const int32_t* rows, int32_t n, const int32_t* n_dev,
+                           void* k_cache, void* v_cache, void* stream, const hg_attn_desc* desc);
 
 /*
  * Evidence kernel, not part of the attention path: streams the same K and V tiles through the

@@ -30,5 +30,14 @@ from .binding import (  # noqa: F401
     hg_kv_evict_begin,
     hg_kv_evict_copy,
     hg_kv_evict_finish,
+    hg_kv_fork,
+    hg_kv_reserve,
+    hg_kv_release,
+    hg_kv_compact,
+    hg_kv_copy_pages,
+    prepare_kv_fork,
+    prepare_kv_reserve,
+    prepare_kv_compact,
+    prepare_kv_copy_pages,
     hg_version,
 )

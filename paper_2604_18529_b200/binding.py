@@ -19,7 +19,7 @@ _lib = None
 
 HG_OK, HG_ERR_INVALID_ARG, HG_ERR_UNSUPPORTED, HG_ERR_CUDA, HG_ERR_WORKSPACE = 0, 1, 2, 3, 4
 HG_DTYPE_F16, HG_DTYPE_BF16 = 0, 1
-HG_DEV_OK, HG_DEV_WAIT_TIMEOUT, HG_DEV_BAD_PAGE, HG_DEV_RANGE = 0, 1, 2, 4
+HG_DEV_OK, HG_DEV_WAIT_TIMEOUT, HG_DEV_BAD_PAGE, HG_DEV_RANGE, HG_DEV_NO_PAGE = 0, 1, 2, 4, 8
 HG_MAX_MERGE_SRC = 8
 HG_FLAG_TEST_STALL = 1
 HG_FLAG_SPARSE_EMPTY = 2
@@ -122,6 +122,16 @@ def lib():
         L.hg_kv_evict_copy.restype = C.c_int
         L.hg_kv_evict_finish.argtypes = [vp, vp, vp, vp, i32, vp, C.POINTER(HgAttnDesc)]
         L.hg_kv_evict_finish.restype = C.c_int
+        L.hg_kv_fork.argtypes = [vp] * 6 + [C.POINTER(HgAttnDesc)]
+        L.hg_kv_fork.restype = C.c_int
+        L.hg_kv_reserve.argtypes = [vp] * 8 + [C.POINTER(HgAttnDesc)]
+        L.hg_kv_reserve.restype = C.c_int
+        L.hg_kv_release.argtypes = [vp, i32, vp, vp, C.POINTER(HgAttnDesc)]
+        L.hg_kv_release.restype = C.c_int
+        L.hg_kv_compact.argtypes = [vp] * 4 + [i32, vp, vp, C.POINTER(HgAttnDesc)]
+        L.hg_kv_compact.restype = C.c_int
+        L.hg_kv_copy_pages.argtypes = [vp] * 3 + [i32] + [vp] * 4 + [C.POINTER(HgAttnDesc)]
+        L.hg_kv_copy_pages.restype = C.c_int
         L.hg_kv_read_probe.argtypes = [vp] * 7 + [C.POINTER(HgAttnDesc)]
         L.hg_kv_read_probe.restype = C.c_int
         L.hg_status_string.argtypes = [C.c_int]
@@ -408,6 +418,111 @@ def hg_kv_evict_finish(src_begin, n_moved, freed_pages, n_freed, desc: HgAttnDes
                                   _dev(freed_pages, "freed_pages", torch.int32), _dev(n_freed, "n_freed", torch.int32),
                                   0 if freed_pages is None else freed_pages.shape[1], _stream(stream), C.byref(desc))
     _check(st, "hg_kv_evict_finish")
+
+
+def _here(t: Optional[torch.Tensor], name: str, dtype=None, numel: int = 0) -> Optional[int]:
+    """``_dev`` for a tensor that must also live on the current device (where the call is launched) and hold at least
+    ``numel`` elements."""
+    p = _dev(t, name, dtype)
+    if t is not None and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if t is not None and t.numel() < numel:
+        raise ValueError(f"{name} has {t.numel()} elements, {numel} are needed")
+    return p
+
+
+def _pool(t: torch.Tensor, name: str) -> int:
+    """A KV pool, or a view of one: addressed through the description's strides, so it need not be contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return t.data_ptr()
+
+
+def _kv_fork_args(src_row, ref_count, seq_lens, tok_begin, tok_end, desc: HgAttnDesc, stream):
+    B = desc.batch
+    return (_here(src_row, "src_row", torch.int32, B), _here(ref_count, "ref_count", torch.int32, desc.num_pages),
+            _here(seq_lens, "seq_lens", torch.int32, B), _here(tok_begin, "tok_begin", torch.int32, B),
+            _here(tok_end, "tok_end", torch.int32, B), _stream(stream), C.byref(desc))
+
+
+def hg_kv_fork(src_row, ref_count, seq_lens, tok_begin, tok_end, desc: HgAttnDesc, stream=None) -> None:
+    """Row b of the block table takes the pages (and lengths) of row src_row[b], all rows at once; negative frees it."""
+    _check(lib().hg_kv_fork(*_kv_fork_args(src_row, ref_count, seq_lens, tok_begin, tok_end, desc, stream)), "hg_kv_fork")
+
+
+def prepare_kv_fork(src_row, ref_count, seq_lens, tok_begin, tok_end, desc: HgAttnDesc, stream=None):
+    """``hg_kv_fork`` with its arguments marshalled once (see ``prepare_partial``)."""
+    return _prepared(lib().hg_kv_fork, _kv_fork_args(src_row, ref_count, seq_lens, tok_begin, tok_end, desc, stream),
+                     (src_row, ref_count, seq_lens, tok_begin, tok_end, desc), "hg_kv_fork")
+
+
+def _kv_reserve_args(seq_lens, n_new, ref_count, copy_src, copy_dst, copy_rows, n_ready, desc: HgAttnDesc, stream):
+    B = desc.batch
+    return (_here(seq_lens, "seq_lens", torch.int32, B), _here(n_new, "n_new", torch.int32, B),
+            _here(ref_count, "ref_count", torch.int32, desc.num_pages), _here(copy_src, "copy_src", torch.int32, B),
+            _here(copy_dst, "copy_dst", torch.int32, B), _here(copy_rows, "copy_rows", torch.int32, B),
+            _here(n_ready, "n_ready", torch.int32, B), _stream(stream), C.byref(desc))
+
+
+def hg_kv_reserve(seq_lens, n_new, ref_count, copy_src, copy_dst, copy_rows, n_ready, desc: HgAttnDesc, stream=None) -> None:
+    """Pages for the next n_new[b] positions of every row; shared pages are replaced (the copies to make are listed in
+    copy_src / copy_dst / copy_rows, for ``hg_kv_copy_pages``)."""
+    _check(lib().hg_kv_reserve(*_kv_reserve_args(seq_lens, n_new, ref_count, copy_src, copy_dst, copy_rows, n_ready, desc, stream)),
+           "hg_kv_reserve")
+
+
+def prepare_kv_reserve(seq_lens, n_new, ref_count, copy_src, copy_dst, copy_rows, n_ready, desc: HgAttnDesc, stream=None):
+    """``hg_kv_reserve`` with its arguments marshalled once (see ``prepare_partial``)."""
+    return _prepared(lib().hg_kv_reserve,
+                     _kv_reserve_args(seq_lens, n_new, ref_count, copy_src, copy_dst, copy_rows, n_ready, desc, stream),
+                     (seq_lens, n_new, ref_count, copy_src, copy_dst, copy_rows, n_ready, desc), "hg_kv_reserve")
+
+
+def hg_kv_release(page_ids, ref_count, desc: HgAttnDesc, stream=None) -> None:
+    """One reference less for every page id of the list (negative ones are skipped), as ``hg_kv_evict`` leaves it."""
+    _check(lib().hg_kv_release(_here(page_ids, "page_ids", torch.int32), page_ids.numel(),
+                               _here(ref_count, "ref_count", torch.int32, desc.num_pages), _stream(stream), C.byref(desc)),
+           "hg_kv_release")
+
+
+def _kv_compact_args(ref_count, remap, move_src, move_dst, n_moves, desc: HgAttnDesc, stream):
+    n = move_src.numel()
+    return (_here(ref_count, "ref_count", torch.int32, desc.num_pages), _here(remap, "remap", torch.int32, desc.num_pages),
+            _here(move_src, "move_src", torch.int32), _here(move_dst, "move_dst", torch.int32, n), n,
+            _here(n_moves, "n_moves", torch.int32, 1), _stream(stream), C.byref(desc))
+
+
+def hg_kv_compact(ref_count, remap, move_src, move_dst, n_moves, desc: HgAttnDesc, stream=None) -> None:
+    """Renames the pages in use to the low end of the pool (at most move_src.numel() of them); the moves to make are
+    listed in move_src / move_dst, for ``hg_kv_copy_pages``."""
+    _check(lib().hg_kv_compact(*_kv_compact_args(ref_count, remap, move_src, move_dst, n_moves, desc, stream)), "hg_kv_compact")
+
+
+def prepare_kv_compact(ref_count, remap, move_src, move_dst, n_moves, desc: HgAttnDesc, stream=None):
+    """``hg_kv_compact`` with its arguments marshalled once (see ``prepare_partial``)."""
+    return _prepared(lib().hg_kv_compact, _kv_compact_args(ref_count, remap, move_src, move_dst, n_moves, desc, stream),
+                     (ref_count, remap, move_src, move_dst, n_moves, desc), "hg_kv_compact")
+
+
+def _kv_copy_pages_args(src, dst, rows, n_pairs, k_cache, v_cache, desc: HgAttnDesc, stream):
+    n = src.numel()
+    return (_here(src, "src", torch.int32), _here(dst, "dst", torch.int32, n), _here(rows, "rows", torch.int32, n), n,
+            _here(n_pairs, "n_pairs", torch.int32, 1), _pool(k_cache, "k_cache"), _pool(v_cache, "v_cache"), _stream(stream),
+            C.byref(desc))
+
+
+def hg_kv_copy_pages(src, dst, rows, n_pairs, k_cache, v_cache, desc: HgAttnDesc, stream=None) -> None:
+    """Copies the first rows[i] token rows (None: all) of page src[i] to page dst[i], K and V; ``n_pairs`` (a device
+    scalar or None) bounds how many pairs of the list count."""
+    _check(lib().hg_kv_copy_pages(*_kv_copy_pages_args(src, dst, rows, n_pairs, k_cache, v_cache, desc, stream)), "hg_kv_copy_pages")
+
+
+def prepare_kv_copy_pages(src, dst, rows, n_pairs, k_cache, v_cache, desc: HgAttnDesc, stream=None):
+    """``hg_kv_copy_pages`` with its arguments marshalled once (see ``prepare_partial``)."""
+    return _prepared(lib().hg_kv_copy_pages, _kv_copy_pages_args(src, dst, rows, n_pairs, k_cache, v_cache, desc, stream),
+                     (src, dst, rows, n_pairs, k_cache, v_cache, desc), "hg_kv_copy_pages")
 
 
 def hg_kv_read_probe(k_cache, v_cache, seq_lens, tok_begin, tok_end, sink, desc: HgAttnDesc, stream=None) -> None:

@@ -6,15 +6,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-namespace hg {
+#include "hg_poolview.cuh"
 
-struct KvPoolView {
-    uint16_t* k;
-    uint16_t* v;
-    const int32_t* block_table;   // may be NULL: identity paging
-    int64_t page_stride, head_stride, tok_stride;
-    int B, Hkv, D, page_size, page_shift, max_pages, num_pages;
-};
+namespace hg {
 
 // Physical page of token t of sequence b, or -1 if it is not resident / out of range.
 __device__ __forceinline__ int kv_page_of(const KvPoolView& pv, int b, int t) {

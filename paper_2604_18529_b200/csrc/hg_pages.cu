@@ -1,0 +1,143 @@
+// Host side of the page operations declared in include/hybridgen_attn.h: argument validation and launches.
+#include "hybridgen_attn.h"
+
+#include <cuda_runtime.h>
+#include <string.h>
+
+#include "hg_hostutil.h"
+#include "hg_pages.cuh"
+
+namespace hg {
+
+// Launches with the programmatic-serialisation attribute (every kernel here waits for its predecessor before its first
+// access), as one cluster of `cluster` CTAs where that is more than 1.
+template <typename... P, typename... A>
+static hg_status launch_pages(void (*kern)(P...), unsigned grid, unsigned threads, size_t smem, int cluster, void* stream, A... args) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    int na = 1;
+    if (cluster > 1) {
+        attr[na].id = cudaLaunchAttributeClusterDimension;
+        attr[na].val.clusterDim.x = (unsigned)cluster; attr[na].val.clusterDim.y = 1; attr[na].val.clusterDim.z = 1;
+        ++na;
+    }
+    cfg.attrs = attr; cfg.numAttrs = (unsigned)na;
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+        cudaGetLastError();
+        return HG_ERR_CUDA;
+    }
+    if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) { cudaGetLastError(); return HG_ERR_CUDA; }
+    return HG_OK;
+}
+
+// Pool and table; the operations that change the table need one (with identity paging a row owns its pages for good).
+static hg_status check_table(const hg_attn_desc* d) {
+    hg_status st = check_pool(d);
+    if (st != HG_OK) return st;
+    if (!d->block_table) return HG_ERR_INVALID_ARG;
+    if ((int64_t)d->batch * d->max_pages > 0x7ffffff0ll) return HG_ERR_UNSUPPORTED;      // a slot's number has 31 bits
+    return HG_OK;
+}
+
+static int sm_count() {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        return 0;
+    }
+    return sms;
+}
+
+}  // namespace hg
+
+using namespace hg;
+
+extern "C" {
+
+hg_status hg_kv_fork(const int32_t* src_row, int32_t* ref_count, int32_t* seq_lens, int32_t* tok_begin, int32_t* tok_end,
+                     void* stream, const hg_attn_desc* desc) {
+    hg_status st = check_table(desc);
+    if (st != HG_OK) return st;
+    if (!src_row || !ref_count || !seq_lens) return HG_ERR_INVALID_ARG;
+    if ((size_t)desc->batch * 4 > FORK_SMEM_MAX) return HG_ERR_UNSUPPORTED;
+    ForkParams p;
+    p.src_row = src_row; p.table = const_cast<int32_t*>(desc->block_table); p.ref = ref_count;
+    p.vec[0] = seq_lens; p.vec[1] = tok_begin; p.vec[2] = tok_end;
+    p.status = desc->status; p.B = desc->batch; p.max_pages = desc->max_pages; p.num_pages = desc->num_pages;
+    // 32 columns (128-byte row pieces) where that leaves a CTA for every SM, down to 8 (one 32-byte sector) for short
+    // tables, and fewer only where the rows of the batch fill the shared memory
+    int shift = 5;
+    while (shift > 3 && (p.max_pages >> shift) < 148) --shift;
+    while (shift > 0 && ((size_t)p.B << shift) * 4 > FORK_SMEM_MAX) --shift;
+    p.cols_shift = shift;
+    const unsigned tiles = (unsigned)((p.max_pages + (1 << shift) - 1) >> shift);
+    return launch_pages(kv_fork_kernel, tiles + 1, FORK_THREADS, ((size_t)p.B << shift) * 4, 1, stream, p);
+}
+
+hg_status hg_kv_release(const int32_t* page_ids, int32_t n, int32_t* ref_count, void* stream, const hg_attn_desc* desc) {
+    hg_status st = check_pool(desc);
+    if (st != HG_OK) return st;
+    if (!page_ids || !ref_count || n < 0) return HG_ERR_INVALID_ARG;
+    if (n == 0) return HG_OK;
+    const unsigned grid = (unsigned)((n + 255) / 256);
+    return launch_pages(kv_release_kernel, grid < 1024 ? grid : 1024, 256, 0, 1, stream, page_ids, (int)n, ref_count,
+                        (int)desc->num_pages, desc->status);
+}
+
+hg_status hg_kv_reserve(const int32_t* seq_lens, const int32_t* n_new, int32_t* ref_count, int32_t* copy_src, int32_t* copy_dst,
+                        int32_t* copy_rows, int32_t* n_ready, void* stream, const hg_attn_desc* desc) {
+    hg_status st = check_table(desc);
+    if (st != HG_OK) return st;
+    if (!seq_lens || !ref_count || !copy_src || !copy_dst || !aligned16(ref_count)) return HG_ERR_INVALID_ARG;
+    if (desc->batch > RESERVE_MAX_BATCH) return HG_ERR_UNSUPPORTED;
+    ReserveParams p;
+    p.seq_lens = seq_lens; p.n_new = n_new; p.table = const_cast<int32_t*>(desc->block_table); p.ref = ref_count;
+    p.copy_src = copy_src; p.copy_dst = copy_dst; p.copy_rows = copy_rows; p.n_ready = n_ready; p.status = desc->status;
+    p.B = desc->batch; p.max_pages = desc->max_pages; p.num_pages = desc->num_pages; p.page_shift = ilog2_exact(desc->page_size);
+    const size_t smem = ((size_t)RESERVE_IDS_PER_CTA + desc->batch) * 4;
+    // a small pool and table: one CTA (its barriers are cheaper than the cluster's, and it can look at every slot there is)
+    if (desc->num_pages <= 8192 && (int64_t)desc->batch * desc->max_pages <= PG_THREADS * RESERVE_MAX_ITER)
+        return launch_pages(kv_reserve_kernel<1>, 1, PG_THREADS, smem, 1, stream, p);
+    return launch_pages(kv_reserve_kernel<8>, 8, PG_THREADS, smem, 8, stream, p);
+}
+
+hg_status hg_kv_compact(int32_t* ref_count, int32_t* remap, int32_t* move_src, int32_t* move_dst, int32_t max_moves,
+                        int32_t* n_moves, void* stream, const hg_attn_desc* desc) {
+    hg_status st = check_table(desc);
+    if (st != HG_OK) return st;
+    if (!ref_count || !remap || !move_src || !move_dst || !n_moves || max_moves < 1 || !aligned16(ref_count)) return HG_ERR_INVALID_ARG;
+    const int sms = sm_count();
+    if (sms < 1) return HG_ERR_CUDA;
+    CompactParams p;
+    p.ref = ref_count; p.remap = remap; p.move_src = move_src; p.move_dst = move_dst; p.n_moves = n_moves;
+    p.num_pages = desc->num_pages; p.max_moves = max_moves;
+    st = desc->num_pages <= 8192 ? launch_pages(kv_compact_kernel<1>, 1, PG_THREADS, 0, 1, stream, p)
+                                 : launch_pages(kv_compact_kernel<8>, 8, PG_THREADS, 0, 8, stream, p);
+    if (st != HG_OK) return st;
+    const size_t n = (size_t)desc->batch * desc->max_pages;
+    const size_t want = (n + 1023) / 1024, most = (size_t)sms * 8;
+    return launch_pages(kv_rename_kernel, (unsigned)(want < most ? want : most), 256, 0, 1, stream, const_cast<int32_t*>(desc->block_table), n,
+                        const_cast<const int32_t*>(remap), const_cast<const int32_t*>(n_moves), (int)desc->num_pages);
+}
+
+hg_status hg_kv_copy_pages(const int32_t* src, const int32_t* dst, const int32_t* rows, int32_t n, const int32_t* n_dev, void* k_cache,
+                           void* v_cache, void* stream, const hg_attn_desc* desc) {
+    hg_status st = check_pool(desc);
+    if (st != HG_OK) return st;
+    if (!src || !dst || !k_cache || !v_cache || n < 0) return HG_ERR_INVALID_ARG;
+    if (!aligned16(k_cache) || !aligned16(v_cache)) return HG_ERR_INVALID_ARG;
+    if (n == 0) return HG_OK;
+    const int sms = sm_count();
+    if (sms < 1) return HG_ERR_CUDA;
+    const long long units = (long long)n * desc->num_kv_heads * 2, ctas = (units + COPY_THREADS / 32 - 1) / (COPY_THREADS / 32);
+    const long long most = (long long)sms * (2048 / COPY_THREADS);
+    return launch_pages(kv_copy_pages_kernel, (unsigned)(ctas < most ? ctas : most), COPY_THREADS, 0, 1, stream,
+                        pool_view(desc, k_cache, v_cache), src, dst, rows, (int)n, n_dev, desc->status);
+}
+
+}  // extern "C"

@@ -1,0 +1,561 @@
+// Page management of the paged KV pool (sm_100a): block-table rows that share pages, the pages' reference counts,
+// copy on write, compaction, and the copies of page contents these operations ask for.
+//
+// The only allocator state is ref_count[num_pages]: how many block-table entries (and other holders) use a page.  A page
+// is free when its count is 0, and free pages are handed out lowest id first, so every result is a function of the
+// arguments alone: no list whose order would depend on timing, no atomic whose order shows.  Table operations are a few
+// kilobytes to a few megabytes of integers and bound by latency; copying is bound by HBM.
+#pragma once
+
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "hg_poolview.cuh"
+
+namespace hg {
+
+// The kernels below are launched as programmatic dependents of whatever precedes them in the stream: the launch
+// itself overlaps the predecessor, nothing is read or written before this returns.
+__device__ __forceinline__ void pages_begin() {
+    cudaTriggerProgrammaticLaunchCompletion();
+    cudaGridDependencySynchronize();
+}
+
+// ---- fork: rows of the block table take other rows' pages ----------------------------------------------------------
+
+constexpr int FORK_THREADS = 512;
+constexpr int FORK_SMEM_MAX = 160 * 1024;
+
+struct ForkParams {
+    const int32_t* src_row;          // [B]
+    int32_t* table;                  // [B][max_pages]
+    int32_t* ref;                    // [num_pages]
+    int32_t* vec[3];                 // seq_lens, tok_begin, tok_end (each may be NULL)
+    int32_t* status;
+    int B, max_pages, num_pages;
+    int cols_shift;                  // log2 of the block-table columns one CTA handles
+};
+
+// Columns of the table are independent of one another: a CTA stages its columns of every changed row's new contents in
+// shared memory, and writes only after all have been read, so rows may be each other's sources (a beam step re-orders
+// all rows in place).  Counts move by +1 / -1 per entry; entries that stay the same (the part beams have in common)
+// touch no count.  The last CTA moves the per-sequence lengths the same way.
+__global__ void __launch_bounds__(FORK_THREADS) kv_fork_kernel(const ForkParams p) {
+    extern __shared__ int32_t fork_stage[];
+    pages_begin();
+    const int tid = threadIdx.x;
+    if (blockIdx.x == gridDim.x - 1) {
+        for (int v = 0; v < 3; ++v) {
+            if (!p.vec[v]) continue;
+            for (int b = tid; b < p.B; b += FORK_THREADS) {
+                const int s = p.src_row[b];
+                if (v == 0 && s >= p.B && p.status) atomicOr(p.status, HG_DEV_RANGE);
+                fork_stage[b] = s < 0 ? 0 : p.vec[v][s < p.B ? s : b];
+            }
+            __syncthreads();
+            for (int b = tid; b < p.B; b += FORK_THREADS) p.vec[v][b] = fork_stage[b];
+            __syncthreads();
+        }
+        return;
+    }
+    const int cols = 1 << p.cols_shift;
+    const int c0 = (int)blockIdx.x << p.cols_shift;
+    const int n = p.B << p.cols_shift;                     // cells of this CTA (fits: B * cols * 4 <= FORK_SMEM_MAX)
+    for (int i = tid; i < n; i += FORK_THREADS) {
+        const int b = i >> p.cols_shift, c = c0 + (i & (cols - 1));
+        const int s = p.src_row[b];
+        if (s == b || s >= p.B || c >= p.max_pages) continue;
+        fork_stage[i] = s < 0 ? -1 : p.table[(size_t)s * p.max_pages + c];
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += FORK_THREADS) {
+        const int b = i >> p.cols_shift, c = c0 + (i & (cols - 1));
+        const int s = p.src_row[b];
+        if (s == b || s >= p.B || c >= p.max_pages) continue;
+        int32_t* const at = p.table + (size_t)b * p.max_pages + c;
+        const int was = *at, now = fork_stage[i];
+        if (was == now) continue;
+        if ((uint32_t)now < (uint32_t)p.num_pages) atomicAdd(p.ref + now, 1);
+        if ((uint32_t)was < (uint32_t)p.num_pages) atomicSub(p.ref + was, 1);
+        *at = now;
+    }
+}
+
+// ---- release: one reference less for every listed page ---------------------------------------------------------------
+
+__global__ void __launch_bounds__(256) kv_release_kernel(const int32_t* __restrict__ ids, int n, int32_t* ref, int num_pages,
+                                                          int32_t* status) {
+    pages_begin();
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+        const int p = ids[i];
+        if (p < 0) continue;
+        bool bad = p >= num_pages;
+        if (!bad && atomicSub(ref + p, 1) <= 0) { atomicAdd(ref + p, 1); bad = true; }   // released more often than held
+        if (bad && status) atomicOr(status, HG_DEV_BAD_PAGE);
+    }
+}
+
+// ---- cluster-wide scans over the reference counts ----------------------------------------------------------------------
+
+constexpr int PG_THREADS = 1024;
+constexpr int PG_WARPS = PG_THREADS / 32;
+
+// Sum over the 32 lanes of the values of lower lanes.
+__device__ __forceinline__ int warp_exclusive(int v, int lane, int& total) {
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    total = __shfl_sync(0xffffffffu, x, 31);
+    return x - v;
+}
+
+// What each CTA of the cluster contributes to the running scan; read by its peers through distributed shared memory.
+struct ClusterScan {
+    int warp_sum[PG_WARPS];
+    int cta_sum;
+};
+
+// Exclusive prefix of one value per WARP over all warps of the cluster, in (CTA, warp) order, and the total.
+template <int CLUSTER>
+__device__ __forceinline__ int cluster_warp_prefix(int v, ClusterScan& s, int rank, int warp, int lane, int& total) {
+    namespace cg = cooperative_groups;
+    if (lane == 0) s.warp_sum[warp] = v;
+    __syncthreads();
+    int cta;
+    const int mine = warp_exclusive(s.warp_sum[lane], lane, cta);
+    int before = __shfl_sync(0xffffffffu, mine, warp);
+    total = cta;
+    if constexpr (CLUSTER > 1) {
+        cg::cluster_group cluster = cg::this_cluster();
+        if (threadIdx.x == 0) s.cta_sum = cta;
+        cluster.sync();
+        total = 0;
+#pragma unroll
+        for (int r = 0; r < CLUSTER; ++r) {
+            const int x = *cluster.map_shared_rank(&s.cta_sum, r);
+            if (r < rank) before += x;
+            total += x;
+        }
+    }
+    return before;
+}
+
+// Orders the cluster's (or the CTA's) global-memory and shared-memory accesses before and after it.
+template <int CLUSTER>
+__device__ __forceinline__ void cluster_sync_all() {
+    __threadfence();
+    if constexpr (CLUSTER > 1) cooperative_groups::this_cluster().sync();
+    else __syncthreads();
+}
+
+// The pages a warp looks after: a contiguous range, whole groups of 128 (32 lanes x 4).
+struct PageRange { int begin, end; };
+template <int CLUSTER>
+__device__ __forceinline__ PageRange warp_pages(int num_pages, int rank, int warp) {
+    const int groups = (num_pages + 127) / 128;
+    const int per = (groups + CLUSTER * PG_WARPS - 1) / (CLUSTER * PG_WARPS);
+    const long long b = (long long)(rank * PG_WARPS + warp) * per * 128;
+    PageRange r;
+    r.begin = (int)(b < num_pages ? b : num_pages);
+    r.end = (int)(b + (long long)per * 128 < num_pages ? b + (long long)per * 128 : num_pages);
+    return r;
+}
+
+// Four counts from p on (a missing one reads as `pad`).  p is a multiple of 4, ref 16-byte aligned.
+__device__ __forceinline__ int4 load_refs(const int32_t* ref, int p, int num_pages, int pad) {
+    if (p + 3 < num_pages) return __ldcg(reinterpret_cast<const int4*>(ref + p));
+    int4 v;
+    v.x = p < num_pages ? __ldcg(ref + p) : pad;
+    v.y = p + 1 < num_pages ? __ldcg(ref + p + 1) : pad;
+    v.z = p + 2 < num_pages ? __ldcg(ref + p + 2) : pad;
+    v.w = pad;
+    return v;
+}
+
+// ---- reserve: pages for the next tokens, copy on write -----------------------------------------------------------------
+
+struct ReserveParams {
+    const int32_t* seq_lens;         // [B]
+    const int32_t* n_new;            // [B] or NULL: one each
+    int32_t* table;
+    int32_t* ref;
+    int32_t* copy_src;               // [B]
+    int32_t* copy_dst;               // [B]
+    int32_t* copy_rows;              // [B] or NULL
+    int32_t* n_ready;                // [B] or NULL
+    int32_t* status;
+    int B, max_pages, num_pages, page_shift;
+};
+
+constexpr int RESERVE_MAX_BATCH = 16384;
+// Free-page ids a CTA of the cluster keeps, and slots one thread can look at: together the pages a call can hand out.
+constexpr int RESERVE_IDS_PER_CTA = 32768;
+constexpr int RESERVE_MAX_ITER = 32;
+
+// The block-table slots that hold positions [len, len + n_new) of sequence b.
+struct SlotRange { int first, count, len, n; bool cut; };
+__device__ __forceinline__ SlotRange reserve_slots(const ReserveParams& p, int b) {
+    SlotRange r;
+    r.len = max(p.seq_lens[b], 0);
+    r.n = p.n_new ? p.n_new[b] : 1;
+    r.first = r.len >> p.page_shift;
+    r.cut = false;
+    if (r.n <= 0) { r.n = 0; r.count = 0; return r; }
+    const long long room = ((long long)p.max_pages << p.page_shift) - r.len;
+    if (r.n > room) { r.cut = true; r.n = (int)(room > 0 ? room : 0); }
+    r.count = r.n > 0 ? (int)(((long long)r.len + r.n - 1) >> p.page_shift) - r.first + 1 : 0;
+    return r;
+}
+
+// One cluster does the whole call: its phases (give up a reference - find the last writer - rank the needs - hand out)
+// depend on one another, and a cluster barrier costs a few hundred nanoseconds where a launch costs microseconds.
+//
+// A page with `refs` references that k sequences of this call are about to write stays with the last of them exactly
+// when k = refs (nobody else reads it); all others copy.  That is what serving the sequences one after the other gives.
+// In parallel: every writer takes its reference off; a count that is still positive says that others remain; else the
+// writers leave the largest of their (sequence, slot) numbers there, as -(number + 1).
+template <int CLUSTER>
+__global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(const ReserveParams p) {
+    namespace cg = cooperative_groups;
+    extern __shared__ int32_t reserve_smem[];
+    int32_t* const ids = reserve_smem;                            // this CTA's share of the free ids, by rank
+    int32_t* const cum = reserve_smem + RESERVE_IDS_PER_CTA;      // cum[b]: slots of sequences < b
+    __shared__ ClusterScan scan_a, scan_b;
+    __shared__ int s_warp[PG_WARPS], s_carry;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = CLUSTER > 1 ? (int)cg::this_cluster().block_rank() : 0;
+    pages_begin();
+
+    // ---- slots per sequence, and what is known without looking at any page ----
+    if (tid == 0) s_carry = 0;
+    __syncthreads();
+    for (int b0 = 0; b0 < p.B; b0 += PG_THREADS) {
+        const int b = b0 + tid;
+        SlotRange r;
+        r.count = 0;
+        if (b < p.B) r = reserve_slots(p, b);
+        int wt;
+        const int ex = warp_exclusive(r.count, lane, wt);
+        if (lane == 31) s_warp[warp] = wt;
+        __syncthreads();
+        int ct;
+        const int wx = warp_exclusive(s_warp[lane], lane, ct);
+        const int base = s_carry + __shfl_sync(0xffffffffu, wx, warp);
+        if (b < p.B) {
+            cum[b] = base + ex;
+            if (rank == 0) {
+                p.copy_src[b] = -1;
+                p.copy_dst[b] = -1;
+                if (p.copy_rows) p.copy_rows[b] = 0;
+                if (p.n_ready) p.n_ready[b] = r.n;
+                if (r.cut && p.status) atomicOr(p.status, HG_DEV_RANGE);
+            }
+        }
+        __syncthreads();
+        if (tid == 0) s_carry += ct;
+        __syncthreads();
+    }
+    // (B slots' sum fits: max_pages <= 2^31 / B is checked by the host)
+    const int wanted = s_carry;
+    constexpr int LANES = CLUSTER * PG_THREADS;
+    const int T = min(wanted, LANES * RESERVE_MAX_ITER);         // later slots are left for another call (n_ready says so)
+    const int max_ids = CLUSTER * RESERVE_IDS_PER_CTA;
+
+    // ---- the lowest free ids, by rank, into the CTAs' shared memory ----
+    {
+        const PageRange pr = warp_pages<CLUSTER>(p.num_pages, rank, warp);
+        int mine = 0;
+        for (int g = pr.begin; g < pr.end; g += 128) {
+            const int4 v = load_refs(p.ref, g + lane * 4, p.num_pages, 1);
+            mine += (v.x == 0) + (v.y == 0) + (v.z == 0) + (v.w == 0);
+        }
+        mine = __reduce_add_sync(0xffffffffu, mine);
+        int total;
+        int at = cluster_warp_prefix<CLUSTER>(mine, scan_a, rank, warp, lane, total);
+        const int limit = min(T, max_ids);
+        for (int g = pr.begin; g < pr.end && at < limit; g += 128) {
+            const int id = g + lane * 4;
+            const int4 v = load_refs(p.ref, id, p.num_pages, 1);
+            const int f[4] = {v.x == 0, v.y == 0, v.z == 0, v.w == 0};
+            int step;
+            int r = at + warp_exclusive(f[0] + f[1] + f[2] + f[3], lane, step);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (f[j] && r < limit) {
+                    if constexpr (CLUSTER > 1) cg::this_cluster().map_shared_rank(ids, r & (CLUSTER - 1))[r / CLUSTER] = id + j;
+                    else ids[r] = id + j;
+                }
+                r += f[j];
+            }
+            at += step;
+        }
+        s_carry = total;                                         // (every thread stores the same value)
+    }
+    cluster_sync_all<CLUSTER>();
+    const int n_free = min(s_carry, max_ids);
+
+    // ---- this thread's slots: a contiguous range per warp, consecutive slots on consecutive lanes ----
+    const int iters = (T + LANES - 1) / LANES;
+    const int first = (rank * PG_WARPS + warp) * iters * 32 + lane;
+    auto slot_of = [&](int i, int& b, int& slot) {               // the sequence whose range holds slot number i
+        int lo = 0, hi = p.B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (cum[mid] <= i) lo = mid;
+            else hi = mid - 1;
+        }
+        b = lo;
+        slot = (max(p.seq_lens[b], 0) >> p.page_shift) + i - cum[b];
+    };
+    auto cell = [&](int i, int& b, int& slot) -> int32_t* {
+        slot_of(i, b, slot);
+        return p.table + (size_t)b * p.max_pages + slot;
+    };
+    uint32_t need = 0, keep = 0, got = 0;                        // one bit per iteration
+    for (int k = 0; k < iters; ++k) {
+        const int i = first + k * 32;
+        if (i >= T) break;
+        int b, slot;
+        const int e = *cell(i, b, slot);
+        if ((uint32_t)e < (uint32_t)p.num_pages) atomicSub(p.ref + e, 1);
+    }
+    cluster_sync_all<CLUSTER>();
+    for (int k = 0; k < iters; ++k) {
+        const int i = first + k * 32;
+        if (i >= T) break;
+        int b, slot;
+        const int e = *cell(i, b, slot);
+        if ((uint32_t)e < (uint32_t)p.num_pages && __ldcg(p.ref + e) <= 0) atomicMin(p.ref + e, -(b * p.max_pages + slot + 1));
+    }
+    cluster_sync_all<CLUSTER>();
+    int count = 0;
+    for (int k = 0; k < iters; ++k) {
+        const int i = first + k * 32;
+        if (i >= T) break;
+        int b, slot;
+        const int e = *cell(i, b, slot);
+        bool n = e < 0;
+        if ((uint32_t)e < (uint32_t)p.num_pages) {
+            n = __ldcg(p.ref + e) != -(b * p.max_pages + slot + 1);
+            if (!n) keep |= 1u << k;
+        }
+        if (n) { need |= 1u << k; ++count; }
+    }
+    count = __reduce_add_sync(0xffffffffu, count);
+    int needs;
+    int at = cluster_warp_prefix<CLUSTER>(count, scan_b, rank, warp, lane, needs);
+    if (needs > n_free && rank == 0 && tid == 0 && p.status) atomicOr(p.status, HG_DEV_NO_PAGE);
+    for (int k = 0; k < iters; ++k) {
+        const int i = first + k * 32;
+        const bool n = (need >> k) & 1u;
+        const uint32_t votes = __ballot_sync(0xffffffffu, n);
+        const int r = at + __popc(votes & ((1u << lane) - 1u));
+        at += __popc(votes);
+        if (!n || r >= n_free) continue;
+        got |= 1u << k;
+        int id;
+        if constexpr (CLUSTER > 1) id = cg::this_cluster().map_shared_rank(ids, r & (CLUSTER - 1))[r / CLUSTER];
+        else id = ids[r];
+        int b, slot;
+        int32_t* const at_cell = cell(i, b, slot);
+        const int e = *at_cell;
+        *at_cell = id;
+        p.ref[id] = 1;
+        const int len = max(p.seq_lens[b], 0), in_page = len & ((1 << p.page_shift) - 1);
+        if (e >= 0 && slot == (len >> p.page_shift) && in_page) {   // the page holds tokens that the sequence keeps
+            p.copy_src[b] = e;
+            p.copy_dst[b] = id;
+            if (p.copy_rows) p.copy_rows[b] = in_page;
+        }
+    }
+    cluster_sync_all<CLUSTER>();                                  // the counts are not looked at any more for who keeps what
+    auto stop_at = [&](int b, int slot) {                         // positions from this slot on are not ready
+        if (!p.n_ready) return;
+        const long long t = ((long long)slot << p.page_shift) - max(p.seq_lens[b], 0);
+        atomicMin(p.n_ready + b, (int)(t > 0 ? t : 0));
+    };
+    for (int k = 0; k < iters; ++k) {
+        const int i = first + k * 32;
+        if (i >= T) break;
+        const bool n = (need >> k) & 1u, g = (got >> k) & 1u, kp = (keep >> k) & 1u;
+        if (n ? g : false) continue;
+        int b, slot;
+        const int e = *cell(i, b, slot);
+        if (kp) {
+            atomicAdd(p.ref + e, b * p.max_pages + slot + 2);     // back from -(number + 1) to one reference
+        } else if (n) {                                           // no page left: the slot stays as it was
+            if (e >= 0) atomicAdd(p.ref + e, 1);
+            stop_at(b, slot);
+        } else {                                                  // an entry outside the pool
+            if (p.status) atomicOr(p.status, HG_DEV_BAD_PAGE);
+            stop_at(b, slot);
+        }
+    }
+    for (int i = T + rank * PG_THREADS + tid; i < wanted; i += LANES) {       // beyond what one call looks at
+        int b, slot;
+        slot_of(i, b, slot);
+        stop_at(b, slot);
+    }
+    if (needs <= n_free) {                                        // (uniform over the cluster)
+        if constexpr (CLUSTER > 1) cg::this_cluster().sync();     // peers' shared memory stays until all have read it
+        return;
+    }
+    cluster_sync_all<CLUSTER>();
+    for (int k = 0; k < iters; ++k) {                             // a kept page that a sharer without a copy still reads
+        if (!((keep >> k) & 1u)) continue;
+        int b, slot;
+        const int e = *cell(first + k * 32, b, slot);
+        if (__ldcg(p.ref + e) > 1) stop_at(b, slot);
+    }
+    if constexpr (CLUSTER > 1) cg::this_cluster().sync();
+}
+
+// ---- compact: the pages in use move to the low end of the pool ------------------------------------------------------------
+
+struct CompactParams {
+    int32_t* ref;
+    int32_t* remap;                  // [num_pages]
+    int32_t* move_src;               // [max_moves]
+    int32_t* move_dst;               // [max_moves]
+    int32_t* n_moves;
+    int num_pages, max_moves;
+};
+
+// U pages in use.  Holes (free ids below U) are as many as strays (used ids from U on): the k-th lowest hole takes the
+// k-th highest stray, so a call that may move only a few pages still shortens the used range from its end.
+template <int CLUSTER>
+__global__ void __launch_bounds__(PG_THREADS) kv_compact_kernel(const CompactParams p) {
+    namespace cg = cooperative_groups;
+    __shared__ ClusterScan scan;
+    __shared__ int s_below;                                       // pages in use below U
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = CLUSTER > 1 ? (int)cg::this_cluster().block_rank() : 0;
+    pages_begin();
+    const PageRange pr = warp_pages<CLUSTER>(p.num_pages, rank, warp);
+    int mine = 0;
+    for (int g = pr.begin; g < pr.end; g += 128) {
+        const int4 v = load_refs(p.ref, g + lane * 4, p.num_pages, 0);
+        mine += (v.x > 0) + (v.y > 0) + (v.z > 0) + (v.w > 0);
+    }
+    mine = __reduce_add_sync(0xffffffffu, mine);
+    int U;
+    const int before = cluster_warp_prefix<CLUSTER>(mine, scan, rank, warp, lane, U);
+    // used ids below U: the warp whose range holds U counts; it tells every CTA
+    if (U >= pr.begin && U < pr.end) {
+        int below = 0;
+        for (int g = pr.begin; g < U; g += 128) {
+            const int id = g + lane * 4;
+            const int4 v = load_refs(p.ref, id, p.num_pages, 0);
+            below += (v.x > 0 && id < U) + (v.y > 0 && id + 1 < U) + (v.z > 0 && id + 2 < U) + (v.w > 0 && id + 3 < U);
+        }
+        below = before + __reduce_add_sync(0xffffffffu, below);
+        if (lane == 0) {
+            if constexpr (CLUSTER > 1) {
+                for (int r = 0; r < CLUSTER; ++r) *cg::this_cluster().map_shared_rank(&s_below, r) = below;
+            } else {
+                s_below = below;
+            }
+        }
+    } else if (U == p.num_pages && tid == 0) {
+        s_below = U;                                              // a full pool: no stray anywhere
+    }
+    cluster_sync_all<CLUSTER>();
+    const int below = s_below, strays = U - below, moves = min(strays, p.max_moves);
+    int at = before;                                              // pages in use below this warp's position
+    for (int g = pr.begin; g < pr.end; g += 128) {
+        const int id0 = g + lane * 4;
+        const int4 v = load_refs(p.ref, id0, p.num_pages, 0);
+        const bool used4[4] = {v.x > 0, v.y > 0, v.z > 0, v.w > 0};
+        int step;
+        int used_before = at + warp_exclusive(used4[0] + used4[1] + used4[2] + used4[3], lane, step);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int id = id0 + j;
+            if (id < p.num_pages) {
+                const int hole = id - used_before, stray = strays - 1 - (used_before - below);
+                if (!used4[j] && id < U && hole < moves) p.move_dst[hole] = id;
+                if (used4[j] && id >= U && stray < moves) p.move_src[stray] = id;
+                p.remap[id] = id;
+            }
+            used_before += used4[j];
+        }
+        at += step;
+    }
+    for (int i = moves + rank * PG_THREADS + tid; i < p.max_moves; i += CLUSTER * PG_THREADS) {
+        p.move_src[i] = -1;
+        p.move_dst[i] = -1;
+    }
+    if (rank == 0 && tid == 0) *p.n_moves = moves;
+    cluster_sync_all<CLUSTER>();
+    for (int i = rank * PG_THREADS + tid; i < moves; i += CLUSTER * PG_THREADS) {   // all pairs are known: move the counts
+        const int src = __ldcg(p.move_src + i), dst = __ldcg(p.move_dst + i);
+        p.remap[src] = dst;
+        p.ref[dst] = __ldcg(p.ref + src);
+        p.ref[src] = 0;
+    }
+}
+
+// Renames the entries of the block table.
+__global__ void __launch_bounds__(256) kv_rename_kernel(int32_t* table, size_t n, const int32_t* __restrict__ remap,
+                                                         const int32_t* __restrict__ n_moves, int num_pages) {
+    pages_begin();
+    if (*n_moves == 0) return;
+    const size_t step = (size_t)gridDim.x * 256;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
+        const int e = table[i];
+        if ((uint32_t)e >= (uint32_t)num_pages) continue;
+        const int to = remap[e];
+        if (to != e) table[i] = to;
+    }
+}
+
+// ---- copying pages --------------------------------------------------------------------------------------------------------
+
+constexpr int COPY_THREADS = 256;
+
+// A warp per (pair, tensor, KV head): the head's block of a page, 2 to 64 KB, in 16-byte vectors.
+__global__ void __launch_bounds__(COPY_THREADS) kv_copy_pages_kernel(KvPoolView pv, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+                                                                      const int32_t* __restrict__ rows, int n,
+                                                                      const int32_t* __restrict__ n_dev, int32_t* status) {
+    pages_begin();
+    const int pairs = n_dev ? max(0, min(*n_dev, n)) : n;
+    const int lane = threadIdx.x & 31;
+    const int vec_shift = pv.D == 128 ? 4 : 3;                    // 16-byte vectors per row, as a power of two
+    const long long units = (long long)pairs * pv.Hkv * 2;
+    const long long step = (long long)gridDim.x * (COPY_THREADS / 32);
+    for (long long u = (long long)blockIdx.x * (COPY_THREADS / 32) + (threadIdx.x >> 5); u < units; u += step) {
+        const int pair = (int)(u / (pv.Hkv * 2)), r = (int)(u - (long long)pair * pv.Hkv * 2);
+        const int s = src[pair], d = dst[pair];
+        const int nr = rows ? max(0, min(rows[pair], pv.page_size)) : pv.page_size;
+        if (s < 0 || d < 0 || nr == 0 || s == d) continue;
+        if (s >= pv.num_pages || d >= pv.num_pages) {
+            if (lane == 0 && status) atomicOr(status, HG_DEV_BAD_PAGE);
+            continue;
+        }
+        uint16_t* const pool = (r & 1) ? pv.v : pv.k;
+        const int64_t head = (int64_t)(r >> 1) * pv.head_stride;
+        const uint16_t* const from = pool + (int64_t)s * pv.page_stride + head;
+        uint16_t* const to = pool + (int64_t)d * pv.page_stride + head;
+        const int nv = nr << vec_shift;
+        constexpr int UNROLL = 8;
+        for (int base = lane; base < nv; base += 32 * UNROLL) {
+            uint4 x[UNROLL];
+            int64_t off[UNROLL];
+#pragma unroll
+            for (int j = 0; j < UNROLL; ++j) {
+                const int i = base + 32 * j;
+                off[j] = (int64_t)(i >> vec_shift) * pv.tok_stride + (int64_t)(i & ((1 << vec_shift) - 1)) * 8;
+                if (i < nv) x[j] = *reinterpret_cast<const uint4*>(from + off[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < UNROLL; ++j)
+                if (base + 32 * j < nv) *reinterpret_cast<uint4*>(to + off[j]) = x[j];
+        }
+    }
+}
+
+}  // namespace hg
