@@ -409,6 +409,65 @@ hg_status hg_kv_evict_finish(const int32_t* src_begin, const int32_t* n_moved, i
                              int32_t max_freed, void* stream, const hg_attn_desc* desc);
 
 /*
+ * Groups of sequences that share a prefix (host struct, dev arrays).
+ *
+ * Sequence b belongs to group seq_group[b]; any value outside [0, num_groups) means that it shares nothing.  The shared
+ * tokens of group g are the positions [group_begin[g], group_end[g]) of block-table row group_row[g] - usually the row of
+ * one of its members, whose first pages every member's row lists too (hg_kv_fork makes such rows).  Ranges are read on
+ * the device and clamped to the row (HG_DEV_RANGE when that cuts something off, or when group_row lies outside the
+ * table: such a group is empty).  The chunk grid is that of hg_attn_desc, with its own chunk size: chunk_tokens a multiple
+ * of 128 and of page_size; num_chunks must be >= every group's number of chunks.
+ */
+#define HG_MAX_GROUPS 512
+typedef struct hg_prefix_desc {
+    uint32_t struct_size;        /* sizeof(hg_prefix_desc) */
+    int32_t num_groups;          /* NG, at most HG_MAX_GROUPS */
+    const int32_t* seq_group;    /* dev [B] */
+    const int32_t* group_row;    /* dev [NG] */
+    const int32_t* group_begin;  /* dev [NG] */
+    const int32_t* group_end;    /* dev [NG] */
+    int32_t chunk_tokens;
+    int32_t num_chunks;          /* NC: chunk slots per (sequence, head) in o/m/l_part */
+} hg_prefix_desc;
+
+/*
+ * Softmax partials over the shared prefixes: hg_attn_partial for the tokens of the groups, with every group's K and V
+ * read once for all its members instead of once per member (the paper's batches decode independent sequences; requests
+ * with a common prompt, beams and parallel samples do not).  One more source for hg_attn_merge.
+ *
+ *   q       dev [B][Hq][D], dtype as desc->dtype, 16-byte aligned; one query per sequence
+ *   o_part, m_part, l_part   dev float [B][Hq][NC][D] / [B][Hq][NC], NC = prefix->num_chunks: as in hg_attn_partial; a
+ *           sequence without a group, and slots beyond a group's chunks, are empty (HG_FLAG_SPARSE_EMPTY applies)
+ * Of desc: batch, heads, head_dim, dtype, the KV addressing, scale, flags and status are used.  Accumulation is fp32 and P is
+ * carried as a two-term (hi + lo) 16-bit expansion, as in hg_attn_partial.
+ */
+hg_status hg_attn_prefix_partial(const void* q, const void* k_cache, const void* v_cache, float* o_part, float* m_part, float* l_part,
+                                 void* stream, const hg_attn_desc* desc, const hg_prefix_desc* prefix);
+
+/*
+ * A chunk size for hg_attn_prefix_partial: shared_tokens and num_members are summed over the num_groups groups (estimates
+ * will do).  Always a multiple of 128 and of page_size.  Returns 0 for invalid arguments.  No CUDA call is made.
+ */
+int32_t hg_attn_prefix_suggest_chunk(int64_t shared_tokens, int32_t num_groups, int32_t num_members, int32_t num_q_heads,
+                                     int32_t num_kv_heads, int32_t page_size);
+
+/* Bytes of device workspace hg_attn_decode_shared needs; 0 for an invalid description. */
+size_t hg_attn_shared_workspace_bytes(const hg_attn_desc* desc, const hg_prefix_desc* prefix);
+
+/*
+ * One decode step of a batch with shared prefixes: hg_attn_prefix_partial, hg_attn_partial over every sequence's OWN
+ * tokens [tok_begin, tok_end), and the merge of both with n_host_src (at most HG_MAX_MERGE_SRC - 2) further sources.  The
+ * result is attention over all of them together; a token that lies in both a group's slice and a member's own counts
+ * twice, so tok_begin[b] is usually the group's end.  A sequence without a group simply has all its tokens in
+ * [tok_begin, tok_end).  workspace: dev, 256-byte aligned, at least hg_attn_shared_workspace_bytes(); it holds the work
+ * counter too, and HG_FLAG_COUNTER_CLEAN speaks about that one (see there).
+ */
+hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* v_cache, const int32_t* seq_lens,
+                                const int32_t* tok_begin, const int32_t* tok_end, const hg_partial_src* host_partials,
+                                int32_t n_host_src, float* out, float* lse, void* workspace, size_t workspace_bytes, void* stream,
+                                const hg_attn_desc* desc, const hg_prefix_desc* prefix);
+
+/*
  * Page management: block-table rows that share pages.
  *
  * Section 4.8's paged cache with residency metadata needs somebody to hand out pages, and sequences that branch (beams,

@@ -30,6 +30,12 @@ from .binding import (  # noqa: F401
     hg_kv_evict_begin,
     hg_kv_evict_copy,
     hg_kv_evict_finish,
+    prefix_desc,
+    hg_attn_prefix_partial,
+    hg_attn_prefix_suggest_chunk,
+    hg_attn_shared_workspace_bytes,
+    hg_attn_decode_shared,
+    prepare_decode_shared,
     hg_kv_fork,
     hg_kv_reserve,
     hg_kv_release,

@@ -21,6 +21,7 @@ HG_OK, HG_ERR_INVALID_ARG, HG_ERR_UNSUPPORTED, HG_ERR_CUDA, HG_ERR_WORKSPACE = 0
 HG_DTYPE_F16, HG_DTYPE_BF16 = 0, 1
 HG_DEV_OK, HG_DEV_WAIT_TIMEOUT, HG_DEV_BAD_PAGE, HG_DEV_RANGE, HG_DEV_NO_PAGE = 0, 1, 2, 4, 8
 HG_MAX_MERGE_SRC = 8
+HG_MAX_GROUPS = 512
 HG_FLAG_TEST_STALL = 1
 HG_FLAG_SPARSE_EMPTY = 2
 HG_FLAG_COUNTER_CLEAN = 4
@@ -80,6 +81,19 @@ class HgLogitsDesc(C.Structure):
     ]
 
 
+class HgPrefixDesc(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32),
+        ("num_groups", C.c_int32),
+        ("seq_group", C.c_void_p),
+        ("group_row", C.c_void_p),
+        ("group_begin", C.c_void_p),
+        ("group_end", C.c_void_p),
+        ("chunk_tokens", C.c_int32),
+        ("num_chunks", C.c_int32),
+    ]
+
+
 class HgPartialSrc(C.Structure):
     _fields_ = [("o", C.c_void_p), ("m", C.c_void_p), ("l", C.c_void_p), ("nc", C.c_int32), ("reserved", C.c_int32)]
 
@@ -122,6 +136,15 @@ def lib():
         L.hg_kv_evict_copy.restype = C.c_int
         L.hg_kv_evict_finish.argtypes = [vp, vp, vp, vp, i32, vp, C.POINTER(HgAttnDesc)]
         L.hg_kv_evict_finish.restype = C.c_int
+        L.hg_attn_prefix_partial.argtypes = [vp] * 7 + [C.POINTER(HgAttnDesc), C.POINTER(HgPrefixDesc)]
+        L.hg_attn_prefix_partial.restype = C.c_int
+        L.hg_attn_prefix_suggest_chunk.argtypes = [C.c_int64] + [i32] * 5
+        L.hg_attn_prefix_suggest_chunk.restype = i32
+        L.hg_attn_shared_workspace_bytes.argtypes = [C.POINTER(HgAttnDesc), C.POINTER(HgPrefixDesc)]
+        L.hg_attn_shared_workspace_bytes.restype = C.c_size_t
+        L.hg_attn_decode_shared.argtypes = [vp] * 6 + [C.POINTER(HgPartialSrc), i32, vp, vp, vp, C.c_size_t, vp, C.POINTER(HgAttnDesc),
+                                                       C.POINTER(HgPrefixDesc)]
+        L.hg_attn_decode_shared.restype = C.c_int
         L.hg_kv_fork.argtypes = [vp] * 6 + [C.POINTER(HgAttnDesc)]
         L.hg_kv_fork.restype = C.c_int
         L.hg_kv_reserve.argtypes = [vp] * 8 + [C.POINTER(HgAttnDesc)]
@@ -438,6 +461,84 @@ def _pool(t: torch.Tensor, name: str) -> int:
     if t.device.index != torch.cuda.current_device():
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
     return t.data_ptr()
+
+
+def prefix_desc(*, seq_group: torch.Tensor, group_row: torch.Tensor, group_begin: torch.Tensor, group_end: torch.Tensor,
+                chunk_tokens: int, num_chunks: int) -> HgPrefixDesc:
+    """Fill an ``hg_prefix_desc`` (int32 CUDA tensors: seq_group [B], the others [num_groups]); keeps them alive."""
+    d = HgPrefixDesc()
+    d.struct_size = C.sizeof(HgPrefixDesc)
+    d.num_groups = group_row.numel()
+    d.seq_group = _dev(seq_group, "seq_group", torch.int32)
+    d.group_row = _dev(group_row, "group_row", torch.int32)
+    d.group_begin = _dev(group_begin, "group_begin", torch.int32)
+    d.group_end = _dev(group_end, "group_end", torch.int32)
+    if group_begin.numel() != d.num_groups or group_end.numel() != d.num_groups:
+        raise ValueError("group_row, group_begin and group_end must have one element per group")
+    d.chunk_tokens, d.num_chunks = chunk_tokens, num_chunks
+    d._keep = (seq_group, group_row, group_begin, group_end)
+    return d
+
+
+def _check_groups(desc: HgAttnDesc, prefix: HgPrefixDesc) -> None:
+    seq_group = prefix._keep[0]
+    if seq_group.numel() < desc.batch:
+        raise ValueError(f"seq_group has {seq_group.numel()} elements, the batch {desc.batch}")
+    if seq_group.device.index != torch.cuda.current_device():
+        raise ValueError(f"seq_group is on {seq_group.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def hg_attn_prefix_partial(q, k_cache, v_cache, o_part, m_part, l_part, desc: HgAttnDesc, prefix: HgPrefixDesc, stream=None) -> None:
+    """Chunk partials (o, m, l) of the groups' shared prefixes; one more source for ``hg_attn_merge``."""
+    _check_groups(desc, prefix)
+    n = desc.batch * desc.num_q_heads * prefix.num_chunks
+    st = lib().hg_attn_prefix_partial(_here(q, "q"), _pool(k_cache, "k_cache"), _pool(v_cache, "v_cache"),
+                                      _here(o_part, "o_part", torch.float32, n * desc.head_dim),
+                                      _here(m_part, "m_part", torch.float32, n), _here(l_part, "l_part", torch.float32, n),
+                                      _stream(stream), C.byref(desc), C.byref(prefix))
+    _check(st, "hg_attn_prefix_partial")
+
+
+def hg_attn_prefix_suggest_chunk(shared_tokens: int, num_groups: int, num_members: int, num_q_heads: int, num_kv_heads: int,
+                                 page_size: int) -> int:
+    """A chunk size (tokens) for ``hg_attn_prefix_partial``; tokens and members are summed over the groups."""
+    n = int(lib().hg_attn_prefix_suggest_chunk(shared_tokens, num_groups, num_members, num_q_heads, num_kv_heads, page_size))
+    if n == 0:
+        raise HgError(HG_ERR_INVALID_ARG, "hg_attn_prefix_suggest_chunk")
+    return n
+
+
+def hg_attn_shared_workspace_bytes(desc: HgAttnDesc, prefix: HgPrefixDesc) -> int:
+    n = int(lib().hg_attn_shared_workspace_bytes(C.byref(desc), C.byref(prefix)))
+    if n == 0:
+        raise HgError(HG_ERR_INVALID_ARG, "hg_attn_shared_workspace_bytes")
+    return n
+
+
+def _decode_shared_args(q, k_cache, v_cache, seq_lens, tok_begin, tok_end, partials, out, lse, workspace, desc, prefix, stream):
+    _check_groups(desc, prefix)
+    B, rows = desc.batch, desc.batch * desc.num_q_heads
+    arr = _src_array(partials, host=False)
+    return (_here(q, "q"), _pool(k_cache, "k_cache"), _pool(v_cache, "v_cache"), _here(seq_lens, "seq_lens", torch.int32, B),
+            _here(tok_begin, "tok_begin", torch.int32, B), _here(tok_end, "tok_end", torch.int32, B), arr, len(partials),
+            _here(out, "out", torch.float32, rows * desc.head_dim), _here(lse, "lse", torch.float32, rows),
+            _here(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream), C.byref(desc),
+            C.byref(prefix))
+
+
+def hg_attn_decode_shared(q, k_cache, v_cache, seq_lens, tok_begin, tok_end, host_partials, out, lse, workspace, desc: HgAttnDesc,
+                          prefix: HgPrefixDesc, stream=None) -> None:
+    """One decode step over the groups' shared prefixes and every sequence's own tokens [tok_begin, tok_end), merged."""
+    _check(lib().hg_attn_decode_shared(*_decode_shared_args(q, k_cache, v_cache, seq_lens, tok_begin, tok_end, host_partials, out, lse,
+                                                            workspace, desc, prefix, stream)), "hg_attn_decode_shared")
+
+
+def prepare_decode_shared(q, k_cache, v_cache, seq_lens, tok_begin, tok_end, host_partials, out, lse, workspace, desc: HgAttnDesc,
+                          prefix: HgPrefixDesc, stream=None):
+    """``hg_attn_decode_shared`` with its arguments marshalled once (see ``prepare_partial``)."""
+    args = _decode_shared_args(q, k_cache, v_cache, seq_lens, tok_begin, tok_end, host_partials, out, lse, workspace, desc, prefix, stream)
+    keep = (q, k_cache, v_cache, seq_lens, tok_begin, tok_end, host_partials, out, lse, workspace, desc, prefix)
+    return _prepared(lib().hg_attn_decode_shared, args, keep, "hg_attn_decode_shared")
 
 
 def _kv_fork_args(src_row, ref_count, seq_lens, tok_begin, tok_end, desc: HgAttnDesc, stream):
