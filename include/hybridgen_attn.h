@@ -55,7 +55,8 @@ typedef enum hg_dtype { HG_DTYPE_F16 = 0, HG_DTYPE_BF16 = 1 } hg_dtype;
 
 /* bits of hg_attn_desc.flags */
 #define HG_FLAG_NONE 0u
-#define HG_FLAG_TEST_STALL 1u /* testing aid: the loader of hg_attn_partial / hg_kv_read_probe never fills a
+#define HG_FLAG_TEST_STALL 1u /* testing aid: the loader of hg_attn_partial, hg_attn_prefix_partial or
+                                 hg_kv_read_probe never fills a
                                  stage, so every wait runs into its time limit (about 2 s); the call then
                                  reports HG_DEV_WAIT_TIMEOUT through *status and returns normally */
 
@@ -460,7 +461,7 @@ size_t hg_attn_shared_workspace_bytes(const hg_attn_desc* desc, const hg_prefix_
  * result is attention over all of them together; a token that lies in both a group's slice and a member's own counts
  * twice, so tok_begin[b] is usually the group's end.  A sequence without a group simply has all its tokens in
  * [tok_begin, tok_end).  workspace: dev, 256-byte aligned, at least hg_attn_shared_workspace_bytes(); it holds the work
- * counter too, and HG_FLAG_COUNTER_CLEAN speaks about that one (see there).
+ * counter too, which the call clears on its way in any case.
  */
 hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* v_cache, const int32_t* seq_lens,
                                 const int32_t* tok_begin, const int32_t* tok_end, const hg_partial_src* host_partials,

@@ -7,6 +7,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "hg_hostutil.h"
 #include "hg_prefix.cuh"
 
@@ -20,34 +22,84 @@ static hg_status check_prefix(const hg_attn_desc* d, const hg_prefix_desc* x) {
     if (!x->seq_group || !x->group_row || !x->group_begin || !x->group_end) return HG_ERR_INVALID_ARG;
     if (x->num_groups > HG_MAX_GROUPS) return HG_ERR_UNSUPPORTED;
     if (x->chunk_tokens % 128 || x->chunk_tokens % d->page_size) return HG_ERR_UNSUPPORTED;
-    if ((int64_t)d->max_pages * d->page_size > 0x7fffff00ll) return HG_ERR_UNSUPPORTED;       // token positions have 31 bits
+    if ((int64_t)d->max_pages * d->page_size > 0x7fffff00ll) return HG_ERR_UNSUPPORTED;       // token positions have 31 bits,
+    const int64_t rows = (int64_t)d->batch * d->num_q_heads;                                   // and so have partials of a
+    if (rows * x->num_chunks > 0x7fffffffll) return HG_ERR_UNSUPPORTED;                        // call and items of a group
+    if ((rows / 128 + 2ll * d->num_kv_heads) * x->num_chunks > 0x7fffffffll) return HG_ERR_UNSUPPORTED;
+    return HG_OK;
+}
+
+// The pool as in hg_attn_partial, {d within a 64-element half, token in page, half, head, page}, but ONE half a box: the
+// tensor cores want the 128 token rows of a tile's half at one stride, whatever the page size.
+static hg_status make_prefix_maps(const hg_attn_desc* d, const void* k, const void* v, CUtensorMap* tk, CUtensorMap* tv) {
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return HG_ERR_CUDA;
+    cuuint64_t dims[5] = {64, (cuuint64_t)d->page_size, (cuuint64_t)(d->head_dim / 64), (cuuint64_t)d->num_kv_heads, (cuuint64_t)d->num_pages};
+    cuuint64_t strides[4] = {(cuuint64_t)d->tok_stride * 2u, 128u, (cuuint64_t)d->head_stride * 2u, (cuuint64_t)d->page_stride * 2u};
+    if (d->num_kv_heads == 1) strides[2] = strides[0];     // unused dimensions still need a legal stride
+    if (d->num_pages == 1) strides[3] = strides[0];
+    cuuint32_t box[5] = {64, (cuuint32_t)(d->page_size < PFX_TILE ? d->page_size : PFX_TILE), 1, 1, 1};
+    cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    const CUtensorMapDataType dt = d->dtype == HG_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const void* base[2] = {k, v};
+    CUtensorMap* out[2] = {tk, tv};
+    for (int i = 0; i < 2; ++i)
+        if (enc(out[i], dt, 5, const_cast<void*>(base[i]), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return HG_ERR_UNSUPPORTED;   // a stride pattern the TMA unit cannot express
     return HG_OK;
 }
 
 template <int D, bool BF16>
-static hg_status launch_prefix(const PrefixParams& p, cudaStream_t st) {
-    const int row_blocks = (int)(((long long)p.B * p.G + PFX_ROWS - 1) / PFX_ROWS);
-    prefix_partial_kernel<D, BF16><<<dim3((unsigned)p.NC, (unsigned)(p.Hkv * row_blocks), (unsigned)(p.NG + 1)), PFX_THREADS, 0, st>>>(p, row_blocks);
-    return cudaGetLastError() == cudaSuccess ? HG_OK : HG_ERR_CUDA;
+static hg_status launch_prefix(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, cudaStream_t st, bool pdl) {
+    static std::atomic<int> sms_of[kMaxDevices];           // set once the device's shared-memory opt-in is in force; zero-initialised
+    auto kern = prefix_partial_kernel<D, BF16>;
+    constexpr size_t smem = pfx_smem_bytes<D>();
+    static_assert(smem <= 227 * 1024, "shared memory of one SM");
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return HG_ERR_CUDA; }
+    int sms = sms_of[dev].load(std::memory_order_acquire);
+    if (sms == 0) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+            cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) {
+            cudaGetLastError();
+            return HG_ERR_CUDA;
+        }
+        sms_of[dev].store(sms, std::memory_order_release);   // racing threads store the same value
+    }
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3((unsigned)sms); cfg.blockDim = dim3(PFX_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = pdl ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, kern, tk, tv, p) != cudaSuccess) { cudaGetLastError(); return HG_ERR_CUDA; }
+    return HG_OK;
 }
 
-static hg_status run_prefix(const void* q, const void* k, const void* v, float* o_part, float* m_part, float* l_part, void* stream,
-                            const hg_attn_desc* d, const hg_prefix_desc* x) {
+static hg_status run_prefix(const void* q, const void* k, const void* v, float* o_part, float* m_part, float* l_part, int32_t* zero,
+                            void* stream, const hg_attn_desc* d, const hg_prefix_desc* x) {
     PrefixParams p;
     memset(&p, 0, sizeof p);
-    p.q = static_cast<const uint16_t*>(q); p.k = static_cast<const uint16_t*>(k); p.v = static_cast<const uint16_t*>(v);
+    CUtensorMap tk, tv;
+    hg_status st = make_prefix_maps(d, k, v, &tk, &tv);
+    if (st != HG_OK) return st;
+    p.q = static_cast<const uint16_t*>(q);
     p.block_table = d->block_table; p.seq_group = x->seq_group; p.group_row = x->group_row;
     p.group_begin = x->group_begin; p.group_end = x->group_end;
-    p.o_part = o_part; p.m_part = m_part; p.l_part = l_part; p.status = d->status;
-    p.page_stride = d->page_stride; p.head_stride = d->head_stride; p.tok_stride = d->tok_stride;
+    p.o_part = o_part; p.m_part = m_part; p.l_part = l_part; p.status = d->status; p.zero = zero;
     p.B = d->batch; p.Hq = d->num_q_heads; p.Hkv = d->num_kv_heads; p.G = p.Hq / p.Hkv;
     p.NG = x->num_groups; p.NC = x->num_chunks; p.C = x->chunk_tokens;
     p.page_size = d->page_size; p.page_shift = ilog2_exact(d->page_size); p.max_pages = d->max_pages; p.num_pages = d->num_pages;
     p.sparse_empty = (d->flags & HG_FLAG_SPARSE_EMPTY) ? 1 : 0;
+    p.test_stall = (d->flags & HG_FLAG_TEST_STALL) ? 1 : 0;
     p.scale = d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->head_dim);
+    p.scale_log2 = p.scale * 1.4426950408889634f;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
-    if (d->head_dim == 128) return d->dtype == HG_DTYPE_BF16 ? launch_prefix<128, true>(p, cs) : launch_prefix<128, false>(p, cs);
-    return d->dtype == HG_DTYPE_BF16 ? launch_prefix<64, true>(p, cs) : launch_prefix<64, false>(p, cs);
+    const bool bf16 = d->dtype == HG_DTYPE_BF16, pdl = !desc_tune(d).off(HG_TUNE_NO_PDL);
+    if (d->head_dim == 128) return bf16 ? launch_prefix<128, true>(tk, tv, p, cs, pdl) : launch_prefix<128, false>(tk, tv, p, cs, pdl);
+    return bf16 ? launch_prefix<64, true>(tk, tv, p, cs, pdl) : launch_prefix<64, false>(tk, tv, p, cs, pdl);
 }
 
 // Workspace of the joined step: the shared partials in front, behind them what hg_attn_decode's partial half needs.
@@ -80,7 +132,7 @@ hg_status hg_attn_prefix_partial(const void* q, const void* k_cache, const void*
     if (st != HG_OK) return st;
     if (!q || !k_cache || !v_cache || !o_part || !m_part || !l_part) return HG_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(o_part)) return HG_ERR_INVALID_ARG;
-    return run_prefix(q, k_cache, v_cache, o_part, m_part, l_part, stream, desc, prefix);
+    return run_prefix(q, k_cache, v_cache, o_part, m_part, l_part, nullptr, stream, desc, prefix);
 }
 
 int32_t hg_attn_prefix_suggest_chunk(int64_t shared_tokens, int32_t num_groups, int32_t num_members, int32_t num_q_heads,
@@ -119,8 +171,10 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
     dd.struct_size = sizeof dd;
     dd.flags |= HG_FLAG_SPARSE_EMPTY;                                  // the partials are private to this call and its merge
     dd.sched_counter = reinterpret_cast<int32_t*>(ws + w.sched);
-    st = run_prefix(q, k_cache, v_cache, at(w.po), at(w.pm), at(w.pl), stream, &dd, prefix);
+    // the shared kernel clears the work counter on its way, so that no clearing stands between it and the own partials' kernel
+    st = run_prefix(q, k_cache, v_cache, at(w.po), at(w.pm), at(w.pl), dd.sched_counter, stream, &dd, prefix);
     if (st != HG_OK) return st;
+    dd.flags |= HG_FLAG_COUNTER_CLEAN;
     st = hg_attn_partial(q, k_cache, v_cache, seq_lens, tok_begin, tok_end, at(w.o), at(w.m), at(w.l), stream, &dd);
     if (st != HG_OK) return st;
     hg_partial_src src[HG_MAX_MERGE_SRC];

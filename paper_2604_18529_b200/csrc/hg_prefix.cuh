@@ -4,19 +4,33 @@
 // group's members, G per member, are the rows of a matrix Q (R = members x G rows), and per chunk of tokens
 //     S = Q K^T,   m = row max of scale S,   P = e^{scale S - m},   l = row sum of P,   o = P V
 // is what hg_attn_partial computes for one sequence at a time, with K and V read once instead of once per member.
+// Both products run on tcgen05.mma with their accumulators in tensor memory; P is carried as hi + lo 16-bit terms (two
+// products), so the arithmetic is 1.5 times that of a single-term P: up to about 230 rows per KV head the stream of K and V
+// from HBM is the bound, above that the tensor cores.
+//
+// One CTA per SM, persistent.  It runs two STREAMS, each with 128 rows: a tile of 128 tokens is S (128 x 128 fp32 in
+// tensor memory), turned by the stream's four softmax warps (a thread owns a row) into P in the same columns (32 columns
+// of S give 16 of hi and 16 of lo terms), which is the A operand of P V.  While one stream's warps do exponentials, the
+// tensor cores work for the other.  A work item is
+//   wide    (group, chunk, KV head, 256 rows; the streams share every K and V tile), for more than 128 rows;
+//   narrow  (group, two chunks, KV head, up to 128 rows; the streams share Q and take a chunk each).
+// So few rows never leave a stream idle, and no stream's result has to be combined with the other's.
+//
+// Roles: warps 0-7 softmax and epilogue; 8 and 9 load K and V tiles (TMA, a page of 16 to 128 tokens and 64 components
+// a box, a ring of tiles that alternates K and V); 10 issues the products; 11 decodes the work items and gathers the
+// members; 12-15 gather the query rows.  Every wait is bounded.
 #pragma once
 
 #include <cuda_runtime.h>
 #include <stdint.h>
 
 #include "hg_device.cuh"
+#include "hg_tcgen05.cuh"
 
 namespace hg {
 
 struct PrefixParams {
     const uint16_t* q;               // [B][Hq][D]
-    const uint16_t* k;
-    const uint16_t* v;
     const int32_t* block_table;      // [B][max_pages], or NULL: identity paging
     const int32_t* seq_group;        // [B]
     const int32_t* group_row;        // [NG]
@@ -26,15 +40,15 @@ struct PrefixParams {
     float* m_part;                   // [B][Hq][NC]
     float* l_part;
     int32_t* status;
-    int64_t page_stride, head_stride, tok_stride;
+    int32_t* zero;                   // two words to clear on the way (the work counter of the launch that follows), or NULL
     int B, Hq, Hkv, G, NG, NC, C;
     int page_size, page_shift, max_pages, num_pages;
-    int sparse_empty;
-    float scale;
+    int sparse_empty, test_stall;
+    float scale, scale_log2;
 };
 
 // The slice of a group, clamped to its block-table row, and its chunks.
-struct GroupSlice { int row, begin, end, chunk0, nc; bool bad; };
+struct GroupSlice { int row, begin, end, nc; bool bad; };
 
 __device__ __forceinline__ GroupSlice group_slice(const PrefixParams& p, int g) {
     GroupSlice s;
@@ -45,111 +59,595 @@ __device__ __forceinline__ GroupSlice group_slice(const PrefixParams& p, int g) 
     const long long room = (long long)p.max_pages << p.page_shift;
     if (s.end > room) { s.end = (int)room; s.bad = true; }
     if (s.end > s.begin && (s.row < 0 || s.row >= p.B)) { s.end = s.begin; s.bad = true; }
-    s.chunk0 = s.begin / p.C;
-    s.nc = s.end > s.begin ? min((s.end - 1) / p.C - s.chunk0 + 1, p.NC) : 0;
+    s.nc = s.end > s.begin ? min((s.end - 1) / p.C - s.begin / p.C + 1, p.NC) : 0;
     return s;
 }
 
-constexpr int PFX_ROWS = 32, PFX_TOK = 16, PFX_THREADS = 256;
+constexpr int PFX_TILE = 128;                 // tokens per tile, rows per stream
+constexpr int PFX_THREADS = 512;
+constexpr int PFX_K_WARP = 8, PFX_V_WARP = 9, PFX_MMA_WARP = 10, PFX_ITEM_WARP = 11, PFX_Q_WARP = 12;
+constexpr int PFX_MAX_SLOTS = 10;
+constexpr int PFX_MAX_GROUPS = 512;
+constexpr uint32_t PFX_S_COL = 0, PFX_O_COL = 256;      // tensor memory: S / P of the streams, 128 columns each, then their O
 
-// One CTA per (chunk, KV head and block of 32 rows, group); group NG stands for the sequences without one.
+template <int D> __host__ __device__ constexpr int pfx_tile_bytes() { return PFX_TILE * D * 2; }
+template <int D> __host__ __device__ constexpr int pfx_slots() { return D == 128 ? 5 : 10; }
+
+// One work item, published by the item warp.
+struct PfxItem {
+    int valid;                       // 0: no more items
+    int row, h;                      // block-table row, KV head
+    int wide;
+    int chunk;                       // chunk slot of stream 0 (stream 1: the same, or the next one)
+    int r0, rows;                    // first row of the group, rows in this item
+    int m0;                          // number of the first member in `members`
+    int lo[2], hi[2];                // the streams' tokens
+    int tiles[2];
+};
+
+struct PfxCtl {
+    uint64_t full[PFX_MAX_SLOTS], empty[PFX_MAX_SLOTS];
+    uint64_t s_full[2], p_full[2], o_full[2];
+    uint64_t q_full, q_free, drain;
+    uint64_t item_full[2], item_empty[2];
+    PfxItem item[2];
+    uint32_t tmem;
+    int abort;
+    uint8_t bad[16];                 // per tile, in load order: 16-token pieces of the tile whose page was refused
+    uint8_t stream_bad[2];           // the same for the tile a stream's softmax warps are about to read
+    uint16_t members[2][256];        // sequences of the item's rows, in ascending order
+    uint16_t group_n[PFX_MAX_GROUPS];
+};
+
+template <int D> constexpr size_t pfx_smem_bytes() {
+    return (size_t)(2 + pfx_slots<D>()) * pfx_tile_bytes<D>() + sizeof(PfxCtl);
+}
+
+// First token of a stream's tile i, and the number of tile (stream s, i) in the order in which tiles are loaded.
+__device__ __forceinline__ int pfx_tile_token(const PfxItem& it, int s, int i) { return (it.lo[s] & ~(PFX_TILE - 1)) + i * PFX_TILE; }
+__device__ __forceinline__ int pfx_tile_index(const PfxItem& it, int s, int i) {
+    if (it.wide) return i;
+    return s == 0 ? i + min(i, it.tiles[1]) : min(i + 1, it.tiles[0]) + i;
+}
+__device__ __forceinline__ int pfx_total_tiles(const PfxItem& it) { return it.wide ? it.tiles[0] : it.tiles[0] + it.tiles[1]; }
+
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+
+// Two weights -> packed hi terms (rounded) and packed lo terms (what that left, rounded): at most 2^-18 (bf16) or 2^-24
+// (fp16) of a weight is lost.
+template <bool BF16>
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+    hi = pack2<BF16>(a, b);
+    const float2 f = unpack2<BF16>(hi);
+    lo = pack2<BF16>(a - f.x, b - f.y);
+}
+
+__device__ __forceinline__ void st_global_hint4(float* addr, float4 v, uint64_t policy) {
+    asm volatile("st.global.L2::cache_hint.v4.f32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "l"(policy)
+                 : "memory");
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
 template <int D, bool BF16>
-__global__ void __launch_bounds__(PFX_THREADS) prefix_partial_kernel(const PrefixParams p, int row_blocks) {
+__global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                                                                         const PrefixParams p) {
+    constexpr int S = pfx_slots<D>();
+    constexpr int TILE_BYTES = pfx_tile_bytes<D>();
+    constexpr int HALVES = D / 64;
+    constexpr uint32_t HALF_BYTES = PFX_TILE * 128;
+    constexpr uint32_t FMT = BF16 ? 1u : 0u;
+    // instruction descriptors: fp32 accumulator, 16-bit A and B, M = 128; S: both K-major, N = 128 tokens; O: B (V) with
+    // its components contiguous (N-major), N = D
+    constexpr uint32_t IDESC_S = (1u << 4) | (FMT << 7) | (FMT << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+    constexpr uint32_t IDESC_O = (1u << 4) | (FMT << 7) | (FMT << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
     const float NEG_INF = __int_as_float(0xff800000);
-    __shared__ float qs[PFX_ROWS][D + 1], ks[PFX_TOK][D + 1], vs[PFX_TOK][D], ss[PFX_ROWS][PFX_TOK + 1];
-    __shared__ int rows[PFX_ROWS], phys[PFX_TOK];
-    const int tid = threadIdx.x, g = blockIdx.z, c = blockIdx.x, h = blockIdx.y / row_blocks, rb = blockIdx.y % row_blocks;
-    if (tid < PFX_ROWS) {
-        // row r of the group: head r % G of its member number r / G
-        const int r = rb * PFX_ROWS + tid, want = r / p.G;
-        int found = -1, n = 0;
-        for (int b = 0; b < p.B; ++b) {
-            const int sg = p.seq_group[b];
-            const bool in = g < p.NG ? sg == g : (sg < 0 || sg >= p.NG);
-            if (in && n++ == want) found = b;
+
+    extern __shared__ __align__(1024) uint8_t pfx_raw[];
+    uint8_t* const ring = pfx_raw + 2 * TILE_BYTES;                // Q of the two streams in front
+    PfxCtl& ctl = *reinterpret_cast<PfxCtl*>(pfx_raw + (2 + S) * TILE_BYTES);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int* const abort_flag = &ctl.abort;
+
+    if (tid == 0) {
+        prefetch_tensormap(&tmK);
+        prefetch_tensormap(&tmV);
+        for (int i = 0; i < S; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&ctl.s_full[s], 2);                          // the products' completion, and the tile's description
+            mbar_init(&ctl.p_full[s], 4);
+            mbar_init(&ctl.o_full[s], 1);
+            mbar_init(&ctl.item_full[s], 1);
+            mbar_init(&ctl.item_empty[s], 8 + 3 + 4);
         }
-        rows[tid] = found < 0 ? -1 : found * p.Hq + h * p.G + r % p.G;
+        mbar_init(&ctl.q_full, 4);
+        mbar_init(&ctl.q_free, 1);
+        mbar_init(&ctl.drain, 1);
+        ctl.abort = 0;
+        fence_barrier_init();
+    }
+    if (warp == PFX_MMA_WARP) {
+        tmem_alloc(&ctl.tmem, 512);
+        tmem_relinquish();
+    }
+    int* const count = reinterpret_cast<int*>(pfx_raw);            // (Q's place: nothing else writes there before the first item)
+    for (int g = tid; g < p.NG; g += PFX_THREADS) count[g] = 0;
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&ctl.tmem);
+
+    cudaTriggerProgrammaticLaunchCompletion();
+    cudaGridDependencySynchronize();
+    const bool skip = p.status && (*reinterpret_cast<volatile int32_t*>(p.status) & HG_DEV_WAIT_TIMEOUT);
+    for (int b = tid; b < p.B; b += PFX_THREADS) {
+        const uint32_t g = (uint32_t)p.seq_group[b];
+        if (g < (uint32_t)p.NG) atomicAdd(&count[g], 1);
+    }
+    if (blockIdx.x == 0 && p.zero && tid < 2) p.zero[tid] = 0;
+    __syncthreads();
+    for (int g = tid; g < p.NG; g += PFX_THREADS) {
+        ctl.group_n[g] = (uint16_t)count[g];
+        if (blockIdx.x == 0 && p.status && group_slice(p, g).bad) atomicOr(p.status, HG_DEV_RANGE);
     }
     __syncthreads();
-    if (rows[0] < 0) return;
-    GroupSlice sl;
-    sl.nc = 0;
-    if (g < p.NG) {
-        sl = group_slice(p, g);
-        if (sl.bad && tid == 0 && p.status) atomicOr(p.status, HG_DEV_RANGE);
-    }
-    if (c >= sl.nc) {
-        for (int r = 0; r < PFX_ROWS && rows[r] >= 0; ++r) {
-            const size_t slot = (size_t)rows[r] * p.NC + c;
-            if (tid == 0) { p.m_part[slot] = NEG_INF; p.l_part[slot] = 0.f; }
-            if (!p.sparse_empty && tid < D) p.o_part[slot * D + tid] = 0.f;
-        }
-        return;
-    }
-    const int t_lo = max(sl.begin, (sl.chunk0 + c) * p.C), t_hi = min(sl.end, (sl.chunk0 + c + 1) * p.C);
-    for (int i = tid; i < PFX_ROWS * D; i += PFX_THREADS) {
-        const int r = i / D, d = i % D;
-        float x = 0.f;
-        if (rows[r] >= 0) {
-            const uint16_t w = p.q[(size_t)rows[r] * D + d];
-            x = unpack2<BF16>((uint32_t)w).x;
-        }
-        qs[r][d] = x;
-    }
-    const int row = tid / 8, part = tid % 8;                       // eight threads per row
-    constexpr int PER = D / 8;
-    float acc[PER], m = NEG_INF, l = 0.f;
-    for (int i = 0; i < PER; ++i) acc[i] = 0.f;
-    for (int t0 = t_lo; t0 < t_hi; t0 += PFX_TOK) {
-        const int n = min(PFX_TOK, t_hi - t0);
-        __syncthreads();
-        if (tid < n) {
-            const int pg = (t0 + tid) >> p.page_shift;
-            int e = p.block_table ? p.block_table[(size_t)sl.row * p.max_pages + pg] : sl.row * p.max_pages + pg;
-            if (e < 0 || e >= p.num_pages) { e = -1; if (p.status) atomicOr(p.status, HG_DEV_BAD_PAGE); }
-            phys[tid] = e;
-        }
-        __syncthreads();
-        for (int i = tid; i < n * D; i += PFX_THREADS) {
-            const int t = i / D, d = i % D;
-            float a = 0.f, b = 0.f;
-            if (phys[t] >= 0) {
-                const int64_t off = (int64_t)phys[t] * p.page_stride + (int64_t)h * p.head_stride +
-                                    (int64_t)((t0 + t) & (p.page_size - 1)) * p.tok_stride + d;
-                a = unpack2<BF16>((uint32_t)p.k[off]).x;
-                b = unpack2<BF16>((uint32_t)p.v[off]).x;
+
+    int issued = 0;                                                // (loaders) tiles requested so far
+    if (skip) {
+        // an earlier call timed out: no work until the caller has cleared the word
+    } else if (warp == PFX_ITEM_WARP) {
+        // =============================== item warp: decodes work items, one ahead ===============================
+        int gb = 0;                                                // first of the 32 groups in the lanes
+        long long base = 0;                                        // items of the groups before them
+        GroupSlice sl;
+        int R = 0, wide_tiles = 0, narrow_rows = 0, n_items = 0, before = 0, block_items = 0;
+        auto load_groups = [&]() {
+            n_items = 0;
+            sl.nc = 0;
+            if (gb + lane < p.NG) {
+                sl = group_slice(p, gb + lane);
+                R = ctl.group_n[gb + lane] * p.G;
+                const int rem = R % 256;
+                wide_tiles = R / 256 + (rem > 128 ? 1 : 0);
+                narrow_rows = rem <= 128 ? rem : 0;
+                n_items = p.Hkv * (wide_tiles * sl.nc + (narrow_rows > 0 ? (sl.nc + 1) / 2 : 0));
             }
-            ks[t][d] = a;
-            vs[t][d] = b;
+            int x = n_items;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, x, o);
+                if (lane >= o) x += y;
+            }
+            before = x - n_items;
+            block_items = __shfl_sync(0xffffffffu, x, 31);
+        };
+        load_groups();
+        bool ok = true;
+        int k = 0;
+        for (long long i = blockIdx.x; ok; i += gridDim.x, ++k) {
+            while (gb < p.NG && i >= base + block_items) { base += block_items; gb += 32; load_groups(); }
+            const int j = k & 1;
+            if (k >= 2) ok = warp_wait(&ctl.item_empty[j], (uint32_t)((k - 2) >> 1) & 1u, abort_flag);
+            if (!ok) break;
+            PfxItem& it = ctl.item[j];
+            if (gb >= p.NG) {
+                if (lane == 0) { it.valid = 0; mbar_arrive(&ctl.item_full[j]); }
+                break;
+            }
+            const int at = (int)(i - base);
+            const bool mine = at >= before && at < before + n_items;
+            const int src = __ffs(__ballot_sync(0xffffffffu, mine)) - 1;
+            int m0 = 0, members = 0;
+            if (mine) {
+                int e = at - before;
+                const int wides = p.Hkv * wide_tiles * sl.nc;
+                it.valid = 1;
+                it.row = sl.row;
+                const int chunk0 = sl.begin / p.C;
+                int c;
+                if (e < wides) {                                   // row tiles fastest: CTAs side by side read the same tiles
+                    const int t = e % wide_tiles; e /= wide_tiles;
+                    it.h = e % p.Hkv; c = e / p.Hkv;
+                    it.wide = 1;
+                    it.r0 = t * 256;
+                    it.rows = min(256, R - it.r0);
+                } else {
+                    e -= wides;
+                    it.h = e % p.Hkv; c = e / p.Hkv * 2;
+                    it.wide = 0;
+                    it.r0 = R / 256 * 256;
+                    it.rows = narrow_rows;
+                }
+                it.chunk = c;
+                for (int s = 0; s < 2; ++s) {
+                    const int cs = it.wide ? c : c + s;
+                    it.lo[s] = max(sl.begin, (chunk0 + cs) * p.C);
+                    it.hi[s] = cs < sl.nc ? (int)min((long long)sl.end, (long long)(chunk0 + cs + 1) * p.C) : it.lo[s];
+                    it.tiles[s] = it.hi[s] > it.lo[s] ? (it.hi[s] - (it.lo[s] & ~(PFX_TILE - 1)) + PFX_TILE - 1) / PFX_TILE : 0;
+                }
+                m0 = it.r0 / p.G;
+                members = (it.r0 + it.rows - 1) / p.G - m0 + 1;
+                it.m0 = m0;
+            }
+            m0 = __shfl_sync(0xffffffffu, m0, src);
+            members = __shfl_sync(0xffffffffu, members, src);
+            const int g = gb + src;
+            int seen = 0;                                          // members met so far
+            for (int b0 = 0; b0 < p.B && seen < m0 + members; b0 += 128) {
+                int sg[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) sg[u] = b0 + u * 32 + lane < p.B ? p.seq_group[b0 + u * 32 + lane] : -1;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t in = __ballot_sync(0xffffffffu, sg[u] == g);
+                    const int r = seen + __popc(in & ((1u << lane) - 1u)) - m0;
+                    if (sg[u] == g && r >= 0 && r < members) ctl.members[j][r] = (uint16_t)(b0 + u * 32 + lane);
+                    seen += __popc(in);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.item_full[j]);
         }
-        __syncthreads();
-        float mx = NEG_INF;
-        for (int t = part; t < n; t += 8) {
-            float s = 0.f;
-            for (int d = 0; d < D; ++d) s = fmaf(qs[row][d], ks[t][d], s);
-            s = phys[t] >= 0 ? s * p.scale : NEG_INF;
-            ss[row][t] = s;
-            mx = fmaxf(mx, s);
+    } else if (warp == PFX_K_WARP || warp == PFX_V_WARP) {
+        // =============================== loaders: K tiles and V tiles, alternately in the ring ===============================
+        const bool is_k = warp == PFX_K_WARP;
+        const CUtensorMap* const tm = is_k ? &tmK : &tmV;
+        const uint64_t policy = l2_evict_first_policy();
+        const int box_rows = min(p.page_size, PFX_TILE), boxes = PFX_TILE / box_rows * HALVES;
+        const int piece = lane / HALVES, half = lane % HALVES;     // this lane's box: a page (or part of one) and a half
+        bool ok = true;
+        int n = 0;                                                 // tiles of earlier items
+        for (int k = 0; ok; ++k) {
+            const int j = k & 1;
+            ok = warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
+            if (!ok) break;
+            const PfxItem it = ctl.item[j];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.item_empty[j]);
+            if (!it.valid) break;
+            const int total = pfx_total_tiles(it), both = min(it.tiles[0], it.tiles[1]);
+            // the block-table entry of this lane's box of tile x (in load order); -1: not wanted, -2: refused
+            int lo = 0, hi = 0, t = 0;
+            auto entry = [&](int x) -> int {
+                int s = 0, i = x;
+                if (!it.wide) {
+                    if (x < 2 * both) { s = x & 1; i = x >> 1; }
+                    else { s = it.tiles[0] > both ? 0 : 1; i = x - both; }
+                }
+                lo = it.lo[s]; hi = it.hi[s];
+                t = pfx_tile_token(it, s, i) + piece * box_rows;
+                if (lane >= boxes || x >= total || t >= hi || t + box_rows <= lo) return -1;
+                const int e = p.block_table ? p.block_table[(size_t)it.row * p.max_pages + (t >> p.page_shift)]
+                                            : it.row * p.max_pages + (t >> p.page_shift);
+                return (uint32_t)e < (uint32_t)p.num_pages ? e : -2;
+            };
+            int next = entry(0), next_t = t;
+            for (int x = 0; x < total; ++x) {
+                const int e = next, row = next_t & (p.page_size - 1);
+                next = entry(x + 1);                               // one tile ahead: the look-up is not waited for
+                next_t = t;
+                const int seq = 2 * (n + x) + (is_k ? 0 : 1), slot = seq % S;
+                const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, e >= 0)) * (uint32_t)box_rows * 128u;
+                uint32_t bad = 0;
+                if (__any_sync(0xffffffffu, e == -2)) {
+                    if (e == -2) {
+                        bad = ((1u << (box_rows >> 4)) - 1u) << (piece * (box_rows >> 4));
+                        if (p.status && is_k) atomicOr(p.status, HG_DEV_BAD_PAGE);
+                    }
+                    bad = __reduce_or_sync(0xffffffffu, bad);
+                }
+                if (seq >= S) ok = warp_wait(&ctl.empty[slot], (uint32_t)(seq / S - 1) & 1u, abort_flag);
+                if (!ok || p.test_stall) break;
+                if (lane == 0) {
+                    if (is_k) ctl.bad[(n + x) & 15] = (uint8_t)bad;
+                    mbar_arrive_expect_tx(&ctl.full[slot], bytes);
+                }
+                if (e >= 0)
+                    tma_load_5d(ring + slot * TILE_BYTES + half * HALF_BYTES + piece * box_rows * 128, tm, &ctl.full[slot], 0, row, half, it.h, e, policy);
+                issued = n + x + 1;
+            }
+            n += total;
+            if (p.test_stall) break;
         }
-        for (int o = 1; o < 8; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    } else if (warp == PFX_MMA_WARP) {
+        // =============================== tensor-core warp ===============================
+        // (all lanes follow the same control flow; lane 0 issues)
+        bool ok = true;
+        int n = 0;                                                 // tiles of earlier items
+        uint32_t np[2] = {0, 0};                                   // P tiles taken per stream
+        bool held = false;                                         // stream 1's last product of the item before is still to come
+        PfxItem prev;
+        int prev_n = 0;
+        const uint64_t q_desc = tc_smem_desc(smem_u32(pfx_raw), 16u, 1024u, 2u);
+        const uint64_t k_desc = tc_smem_desc(smem_u32(ring), 16u, 1024u, 2u);
+        const uint64_t v_desc = tc_smem_desc(smem_u32(ring), HALF_BYTES, 1024u, 2u);
+        auto scores = [&](const PfxItem& it, int s, int i, bool last) {        // S = Q K^T of a stream's tile
+            const int x = n + pfx_tile_index(it, s, i), seq = 2 * x, slot = seq % S;
+            ok = warp_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
+            if (!ok) return;
+            if (lane == 0) {
+                ctl.stream_bad[s] = ctl.bad[x & 15];
+                tc_fence_after_sync();
+                const uint64_t a = q_desc + (uint64_t)((it.wide ? s : 0) * TILE_BYTES >> 4), b = k_desc + (uint64_t)(slot * TILE_BYTES >> 4);
+                const uint32_t acc = tmem + PFX_S_COL + s * 128;
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) {              // 16 components: 32 bytes of a 128-byte row, halves apart
+                    const uint32_t off = (uint32_t)((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4;
+                    tc_mma_f16(acc, a + off, b + off, IDESC_S, kk ? 1u : 0u);
+                }
+                if (!it.wide || s == 1) tc_commit(&ctl.empty[slot]);
+                if (last) tc_commit(&ctl.q_free);
+                tc_commit(&ctl.s_full[s]);
+                mbar_arrive(&ctl.s_full[s]);
+            }
+            __syncwarp();
+        };
+        auto values = [&](const PfxItem& it, int n0, int s, int i) {           // O += P V of a stream's tile
+            ok = warp_wait(&ctl.p_full[s], np[s] & 1u, abort_flag);
+            if (!ok) return;
+            ++np[s];
+            const int x = n0 + pfx_tile_index(it, s, i), seq = 2 * x + 1, slot = seq % S;
+            ok = warp_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
+            if (!ok) return;
+            const int t = pfx_tile_token(it, s, i);
+            const int c_lo = max(it.lo[s] - t, 0), c_hi = min(it.hi[s] - t, PFX_TILE);
+            const uint32_t bad = ctl.bad[x & 15];
+            if ((c_lo > 0 || c_hi < PFX_TILE || bad) && (!it.wide || s == 0)) {
+                // rows outside the slice, and of refused pages, hold anything (NaN patterns among it): weight 0 times that
+                // must be 0, so clear them (whole 128-byte rows: the swizzle does not matter)
+                uint8_t* const v = ring + slot * TILE_BYTES;
+                for (int u = lane; u < PFX_TILE * HALVES * 8; u += 32) {
+                    const int r = (u >> 3) % PFX_TILE, hf = (u >> 3) / PFX_TILE;
+                    if (r < c_lo || r >= c_hi || ((bad >> (r >> 4)) & 1u)) sts128_zero(smem_u32(v) + hf * HALF_BYTES + r * 128 + (u & 7) * 16);
+                }
+                fence_proxy_async();
+                __syncwarp();
+            }
+            if (lane == 0) {
+                tc_fence_after_sync();
+                const uint64_t b = v_desc + (uint64_t)(slot * TILE_BYTES >> 4);
+                const uint32_t acc = tmem + PFX_O_COL + s * 128, a = tmem + PFX_S_COL + s * 128;
+#pragma unroll
+                for (int kk = 0; kk < PFX_TILE / 16; ++kk) {       // 16 tokens: 8 columns of hi terms, 16 further on their lo terms
+                    const uint32_t ac = a + (kk >> 1) * 32 + (kk & 1) * 8;
+                    tc_mma_f16_ta(acc, ac, b + (uint64_t)(kk * 2048 >> 4), IDESC_O, (i | kk) ? 1u : 0u);
+                    tc_mma_f16_ta(acc, ac + 16, b + (uint64_t)(kk * 2048 >> 4), IDESC_O, 1u);
+                }
+                if (!it.wide || s == 1) tc_commit(&ctl.empty[slot]);
+                if (i == it.tiles[s] - 1) tc_commit(&ctl.o_full[s]);
+            }
+            __syncwarp();
+        };
+        for (int k = 0; ok; ++k) {
+            const int j = k & 1;
+            ok = warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
+            if (!ok) break;
+            const PfxItem it = ctl.item[j];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.item_empty[j]);
+            if (!it.valid) break;
+            ok = warp_wait(&ctl.q_full, (uint32_t)k & 1u, abort_flag);
+            if (!ok) break;
+            int left = it.tiles[0] + it.tiles[1];                  // score products still to issue
+            if (it.tiles[0] > 0) scores(it, 0, 0, --left == 0);
+            if (ok && held) values(prev, prev_n, 1, prev.tiles[1] - 1);
+            held = false;
+            if (ok && it.tiles[1] > 0) scores(it, 1, 0, --left == 0);
+            const int steps = max(it.tiles[0], it.tiles[1]);
+            for (int i = 0; i < steps && ok; ++i) {
+                if (i < it.tiles[0]) {
+                    values(it, n, 0, i);
+                    if (ok && i + 1 < it.tiles[0]) scores(it, 0, i + 1, --left == 0);
+                }
+                if (ok && i < it.tiles[1]) {
+                    if (i + 1 == steps) { held = true; break; }    // behind the next item's first scores
+                    values(it, n, 1, i);
+                    if (ok && i + 1 < it.tiles[1]) scores(it, 1, i + 1, --left == 0);
+                }
+            }
+            prev = it;
+            prev_n = n;
+            n += pfx_total_tiles(it);
+        }
+        if (ok && held) values(prev, prev_n, 1, prev.tiles[1] - 1);
+        if (lane == 0) {                                           // nothing is in flight when the tensor memory is given back
+            int none = 0;
+            tc_commit(&ctl.drain);
+            mbar_wait(&ctl.drain, 0u, &none);
+        }
         __syncwarp();
-        if (mx > m) {
-            const float r = expf(m - mx);
-            l *= r;
-            for (int i = 0; i < PER; ++i) acc[i] *= r;
-            m = mx;
-        }
-        if (m != NEG_INF)
-            for (int t = 0; t < n; ++t) {
-                const float w = expf(ss[row][t] - m);
-                l += w;
-                for (int i = 0; i < PER; ++i) acc[i] = fmaf(w, vs[t][i * 8 + part], acc[i]);
+    } else if (warp >= PFX_Q_WARP) {
+        // =============================== query rows, gathered into the 128-byte-swizzled A tiles ===============================
+        const int t = tid - PFX_Q_WARP * 32;
+        constexpr int VECS = D / 8;                                // 16-byte vectors per row
+        bool ok = true;
+        for (int k = 0; ok; ++k) {
+            const int j = k & 1;
+            ok = warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
+            if (!ok || !ctl.item[j].valid) break;
+            const int rows = ctl.item[j].rows, r0 = ctl.item[j].r0, m0 = ctl.item[j].m0, h = ctl.item[j].h;
+            if (k >= 1) ok = warp_wait(&ctl.q_free, (uint32_t)(k - 1) & 1u, abort_flag);
+            if (!ok) break;
+            const int c = t % VECS;
+            for (int r = t / VECS; r < rows; r += 128 / VECS) {
+                const int m = (r0 + r) / p.G, head = h * p.G + (r0 + r) - m * p.G;
+                const uint16_t* src = p.q + ((size_t)ctl.members[j][m - m0] * p.Hq + head) * D + c * 8;
+                const int rr = r & (PFX_TILE - 1);
+                cp_async16(smem_u32(pfx_raw) + (r >> 7) * TILE_BYTES + (c >> 3) * HALF_BYTES + rr * 128 + (((c & 7) ^ (rr & 7)) << 4), src);
             }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) { mbar_arrive(&ctl.q_full); mbar_arrive(&ctl.item_empty[j]); }
+        }
+    } else {
+        // =============================== softmax warps: S -> P, epilogue ===============================
+        const int s = warp >> 2, w4 = warp & 3;                    // stream, quarter of its rows
+        const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
+        const uint32_t s_tmem = tmem + PFX_S_COL + s * 128 + lanes, o_tmem = tmem + PFX_O_COL + s * 128 + lanes;
+        const float sl = p.scale_log2;
+        const uint64_t keep = l2_evict_last_policy();
+        // slots that hold nothing: sequences without a group, chunks beyond a group's slice
+        for (int b = blockIdx.x * 8 + warp; b < p.B; b += gridDim.x * 8) {
+            const uint32_t g = (uint32_t)p.seq_group[b];
+            const int nc = g < (uint32_t)p.NG ? group_slice(p, (int)g).nc : 0;
+            const int none = p.NC - nc;
+            if (none == 0) continue;
+            for (int i = lane; i < p.Hq * none; i += 32) {
+                const size_t slot = ((size_t)b * p.Hq + i / none) * p.NC + nc + i % none;
+                p.m_part[slot] = NEG_INF;
+                p.l_part[slot] = 0.f;
+            }
+            if (p.sparse_empty) continue;
+            for (int i = 0; i < p.Hq * none; ++i) {
+                const size_t slot = ((size_t)b * p.Hq + i / none) * p.NC + nc + i % none;
+                if (lane < D / 4) reinterpret_cast<float4*>(p.o_part + slot * D)[lane] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+        }
+        bool ok = true;
+        uint32_t ns = 0, no = 0;                                   // tiles and items of this stream so far
+        for (int k = 0; ok; ++k) {
+            const int j = k & 1;
+            ok = warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
+            if (!ok) break;
+            const PfxItem it = ctl.item[j];
+            if (!it.valid) break;
+            const int tiles = it.tiles[s], first_row = (it.wide ? s * PFX_TILE : 0) + w4 * 32;
+            const bool live = first_row < it.rows;                 // some row of this warp exists
+            const bool exists = first_row + lane < it.rows;        // this thread's
+            float m_true = NEG_INF, m_ref = NEG_INF, l = 0.f;      // the maximum, and the one the weights refer to (raw logits)
+            for (int i = 0; i < tiles; ++i, ++ns) {
+                ok = warp_wait(&ctl.s_full[s], ns & 1u, abort_flag);
+                if (!ok) break;
+                tc_fence_after_sync();
+                if (live) {
+                    const int t = pfx_tile_token(it, s, i);
+                    const int c_lo = max(it.lo[s] - t, 0), c_hi = min(it.hi[s] - t, PFX_TILE);
+                    const uint32_t bad = *reinterpret_cast<volatile uint8_t*>(&ctl.stream_bad[s]);
+                    const bool edge = c_lo > 0 || c_hi < PFX_TILE || bad;
+                    uint32_t x[32];
+                    auto mask = [&](int c0) {                      // columns outside the slice or of refused pages
+                        uint32_t out = 0;
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+                            if ((bad >> ((c0 >> 4) + u)) & 1u) out |= 0xffffu << (16 * u);
+#pragma unroll
+                        for (int u = 0; u < 32; ++u)
+                            if (c0 + u < c_lo || c0 + u >= c_hi || ((out >> u) & 1u)) x[u] = 0xff800000u;
+                    };
+                    float mx = NEG_INF;
+#pragma unroll
+                    for (int c0 = 0; c0 < PFX_TILE; c0 += 32) {
+                        tmem_ld_32x32(s_tmem + c0, x);
+                        tmem_ld_wait();
+                        if (edge) mask(c0);
+                        float a = NEG_INF, b = NEG_INF;
+#pragma unroll
+                        for (int u = 0; u < 32; u += 4) {
+                            a = max3(a, __uint_as_float(x[u]), __uint_as_float(x[u + 1]));
+                            b = max3(b, __uint_as_float(x[u + 2]), __uint_as_float(x[u + 3]));
+                        }
+                        mx = max3(mx, a, b);
+                    }
+                    m_true = fmaxf(m_true, mx);
+                    // a row's sums follow its maximum only when that has moved by more than 2^8 (then the weights would leave
+                    // the 16-bit types' comfortable range); the difference is put right at the end.  Each row decides by
+                    // itself, so its result does not depend on its neighbours (rows that do not exist among them)
+                    const bool moved = (m_true - m_ref) * sl > 8.f;
+                    if (__any_sync(0xffffffffu, moved && exists)) {
+                        const float r = !moved ? 1.f : m_ref == NEG_INF ? 0.f : fast_exp2((m_ref - m_true) * sl);
+                        if (moved) m_ref = m_true;
+                        if (i > 0) {
+                            l *= r;
+#pragma unroll 1
+                            for (int c0 = 0; c0 < D; c0 += 32) {
+                                tmem_ld_32x32(o_tmem + c0, x);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int u = 0; u < 32; ++u) x[u] = __float_as_uint(__uint_as_float(x[u]) * r);
+                                tmem_st_32x32(o_tmem + c0, x);
+                            }
+                        }
+                    }
+                    const float off = m_ref == NEG_INF ? 0.f : -m_ref * sl;
+                    float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+                    for (int c0 = 0; c0 < PFX_TILE; c0 += 32) {
+                        tmem_ld_32x32(s_tmem + c0, x);
+                        tmem_ld_wait();
+                        if (edge) mask(c0);
+                        uint32_t w[32];
+#pragma unroll
+                        for (int u = 0; u < 16; ++u) {
+                            const float a = fast_exp2(fmaf(__uint_as_float(x[2 * u]), sl, off));
+                            const float b = fast_exp2(fmaf(__uint_as_float(x[2 * u + 1]), sl, off));
+                            sum0 += a;
+                            sum1 += b;
+                            split2<BF16>(a, b, w[u], w[16 + u]);
+                        }
+                        tmem_st_32x32(s_tmem + c0, w);
+                    }
+                    l += sum0 + sum1;
+                    tmem_st_wait();
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl.p_full[s]);
+            }
+            if (ok && tiles > 0) {
+                ok = warp_wait(&ctl.o_full[s], no & 1u, abort_flag);
+                if (!ok) break;
+                ++no;
+                tc_fence_after_sync();
+                if (live) {
+                    const int r = it.r0 + first_row + lane;
+                    const int m = r / p.G, head = it.h * p.G + r - m * p.G;
+                    const int b = exists ? ctl.members[j][m - it.m0] : 0;
+                    const size_t slot = ((size_t)b * p.Hq + head) * p.NC + it.chunk + (it.wide ? 0 : s);
+                    const float f = m_true == NEG_INF ? 0.f : fast_exp2((m_ref - m_true) * sl);
+                    if (exists) {
+                        p.m_part[slot] = m_true == NEG_INF ? NEG_INF : m_true * p.scale;
+                        p.l_part[slot] = l * f;
+                    }
+#pragma unroll 1
+                    for (int c0 = 0; c0 < D; c0 += 32) {
+                        uint32_t x[32];
+                        tmem_ld_32x32(o_tmem + c0, x);
+                        tmem_ld_wait();
+                        if (exists) {
+                            float* const dst = p.o_part + slot * D + c0;
+#pragma unroll
+                            for (int u = 0; u < 32; u += 4)
+                                st_global_hint4(dst + u, make_float4(__uint_as_float(x[u]) * f, __uint_as_float(x[u + 1]) * f,
+                                                                      __uint_as_float(x[u + 2]) * f, __uint_as_float(x[u + 3]) * f), keep);
+                        }
+                    }
+                }
+                tc_fence_before_sync();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.item_empty[j]);
+        }
     }
-    if (rows[row] < 0) return;
-    const size_t slot = (size_t)rows[row] * p.NC + c;
-    if (part == 0) { p.m_part[slot] = m; p.l_part[slot] = l; }
-    for (int i = 0; i < PER; ++i) p.o_part[slot * D + i * 8 + part] = acc[i];
+    __syncthreads();
+    if (*abort_flag) {
+        if (warp == PFX_K_WARP || warp == PFX_V_WARP) {
+            // unwinding: copies into this CTA's shared memory may still be on their way
+            if (lane == 0) {
+                for (int x = max(0, issued - S); x < issued; ++x) {
+                    int none = 0;
+                    const int seq = 2 * x + (warp == PFX_K_WARP ? 0 : 1);
+                    mbar_wait(&ctl.full[seq % S], (uint32_t)(seq / S) & 1u, &none);
+                }
+            }
+        }
+        if (tid == 0 && p.status) atomicOr(p.status, HG_DEV_WAIT_TIMEOUT);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == PFX_MMA_WARP) tmem_dealloc(tmem, 512);
 }
 
 }  // namespace hg

@@ -321,6 +321,29 @@ def test_same_bits_as_often_as_it_runs_and_for_any_neighbours():
     for _ in range(5):
         again = b.step()
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    # a row's partials do not depend on what stands in the other rows
+    q = b.q.clone()
+    one = b.partial()
+    b.q[1:44] *= 30
+    two = b.partial()
+    for x, y in zip(one, two):
+        assert torch.equal(x[0], y[0]) and torch.equal(x[44:], y[44:])
+    b.q.copy_(q)
+
+
+def test_a_wait_that_runs_out_is_reported():
+    """The loader never fills a tile: the call returns with a status bit, the next ones skip their work until it is cleared."""
+    b = Batch([0, 0, 0], [300], [1, 2, 3], seed=15)
+    b.desc.flags = hg.HG_FLAG_TEST_STALL
+    b.partial()
+    torch.cuda.synchronize()
+    assert int(b.status) == hg.HG_DEV_WAIT_TIMEOUT
+    b.desc.flags = 0
+    o, m, l = b.partial()
+    torch.cuda.synchronize()
+    assert o.isnan().all() and m.isnan().all() and l.isnan().all()
+    b.status.zero_()
+    check_step(b)
 
 
 def test_captured_on_another_stream_beside_a_second_call():
