@@ -438,7 +438,8 @@ typedef struct hg_prefix_desc {
  *
  *   q       dev [B][Hq][D], dtype as desc->dtype, 16-byte aligned; one query per sequence
  *   o_part, m_part, l_part   dev float [B][Hq][NC][D] / [B][Hq][NC], NC = prefix->num_chunks: as in hg_attn_partial; a
- *           sequence without a group, and slots beyond a group's chunks, are empty (HG_FLAG_SPARSE_EMPTY applies)
+ *           sequence without a group, and slots beyond a group's chunks, are empty (HG_FLAG_SPARSE_EMPTY applies);
+ *           o_part 32-byte aligned
  * Of desc: batch, heads, head_dim, dtype, the KV addressing, scale, flags and status are used.  Accumulation is fp32 and P is
  * carried as a two-term (hi + lo) 16-bit expansion, as in hg_attn_partial.
  */

@@ -131,7 +131,7 @@ hg_status hg_attn_prefix_partial(const void* q, const void* k_cache, const void*
     hg_status st = check_prefix(desc, prefix);
     if (st != HG_OK) return st;
     if (!q || !k_cache || !v_cache || !o_part || !m_part || !l_part) return HG_ERR_INVALID_ARG;
-    if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(o_part)) return HG_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || (reinterpret_cast<uintptr_t>(o_part) & 31u)) return HG_ERR_INVALID_ARG;
     return run_prefix(q, k_cache, v_cache, o_part, m_part, l_part, nullptr, stream, desc, prefix);
 }
 

@@ -66,6 +66,7 @@ __device__ __forceinline__ GroupSlice group_slice(const PrefixParams& p, int g) 
 constexpr int PFX_TILE = 128;                 // tokens per tile, rows per stream
 constexpr int PFX_THREADS = 512;
 constexpr int PFX_K_WARP = 8, PFX_V_WARP = 9, PFX_MMA_WARP = 10, PFX_ITEM_WARP = 11, PFX_Q_WARP = 12;
+constexpr int PFX_REGS_SOFTMAX = 200, PFX_REGS_OTHER = 56;     // 256 threads each: together the 128 x 512 of the launch
 constexpr int PFX_MAX_SLOTS = 10;
 constexpr int PFX_MAX_GROUPS = 512;
 constexpr uint32_t PFX_S_COL = 0, PFX_O_COL = 256;      // tensor memory: S / P of the streams, 128 columns each, then their O
@@ -87,7 +88,8 @@ struct PfxItem {
 
 struct PfxCtl {
     uint64_t full[PFX_MAX_SLOTS], empty[PFX_MAX_SLOTS];
-    uint64_t s_full[2], p_full[2], o_full[2];
+    uint64_t s_full[2], p_full[2][2], o_full[2];      // p_full: first and second half of a tile's tokens
+    uint64_t edge;
     uint64_t q_full, q_free, drain;
     uint64_t item_full[2], item_empty[2];
     PfxItem item[2];
@@ -111,19 +113,19 @@ __device__ __forceinline__ int pfx_tile_index(const PfxItem& it, int s, int i) {
 }
 __device__ __forceinline__ int pfx_total_tiles(const PfxItem& it) { return it.wide ? it.tiles[0] : it.tiles[0] + it.tiles[1]; }
 
-__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
-
 // Two weights -> packed hi terms (rounded) and packed lo terms (what that left, rounded): at most 2^-18 (bf16) or 2^-24
 // (fp16) of a weight is lost.
 template <bool BF16>
-__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
-    hi = pack2<BF16>(a, b);
-    const float2 f = unpack2<BF16>(hi);
-    lo = pack2<BF16>(a - f.x, b - f.y);
+__device__ __forceinline__ void split2(float2 w, uint32_t& hi, uint32_t& lo) {
+    hi = pack2<BF16>(w.x, w.y);
+    const float2 rest = fma2(unpack2<BF16>(hi), make_float2(-1.f, -1.f), w);
+    lo = pack2<BF16>(rest.x, rest.y);
 }
 
-__device__ __forceinline__ void st_global_hint4(float* addr, float4 v, uint64_t policy) {
-    asm volatile("st.global.L2::cache_hint.v4.f32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "l"(policy)
+// A whole 32-byte sector.
+__device__ __forceinline__ void st_global_hint8(float* addr, const float (&v)[8], uint64_t policy) {
+    asm volatile("st.global.L2::cache_hint.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8}, %9;"
+                 ::"l"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "l"(policy)
                  : "memory");
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
@@ -156,7 +158,8 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
         for (int i = 0; i < S; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&ctl.s_full[s], 2);                          // the products' completion, and the tile's description
-            mbar_init(&ctl.p_full[s], 4);
+            mbar_init(&ctl.p_full[s][0], 4);
+            mbar_init(&ctl.p_full[s][1], 4);
             mbar_init(&ctl.o_full[s], 1);
             mbar_init(&ctl.item_full[s], 1);
             mbar_init(&ctl.item_empty[s], 8 + 3 + 4);
@@ -164,6 +167,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
         mbar_init(&ctl.q_full, 4);
         mbar_init(&ctl.q_free, 1);
         mbar_init(&ctl.drain, 1);
+        mbar_init(&ctl.edge, 1);
         ctl.abort = 0;
         fence_barrier_init();
     }
@@ -194,9 +198,14 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
     __syncthreads();
 
     int issued = 0;                                                // (loaders) tiles requested so far
+    uint32_t edges = 0;                                            // (V loader) tiles that went over the edge barrier
+    bool edge_open = false;                                        // ... and one that is still on its way
+    // 512 threads x 128 registers at the launch: the softmax warps, which hold a whole row of S, take 72 from the others
     if (skip) {
         // an earlier call timed out: no work until the caller has cleared the word
-    } else if (warp == PFX_ITEM_WARP) {
+    } else if (warp >= 8) {
+      reg_shrink<PFX_REGS_OTHER>();
+      if (warp == PFX_ITEM_WARP) {
         // =============================== item warp: decodes work items, one ahead ===============================
         int gb = 0;                                                // first of the 32 groups in the lanes
         long long base = 0;                                        // items of the groups before them
@@ -289,7 +298,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl.item_full[j]);
         }
-    } else if (warp == PFX_K_WARP || warp == PFX_V_WARP) {
+      } else if (warp == PFX_K_WARP || warp == PFX_V_WARP) {
         // =============================== loaders: K tiles and V tiles, alternately in the ring ===============================
         const bool is_k = warp == PFX_K_WARP;
         const CUtensorMap* const tm = is_k ? &tmK : &tmV;
@@ -322,11 +331,10 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                                             : it.row * p.max_pages + (t >> p.page_shift);
                 return (uint32_t)e < (uint32_t)p.num_pages ? e : -2;
             };
-            int next = entry(0), next_t = t;
+            int next = entry(0);
             for (int x = 0; x < total; ++x) {
-                const int e = next, row = next_t & (p.page_size - 1);
+                const int e = next, row = t & (p.page_size - 1), t_x = t - piece * box_rows, lo_x = lo, hi_x = hi;
                 next = entry(x + 1);                               // one tile ahead: the look-up is not waited for
-                next_t = t;
                 const int seq = 2 * (n + x) + (is_k ? 0 : 1), slot = seq % S;
                 const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, e >= 0)) * (uint32_t)box_rows * 128u;
                 uint32_t bad = 0;
@@ -339,125 +347,121 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                 }
                 if (seq >= S) ok = warp_wait(&ctl.empty[slot], (uint32_t)(seq / S - 1) & 1u, abort_flag);
                 if (!ok || p.test_stall) break;
+                // V rows outside the slice, and of refused pages, hold anything (NaN patterns among it) and meet weights of 0:
+                // such a tile lands on a barrier of its own and is handed on when those rows are cleared
+                const int c_lo = max(lo_x - t_x, 0), c_hi = min(hi_x - t_x, PFX_TILE);
+                const bool edge = !is_k && (c_lo > 0 || c_hi < PFX_TILE || bad);
+                uint64_t* const landed = edge ? &ctl.edge : &ctl.full[slot];
+                uint8_t* const tile = ring + slot * TILE_BYTES;
                 if (lane == 0) {
                     if (is_k) ctl.bad[(n + x) & 15] = (uint8_t)bad;
-                    mbar_arrive_expect_tx(&ctl.full[slot], bytes);
+                    mbar_arrive_expect_tx(landed, bytes);
                 }
-                if (e >= 0)
-                    tma_load_5d(ring + slot * TILE_BYTES + half * HALF_BYTES + piece * box_rows * 128, tm, &ctl.full[slot], 0, row, half, it.h, e, policy);
+                if (e >= 0) tma_load_5d(tile + half * HALF_BYTES + piece * box_rows * 128, tm, landed, 0, row, half, it.h, e, policy);
+                if (edge) {
+                    ok = warp_wait(&ctl.edge, edges & 1u, abort_flag);
+                    if (!ok) { edge_open = true; break; }
+                    ++edges;
+                    for (int u = lane; u < PFX_TILE * HALVES * 8; u += 32) {     // whole 128-byte rows: the swizzle does not matter
+                        const int r = (u >> 3) % PFX_TILE, hf = (u >> 3) / PFX_TILE;
+                        if (r < c_lo || r >= c_hi || ((bad >> (r >> 4)) & 1u)) sts128_zero(smem_u32(tile) + hf * HALF_BYTES + r * 128 + (u & 7) * 16);
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&ctl.full[slot]);
+                }
                 issued = n + x + 1;
             }
             n += total;
             if (p.test_stall) break;
         }
-    } else if (warp == PFX_MMA_WARP) {
-        // =============================== tensor-core warp ===============================
-        // (all lanes follow the same control flow; lane 0 issues)
-        bool ok = true;
-        int n = 0;                                                 // tiles of earlier items
-        uint32_t np[2] = {0, 0};                                   // P tiles taken per stream
-        bool held = false;                                         // stream 1's last product of the item before is still to come
-        PfxItem prev;
-        int prev_n = 0;
-        const uint64_t q_desc = tc_smem_desc(smem_u32(pfx_raw), 16u, 1024u, 2u);
-        const uint64_t k_desc = tc_smem_desc(smem_u32(ring), 16u, 1024u, 2u);
-        const uint64_t v_desc = tc_smem_desc(smem_u32(ring), HALF_BYTES, 1024u, 2u);
-        auto scores = [&](const PfxItem& it, int s, int i, bool last) {        // S = Q K^T of a stream's tile
-            const int x = n + pfx_tile_index(it, s, i), seq = 2 * x, slot = seq % S;
-            ok = warp_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
-            if (!ok) return;
-            if (lane == 0) {
+      } else if (warp == PFX_MMA_WARP) {
+        // =============================== tensor-core warp: one thread issues all products ===============================
+        if (elect_one()) {
+            bool ok = true;
+            int n = 0, prev_n = 0;                                 // tiles before this item, and before the previous one
+            uint32_t np[2] = {0, 0};                               // P tiles taken per stream
+            bool held = false;                                     // stream 1's last products of the item before are still to come
+            PfxItem it, prev;
+            const uint64_t q_desc = tc_smem_desc(smem_u32(pfx_raw), 16u, 1024u, 2u);
+            const uint64_t k_desc = tc_smem_desc(smem_u32(ring), 16u, 1024u, 2u);
+            const uint64_t v_desc = tc_smem_desc(smem_u32(ring), HALF_BYTES, 1024u, 2u);
+            auto scores = [&](int s, int i, bool last) {           // S = Q K^T of a stream's tile
+                const int x = n + pfx_tile_index(it, s, i), seq = 2 * x, slot = seq % S;
+                ok = mbar_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
+                if (!ok) return;
                 ctl.stream_bad[s] = ctl.bad[x & 15];
                 tc_fence_after_sync();
-                const uint64_t a = q_desc + (uint64_t)((it.wide ? s : 0) * TILE_BYTES >> 4), b = k_desc + (uint64_t)(slot * TILE_BYTES >> 4);
+                const uint64_t a = q_desc + (uint32_t)((it.wide ? s : 0) * (TILE_BYTES >> 4)), b = k_desc + (uint32_t)(slot * (TILE_BYTES >> 4));
                 const uint32_t acc = tmem + PFX_S_COL + s * 128;
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {              // 16 components: 32 bytes of a 128-byte row, halves apart
                     const uint32_t off = (uint32_t)((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4;
-                    tc_mma_f16(acc, a + off, b + off, IDESC_S, kk ? 1u : 0u);
+                    tc_mma_f16_ss(acc, a + off, b + off, IDESC_S, kk ? 1u : 0u);
                 }
+                tc_commit(&ctl.s_full[s]);
                 if (!it.wide || s == 1) tc_commit(&ctl.empty[slot]);
                 if (last) tc_commit(&ctl.q_free);
-                tc_commit(&ctl.s_full[s]);
                 mbar_arrive(&ctl.s_full[s]);
-            }
-            __syncwarp();
-        };
-        auto values = [&](const PfxItem& it, int n0, int s, int i) {           // O += P V of a stream's tile
-            ok = warp_wait(&ctl.p_full[s], np[s] & 1u, abort_flag);
-            if (!ok) return;
-            ++np[s];
-            const int x = n0 + pfx_tile_index(it, s, i), seq = 2 * x + 1, slot = seq % S;
-            ok = warp_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
-            if (!ok) return;
-            const int t = pfx_tile_token(it, s, i);
-            const int c_lo = max(it.lo[s] - t, 0), c_hi = min(it.hi[s] - t, PFX_TILE);
-            const uint32_t bad = ctl.bad[x & 15];
-            if ((c_lo > 0 || c_hi < PFX_TILE || bad) && (!it.wide || s == 0)) {
-                // rows outside the slice, and of refused pages, hold anything (NaN patterns among it): weight 0 times that
-                // must be 0, so clear them (whole 128-byte rows: the swizzle does not matter)
-                uint8_t* const v = ring + slot * TILE_BYTES;
-                for (int u = lane; u < PFX_TILE * HALVES * 8; u += 32) {
-                    const int r = (u >> 3) % PFX_TILE, hf = (u >> 3) / PFX_TILE;
-                    if (r < c_lo || r >= c_hi || ((bad >> (r >> 4)) & 1u)) sts128_zero(smem_u32(v) + hf * HALF_BYTES + r * 128 + (u & 7) * 16);
-                }
-                fence_proxy_async();
-                __syncwarp();
-            }
-            if (lane == 0) {
-                tc_fence_after_sync();
-                const uint64_t b = v_desc + (uint64_t)(slot * TILE_BYTES >> 4);
+            };
+            auto values = [&](const PfxItem& im, int n0, int s, int i) {       // O += P V of a stream's tile, half by half
+                const int x = n0 + pfx_tile_index(im, s, i), seq = 2 * x + 1, slot = seq % S;
+                ok = mbar_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
+                const uint64_t b = v_desc + (uint32_t)(slot * (TILE_BYTES >> 4));
                 const uint32_t acc = tmem + PFX_O_COL + s * 128, a = tmem + PFX_S_COL + s * 128;
 #pragma unroll
-                for (int kk = 0; kk < PFX_TILE / 16; ++kk) {       // 16 tokens: 8 columns of hi terms, 16 further on their lo terms
-                    const uint32_t ac = a + (kk >> 1) * 32 + (kk & 1) * 8;
-                    tc_mma_f16_ta(acc, ac, b + (uint64_t)(kk * 2048 >> 4), IDESC_O, (i | kk) ? 1u : 0u);
-                    tc_mma_f16_ta(acc, ac + 16, b + (uint64_t)(kk * 2048 >> 4), IDESC_O, 1u);
+                for (int part = 0; part < 2; ++part) {
+                    ok = ok && mbar_wait(&ctl.p_full[s][part], np[s] & 1u, abort_flag);
+                    if (!ok) return;
+                    tc_fence_after_sync();
+#pragma unroll
+                    for (int kk = part * 4; kk < part * 4 + 4; ++kk) {         // 16 tokens: 8 columns of hi terms, 16 further on their lo terms
+                        const uint32_t ac = a + (kk >> 1) * 32 + (kk & 1) * 8;
+                        tc_mma_f16_ts(acc, ac, b + (uint32_t)(kk * 2048 >> 4), IDESC_O, kk ? 1u : (i ? 1u : 0u));
+                        tc_mma_f16_ts(acc, ac + 16, b + (uint32_t)(kk * 2048 >> 4), IDESC_O, 1u);
+                    }
                 }
-                if (!it.wide || s == 1) tc_commit(&ctl.empty[slot]);
-                if (i == it.tiles[s] - 1) tc_commit(&ctl.o_full[s]);
+                ++np[s];
+                if (!im.wide || s == 1) tc_commit(&ctl.empty[slot]);
+                if (i == im.tiles[s] - 1) tc_commit(&ctl.o_full[s]);
+            };
+            for (int k = 0; ok; ++k) {
+                const int j = k & 1;
+                ok = mbar_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
+                if (!ok) break;
+                it = ctl.item[j];
+                mbar_arrive(&ctl.item_empty[j]);
+                if (!it.valid) break;
+                ok = mbar_wait(&ctl.q_full, (uint32_t)k & 1u, abort_flag);
+                if (!ok) break;
+                int left = it.tiles[0] + it.tiles[1];              // score products still to issue
+                if (it.tiles[0] > 0) scores(0, 0, --left == 0);
+                if (ok && held) values(prev, prev_n, 1, prev.tiles[1] - 1);
+                held = false;
+                if (ok && it.tiles[1] > 0) scores(1, 0, --left == 0);
+                const int steps = max(it.tiles[0], it.tiles[1]);
+                for (int i = 0; i < steps && ok; ++i) {
+                    if (i < it.tiles[0]) {
+                        values(it, n, 0, i);
+                        if (ok && i + 1 < it.tiles[0]) scores(0, i + 1, --left == 0);
+                    }
+                    if (ok && i < it.tiles[1]) {
+                        if (i + 1 == steps) { held = true; break; }            // behind the next item's first scores
+                        values(it, n, 1, i);
+                        if (ok && i + 1 < it.tiles[1]) scores(1, i + 1, --left == 0);
+                    }
+                }
+                prev = it;
+                prev_n = n;
+                n += pfx_total_tiles(it);
             }
-            __syncwarp();
-        };
-        for (int k = 0; ok; ++k) {
-            const int j = k & 1;
-            ok = warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
-            if (!ok) break;
-            const PfxItem it = ctl.item[j];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl.item_empty[j]);
-            if (!it.valid) break;
-            ok = warp_wait(&ctl.q_full, (uint32_t)k & 1u, abort_flag);
-            if (!ok) break;
-            int left = it.tiles[0] + it.tiles[1];                  // score products still to issue
-            if (it.tiles[0] > 0) scores(it, 0, 0, --left == 0);
             if (ok && held) values(prev, prev_n, 1, prev.tiles[1] - 1);
-            held = false;
-            if (ok && it.tiles[1] > 0) scores(it, 1, 0, --left == 0);
-            const int steps = max(it.tiles[0], it.tiles[1]);
-            for (int i = 0; i < steps && ok; ++i) {
-                if (i < it.tiles[0]) {
-                    values(it, n, 0, i);
-                    if (ok && i + 1 < it.tiles[0]) scores(it, 0, i + 1, --left == 0);
-                }
-                if (ok && i < it.tiles[1]) {
-                    if (i + 1 == steps) { held = true; break; }    // behind the next item's first scores
-                    values(it, n, 1, i);
-                    if (ok && i + 1 < it.tiles[1]) scores(it, 1, i + 1, --left == 0);
-                }
-            }
-            prev = it;
-            prev_n = n;
-            n += pfx_total_tiles(it);
-        }
-        if (ok && held) values(prev, prev_n, 1, prev.tiles[1] - 1);
-        if (lane == 0) {                                           // nothing is in flight when the tensor memory is given back
-            int none = 0;
+            int none = 0;                                          // nothing is in flight when the tensor memory is given back
             tc_commit(&ctl.drain);
             mbar_wait(&ctl.drain, 0u, &none);
         }
         __syncwarp();
-    } else if (warp >= PFX_Q_WARP) {
+      } else {
         // =============================== query rows, gathered into the 128-byte-swizzled A tiles ===============================
         const int t = tid - PFX_Q_WARP * 32;
         constexpr int VECS = D / 8;                                // 16-byte vectors per row
@@ -481,7 +485,9 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             __syncwarp();
             if (lane == 0) { mbar_arrive(&ctl.q_full); mbar_arrive(&ctl.item_empty[j]); }
         }
+      }
     } else {
+        reg_grow<PFX_REGS_SOFTMAX>();
         // =============================== softmax warps: S -> P, epilogue ===============================
         const int s = warp >> 2, w4 = warp & 3;                    // stream, quarter of its rows
         const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
@@ -526,30 +532,23 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                     const int c_lo = max(it.lo[s] - t, 0), c_hi = min(it.hi[s] - t, PFX_TILE);
                     const uint32_t bad = *reinterpret_cast<volatile uint8_t*>(&ctl.stream_bad[s]);
                     const bool edge = c_lo > 0 || c_hi < PFX_TILE || bad;
-                    uint32_t x[32];
-                    auto mask = [&](int c0) {                      // columns outside the slice or of refused pages
-                        uint32_t out = 0;
+                    float x[PFX_TILE];
 #pragma unroll
-                        for (int u = 0; u < 2; ++u)
-                            if ((bad >> ((c0 >> 4) + u)) & 1u) out |= 0xffffu << (16 * u);
+                    for (int c0 = 0; c0 < PFX_TILE; c0 += 32) tmem_ld_32x32(s_tmem + c0, *reinterpret_cast<uint32_t(*)[32]>(&x[c0]));
+                    tmem_ld_wait();
+                    if (edge) {                                    // columns outside the slice or of refused pages
 #pragma unroll
-                        for (int u = 0; u < 32; ++u)
-                            if (c0 + u < c_lo || c0 + u >= c_hi || ((out >> u) & 1u)) x[u] = 0xff800000u;
-                    };
-                    float mx = NEG_INF;
-#pragma unroll
-                    for (int c0 = 0; c0 < PFX_TILE; c0 += 32) {
-                        tmem_ld_32x32(s_tmem + c0, x);
-                        tmem_ld_wait();
-                        if (edge) mask(c0);
-                        float a = NEG_INF, b = NEG_INF;
-#pragma unroll
-                        for (int u = 0; u < 32; u += 4) {
-                            a = max3(a, __uint_as_float(x[u]), __uint_as_float(x[u + 1]));
-                            b = max3(b, __uint_as_float(x[u + 2]), __uint_as_float(x[u + 3]));
-                        }
-                        mx = max3(mx, a, b);
+                        for (int u = 0; u < PFX_TILE; ++u)
+                            if (u < c_lo || u >= c_hi || ((bad >> (u >> 4)) & 1u)) x[u] = NEG_INF;
                     }
+                    float mx4[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) mx4[c] = fmaxf(x[2 * c], x[2 * c + 1]);
+#pragma unroll
+                    for (int u = 8; u < PFX_TILE; u += 8)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) mx4[c] = max3(mx4[c], x[u + 2 * c], x[u + 2 * c + 1]);
+                    const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
                     m_true = fmaxf(m_true, mx);
                     // a row's sums follow its maximum only when that has moved by more than 2^8 (then the weights would leave
                     // the 16-bit types' comfortable range); the difference is put right at the end.  Each row decides by
@@ -561,39 +560,46 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                         if (i > 0) {
                             l *= r;
 #pragma unroll 1
-                            for (int c0 = 0; c0 < D; c0 += 32) {
-                                tmem_ld_32x32(o_tmem + c0, x);
+                            for (int c0 = 0; c0 < D; c0 += 8) {
+                                uint32_t y[8];
+                                tmem_ld_32x8(o_tmem + c0, y);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int u = 0; u < 32; ++u) x[u] = __float_as_uint(__uint_as_float(x[u]) * r);
-                                tmem_st_32x32(o_tmem + c0, x);
+                                for (int u = 0; u < 8; ++u) y[u] = __float_as_uint(__uint_as_float(y[u]) * r);
+                                tmem_st_32x8(o_tmem + c0, y);
                             }
                         }
                     }
                     const float off = m_ref == NEG_INF ? 0.f : -m_ref * sl;
-                    float sum0 = 0.f, sum1 = 0.f;
+                    const float2 sl2 = make_float2(sl, sl), off2 = make_float2(off, off);
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                     for (int c0 = 0; c0 < PFX_TILE; c0 += 32) {
-                        tmem_ld_32x32(s_tmem + c0, x);
-                        tmem_ld_wait();
-                        if (edge) mask(c0);
                         uint32_t w[32];
 #pragma unroll
                         for (int u = 0; u < 16; ++u) {
-                            const float a = fast_exp2(fmaf(__uint_as_float(x[2 * u]), sl, off));
-                            const float b = fast_exp2(fmaf(__uint_as_float(x[2 * u + 1]), sl, off));
-                            sum0 += a;
-                            sum1 += b;
-                            split2<BF16>(a, b, w[u], w[16 + u]);
+                            float2 e = fma2(make_float2(x[c0 + 2 * u], x[c0 + 2 * u + 1]), sl2, off2);
+                            e.x = fast_exp2(e.x);
+                            e.y = fast_exp2(e.y);
+                            sum[u & 1] = add2(sum[u & 1], e);
+                            split2<BF16>(e, w[u], w[16 + u]);
                         }
                         tmem_st_32x32(s_tmem + c0, w);
+                        if (c0 == 32) {                            // the first half of the tokens can be multiplied
+                            tmem_st_wait();
+                            tc_fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&ctl.p_full[s][0]);
+                        }
                     }
-                    l += sum0 + sum1;
+                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     tmem_st_wait();
+                } else if (lane == 0) {
+                    mbar_arrive(&ctl.p_full[s][0]);
                 }
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&ctl.p_full[s]);
+                if (lane == 0) mbar_arrive(&ctl.p_full[s][1]);
             }
             if (ok && tiles > 0) {
                 ok = warp_wait(&ctl.o_full[s], no & 1u, abort_flag);
@@ -610,17 +616,18 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                         p.m_part[slot] = m_true == NEG_INF ? NEG_INF : m_true * p.scale;
                         p.l_part[slot] = l * f;
                     }
-#pragma unroll 1
-                    for (int c0 = 0; c0 < D; c0 += 32) {
-                        uint32_t x[32];
-                        tmem_ld_32x32(o_tmem + c0, x);
-                        tmem_ld_wait();
-                        if (exists) {
-                            float* const dst = p.o_part + slot * D + c0;
+                    uint32_t x[D];
 #pragma unroll
-                            for (int u = 0; u < 32; u += 4)
-                                st_global_hint4(dst + u, make_float4(__uint_as_float(x[u]) * f, __uint_as_float(x[u + 1]) * f,
-                                                                      __uint_as_float(x[u + 2]) * f, __uint_as_float(x[u + 3]) * f), keep);
+                    for (int c0 = 0; c0 < D; c0 += 32) tmem_ld_32x32(o_tmem + c0, *reinterpret_cast<uint32_t(*)[32]>(&x[c0]));
+                    tmem_ld_wait();
+                    if (exists) {
+                        float* const dst = p.o_part + slot * D;
+#pragma unroll
+                        for (int c0 = 0; c0 < D; c0 += 8) {
+                            float y[8];
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) y[u] = __uint_as_float(x[c0 + u]) * f;
+                            st_global_hint8(dst + c0, y, keep);
                         }
                     }
                 }
@@ -640,6 +647,8 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                     const int seq = 2 * x + (warp == PFX_K_WARP ? 0 : 1);
                     mbar_wait(&ctl.full[seq % S], (uint32_t)(seq / S) & 1u, &none);
                 }
+                int none = 0;
+                if (edge_open) mbar_wait(&ctl.edge, edges & 1u, &none);
             }
         }
         if (tid == 0 && p.status) atomicOr(p.status, HG_DEV_WAIT_TIMEOUT);
