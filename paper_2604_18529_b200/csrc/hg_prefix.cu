@@ -140,7 +140,25 @@ int32_t hg_attn_prefix_suggest_chunk(int64_t shared_tokens, int32_t num_groups, 
     if (shared_tokens < 0 || num_groups < 1 || num_members < 0 || num_kv_heads < 1 || num_q_heads < 1 || num_q_heads % num_kv_heads) return 0;
     const int shift = ilog2_exact(page_size);
     if (shift < 4 || shift > 8) return 0;
-    return 256;
+    // Work items are dealt out in turn, one at a time to each of 148 SMs, so the number of items should fill whole rounds;
+    // against many short items stand their epilogues and the merge, which reads every chunk's partials.  The costs, in
+    // microseconds, are those measured at 128 components: 2 per step of an item (128 tokens for two row tiles), 4 per item,
+    // 1e-4 per partial row in the merge.  Groups count as if all were of the average size.
+    const int64_t unit = page_size > PFX_TILE ? page_size / PFX_TILE : 1;
+    int64_t tiles = (shared_tokens / num_groups + PFX_TILE - 1) / PFX_TILE;
+    if (tiles < 1) tiles = 1;
+    const int64_t rows = ((int64_t)num_members + num_groups - 1) / num_groups * (num_q_heads / num_kv_heads), rem = rows % 256;
+    const int64_t wide = rows / 256 + (rem > 128 ? 1 : 0), narrow = rem > 0 && rem <= 128 ? 1 : 0;
+    int64_t best = unit;
+    double best_cost = 0;
+    for (int64_t n = 1; n <= tiles && n <= 600; ++n) {
+        const int64_t c = ((tiles + n - 1) / n + unit - 1) / unit * unit, nc = (tiles + c - 1) / c;
+        const int64_t items = num_groups * (int64_t)num_kv_heads * (wide * nc + narrow * ((nc + 1) / 2));
+        const double cost = (double)((items + 147) / 148) * (2.0 * (double)c + 4.0) + 1e-4 * (double)nc * num_members * num_q_heads;
+        if (n == 1 || cost < best_cost) { best = c; best_cost = cost; }
+    }
+    const int64_t most = 0x7fffffffll / PFX_TILE / unit * unit;
+    return (int32_t)((best < most ? best : most) * PFX_TILE);
 }
 
 size_t hg_attn_shared_workspace_bytes(const hg_attn_desc* desc, const hg_prefix_desc* prefix) {

@@ -88,7 +88,7 @@ struct PfxItem {
 
 struct PfxCtl {
     uint64_t full[PFX_MAX_SLOTS], empty[PFX_MAX_SLOTS];
-    uint64_t s_full[2], p_full[2][2], o_full[2];      // p_full: first and second half of a tile's tokens
+    uint64_t s_full[2], p_full[2][4], o_full[2];      // p_full: the quarters of a tile's tokens
     uint64_t edge;
     uint64_t q_full, q_free, drain;
     uint64_t item_full[2], item_empty[2];
@@ -158,8 +158,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
         for (int i = 0; i < S; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&ctl.s_full[s], 2);                          // the products' completion, and the tile's description
-            mbar_init(&ctl.p_full[s][0], 4);
-            mbar_init(&ctl.p_full[s][1], 4);
+            for (int c = 0; c < 4; ++c) mbar_init(&ctl.p_full[s][c], 4);
             mbar_init(&ctl.o_full[s], 1);
             mbar_init(&ctl.item_full[s], 1);
             mbar_init(&ctl.item_empty[s], 8 + 3 + 4);
@@ -404,18 +403,18 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                 if (last) tc_commit(&ctl.q_free);
                 mbar_arrive(&ctl.s_full[s]);
             };
-            auto values = [&](const PfxItem& im, int n0, int s, int i) {       // O += P V of a stream's tile, half by half
+            auto values = [&](const PfxItem& im, int n0, int s, int i) {       // O += P V of a stream's tile, quarter by quarter
                 const int x = n0 + pfx_tile_index(im, s, i), seq = 2 * x + 1, slot = seq % S;
                 ok = mbar_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
                 const uint64_t b = v_desc + (uint32_t)(slot * (TILE_BYTES >> 4));
                 const uint32_t acc = tmem + PFX_O_COL + s * 128, a = tmem + PFX_S_COL + s * 128;
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
+                for (int part = 0; part < 4; ++part) {
                     ok = ok && mbar_wait(&ctl.p_full[s][part], np[s] & 1u, abort_flag);
                     if (!ok) return;
                     tc_fence_after_sync();
 #pragma unroll
-                    for (int kk = part * 4; kk < part * 4 + 4; ++kk) {         // 16 tokens: 8 columns of hi terms, 16 further on their lo terms
+                    for (int kk = part * 2; kk < part * 2 + 2; ++kk) {         // 16 tokens: 8 columns of hi terms, 16 further on their lo terms
                         const uint32_t ac = a + (kk >> 1) * 32 + (kk & 1) * 8;
                         tc_mma_f16_ts(acc, ac, b + (uint32_t)(kk * 2048 >> 4), IDESC_O, kk ? 1u : (i ? 1u : 0u));
                         tc_mma_f16_ts(acc, ac + 16, b + (uint32_t)(kk * 2048 >> 4), IDESC_O, 1u);
@@ -585,21 +584,17 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                             split2<BF16>(e, w[u], w[16 + u]);
                         }
                         tmem_st_32x32(s_tmem + c0, w);
-                        if (c0 == 32) {                            // the first half of the tokens can be multiplied
-                            tmem_st_wait();
-                            tc_fence_before_sync();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&ctl.p_full[s][0]);
-                        }
+                        tmem_st_wait();                            // this quarter of the tokens can be multiplied
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&ctl.p_full[s][c0 / 32]);
                     }
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                    tmem_st_wait();
-                } else if (lane == 0) {
-                    mbar_arrive(&ctl.p_full[s][0]);
+                } else {
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane < 4) mbar_arrive(&ctl.p_full[s][lane]);
                 }
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&ctl.p_full[s][1]);
             }
             if (ok && tiles > 0) {
                 ok = warp_wait(&ctl.o_full[s], no & 1u, abort_flag);
