@@ -41,14 +41,34 @@ struct PrefixParams {
     float* l_part;
     int32_t* status;
     int32_t* zero;                   // two words to clear on the way (the work counter of the launch that follows), or NULL
+    // the sequences' own tokens, as further items of the same launch (own = 0: not part of it)
+    const int32_t* seq_lens;         // [B]
+    const int32_t* tok_begin;        // [B]
+    const int32_t* tok_end;          // [B]
+    float* own_o;                    // [B][Hq][own_NC][D]
+    float* own_m;
+    float* own_l;
+    int own, own_NC, own_C;
     int B, Hq, Hkv, G, NG, NC, C;
     int page_size, page_shift, max_pages, num_pages;
     int sparse_empty, test_stall;
     float scale, scale_log2;
 };
 
-// The slice of a group, clamped to its block-table row, and its chunks.
+// The slice of a group (or a sequence's own one), clamped to its block-table row, and its chunks.
 struct GroupSlice { int row, begin, end, nc; bool bad; };
+
+__device__ __forceinline__ GroupSlice own_slice(const PrefixParams& p, int b) {
+    GroupSlice s;
+    s.row = b;
+    s.begin = max(p.tok_begin[b], 0);
+    s.end = min(p.tok_end[b], p.seq_lens[b]);
+    s.bad = false;
+    const long long room = (long long)p.max_pages << p.page_shift;
+    if (s.end > room && s.end > s.begin) { s.end = (int)room; s.bad = true; }
+    s.nc = s.end > s.begin ? min((s.end - 1) / p.own_C - s.begin / p.own_C + 1, p.own_NC) : 0;
+    return s;
+}
 
 __device__ __forceinline__ GroupSlice group_slice(const PrefixParams& p, int g) {
     GroupSlice s;
@@ -77,13 +97,17 @@ template <int D> __host__ __device__ constexpr int pfx_slots() { return D == 128
 // One work item, published by the item warp.
 struct PfxItem {
     int valid;                       // 0: no more items
+    int own;                         // a sequence's own tokens, not a group's
     int row, h;                      // block-table row, KV head
     int wide;
     int chunk;                       // chunk slot of stream 0 (stream 1: the same, or the next one)
     int r0, rows;                    // first row of the group, rows in this item
     int m0;                          // number of the first member in `members`
-    int lo[2], hi[2];                // the streams' tokens
-    int tiles[2];
+    int lo0, lo1, hi0, hi1;          // the streams' tokens
+    int tiles0, tiles1;
+    __device__ __forceinline__ int lo(int s) const { return s ? lo1 : lo0; }
+    __device__ __forceinline__ int hi(int s) const { return s ? hi1 : hi0; }
+    __device__ __forceinline__ int tiles(int s) const { return s ? tiles1 : tiles0; }
 };
 
 struct PfxCtl {
@@ -98,7 +122,7 @@ struct PfxCtl {
     uint8_t bad[16];                 // per tile, in load order: 16-token pieces of the tile whose page was refused
     uint8_t stream_bad[2];           // the same for the tile a stream's softmax warps are about to read
     uint16_t members[2][256];        // sequences of the item's rows, in ascending order
-    uint16_t group_n[PFX_MAX_GROUPS];
+    uint32_t group_n[PFX_MAX_GROUPS / 2];      // members per group, two 16-bit numbers a word (a batch has less than 2^16 sequences)
 };
 
 template <int D> constexpr size_t pfx_smem_bytes() {
@@ -106,12 +130,12 @@ template <int D> constexpr size_t pfx_smem_bytes() {
 }
 
 // First token of a stream's tile i, and the number of tile (stream s, i) in the order in which tiles are loaded.
-__device__ __forceinline__ int pfx_tile_token(const PfxItem& it, int s, int i) { return (it.lo[s] & ~(PFX_TILE - 1)) + i * PFX_TILE; }
+__device__ __forceinline__ int pfx_tile_token(const PfxItem& it, int s, int i) { return (it.lo(s) & ~(PFX_TILE - 1)) + i * PFX_TILE; }
 __device__ __forceinline__ int pfx_tile_index(const PfxItem& it, int s, int i) {
     if (it.wide) return i;
-    return s == 0 ? i + min(i, it.tiles[1]) : min(i + 1, it.tiles[0]) + i;
+    return s == 0 ? i + min(i, it.tiles(1)) : min(i + 1, it.tiles(0)) + i;
 }
-__device__ __forceinline__ int pfx_total_tiles(const PfxItem& it) { return it.wide ? it.tiles[0] : it.tiles[0] + it.tiles[1]; }
+__device__ __forceinline__ int pfx_total_tiles(const PfxItem& it) { return it.wide ? it.tiles(0) : it.tiles(0) + it.tiles(1); }
 
 // Two weights -> packed hi terms (rounded) and packed lo terms (what that left, rounded): at most 2^-18 (bf16) or 2^-24
 // (fp16) of a weight is lost.
@@ -127,6 +151,17 @@ __device__ __forceinline__ void st_global_hint8(float* addr, const float (&v)[8]
     asm volatile("st.global.L2::cache_hint.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8}, %9;"
                  ::"l"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "l"(policy)
                  : "memory");
+}
+template <int N>
+__device__ __forceinline__ float row_max(const float* x) {
+    float m[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) m[c] = fmaxf(x[2 * c], x[2 * c + 1]);
+#pragma unroll
+    for (int u = 8; u < N; u += 8)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) m[c] = max3(m[c], x[u + 2 * c], x[u + 2 * c + 1]);
+    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -174,48 +209,52 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
         tmem_alloc(&ctl.tmem, 512);
         tmem_relinquish();
     }
-    int* const count = reinterpret_cast<int*>(pfx_raw);            // (Q's place: nothing else writes there before the first item)
-    for (int g = tid; g < p.NG; g += PFX_THREADS) count[g] = 0;
+    for (int g = tid; g < PFX_MAX_GROUPS / 2; g += PFX_THREADS) ctl.group_n[g] = 0;
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&ctl.tmem);
 
-    cudaTriggerProgrammaticLaunchCompletion();
-    cudaGridDependencySynchronize();
-    const bool skip = p.status && (*reinterpret_cast<volatile int32_t*>(p.status) & HG_DEV_WAIT_TIMEOUT);
-    for (int b = tid; b < p.B; b += PFX_THREADS) {
-        const uint32_t g = (uint32_t)p.seq_group[b];
-        if (g < (uint32_t)p.NG) atomicAdd(&count[g], 1);
-    }
-    if (blockIdx.x == 0 && p.zero && tid < 2) p.zero[tid] = 0;
-    __syncthreads();
-    for (int g = tid; g < p.NG; g += PFX_THREADS) {
-        ctl.group_n[g] = (uint16_t)count[g];
-        if (blockIdx.x == 0 && p.status && group_slice(p, g).bad) atomicOr(p.status, HG_DEV_RANGE);
-    }
-    __syncthreads();
-
     int issued = 0;                                                // (loaders) tiles requested so far
     uint32_t edges = 0;                                            // (V loader) tiles that went over the edge barrier
     bool edge_open = false;                                        // ... and one that is still on its way
+    cudaTriggerProgrammaticLaunchCompletion();
+    auto timed_out = [&]() { return p.status && (*reinterpret_cast<volatile int32_t*>(p.status) & HG_DEV_WAIT_TIMEOUT); };
     // 512 threads x 128 registers at the launch: the softmax warps, which hold a whole row of S, take 72 from the others
-    if (skip) {
-        // an earlier call timed out: no work until the caller has cleared the word
-    } else if (warp >= 8) {
+    if (warp >= 8) {
       reg_shrink<PFX_REGS_OTHER>();
-      if (warp == PFX_ITEM_WARP) {
+      cudaGridDependencySynchronize();
+      GroupSlice first_slice;                                      // (item warp) on its way while the members are counted
+      first_slice.nc = 0;
+      if (warp == PFX_ITEM_WARP && lane < p.NG) first_slice = group_slice(p, lane);
+      for (int b = tid - 256; b < p.B; b += 256) {
+          const uint32_t g = (uint32_t)p.seq_group[b];
+          if (g < (uint32_t)p.NG) atomicAdd(&ctl.group_n[g >> 1], (g & 1) ? 0x10000u : 1u);
+      }
+      if (blockIdx.x == 0 && p.zero && tid < 258) p.zero[tid - 256] = 0;
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      if (timed_out()) {
+          // an earlier call ran into its limit: no work until the caller has cleared the word
+      } else if (warp == PFX_ITEM_WARP) {
         // =============================== item warp: decodes work items, one ahead ===============================
-        int gb = 0;                                                // first of the 32 groups in the lanes
-        long long base = 0;                                        // items of the groups before them
-        GroupSlice sl;
+        // units: the groups, then (where they are part of the launch) the sequences; 32 at a time in the lanes
+        const int group_units = (p.NG + 31) & ~31, units = group_units + (p.own ? p.B : 0);
+        int ub = 0;                                                // first of the units in the lanes
+        long long base = 0;                                        // items of the units before them
+        GroupSlice sl = first_slice;
         int R = 0, wide_tiles = 0, narrow_rows = 0, n_items = 0, before = 0, block_items = 0;
-        auto load_groups = [&]() {
+        auto load_units = [&]() {
             n_items = 0;
-            sl.nc = 0;
-            if (gb + lane < p.NG) {
-                sl = group_slice(p, gb + lane);
-                R = ctl.group_n[gb + lane] * p.G;
+            R = 0;
+            const int u = ub + lane;
+            if (ub < group_units) {
+                if (ub > 0 && u < p.NG) sl = group_slice(p, u);
+                if (u < p.NG) R = (int)((ctl.group_n[u >> 1] >> ((u & 1) * 16)) & 0xffffu) * p.G;
+            } else if (u < units) {
+                sl = own_slice(p, u - group_units);
+                R = p.G;
+            }
+            if (R > 0) {
                 const int rem = R % 256;
                 wide_tiles = R / 256 + (rem > 128 ? 1 : 0);
                 narrow_rows = rem <= 128 ? rem : 0;
@@ -230,29 +269,35 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             before = x - n_items;
             block_items = __shfl_sync(0xffffffffu, x, 31);
         };
-        load_groups();
+        load_units();
         bool ok = true;
         int k = 0;
         for (long long i = blockIdx.x; ok; i += gridDim.x, ++k) {
-            while (gb < p.NG && i >= base + block_items) { base += block_items; gb += 32; load_groups(); }
+            while (ub < units && i >= base + block_items) {
+                base += block_items;
+                ub += 32;
+                if (ub < units) load_units();
+            }
             const int j = k & 1;
             if (k >= 2) ok = warp_wait(&ctl.item_empty[j], (uint32_t)((k - 2) >> 1) & 1u, abort_flag);
             if (!ok) break;
             PfxItem& it = ctl.item[j];
-            if (gb >= p.NG) {
+            if (ub >= units) {
                 if (lane == 0) { it.valid = 0; mbar_arrive(&ctl.item_full[j]); }
                 break;
             }
             const int at = (int)(i - base);
             const bool mine = at >= before && at < before + n_items;
             const int src = __ffs(__ballot_sync(0xffffffffu, mine)) - 1;
+            const bool own = ub >= group_units;
             int m0 = 0, members = 0;
             if (mine) {
                 int e = at - before;
-                const int wides = p.Hkv * wide_tiles * sl.nc;
+                const int wides = p.Hkv * wide_tiles * sl.nc, C = own ? p.own_C : p.C;
                 it.valid = 1;
+                it.own = own;
                 it.row = sl.row;
-                const int chunk0 = sl.begin / p.C;
+                const int chunk0 = sl.begin / C;
                 int c;
                 if (e < wides) {                                   // row tiles fastest: CTAs side by side read the same tiles
                     const int t = e % wide_tiles; e /= wide_tiles;
@@ -270,17 +315,25 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                 it.chunk = c;
                 for (int s = 0; s < 2; ++s) {
                     const int cs = it.wide ? c : c + s;
-                    it.lo[s] = max(sl.begin, (chunk0 + cs) * p.C);
-                    it.hi[s] = cs < sl.nc ? (int)min((long long)sl.end, (long long)(chunk0 + cs + 1) * p.C) : it.lo[s];
-                    it.tiles[s] = it.hi[s] > it.lo[s] ? (it.hi[s] - (it.lo[s] & ~(PFX_TILE - 1)) + PFX_TILE - 1) / PFX_TILE : 0;
+                    const int lo = max(sl.begin, (chunk0 + cs) * C);
+                    const int hi = cs < sl.nc ? (int)min((long long)sl.end, (long long)(chunk0 + cs + 1) * C) : lo;
+                    (s ? it.lo1 : it.lo0) = lo;
+                    (s ? it.hi1 : it.hi0) = hi;
+                    (s ? it.tiles1 : it.tiles0) = hi > lo ? (hi - (lo & ~(PFX_TILE - 1)) + PFX_TILE - 1) / PFX_TILE : 0;
                 }
                 m0 = it.r0 / p.G;
                 members = (it.r0 + it.rows - 1) / p.G - m0 + 1;
                 it.m0 = m0;
+                if (own) ctl.members[j][0] = (uint16_t)sl.row;
+            }
+            if (own) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl.item_full[j]);
+                continue;
             }
             m0 = __shfl_sync(0xffffffffu, m0, src);
             members = __shfl_sync(0xffffffffu, members, src);
-            const int g = gb + src;
+            const int g = ub + src;
             int seen = 0;                                          // members met so far
             for (int b0 = 0; b0 < p.B && seen < m0 + members; b0 += 128) {
                 int sg[4];
@@ -314,16 +367,16 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl.item_empty[j]);
             if (!it.valid) break;
-            const int total = pfx_total_tiles(it), both = min(it.tiles[0], it.tiles[1]);
+            const int total = pfx_total_tiles(it), both = min(it.tiles(0), it.tiles(1));
             // the block-table entry of this lane's box of tile x (in load order); -1: not wanted, -2: refused
             int lo = 0, hi = 0, t = 0;
             auto entry = [&](int x) -> int {
                 int s = 0, i = x;
                 if (!it.wide) {
                     if (x < 2 * both) { s = x & 1; i = x >> 1; }
-                    else { s = it.tiles[0] > both ? 0 : 1; i = x - both; }
+                    else { s = it.tiles(0) > both ? 0 : 1; i = x - both; }
                 }
-                lo = it.lo[s]; hi = it.hi[s];
+                lo = it.lo(s); hi = it.hi(s);
                 t = pfx_tile_token(it, s, i) + piece * box_rows;
                 if (lane >= boxes || x >= total || t >= hi || t + box_rows <= lo) return -1;
                 const int e = p.block_table ? p.block_table[(size_t)it.row * p.max_pages + (t >> p.page_shift)]
@@ -422,7 +475,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                 }
                 ++np[s];
                 if (!im.wide || s == 1) tc_commit(&ctl.empty[slot]);
-                if (i == im.tiles[s] - 1) tc_commit(&ctl.o_full[s]);
+                if (i == im.tiles(s) - 1) tc_commit(&ctl.o_full[s]);
             };
             for (int k = 0; ok; ++k) {
                 const int j = k & 1;
@@ -433,28 +486,28 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                 if (!it.valid) break;
                 ok = mbar_wait(&ctl.q_full, (uint32_t)k & 1u, abort_flag);
                 if (!ok) break;
-                int left = it.tiles[0] + it.tiles[1];              // score products still to issue
-                if (it.tiles[0] > 0) scores(0, 0, --left == 0);
-                if (ok && held) values(prev, prev_n, 1, prev.tiles[1] - 1);
+                int left = it.tiles(0) + it.tiles(1);              // score products still to issue
+                if (it.tiles(0) > 0) scores(0, 0, --left == 0);
+                if (ok && held) values(prev, prev_n, 1, prev.tiles(1) - 1);
                 held = false;
-                if (ok && it.tiles[1] > 0) scores(1, 0, --left == 0);
-                const int steps = max(it.tiles[0], it.tiles[1]);
+                if (ok && it.tiles(1) > 0) scores(1, 0, --left == 0);
+                const int steps = max(it.tiles(0), it.tiles(1));
                 for (int i = 0; i < steps && ok; ++i) {
-                    if (i < it.tiles[0]) {
+                    if (i < it.tiles(0)) {
                         values(it, n, 0, i);
-                        if (ok && i + 1 < it.tiles[0]) scores(0, i + 1, --left == 0);
+                        if (ok && i + 1 < it.tiles(0)) scores(0, i + 1, --left == 0);
                     }
-                    if (ok && i < it.tiles[1]) {
+                    if (ok && i < it.tiles(1)) {
                         if (i + 1 == steps) { held = true; break; }            // behind the next item's first scores
                         values(it, n, 1, i);
-                        if (ok && i + 1 < it.tiles[1]) scores(1, i + 1, --left == 0);
+                        if (ok && i + 1 < it.tiles(1)) scores(1, i + 1, --left == 0);
                     }
                 }
                 prev = it;
                 prev_n = n;
                 n += pfx_total_tiles(it);
             }
-            if (ok && held) values(prev, prev_n, 1, prev.tiles[1] - 1);
+            if (ok && held) values(prev, prev_n, 1, prev.tiles(1) - 1);
             int none = 0;                                          // nothing is in flight when the tensor memory is given back
             tc_commit(&ctl.drain);
             mbar_wait(&ctl.drain, 0u, &none);
@@ -491,44 +544,63 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
         const int s = warp >> 2, w4 = warp & 3;                    // stream, quarter of its rows
         const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
         const uint32_t s_tmem = tmem + PFX_S_COL + s * 128 + lanes, o_tmem = tmem + PFX_O_COL + s * 128 + lanes;
-        const float sl = p.scale_log2;
+        const float sc = p.scale_log2;
         const uint64_t keep = l2_evict_last_policy();
-        // slots that hold nothing: sequences without a group, chunks beyond a group's slice
+        // slots that hold nothing: sequences without a group, chunks beyond a slice
+        auto write_empty = [&](int b, int nc, int NC, float* m_out, float* l_out, float* o_out) {
+            const int none = NC - nc;
+            for (int i = lane; i < p.Hq * none; i += 32) {
+                const size_t slot = ((size_t)b * p.Hq + i / none) * NC + nc + i % none;
+                m_out[slot] = NEG_INF;
+                l_out[slot] = 0.f;
+            }
+            if (p.sparse_empty) return;
+            for (int i = 0; i < p.Hq * none; ++i) {
+                const size_t slot = ((size_t)b * p.Hq + i / none) * NC + nc + i % none;
+                if (lane < D / 4) reinterpret_cast<float4*>(o_out + slot * D)[lane] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+        };
+        auto write_empties = [&]() {
         for (int b = blockIdx.x * 8 + warp; b < p.B; b += gridDim.x * 8) {
             const uint32_t g = (uint32_t)p.seq_group[b];
-            const int nc = g < (uint32_t)p.NG ? group_slice(p, (int)g).nc : 0;
-            const int none = p.NC - nc;
-            if (none == 0) continue;
-            for (int i = lane; i < p.Hq * none; i += 32) {
-                const size_t slot = ((size_t)b * p.Hq + i / none) * p.NC + nc + i % none;
-                p.m_part[slot] = NEG_INF;
-                p.l_part[slot] = 0.f;
-            }
-            if (p.sparse_empty) continue;
-            for (int i = 0; i < p.Hq * none; ++i) {
-                const size_t slot = ((size_t)b * p.Hq + i / none) * p.NC + nc + i % none;
-                if (lane < D / 4) reinterpret_cast<float4*>(p.o_part + slot * D)[lane] = make_float4(0.f, 0.f, 0.f, 0.f);
-            }
+            write_empty(b, g < (uint32_t)p.NG ? group_slice(p, (int)g).nc : 0, p.NC, p.m_part, p.l_part, p.o_part);
+            if (!p.own) continue;
+            const GroupSlice sl = own_slice(p, b);
+            if (sl.bad && lane == 0 && p.status) atomicOr(p.status, HG_DEV_RANGE);
+            write_empty(b, sl.nc, p.own_NC, p.own_m, p.own_l, p.own_o);
         }
+        for (int g = blockIdx.x * 256 + tid; g < p.NG; g += gridDim.x * 256)
+            if (p.status && group_slice(p, g).bad) atomicOr(p.status, HG_DEV_RANGE);
+        };
         bool ok = true;
         uint32_t ns = 0, no = 0;                                   // tiles and items of this stream so far
-        for (int k = 0; ok; ++k) {
+        // Round -1 runs a tile's code on whatever stands in tensor memory and hands nothing on, before the wait for the
+        // kernel in front of this one: the tile's instructions (some 20 KB) are in the caches when the first S is there
+        for (int k = -1; ok; ++k) {
             const int j = k & 1;
-            ok = warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
-            if (!ok) break;
-            const PfxItem it = ctl.item[j];
-            if (!it.valid) break;
-            const int tiles = it.tiles[s], first_row = (it.wide ? s * PFX_TILE : 0) + w4 * 32;
-            const bool live = first_row < it.rows;                 // some row of this warp exists
-            const bool exists = first_row + lane < it.rows;        // this thread's
-            float m_true = NEG_INF, m_ref = NEG_INF, l = 0.f;      // the maximum, and the one the weights refer to (raw logits)
-            for (int i = 0; i < tiles; ++i, ++ns) {
-                ok = warp_wait(&ctl.s_full[s], ns & 1u, abort_flag);
+            const bool dry = k < 0;
+            int lo = 0, hi = PFX_TILE, tiles = 1, rows = PFX_TILE, wide = 0;      // (of the dry round)
+            if (!dry) {
+                ok = warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
                 if (!ok) break;
+                const PfxItem& it = ctl.item[j];
+                if (!it.valid) break;
+                lo = it.lo(s); hi = it.hi(s); tiles = it.tiles(s); rows = it.rows; wide = it.wide;
+            }
+            const int first_row = (wide ? s * PFX_TILE : 0) + w4 * 32;
+            const bool live = first_row < rows;                    // some row of this warp exists
+            const bool exists = first_row + lane < rows;           // this thread's
+            float m_true = NEG_INF, m_ref = NEG_INF, l = 0.f;      // the maximum, and the one the weights refer to (raw logits)
+            for (int i = 0; i < tiles; ++i) {
+                if (!dry) {
+                    ok = warp_wait(&ctl.s_full[s], ns & 1u, abort_flag);
+                    if (!ok) break;
+                    ++ns;
+                }
                 tc_fence_after_sync();
                 if (live) {
-                    const int t = pfx_tile_token(it, s, i);
-                    const int c_lo = max(it.lo[s] - t, 0), c_hi = min(it.hi[s] - t, PFX_TILE);
+                    const int t = (lo & ~(PFX_TILE - 1)) + i * PFX_TILE;
+                    const int c_lo = max(lo - t, 0), c_hi = min(hi - t, PFX_TILE);
                     const uint32_t bad = *reinterpret_cast<volatile uint8_t*>(&ctl.stream_bad[s]);
                     const bool edge = c_lo > 0 || c_hi < PFX_TILE || bad;
                     float x[PFX_TILE];
@@ -540,21 +612,14 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                         for (int u = 0; u < PFX_TILE; ++u)
                             if (u < c_lo || u >= c_hi || ((bad >> (u >> 4)) & 1u)) x[u] = NEG_INF;
                     }
-                    float mx4[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) mx4[c] = fmaxf(x[2 * c], x[2 * c + 1]);
-#pragma unroll
-                    for (int u = 8; u < PFX_TILE; u += 8)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) mx4[c] = max3(mx4[c], x[u + 2 * c], x[u + 2 * c + 1]);
-                    const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+                    const float mx = row_max<PFX_TILE>(x);
                     m_true = fmaxf(m_true, mx);
                     // a row's sums follow its maximum only when that has moved by more than 2^8 (then the weights would leave
                     // the 16-bit types' comfortable range); the difference is put right at the end.  Each row decides by
                     // itself, so its result does not depend on its neighbours (rows that do not exist among them)
-                    const bool moved = (m_true - m_ref) * sl > 8.f;
+                    const bool moved = (m_true - m_ref) * sc > 8.f;
                     if (__any_sync(0xffffffffu, moved && exists)) {
-                        const float r = !moved ? 1.f : m_ref == NEG_INF ? 0.f : fast_exp2((m_ref - m_true) * sl);
+                        const float r = !moved ? 1.f : m_ref == NEG_INF ? 0.f : fast_exp2((m_ref - m_true) * sc);
                         if (moved) m_ref = m_true;
                         if (i > 0) {
                             l *= r;
@@ -569,26 +634,32 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                             }
                         }
                     }
-                    const float off = m_ref == NEG_INF ? 0.f : -m_ref * sl;
-                    const float2 sl2 = make_float2(sl, sl), off2 = make_float2(off, off);
+                    const float off = m_ref == NEG_INF ? 0.f : -m_ref * sc;
+                    const float2 sc2 = make_float2(sc, sc), off2 = make_float2(off, off);
                     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    // a quarter of the tokens at a time; each is handed over when the next one's weights are computed (a store
+                    // into tensor memory takes some 300 cycles to complete while the tensor cores work)
+                    auto hand_over = [&](int c) {
+                        tmem_st_wait();
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0 && !dry) mbar_arrive(&ctl.p_full[s][c]);
+                    };
 #pragma unroll
-                    for (int c0 = 0; c0 < PFX_TILE; c0 += 32) {
+                    for (int c = 0; c < 4; ++c) {
                         uint32_t w[32];
 #pragma unroll
                         for (int u = 0; u < 16; ++u) {
-                            float2 e = fma2(make_float2(x[c0 + 2 * u], x[c0 + 2 * u + 1]), sl2, off2);
+                            float2 e = fma2(make_float2(x[c * 32 + 2 * u], x[c * 32 + 2 * u + 1]), sc2, off2);
                             e.x = fast_exp2(e.x);
                             e.y = fast_exp2(e.y);
                             sum[u & 1] = add2(sum[u & 1], e);
                             split2<BF16>(e, w[u], w[16 + u]);
                         }
-                        tmem_st_32x32(s_tmem + c0, w);
-                        tmem_st_wait();                            // this quarter of the tokens can be multiplied
-                        tc_fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&ctl.p_full[s][c0 / 32]);
+                        if (c > 0) hand_over(c - 1);
+                        if (!dry) tmem_st_32x32(s_tmem + c * 32, w);
                     }
+                    hand_over(3);
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 } else {
                     tc_fence_before_sync();
@@ -596,33 +667,45 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                     if (lane < 4) mbar_arrive(&ctl.p_full[s][lane]);
                 }
             }
+            if (dry) {
+                cudaGridDependencySynchronize();
+                if (timed_out()) break;
+                write_empties();
+                continue;
+            }
             if (ok && tiles > 0) {
                 ok = warp_wait(&ctl.o_full[s], no & 1u, abort_flag);
                 if (!ok) break;
                 ++no;
                 tc_fence_after_sync();
                 if (live) {
+                    const PfxItem& it = ctl.item[j];
                     const int r = it.r0 + first_row + lane;
                     const int m = r / p.G, head = it.h * p.G + r - m * p.G;
                     const int b = exists ? ctl.members[j][m - it.m0] : 0;
-                    const size_t slot = ((size_t)b * p.Hq + head) * p.NC + it.chunk + (it.wide ? 0 : s);
-                    const float f = m_true == NEG_INF ? 0.f : fast_exp2((m_ref - m_true) * sl);
+                    const bool own = it.own;
+                    const size_t slot = ((size_t)b * p.Hq + head) * (own ? p.own_NC : p.NC) + it.chunk + (wide ? 0 : s);
+                    float* const dst = (own ? p.own_o : p.o_part) + slot * D;
+                    const float f = m_true == NEG_INF ? 0.f : fast_exp2((m_ref - m_true) * sc);
                     if (exists) {
-                        p.m_part[slot] = m_true == NEG_INF ? NEG_INF : m_true * p.scale;
-                        p.l_part[slot] = l * f;
+                        (own ? p.own_m : p.m_part)[slot] = m_true == NEG_INF ? NEG_INF : m_true * p.scale;
+                        (own ? p.own_l : p.l_part)[slot] = l * f;
                     }
-                    uint32_t x[D];
+                    {
+#pragma unroll 1
+                        for (int h = 0; h < D; h += 64) {
+                            uint32_t x[64];
+                            tmem_ld_32x32(o_tmem + h, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
+                            tmem_ld_32x32(o_tmem + h + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
+                            tmem_ld_wait();
+                            if (exists)
 #pragma unroll
-                    for (int c0 = 0; c0 < D; c0 += 32) tmem_ld_32x32(o_tmem + c0, *reinterpret_cast<uint32_t(*)[32]>(&x[c0]));
-                    tmem_ld_wait();
-                    if (exists) {
-                        float* const dst = p.o_part + slot * D;
+                            for (int c0 = 0; c0 < 64; c0 += 8) {
+                                float y[8];
 #pragma unroll
-                        for (int c0 = 0; c0 < D; c0 += 8) {
-                            float y[8];
-#pragma unroll
-                            for (int u = 0; u < 8; ++u) y[u] = __uint_as_float(x[c0 + u]) * f;
-                            st_global_hint8(dst + c0, y, keep);
+                                for (int u = 0; u < 8; ++u) y[u] = __uint_as_float(x[c0 + u]) * f;
+                                st_global_hint8(dst + h + c0, y, keep);
+                            }
                         }
                     }
                 }
