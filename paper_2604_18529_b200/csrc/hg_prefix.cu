@@ -107,6 +107,7 @@ static hg_status run_prefix(const void* q, const void* k, const void* v, float* 
     p.test_stall = (d->flags & HG_FLAG_TEST_STALL) ? 1 : 0;
     p.scale = d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->head_dim);
     p.scale_log2 = p.scale * 1.4426950408889634f;
+    p.div_G = make_fast_div((uint32_t)p.G);
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     const bool bf16 = d->dtype == HG_DTYPE_BF16, pdl = !desc_tune(d).off(HG_TUNE_NO_PDL);
     if (d->head_dim == 128) return bf16 ? launch_prefix<128, true>(tk, tv, p, cs, pdl) : launch_prefix<128, false>(tk, tv, p, cs, pdl);

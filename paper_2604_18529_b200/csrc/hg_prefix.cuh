@@ -25,6 +25,7 @@
 #include <stdint.h>
 
 #include "hg_device.cuh"
+#include "hg_partial.cuh"
 #include "hg_tcgen05.cuh"
 
 namespace hg {
@@ -53,6 +54,7 @@ struct PrefixParams {
     int page_size, page_shift, max_pages, num_pages;
     int sparse_empty, test_stall;
     float scale, scale_log2;
+    FastDiv div_G;
 };
 
 // The slice of a group (or a sequence's own one), clamped to its block-table row, and its chunks.
@@ -368,25 +370,30 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             if (lane == 0) mbar_arrive(&ctl.item_empty[j]);
             if (!it.valid) break;
             const int total = pfx_total_tiles(it), both = min(it.tiles(0), it.tiles(1));
-            // the block-table entry of this lane's box of tile x (in load order); -1: not wanted, -2: refused
-            int lo = 0, hi = 0, t = 0;
-            auto entry = [&](int x) -> int {
+            // the block-table entry of this lane's box of tile x (in load order), as it comes: nothing looks at it before its
+            // tile's turn, so the look-up, two tiles ahead, is not waited for
+            struct Box { int lo, hi, t, e; bool want; };
+            auto look_up = [&](int x) -> Box {
                 int s = 0, i = x;
                 if (!it.wide) {
                     if (x < 2 * both) { s = x & 1; i = x >> 1; }
                     else { s = it.tiles(0) > both ? 0 : 1; i = x - both; }
                 }
-                lo = it.lo(s); hi = it.hi(s);
-                t = pfx_tile_token(it, s, i) + piece * box_rows;
-                if (lane >= boxes || x >= total || t >= hi || t + box_rows <= lo) return -1;
-                const int e = p.block_table ? p.block_table[(size_t)it.row * p.max_pages + (t >> p.page_shift)]
-                                            : it.row * p.max_pages + (t >> p.page_shift);
-                return (uint32_t)e < (uint32_t)p.num_pages ? e : -2;
+                Box v;
+                v.lo = it.lo(s); v.hi = it.hi(s);
+                v.t = pfx_tile_token(it, s, i);
+                const int t = v.t + piece * box_rows;
+                v.want = lane < boxes && x < total && t < v.hi && t + box_rows > v.lo;
+                v.e = it.row * p.max_pages + (t >> p.page_shift);
+                if (v.want && p.block_table) v.e = p.block_table[(size_t)it.row * p.max_pages + (t >> p.page_shift)];
+                return v;
             };
-            int next = entry(0);
+            Box b0 = look_up(0), b1 = look_up(1);
             for (int x = 0; x < total; ++x) {
-                const int e = next, row = t & (p.page_size - 1), t_x = t - piece * box_rows, lo_x = lo, hi_x = hi;
-                next = entry(x + 1);                               // one tile ahead: the look-up is not waited for
+                const int lo_x = b0.lo, hi_x = b0.hi, t_x = b0.t, row = (b0.t + piece * box_rows) & (p.page_size - 1);
+                const int e = !b0.want ? -1 : ((uint32_t)b0.e < (uint32_t)p.num_pages ? b0.e : -2);      // -1: not wanted, -2: refused
+                b0 = b1;
+                b1 = look_up(x + 2);
                 const int seq = 2 * (n + x) + (is_k ? 0 : 1), slot = seq % S;
                 const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, e >= 0)) * (uint32_t)box_rows * 128u;
                 uint32_t bad = 0;
@@ -526,11 +533,21 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             if (k >= 1) ok = warp_wait(&ctl.q_free, (uint32_t)(k - 1) & 1u, abort_flag);
             if (!ok) break;
             const int c = t % VECS;
-            for (int r = t / VECS; r < rows; r += 128 / VECS) {
-                const int m = (r0 + r) / p.G, head = h * p.G + (r0 + r) - m * p.G;
-                const uint16_t* src = p.q + ((size_t)ctl.members[j][m - m0] * p.Hq + head) * D + c * 8;
-                const int rr = r & (PFX_TILE - 1);
-                cp_async16(smem_u32(pfx_raw) + (r >> 7) * TILE_BYTES + (c >> 3) * HALF_BYTES + rr * 128 + (((c & 7) ^ (rr & 7)) << 4), src);
+            // eight rows at a time: their look-ups overlap
+            for (int rb = t / VECS; rb < rows; rb += 8 * (128 / VECS)) {
+                const uint16_t* src[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int q = r0 + min(rb + u * (128 / VECS), rows - 1), m = fast_div(q, p.div_G);
+                    src[u] = p.q + ((size_t)ctl.members[j][m - m0] * p.Hq + h * p.G + q - m * p.G) * D + c * 8;
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int r = rb + u * (128 / VECS), rr = r & (PFX_TILE - 1);
+                    if (r >= rows) continue;
+                    const uint32_t at = smem_u32(pfx_raw) + (c >> 3) * HALF_BYTES + (((c & 7) ^ (rr & 7)) << 4);
+                    cp_async16(at + (r >> 7) * TILE_BYTES + rr * 128, src[u]);
+                }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
             fence_proxy_async();
