@@ -485,7 +485,7 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
  *                   the call: src_row[b] = b leaves the row alone, a negative one frees it (entries -1, lengths 0).
  *                   Several rows may take the same one, and rows may take each other's (a beam step).  seq_lens,
  *                   tok_begin and tok_end (the last two may be NULL) move with the rows; counts follow the entries.
- *                   A value of B or more leaves the row alone and sets HG_DEV_RANGE.  Batches up to 40960.
+ *                   A value of B or more leaves the row alone and sets HG_DEV_RANGE.
  *   hg_kv_reserve   makes positions [seq_lens[b], seq_lens[b] + n_new[b]) of every row writable (n_new: dev int32 [B],
  *                   or NULL for one each; 0 or less: nothing): a slot without a page gets one, a page that others use
  *                   too is replaced by a page of the row's own (copy on write).  Sequences are served as if one after

@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "hg_hostutil.h"
 #include "hg_pages.cuh"
 
@@ -27,11 +29,18 @@ static hg_status launch_pages(void (*kern)(P...), unsigned grid, unsigned thread
         ++na;
     }
     cfg.attrs = attr; cfg.numAttrs = (unsigned)na;
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
-        cudaGetLastError();
-        return HG_ERR_CUDA;
-    }
     if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) { cudaGetLastError(); return HG_ERR_CUDA; }
+    return HG_OK;
+}
+
+// Once per kernel and device: the opt-in to `most` bytes of dynamic shared memory.  `done` is the kernel's own (a bit per
+// device; racing threads set the same attribute).
+static hg_status opt_in(const void* kern, size_t most, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return HG_ERR_CUDA; }
+    if ((done.load(std::memory_order_acquire) >> dev) & 1u) return HG_OK;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most) != cudaSuccess) { cudaGetLastError(); return HG_ERR_CUDA; }
+    done.fetch_or(1ull << dev, std::memory_order_release);
     return HG_OK;
 }
 
@@ -45,10 +54,13 @@ static hg_status check_table(const hg_attn_desc* d) {
 }
 
 static int sm_count() {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-        cudaGetLastError();
-        return 0;
+    static std::atomic<int> known[kMaxDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return 0; }
+    int sms = known[dev].load(std::memory_order_relaxed);
+    if (sms == 0) {
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return 0; }
+        known[dev].store(sms, std::memory_order_relaxed);
     }
     return sms;
 }
@@ -64,19 +76,28 @@ hg_status hg_kv_fork(const int32_t* src_row, int32_t* ref_count, int32_t* seq_le
     hg_status st = check_table(desc);
     if (st != HG_OK) return st;
     if (!src_row || !ref_count || !seq_lens) return HG_ERR_INVALID_ARG;
-    if ((size_t)desc->batch * 4 > FORK_SMEM_MAX) return HG_ERR_UNSUPPORTED;
     ForkParams p;
     p.src_row = src_row; p.table = const_cast<int32_t*>(desc->block_table); p.ref = ref_count;
     p.vec[0] = seq_lens; p.vec[1] = tok_begin; p.vec[2] = tok_end;
     p.status = desc->status; p.B = desc->batch; p.max_pages = desc->max_pages; p.num_pages = desc->num_pages;
-    // 32 columns (128-byte row pieces) where that leaves a CTA for every SM, down to 8 (one 32-byte sector) for short
-    // tables, and fewer only where the rows of the batch fill the shared memory
+    // a cluster of 8 CTAs shares a tile's rows once there is work for it (1024 rows of 64 entries: 4.1 us instead of 10.2; 256
+    // rows of 502: 5.7 instead of 4.2); 32 columns (128-byte row pieces) a tile where that
+    // leaves two CTAs for every SM, down to 8 (one 32-byte sector) for short tables, and fewer only where the rows of the
+    // batch fill the shared memory
+    const int cluster = p.B >= 512 ? 8 : 1;
+    const size_t rows = ((size_t)p.B + cluster - 1) / cluster;
     int shift = 5;
-    while (shift > 3 && (p.max_pages >> shift) < 148) --shift;
-    while (shift > 0 && ((size_t)p.B << shift) * 4 > FORK_SMEM_MAX) --shift;
+    while (shift > 3 && (p.max_pages >> shift) * cluster < 296) --shift;
+    while (shift > 0 && (rows << shift) * 4 > FORK_SMEM_MAX) --shift;
     p.cols_shift = shift;
     const unsigned tiles = (unsigned)((p.max_pages + (1 << shift) - 1) >> shift);
-    return launch_pages(kv_fork_kernel, tiles + 1, FORK_THREADS, ((size_t)p.B << shift) * 4, 1, stream, p);
+    const size_t smem = (rows << shift) * 4;
+    static std::atomic<uint64_t> done1, done8;
+    st = cluster == 8 ? opt_in(reinterpret_cast<const void*>(kv_fork_kernel<8>), FORK_SMEM_MAX, done8)
+                      : opt_in(reinterpret_cast<const void*>(kv_fork_kernel<1>), FORK_SMEM_MAX, done1);
+    if (st != HG_OK) return st;
+    return cluster == 8 ? launch_pages(kv_fork_kernel<8>, (tiles + 1) * 8, FORK_THREADS, smem, 8, stream, p)
+                        : launch_pages(kv_fork_kernel<1>, tiles + 1, FORK_THREADS, smem, 1, stream, p);
 }
 
 hg_status hg_kv_release(const int32_t* page_ids, int32_t n, int32_t* ref_count, void* stream, const hg_attn_desc* desc) {
@@ -100,6 +121,11 @@ hg_status hg_kv_reserve(const int32_t* seq_lens, const int32_t* n_new, int32_t* 
     p.copy_src = copy_src; p.copy_dst = copy_dst; p.copy_rows = copy_rows; p.n_ready = n_ready; p.status = desc->status;
     p.B = desc->batch; p.max_pages = desc->max_pages; p.num_pages = desc->num_pages; p.page_shift = ilog2_exact(desc->page_size);
     const size_t smem = ((size_t)RESERVE_IDS_PER_CTA + desc->batch) * 4;
+    static std::atomic<uint64_t> done1, done8;
+    constexpr size_t most = ((size_t)RESERVE_IDS_PER_CTA + RESERVE_MAX_BATCH) * 4;
+    st = opt_in(reinterpret_cast<const void*>(kv_reserve_kernel<1>), most, done1);
+    if (st == HG_OK) st = opt_in(reinterpret_cast<const void*>(kv_reserve_kernel<8>), most, done8);
+    if (st != HG_OK) return st;
     // a small pool and table: one CTA (its barriers are cheaper than the cluster's, and it can look at every slot there is)
     if (desc->num_pages <= 8192 && (int64_t)desc->batch * desc->max_pages <= PG_THREADS * RESERVE_MAX_ITER)
         return launch_pages(kv_reserve_kernel<1>, 1, PG_THREADS, smem, 1, stream, p);

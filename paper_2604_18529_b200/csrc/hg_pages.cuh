@@ -22,66 +22,6 @@ __device__ __forceinline__ void pages_begin() {
     cudaGridDependencySynchronize();
 }
 
-// ---- fork: rows of the block table take other rows' pages ----------------------------------------------------------
-
-constexpr int FORK_THREADS = 512;
-constexpr int FORK_SMEM_MAX = 160 * 1024;
-
-struct ForkParams {
-    const int32_t* src_row;          // [B]
-    int32_t* table;                  // [B][max_pages]
-    int32_t* ref;                    // [num_pages]
-    int32_t* vec[3];                 // seq_lens, tok_begin, tok_end (each may be NULL)
-    int32_t* status;
-    int B, max_pages, num_pages;
-    int cols_shift;                  // log2 of the block-table columns one CTA handles
-};
-
-// Columns of the table are independent of one another: a CTA stages its columns of every changed row's new contents in
-// shared memory, and writes only after all have been read, so rows may be each other's sources (a beam step re-orders
-// all rows in place).  Counts move by +1 / -1 per entry; entries that stay the same (the part beams have in common)
-// touch no count.  The last CTA moves the per-sequence lengths the same way.
-__global__ void __launch_bounds__(FORK_THREADS) kv_fork_kernel(const ForkParams p) {
-    extern __shared__ int32_t fork_stage[];
-    pages_begin();
-    const int tid = threadIdx.x;
-    if (blockIdx.x == gridDim.x - 1) {
-        for (int v = 0; v < 3; ++v) {
-            if (!p.vec[v]) continue;
-            for (int b = tid; b < p.B; b += FORK_THREADS) {
-                const int s = p.src_row[b];
-                if (v == 0 && s >= p.B && p.status) atomicOr(p.status, HG_DEV_RANGE);
-                fork_stage[b] = s < 0 ? 0 : p.vec[v][s < p.B ? s : b];
-            }
-            __syncthreads();
-            for (int b = tid; b < p.B; b += FORK_THREADS) p.vec[v][b] = fork_stage[b];
-            __syncthreads();
-        }
-        return;
-    }
-    const int cols = 1 << p.cols_shift;
-    const int c0 = (int)blockIdx.x << p.cols_shift;
-    const int n = p.B << p.cols_shift;                     // cells of this CTA (fits: B * cols * 4 <= FORK_SMEM_MAX)
-    for (int i = tid; i < n; i += FORK_THREADS) {
-        const int b = i >> p.cols_shift, c = c0 + (i & (cols - 1));
-        const int s = p.src_row[b];
-        if (s == b || s >= p.B || c >= p.max_pages) continue;
-        fork_stage[i] = s < 0 ? -1 : p.table[(size_t)s * p.max_pages + c];
-    }
-    __syncthreads();
-    for (int i = tid; i < n; i += FORK_THREADS) {
-        const int b = i >> p.cols_shift, c = c0 + (i & (cols - 1));
-        const int s = p.src_row[b];
-        if (s == b || s >= p.B || c >= p.max_pages) continue;
-        int32_t* const at = p.table + (size_t)b * p.max_pages + c;
-        const int was = *at, now = fork_stage[i];
-        if (was == now) continue;
-        if ((uint32_t)now < (uint32_t)p.num_pages) atomicAdd(p.ref + now, 1);
-        if ((uint32_t)was < (uint32_t)p.num_pages) atomicSub(p.ref + was, 1);
-        *at = now;
-    }
-}
-
 // ---- release: one reference less for every listed page ---------------------------------------------------------------
 
 __global__ void __launch_bounds__(256) kv_release_kernel(const int32_t* __restrict__ ids, int n, int32_t* ref, int num_pages,
@@ -144,12 +84,91 @@ __device__ __forceinline__ int cluster_warp_prefix(int v, ClusterScan& s, int ra
     return before;
 }
 
-// Orders the cluster's (or the CTA's) global-memory and shared-memory accesses before and after it.
+// Orders the cluster's (or the CTA's) global-memory and shared-memory accesses before and after it: the cluster barrier
+// releases and acquires at cluster scope, and what CTAs exchange through global memory is written by atomics or plain
+// stores and read past the L1 (__ldcg).
 template <int CLUSTER>
 __device__ __forceinline__ void cluster_sync_all() {
-    __threadfence();
     if constexpr (CLUSTER > 1) cooperative_groups::this_cluster().sync();
     else __syncthreads();
+}
+
+// ---- fork: rows of the block table take other rows' pages ----------------------------------------------------------
+
+constexpr int FORK_THREADS = 512;
+constexpr int FORK_UNROLL = 4;
+constexpr int FORK_SMEM_MAX = 160 * 1024;
+
+struct ForkParams {
+    const int32_t* src_row;          // [B]
+    int32_t* table;                  // [B][max_pages]
+    int32_t* ref;                    // [num_pages]
+    int32_t* vec[3];                 // seq_lens, tok_begin, tok_end (each may be NULL)
+    int32_t* status;
+    int B, max_pages, num_pages;
+    int cols_shift;                  // log2 of the block-table columns one cluster handles
+};
+
+// Columns of the table are independent of one another: a cluster stages its columns of every changed row's new contents in
+// shared memory (a share of the rows per CTA), and writes only after all have been read, so rows may be each other's
+// sources (a beam step re-orders all rows in place).  Counts move by +1 / -1 per entry; entries that stay the same (the part
+// beams have in common) touch no count.  The last cluster moves the per-sequence lengths the same way.
+template <int CLUSTER>
+__global__ void __launch_bounds__(FORK_THREADS) kv_fork_kernel(const ForkParams p) {
+    extern __shared__ int32_t fork_stage[];
+    const int tid = threadIdx.x;
+    const int rank = (int)blockIdx.x % CLUSTER, tile = (int)blockIdx.x / CLUSTER;
+    const int r0 = (int)((long long)p.B * rank / CLUSTER), r1 = (int)((long long)p.B * (rank + 1) / CLUSTER);
+    pages_begin();
+    if (tile == (int)gridDim.x / CLUSTER - 1) {
+        for (int v = 0; v < 3; ++v) {
+            if (!p.vec[v]) continue;                       // (uniform)
+            for (int b = r0 + tid; b < r1; b += FORK_THREADS) {
+                const int s = p.src_row[b];
+                if (v == 0 && s >= p.B && p.status) atomicOr(p.status, HG_DEV_RANGE);
+                fork_stage[b - r0] = s < 0 ? 0 : p.vec[v][s < p.B ? s : b];
+            }
+            cluster_sync_all<CLUSTER>();
+            for (int b = r0 + tid; b < r1; b += FORK_THREADS) p.vec[v][b] = fork_stage[b - r0];
+            __syncthreads();
+        }
+        return;
+    }
+    const int cols = 1 << p.cols_shift, c0 = tile << p.cols_shift;
+    const int n = (r1 - r0) << p.cols_shift;               // cells of this CTA (n * 4 <= FORK_SMEM_MAX)
+    // f(cell number, row, source, column) for this thread's cells, four look-ups of the source rows in flight
+    auto for_cells = [&](auto load, auto use) {
+        for (int i0 = tid; i0 < n; i0 += FORK_UNROLL * FORK_THREADS) {
+            int src[FORK_UNROLL], val[FORK_UNROLL];
+#pragma unroll
+            for (int u = 0; u < FORK_UNROLL; ++u) {
+                const int i = i0 + u * FORK_THREADS, b = r0 + (i >> p.cols_shift), c = c0 + (i & (cols - 1));
+                src[u] = i < n && c < p.max_pages ? p.src_row[b] : b;
+                if (src[u] >= p.B) src[u] = b;             // unchanged
+            }
+#pragma unroll
+            for (int u = 0; u < FORK_UNROLL; ++u) {
+                const int i = i0 + u * FORK_THREADS, b = r0 + (i >> p.cols_shift);
+                if (src[u] != b) val[u] = load(b, src[u], c0 + (i & (cols - 1)));
+            }
+#pragma unroll
+            for (int u = 0; u < FORK_UNROLL; ++u) {
+                const int i = i0 + u * FORK_THREADS, b = r0 + (i >> p.cols_shift);
+                if (src[u] != b) use(i, b, c0 + (i & (cols - 1)), val[u]);
+            }
+        }
+    };
+    for_cells([&](int, int s, int c) { return s < 0 ? -1 : p.table[(size_t)s * p.max_pages + c]; },
+              [&](int i, int, int, int v) { fork_stage[i] = v; });
+    cluster_sync_all<CLUSTER>();
+    for_cells([&](int b, int, int c) { return p.table[(size_t)b * p.max_pages + c]; },
+              [&](int i, int b, int c, int was) {
+                  const int now = fork_stage[i];
+                  if (was == now) return;
+                  if ((uint32_t)now < (uint32_t)p.num_pages) atomicAdd(p.ref + now, 1);
+                  if ((uint32_t)was < (uint32_t)p.num_pages) atomicSub(p.ref + was, 1);
+                  p.table[(size_t)b * p.max_pages + c] = now;
+              });
 }
 
 // The pages a warp looks after: a contiguous range, whole groups of 128 (32 lanes x 4).
@@ -211,13 +230,15 @@ __device__ __forceinline__ SlotRange reserve_slots(const ReserveParams& p, int b
     return r;
 }
 
-// One cluster does the whole call: its phases (give up a reference - find the last writer - rank the needs - hand out)
-// depend on one another, and a cluster barrier costs a few hundred nanoseconds where a launch costs microseconds.
+// One cluster does the whole call: its phases (find the shared pages - give up references - find the last writer - rank the
+// needs - hand out) depend on one another, and a cluster barrier costs a few hundred nanoseconds where a launch costs
+// microseconds.  Every phase is a round trip to the L2 for one slot per thread; so a thread keeps its first slot in
+// registers, the counts of its pages of the free scan too, and without a shared page the middle phases are left out.
 //
 // A page with `refs` references that k sequences of this call are about to write stays with the last of them exactly
 // when k = refs (nobody else reads it); all others copy.  That is what serving the sequences one after the other gives.
-// In parallel: every writer takes its reference off; a count that is still positive says that others remain; else the
-// writers leave the largest of their (sequence, slot) numbers there, as -(number + 1).
+// In parallel: every writer of a page with more than one reference takes its own off; a count that is still positive says
+// that others remain; else the writers leave the largest of their (sequence, slot) numbers there, as -(number + 1).
 template <int CLUSTER>
 __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(const ReserveParams p) {
     namespace cg = cooperative_groups;
@@ -225,14 +246,21 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(const ReservePar
     int32_t* const ids = reserve_smem;                            // this CTA's share of the free ids, by rank
     int32_t* const cum = reserve_smem + RESERVE_IDS_PER_CTA;      // cum[b]: slots of sequences < b
     __shared__ ClusterScan scan_a, scan_b;
-    __shared__ int s_warp[PG_WARPS], s_carry;
+    __shared__ int s_warp[PG_WARPS], s_carry, s_shared;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = CLUSTER > 1 ? (int)cg::this_cluster().block_rank() : 0;
-    pages_begin();
-
-    // ---- slots per sequence, and what is known without looking at any page ----
     if (tid == 0) s_carry = 0;
     __syncthreads();
+    pages_begin();
+
+    // ---- free pages of this warp's range: counted here, listed below (the first 512 counts stay in registers) ----
+    constexpr int KEEP = 4;
+    const PageRange pr = warp_pages<CLUSTER>(p.num_pages, rank, warp);
+    int4 refs[KEEP];
+#pragma unroll
+    for (int u = 0; u < KEEP; ++u) refs[u] = pr.begin + u * 128 < pr.end ? load_refs(p.ref, pr.begin + u * 128 + lane * 4, p.num_pages, 1) : make_int4(1, 1, 1, 1);
+
+    // ---- slots per sequence, and what is known without looking at any page ----
     for (int b0 = 0; b0 < p.B; b0 += PG_THREADS) {
         const int b = b0 + tid;
         SlotRange r;
@@ -265,21 +293,58 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(const ReservePar
     const int T = min(wanted, LANES * RESERVE_MAX_ITER);         // later slots are left for another call (n_ready says so)
     const int max_ids = CLUSTER * RESERVE_IDS_PER_CTA;
 
+    // ---- this thread's slots: a contiguous range per warp, consecutive slots on consecutive lanes ----
+    const int iters = (T + LANES - 1) / LANES;
+    const int first = (rank * PG_WARPS + warp) * iters * 32 + lane;
+    auto find_slot = [&](int i, int& b, int& slot) {             // the sequence whose range holds slot number i
+        int lo = 0, hi = p.B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (cum[mid] <= i) lo = mid;
+            else hi = mid - 1;
+        }
+        b = lo;
+        slot = (max(p.seq_lens[b], 0) >> p.page_shift) + i - cum[b];
+    };
+    auto cell = [&](int b, int slot) -> int32_t& { return p.table[(size_t)b * p.max_pages + slot]; };
+    int b_0 = 0, slot_0 = 0, e_0 = -1;
+    if (first < T) {
+        find_slot(first, b_0, slot_0);
+        e_0 = cell(b_0, slot_0);
+    }
+    // f(k, sequence, slot, entry) for every slot of this thread
+    auto for_slots = [&](auto f) {
+        if (first < T) f(0, b_0, slot_0, e_0);
+        for (int k = 1; k < iters; ++k) {
+            const int i = first + k * 32;
+            if (i >= T) break;
+            int b, slot;
+            find_slot(i, b, slot);
+            f(k, b, slot, cell(b, slot));
+        }
+    };
+    auto number = [&](int b, int slot) { return b * p.max_pages + slot; };
+    auto in_pool = [&](int e) { return (uint32_t)e < (uint32_t)p.num_pages; };
+    uint32_t need = 0, keep = 0, shared = 0, got = 0;            // one bit per slot
+    for_slots([&](int k, int, int, int e) {
+        if (!in_pool(e)) return;
+        if (__ldcg(p.ref + e) > 1) shared |= 1u << k;
+        else keep |= 1u << k;
+    });
+
     // ---- the lowest free ids, by rank, into the CTAs' shared memory ----
     {
-        const PageRange pr = warp_pages<CLUSTER>(p.num_pages, rank, warp);
+        auto free4 = [&](const int4& v) { return (v.x == 0) + (v.y == 0) + (v.z == 0) + (v.w == 0); };
         int mine = 0;
-        for (int g = pr.begin; g < pr.end; g += 128) {
-            const int4 v = load_refs(p.ref, g + lane * 4, p.num_pages, 1);
-            mine += (v.x == 0) + (v.y == 0) + (v.z == 0) + (v.w == 0);
-        }
+#pragma unroll
+        for (int u = 0; u < KEEP; ++u) mine += free4(refs[u]);
+        for (int g = pr.begin + KEEP * 128; g < pr.end; g += 128) mine += free4(load_refs(p.ref, g + lane * 4, p.num_pages, 1));
         mine = __reduce_add_sync(0xffffffffu, mine);
         int total;
         int at = cluster_warp_prefix<CLUSTER>(mine, scan_a, rank, warp, lane, total);
         const int limit = min(T, max_ids);
-        for (int g = pr.begin; g < pr.end && at < limit; g += 128) {
+        auto list = [&](const int4& v, int g) {
             const int id = g + lane * 4;
-            const int4 v = load_refs(p.ref, id, p.num_pages, 1);
             const int f[4] = {v.x == 0, v.y == 0, v.z == 0, v.w == 0};
             int step;
             int r = at + warp_exclusive(f[0] + f[1] + f[2] + f[3], lane, step);
@@ -292,87 +357,45 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(const ReservePar
                 r += f[j];
             }
             at += step;
-        }
+        };
+#pragma unroll
+        for (int u = 0; u < KEEP; ++u)
+            if (pr.begin + u * 128 < pr.end && at < limit) list(refs[u], pr.begin + u * 128);
+        for (int g = pr.begin + KEEP * 128; g < pr.end && at < limit; g += 128) list(load_refs(p.ref, g + lane * 4, p.num_pages, 1), g);
         s_carry = total;                                         // (every thread stores the same value)
     }
-    cluster_sync_all<CLUSTER>();
+    // ---- is any page shared?  (and: the ids are listed, everybody has read the counts) ----
+    bool any = __syncthreads_or(shared != 0) != 0;
     const int n_free = min(s_carry, max_ids);
-
-    // ---- this thread's slots: a contiguous range per warp, consecutive slots on consecutive lanes ----
-    const int iters = (T + LANES - 1) / LANES;
-    const int first = (rank * PG_WARPS + warp) * iters * 32 + lane;
-    auto slot_of = [&](int i, int& b, int& slot) {               // the sequence whose range holds slot number i
-        int lo = 0, hi = p.B - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (cum[mid] <= i) lo = mid;
-            else hi = mid - 1;
-        }
-        b = lo;
-        slot = (max(p.seq_lens[b], 0) >> p.page_shift) + i - cum[b];
-    };
-    auto cell = [&](int i, int& b, int& slot) -> int32_t* {
-        slot_of(i, b, slot);
-        return p.table + (size_t)b * p.max_pages + slot;
-    };
-    uint32_t need = 0, keep = 0, got = 0;                        // one bit per iteration
-    for (int k = 0; k < iters; ++k) {
-        const int i = first + k * 32;
-        if (i >= T) break;
-        int b, slot;
-        const int e = *cell(i, b, slot);
-        if ((uint32_t)e < (uint32_t)p.num_pages) atomicSub(p.ref + e, 1);
+    if constexpr (CLUSTER > 1) {
+        if (tid == 0) s_shared = any;
+        cg::this_cluster().sync();
+        int x = 0;
+#pragma unroll
+        for (int r = 0; r < CLUSTER; ++r) x |= *cg::this_cluster().map_shared_rank(&s_shared, r);
+        any = x != 0;
     }
-    cluster_sync_all<CLUSTER>();
-    for (int k = 0; k < iters; ++k) {
-        const int i = first + k * 32;
-        if (i >= T) break;
-        int b, slot;
-        const int e = *cell(i, b, slot);
-        if ((uint32_t)e < (uint32_t)p.num_pages && __ldcg(p.ref + e) <= 0) atomicMin(p.ref + e, -(b * p.max_pages + slot + 1));
+    if (any) {
+        for_slots([&](int k, int, int, int e) { if ((shared >> k) & 1u) atomicSub(p.ref + e, 1); });
+        cluster_sync_all<CLUSTER>();
+        for_slots([&](int k, int b, int slot, int e) {
+            if (((shared >> k) & 1u) && __ldcg(p.ref + e) <= 0) atomicMin(p.ref + e, -(number(b, slot) + 1));
+        });
+        cluster_sync_all<CLUSTER>();
     }
-    cluster_sync_all<CLUSTER>();
     int count = 0;
-    for (int k = 0; k < iters; ++k) {
-        const int i = first + k * 32;
-        if (i >= T) break;
-        int b, slot;
-        const int e = *cell(i, b, slot);
+    for_slots([&](int k, int b, int slot, int e) {
         bool n = e < 0;
-        if ((uint32_t)e < (uint32_t)p.num_pages) {
-            n = __ldcg(p.ref + e) != -(b * p.max_pages + slot + 1);
+        if ((shared >> k) & 1u) {
+            n = __ldcg(p.ref + e) != -(number(b, slot) + 1);
             if (!n) keep |= 1u << k;
         }
         if (n) { need |= 1u << k; ++count; }
-    }
+    });
     count = __reduce_add_sync(0xffffffffu, count);
     int needs;
-    int at = cluster_warp_prefix<CLUSTER>(count, scan_b, rank, warp, lane, needs);
+    int at = cluster_warp_prefix<CLUSTER>(count, scan_b, rank, warp, lane, needs);      // (everybody knows who keeps what)
     if (needs > n_free && rank == 0 && tid == 0 && p.status) atomicOr(p.status, HG_DEV_NO_PAGE);
-    for (int k = 0; k < iters; ++k) {
-        const int i = first + k * 32;
-        const bool n = (need >> k) & 1u;
-        const uint32_t votes = __ballot_sync(0xffffffffu, n);
-        const int r = at + __popc(votes & ((1u << lane) - 1u));
-        at += __popc(votes);
-        if (!n || r >= n_free) continue;
-        got |= 1u << k;
-        int id;
-        if constexpr (CLUSTER > 1) id = cg::this_cluster().map_shared_rank(ids, r & (CLUSTER - 1))[r / CLUSTER];
-        else id = ids[r];
-        int b, slot;
-        int32_t* const at_cell = cell(i, b, slot);
-        const int e = *at_cell;
-        *at_cell = id;
-        p.ref[id] = 1;
-        const int len = max(p.seq_lens[b], 0), in_page = len & ((1 << p.page_shift) - 1);
-        if (e >= 0 && slot == (len >> p.page_shift) && in_page) {   // the page holds tokens that the sequence keeps
-            p.copy_src[b] = e;
-            p.copy_dst[b] = id;
-            if (p.copy_rows) p.copy_rows[b] = in_page;
-        }
-    }
-    cluster_sync_all<CLUSTER>();                                  // the counts are not looked at any more for who keeps what
     auto stop_at = [&](int b, int slot) {                         // positions from this slot on are not ready
         if (!p.n_ready) return;
         const long long t = ((long long)slot << p.page_shift) - max(p.seq_lens[b], 0);
@@ -380,38 +403,54 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(const ReservePar
     };
     for (int k = 0; k < iters; ++k) {
         const int i = first + k * 32;
-        if (i >= T) break;
-        const bool n = (need >> k) & 1u, g = (got >> k) & 1u, kp = (keep >> k) & 1u;
-        if (n ? g : false) continue;
-        int b, slot;
-        const int e = *cell(i, b, slot);
-        if (kp) {
-            atomicAdd(p.ref + e, b * p.max_pages + slot + 2);     // back from -(number + 1) to one reference
+        const bool n = (need >> k) & 1u;
+        const uint32_t votes = __ballot_sync(0xffffffffu, n);
+        const int r = at + __popc(votes & ((1u << lane) - 1u));
+        at += __popc(votes);
+        if (i >= T) continue;
+        int b = b_0, slot = slot_0, e = e_0;
+        if (k > 0) {
+            find_slot(i, b, slot);
+            e = cell(b, slot);
+        }
+        if (n && r < n_free) {
+            got |= 1u << k;
+            int id;
+            if constexpr (CLUSTER > 1) id = cg::this_cluster().map_shared_rank(ids, r & (CLUSTER - 1))[r / CLUSTER];
+            else id = ids[r];
+            cell(b, slot) = id;
+            p.ref[id] = 1;
+            const int len = max(p.seq_lens[b], 0), in_page = len & ((1 << p.page_shift) - 1);
+            if (e >= 0 && slot == (len >> p.page_shift) && in_page) {   // the page holds tokens that the sequence keeps
+                p.copy_src[b] = e;
+                p.copy_dst[b] = id;
+                if (p.copy_rows) p.copy_rows[b] = in_page;
+            }
         } else if (n) {                                           // no page left: the slot stays as it was
             if (e >= 0) atomicAdd(p.ref + e, 1);
             stop_at(b, slot);
-        } else {                                                  // an entry outside the pool
+        } else if ((shared >> k) & 1u) {
+            atomicAdd(p.ref + e, number(b, slot) + 2);            // the page's new sole owner: back from -(number + 1) to one
+        } else if (!((keep >> k) & 1u)) {                         // an entry outside the pool
             if (p.status) atomicOr(p.status, HG_DEV_BAD_PAGE);
             stop_at(b, slot);
         }
     }
     for (int i = T + rank * PG_THREADS + tid; i < wanted; i += LANES) {       // beyond what one call looks at
         int b, slot;
-        slot_of(i, b, slot);
+        find_slot(i, b, slot);
         stop_at(b, slot);
     }
-    if (needs <= n_free) {                                        // (uniform over the cluster)
-        if constexpr (CLUSTER > 1) cg::this_cluster().sync();     // peers' shared memory stays until all have read it
-        return;
+    if (needs > n_free) {                                         // (uniform over the cluster)
+        cluster_sync_all<CLUSTER>();
+        for (int k = 0; k < iters; ++k) {                         // a kept page that a sharer without a copy still reads
+            if (!((keep & shared) >> k & 1u)) continue;
+            int b, slot;
+            find_slot(first + k * 32, b, slot);
+            if (__ldcg(p.ref + cell(b, slot)) > 1) stop_at(b, slot);
+        }
     }
-    cluster_sync_all<CLUSTER>();
-    for (int k = 0; k < iters; ++k) {                             // a kept page that a sharer without a copy still reads
-        if (!((keep >> k) & 1u)) continue;
-        int b, slot;
-        const int e = *cell(first + k * 32, b, slot);
-        if (__ldcg(p.ref + e) > 1) stop_at(b, slot);
-    }
-    if constexpr (CLUSTER > 1) cg::this_cluster().sync();
+    if constexpr (CLUSTER > 1) cg::this_cluster().sync();         // peers' shared memory stays until all have read it
 }
 
 // ---- compact: the pages in use move to the low end of the pool ------------------------------------------------------------

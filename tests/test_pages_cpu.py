@@ -134,8 +134,6 @@ def test_table_operations_refuse_identity_paging_and_huge_tables(lib, name):
 
 def test_batch_limits_alignment_and_counts(lib):
     good = lambda i: FAKE   # noqa: E731
-    d = table_desc(batch=40961, max_pages=2)
-    assert CALLS["hg_kv_fork"](lib, C.byref(d), good) == hg.HG_ERR_UNSUPPORTED
     d = table_desc(batch=16385, max_pages=2)
     assert CALLS["hg_kv_reserve"](lib, C.byref(d), good) == hg.HG_ERR_UNSUPPORTED
     d = table_desc()

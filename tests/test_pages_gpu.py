@@ -154,6 +154,25 @@ def test_large_pool_and_batch_take_the_cluster():
     p.reserve([S * P] * B)
 
 
+@pytest.mark.parametrize("B,S", [(64, 3), (65, 40), (129, 300), (700, 33), (16384, 2), (65535, 3)])
+def test_forks_of_large_batches(B, S):
+    """Rows shared out over a cluster; random sources, every row possibly another's."""
+    n = 500
+    g = torch.Generator(device=DEV)
+    g.manual_seed(B)
+    rnd = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=g, device=DEV, dtype=torch.int32)   # noqa: E731
+    table, lens = rnd(-1, n, B, S), rnd(0, 99, B)
+    ref = torch.bincount(table[table >= 0].long(), minlength=n).int()
+    src = torch.where(torch.rand(B, generator=g, device=DEV) < 0.7, rnd(-1, B, B), torch.arange(B, dtype=torch.int32, device=DEV))
+    want = torch.where((src < 0)[:, None], -1, table[src.clamp(min=0).long()])
+    want_lens = torch.where(src < 0, 0, lens[src.clamp(min=0).long()])
+    desc = hg.attn_desc(batch=B, num_q_heads=1, num_kv_heads=1, head_dim=64, dtype="f16", page_size=16, num_pages=n, page_stride=1024,
+                        head_stride=1024, tok_stride=64, block_table=table, max_pages=S, chunk_tokens=64, num_chunks=1)
+    pkg.hg_kv_fork(src, ref, lens, None, None, desc)
+    assert torch.equal(table, want) and torch.equal(lens, want_lens)
+    assert torch.equal(ref, torch.bincount(want[want >= 0].long(), minlength=n).int())
+
+
 def test_one_row_takes_many_pages_and_the_pool_runs_dry():
     p = Pool(3, 4000, 9000, 16, 1, 64)
     assert p.reserve([0, 50000, 100]) == [0, 50000, 100]
