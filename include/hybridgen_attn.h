@@ -448,7 +448,9 @@ hg_status hg_attn_prefix_partial(const void* q, const void* k_cache, const void*
 
 /*
  * A chunk size for hg_attn_prefix_partial: shared_tokens and num_members are summed over the num_groups groups (estimates
- * will do).  Always a multiple of 128 and of page_size.  Returns 0 for invalid arguments.  No CUDA call is made.
+ * will do).  Always a multiple of 128 and of page_size.  Not longer than 2560 tokens: within a chunk P V is summed up by the
+ * tensor cores, which cut off where fp32 arithmetic rounds, so that o is off by about 2.3e-9 of its size per token of the
+ * chunk (the merge adds chunks in fp32).  Returns 0 for invalid arguments.  No CUDA call is made.
  */
 int32_t hg_attn_prefix_suggest_chunk(int64_t shared_tokens, int32_t num_groups, int32_t num_members, int32_t num_q_heads,
                                      int32_t num_kv_heads, int32_t page_size);

@@ -31,7 +31,8 @@ static hg_status check_prefix(const hg_attn_desc* d, const hg_prefix_desc* x) {
 
 // The pool as in hg_attn_partial, {d within a 64-element half, token in page, half, head, page}, but ONE half a box: the
 // tensor cores want the 128 token rows of a tile's half at one stride, whatever the page size.
-static hg_status make_prefix_maps(const hg_attn_desc* d, const void* k, const void* v, CUtensorMap* tk, CUtensorMap* tv) {
+// The queries are a matrix of B * Hq rows, read by rows.
+static hg_status make_prefix_maps(const hg_attn_desc* d, const void* q, const void* k, const void* v, CUtensorMap* tq, CUtensorMap* tk, CUtensorMap* tv) {
     EncodeTiledFn enc = encode_fn();
     if (!enc) return HG_ERR_CUDA;
     cuuint64_t dims[5] = {64, (cuuint64_t)d->page_size, (cuuint64_t)(d->head_dim / 64), (cuuint64_t)d->num_kv_heads, (cuuint64_t)d->num_pages};
@@ -47,11 +48,16 @@ static hg_status make_prefix_maps(const hg_attn_desc* d, const void* k, const vo
         if (enc(out[i], dt, 5, const_cast<void*>(base[i]), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return HG_ERR_UNSUPPORTED;   // a stride pattern the TMA unit cannot express
+    cuuint64_t qdims[2] = {(cuuint64_t)d->head_dim, (cuuint64_t)d->batch * d->num_q_heads}, qstride[1] = {(cuuint64_t)d->head_dim * 2u};
+    cuuint32_t qbox[2] = {64, 1};
+    if (enc(tq, dt, 2, const_cast<void*>(q), qdims, qstride, qbox, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return HG_ERR_UNSUPPORTED;
     return HG_OK;
 }
 
 template <int D, bool BF16>
-static hg_status launch_prefix(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, cudaStream_t st, bool pdl) {
+static hg_status launch_prefix(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, cudaStream_t st, bool pdl) {
     static std::atomic<int> sms_of[kMaxDevices];           // set once the device's shared-memory opt-in is in force; zero-initialised
     auto kern = prefix_partial_kernel<D, BF16>;
     constexpr size_t smem = pfx_smem_bytes<D>();
@@ -74,7 +80,7 @@ static hg_status launch_prefix(const CUtensorMap& tk, const CUtensorMap& tv, con
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = pdl ? 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, kern, tk, tv, p) != cudaSuccess) { cudaGetLastError(); return HG_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, kern, tq, tk, tv, p) != cudaSuccess) { cudaGetLastError(); return HG_ERR_CUDA; }
     return HG_OK;
 }
 
@@ -88,10 +94,9 @@ static hg_status run_prefix(const void* q, const void* k, const void* v, float* 
                             const OwnSlices* own, void* stream, const hg_attn_desc* d, const hg_prefix_desc* x) {
     PrefixParams p;
     memset(&p, 0, sizeof p);
-    CUtensorMap tk, tv;
-    hg_status st = make_prefix_maps(d, k, v, &tk, &tv);
+    CUtensorMap tq, tk, tv;
+    hg_status st = make_prefix_maps(d, q, k, v, &tq, &tk, &tv);
     if (st != HG_OK) return st;
-    p.q = static_cast<const uint16_t*>(q);
     p.block_table = d->block_table; p.seq_group = x->seq_group; p.group_row = x->group_row;
     p.group_begin = x->group_begin; p.group_end = x->group_end;
     p.o_part = o_part; p.m_part = m_part; p.l_part = l_part; p.status = d->status; p.zero = zero;
@@ -110,8 +115,8 @@ static hg_status run_prefix(const void* q, const void* k, const void* v, float* 
     p.div_G = make_fast_div((uint32_t)p.G);
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     const bool bf16 = d->dtype == HG_DTYPE_BF16, pdl = !desc_tune(d).off(HG_TUNE_NO_PDL);
-    if (d->head_dim == 128) return bf16 ? launch_prefix<128, true>(tk, tv, p, cs, pdl) : launch_prefix<128, false>(tk, tv, p, cs, pdl);
-    return bf16 ? launch_prefix<64, true>(tk, tv, p, cs, pdl) : launch_prefix<64, false>(tk, tv, p, cs, pdl);
+    if (d->head_dim == 128) return bf16 ? launch_prefix<128, true>(tq, tk, tv, p, cs, pdl) : launch_prefix<128, false>(tq, tk, tv, p, cs, pdl);
+    return bf16 ? launch_prefix<64, true>(tq, tk, tv, p, cs, pdl) : launch_prefix<64, false>(tq, tk, tv, p, cs, pdl);
 }
 
 // Whether a step's own slices run as items of the shared launch instead of in hg_attn_partial's: when there are so few that
@@ -162,25 +167,29 @@ int32_t hg_attn_prefix_suggest_chunk(int64_t shared_tokens, int32_t num_groups, 
     if (shift < 4 || shift > 8) return 0;
     // Work items are dealt out in turn, one at a time to each of 148 SMs, so the number of items should fill whole rounds;
     // against many short items stand their epilogues and the merge, which reads every chunk's partials.  The costs, in
-    // microseconds, are those measured at 128 components: 2 per step of an item (128 tokens for two row tiles), 4 per item,
-    // 1e-4 per partial row in the merge.  Several groups count as if
-    // all were of the average size, but since they are not, the last round is taken to be one item longer than the average.
+    // microseconds, are those measured at 128 components: 2 per step of an item (128 tokens for two row tiles), 2.5 per item,
+    // 1e-4 per partial row in the merge.  Several groups count as if all were of the average size, but since they are not,
+    // the last round is taken to be one item longer than the average.
+    // A chunk is not longer than 2560 tokens (1024 where few rows make short ones cheap): the tensor cores cut their sums off
+    // where fp32 arithmetic rounds, so a chunk's error grows with its length (measured: 2.3e-9 of the result per token, 1.7e-5
+    // at 7296 tokens), while the merge of the chunks rounds.  (131072 tokens, 32 sequences of 64/8 heads: 212 us a step at 2432
+    // tokens, 214 at 7296; 65536 tokens, 128 sequences: 402 at 1792, 370 at 7296.)
     const int64_t unit = page_size > PFX_TILE ? page_size / PFX_TILE : 1;
     int64_t tiles = (shared_tokens / num_groups + PFX_TILE - 1) / PFX_TILE;
     if (tiles < 1) tiles = 1;
     const int64_t rows = ((int64_t)num_members + num_groups - 1) / num_groups * (num_q_heads / num_kv_heads), rem = rows % 256;
     const int64_t wide = rows / 256 + (rem > 128 ? 1 : 0), narrow = rem > 0 && rem <= 128 ? 1 : 0;
-    int64_t best = unit;
+    const int64_t longest = wide > 0 ? 20 : 8;
+    int64_t best = 0;
     double best_cost = 0;
-    for (int64_t n = 1; n <= tiles && n <= 600; ++n) {
-        const int64_t c = ((tiles + n - 1) / n + unit - 1) / unit * unit, nc = (tiles + c - 1) / c;
+    for (int64_t c = unit; c <= longest; c += unit) {
+        const int64_t nc = (tiles + c - 1) / c;
         const int64_t items = num_groups * (int64_t)num_kv_heads * (wide * nc + narrow * ((nc + 1) / 2));
         const double rounds = num_groups == 1 ? (double)((items + 147) / 148) : (double)items / 148.0 + 1.0;
-        const double cost = rounds * (2.0 * (double)c + 4.0) + 1e-4 * (double)nc * num_members * num_q_heads;
-        if (n == 1 || cost < best_cost) { best = c; best_cost = cost; }
+        const double cost = rounds * (2.0 * (double)c + 2.5) + 1e-4 * (double)nc * num_members * num_q_heads;
+        if (best == 0 || cost < best_cost) { best = c; best_cost = cost; }
     }
-    const int64_t most = 0x7fffffffll / PFX_TILE / unit * unit;
-    return (int32_t)((best < most ? best : most) * PFX_TILE);
+    return (int32_t)(best * PFX_TILE);
 }
 
 size_t hg_attn_shared_workspace_bytes(const hg_attn_desc* desc, const hg_prefix_desc* prefix) {

@@ -31,7 +31,6 @@
 namespace hg {
 
 struct PrefixParams {
-    const uint16_t* q;               // [B][Hq][D]
     const int32_t* block_table;      // [B][max_pages], or NULL: identity paging
     const int32_t* seq_group;        // [B]
     const int32_t* group_row;        // [NG]
@@ -165,12 +164,9 @@ __device__ __forceinline__ float row_max(const float* x) {
         for (int c = 0; c < 4; ++c) m[c] = max3(m[c], x[u + 2 * c], x[u + 2 * c + 1]);
     return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-
 template <int D, bool BF16>
-__global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+__global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                                                                         const __grid_constant__ CUtensorMap tmV,
                                                                          const PrefixParams p) {
     constexpr int S = pfx_slots<D>();
     constexpr int TILE_BYTES = pfx_tile_bytes<D>();
@@ -190,6 +186,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
     volatile int* const abort_flag = &ctl.abort;
 
     if (tid == 0) {
+        prefetch_tensormap(&tmQ);
         prefetch_tensormap(&tmK);
         prefetch_tensormap(&tmV);
         for (int i = 0; i < S; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
@@ -217,7 +214,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
     tc_fence_after_sync();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&ctl.tmem);
 
-    int issued = 0;                                                // (loaders) tiles requested so far
+    int issued = 0, q_issued = 0;                                  // (loaders) tiles, (Q warps) items requested so far
     uint32_t edges = 0;                                            // (V loader) tiles that went over the edge barrier
     bool edge_open = false;                                        // ... and one that is still on its way
     cudaTriggerProgrammaticLaunchCompletion();
@@ -522,37 +519,33 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
         __syncwarp();
       } else {
         // =============================== query rows, gathered into the 128-byte-swizzled A tiles ===============================
-        const int t = tid - PFX_Q_WARP * 32;
-        constexpr int VECS = D / 8;                                // 16-byte vectors per row
+        // four rows and one 64-component half per lane, by the TMA unit (with 16-byte asynchronous copies the 256 rows of an
+        // item took some 7000 cycles, queued behind the epilogue's stores); rows behind the last repeat it
+        const int group = (warp - PFX_Q_WARP) * 16 + lane / HALVES, half = lane % HALVES;
         bool ok = true;
         for (int k = 0; ok; ++k) {
             const int j = k & 1;
             ok = warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
             if (!ok || !ctl.item[j].valid) break;
             const int rows = ctl.item[j].rows, r0 = ctl.item[j].r0, m0 = ctl.item[j].m0, h = ctl.item[j].h;
+            const bool mine = lane < 16 * HALVES && group * 4 < rows;
+            int row[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int q = r0 + min(group * 4 + u, rows - 1), m = fast_div(q, p.div_G);
+                row[u] = mine ? ctl.members[j][m - m0] * p.Hq + h * p.G + q - m * p.G : 0;
+            }
+            const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * 512u;
             if (k >= 1) ok = warp_wait(&ctl.q_free, (uint32_t)(k - 1) & 1u, abort_flag);
             if (!ok) break;
-            const int c = t % VECS;
-            // eight rows at a time: their look-ups overlap
-            for (int rb = t / VECS; rb < rows; rb += 8 * (128 / VECS)) {
-                const uint16_t* src[8];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const int q = r0 + min(rb + u * (128 / VECS), rows - 1), m = fast_div(q, p.div_G);
-                    src[u] = p.q + ((size_t)ctl.members[j][m - m0] * p.Hq + h * p.G + q - m * p.G) * D + c * 8;
-                }
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const int r = rb + u * (128 / VECS), rr = r & (PFX_TILE - 1);
-                    if (r >= rows) continue;
-                    const uint32_t at = smem_u32(pfx_raw) + (c >> 3) * HALF_BYTES + (((c & 7) ^ (rr & 7)) << 4);
-                    cp_async16(at + (r >> 7) * TILE_BYTES + rr * 128, src[u]);
-                }
+            if (lane == 0) {
+                mbar_arrive_expect_tx(&ctl.q_full, bytes);
+                mbar_arrive(&ctl.item_empty[j]);
             }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) { mbar_arrive(&ctl.q_full); mbar_arrive(&ctl.item_empty[j]); }
+            if (mine)
+                tma_gather4(pfx_raw + (group >> 5) * TILE_BYTES + half * HALF_BYTES + (group & 31) * 512, &tmQ, &ctl.q_full, half * 64,
+                            row[0], row[1], row[2], row[3]);
+            q_issued = k + 1;
         }
       }
     } else {
@@ -745,6 +738,10 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                 int none = 0;
                 if (edge_open) mbar_wait(&ctl.edge, edges & 1u, &none);
             }
+        }
+        if (warp == PFX_Q_WARP && lane == 0 && q_issued > 0) {
+            int none = 0;
+            mbar_wait(&ctl.q_full, (uint32_t)(q_issued - 1) & 1u, &none);
         }
         if (tid == 0 && p.status) atomicOr(p.status, HG_DEV_WAIT_TIMEOUT);
     }
