@@ -220,8 +220,16 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
     dd.struct_size = sizeof dd;
     dd.flags |= HG_FLAG_SPARSE_EMPTY;                                  // the partials are private to this call and its merge
     dd.sched_counter = reinterpret_cast<int32_t*>(ws + w.sched);
+    // The chunks of the own slices are private to this call: where there are many, 256 tokens are better than fewer (with
+    // 4000 to 5400 chunk slots of 128 tokens hg_attn_partial takes 26, 32 and 36 us instead of 31, 37 and 40)
+    const int coarse = 256;
+    const int64_t slots = ((int64_t)dd.num_chunks * dd.chunk_tokens + coarse - 1) / coarse + 1;
+    if (dd.chunk_tokens < coarse && slots <= dd.num_chunks && (int64_t)dd.batch * dd.num_kv_heads * dd.num_chunks >= 1024) {
+        dd.chunk_tokens = coarse;
+        dd.num_chunks = (int32_t)slots;
+    }
     const OwnSlices own = {seq_lens, tok_begin, tok_end, at(w.o), at(w.m), at(w.l)};
-    const bool one_launch = own_in_shared_launch(desc);
+    const bool one_launch = own_in_shared_launch(&dd);
     // where the own partials get a launch of their own, the shared kernel clears their work counter on its way, so that no
     // clearing stands between the two
     st = run_prefix(q, k_cache, v_cache, at(w.po), at(w.pm), at(w.pl), one_launch ? nullptr : dd.sched_counter, one_launch ? &own : nullptr, stream, &dd, prefix);
@@ -233,7 +241,7 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
     }
     hg_partial_src src[HG_MAX_MERGE_SRC];
     src[0].o = at(w.po); src[0].m = at(w.pm); src[0].l = at(w.pl); src[0].nc = prefix->num_chunks; src[0].reserved = 0;
-    src[1].o = at(w.o); src[1].m = at(w.m); src[1].l = at(w.l); src[1].nc = desc->num_chunks; src[1].reserved = 0;
+    src[1].o = at(w.o); src[1].m = at(w.m); src[1].l = at(w.l); src[1].nc = dd.num_chunks; src[1].reserved = 0;
     for (int i = 0; i < n_host_src; ++i) src[2 + i] = host_partials[i];
     return hg_attn_merge(src, 2 + n_host_src, out, lse, stream, &dd);
 }
