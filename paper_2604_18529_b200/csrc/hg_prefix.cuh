@@ -164,6 +164,21 @@ __device__ __forceinline__ float row_max(const float* x) {
         for (int c = 0; c < 4; ++c) m[c] = max3(m[c], x[u + 2 * c], x[u + 2 * c + 1]);
     return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
+// mbar_wait / warp_wait with less code around them: this kernel has some twenty waits, and its roles share the instruction
+// cache.  The limit is counted in clock cycles (2 to 3 s).
+constexpr long long PFX_WAIT_CYCLES = 4000000000ll;
+__device__ __forceinline__ bool pfx_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity))
+        if (*abort_flag || clock64() - t0 > PFX_WAIT_CYCLES) { *abort_flag = 1; return false; }
+    return true;
+}
+__device__ __forceinline__ bool pfx_warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    const bool ok = pfx_wait(bar, parity, abort_flag);
+    return __all_sync(0xffffffffu, ok);
+}
+
 template <int D, bool BF16>
 __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                                                                          const __grid_constant__ CUtensorMap tmV,
@@ -278,7 +293,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                 if (ub < units) load_units();
             }
             const int j = k & 1;
-            if (k >= 2) ok = warp_wait(&ctl.item_empty[j], (uint32_t)((k - 2) >> 1) & 1u, abort_flag);
+            if (k >= 2) ok = pfx_warp_wait(&ctl.item_empty[j], (uint32_t)((k - 2) >> 1) & 1u, abort_flag);
             if (!ok) break;
             PfxItem& it = ctl.item[j];
             if (ub >= units) {
@@ -360,7 +375,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
         int n = 0;                                                 // tiles of earlier items
         for (int k = 0; ok; ++k) {
             const int j = k & 1;
-            ok = warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
+            ok = pfx_warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
             if (!ok) break;
             const PfxItem it = ctl.item[j];
             __syncwarp();
@@ -401,7 +416,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                     }
                     bad = __reduce_or_sync(0xffffffffu, bad);
                 }
-                if (seq >= S) ok = warp_wait(&ctl.empty[slot], (uint32_t)(seq / S - 1) & 1u, abort_flag);
+                if (seq >= S) ok = pfx_warp_wait(&ctl.empty[slot], (uint32_t)(seq / S - 1) & 1u, abort_flag);
                 if (!ok || p.test_stall) break;
                 // V rows outside the slice, and of refused pages, hold anything (NaN patterns among it) and meet weights of 0:
                 // such a tile lands on a barrier of its own and is handed on when those rows are cleared
@@ -415,7 +430,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                 }
                 if (e >= 0) tma_load_5d(tile + half * HALF_BYTES + piece * box_rows * 128, tm, landed, 0, row, half, it.h, e, policy);
                 if (edge) {
-                    ok = warp_wait(&ctl.edge, edges & 1u, abort_flag);
+                    ok = pfx_warp_wait(&ctl.edge, edges & 1u, abort_flag);
                     if (!ok) { edge_open = true; break; }
                     ++edges;
                     for (int u = lane; u < PFX_TILE * HALVES * 8; u += 32) {     // whole 128-byte rows: the swizzle does not matter
@@ -444,7 +459,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             const uint64_t v_desc = tc_smem_desc(smem_u32(ring), HALF_BYTES, 1024u, 2u);
             auto scores = [&](int s, int i, bool last) {           // S = Q K^T of a stream's tile
                 const int x = n + pfx_tile_index(it, s, i), seq = 2 * x, slot = seq % S;
-                ok = mbar_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
+                ok = pfx_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
                 if (!ok) return;
                 ctl.stream_bad[s] = ctl.bad[x & 15];
                 tc_fence_after_sync();
@@ -462,12 +477,12 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             };
             auto values = [&](const PfxItem& im, int n0, int s, int i) {       // O += P V of a stream's tile, quarter by quarter
                 const int x = n0 + pfx_tile_index(im, s, i), seq = 2 * x + 1, slot = seq % S;
-                ok = mbar_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
+                ok = pfx_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
                 const uint64_t b = v_desc + (uint32_t)(slot * (TILE_BYTES >> 4));
                 const uint32_t acc = tmem + PFX_O_COL + s * 128, a = tmem + PFX_S_COL + s * 128;
 #pragma unroll
                 for (int part = 0; part < 4; ++part) {
-                    ok = ok && mbar_wait(&ctl.p_full[s][part], np[s] & 1u, abort_flag);
+                    ok = ok && pfx_wait(&ctl.p_full[s][part], np[s] & 1u, abort_flag);
                     if (!ok) return;
                     tc_fence_after_sync();
 #pragma unroll
@@ -483,12 +498,12 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             };
             for (int k = 0; ok; ++k) {
                 const int j = k & 1;
-                ok = mbar_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
+                ok = pfx_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
                 if (!ok) break;
                 it = ctl.item[j];
                 mbar_arrive(&ctl.item_empty[j]);
                 if (!it.valid) break;
-                ok = mbar_wait(&ctl.q_full, (uint32_t)k & 1u, abort_flag);
+                ok = pfx_wait(&ctl.q_full, (uint32_t)k & 1u, abort_flag);
                 if (!ok) break;
                 int left = it.tiles(0) + it.tiles(1);              // score products still to issue
                 if (it.tiles(0) > 0) scores(0, 0, --left == 0);
@@ -514,7 +529,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             if (ok && held) values(prev, prev_n, 1, prev.tiles(1) - 1);
             int none = 0;                                          // nothing is in flight when the tensor memory is given back
             tc_commit(&ctl.drain);
-            mbar_wait(&ctl.drain, 0u, &none);
+            pfx_wait(&ctl.drain, 0u, &none);
         }
         __syncwarp();
       } else {
@@ -525,7 +540,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
         bool ok = true;
         for (int k = 0; ok; ++k) {
             const int j = k & 1;
-            ok = warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
+            ok = pfx_warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
             if (!ok || !ctl.item[j].valid) break;
             const int rows = ctl.item[j].rows, r0 = ctl.item[j].r0, m0 = ctl.item[j].m0, h = ctl.item[j].h;
             const bool mine = lane < 16 * HALVES && group * 4 < rows;
@@ -536,7 +551,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                 row[u] = mine ? ctl.members[j][m - m0] * p.Hq + h * p.G + q - m * p.G : 0;
             }
             const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * 512u;
-            if (k >= 1) ok = warp_wait(&ctl.q_free, (uint32_t)(k - 1) & 1u, abort_flag);
+            if (k >= 1) ok = pfx_warp_wait(&ctl.q_free, (uint32_t)(k - 1) & 1u, abort_flag);
             if (!ok) break;
             if (lane == 0) {
                 mbar_arrive_expect_tx(&ctl.q_full, bytes);
@@ -591,7 +606,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             const bool dry = k < 0;
             int lo = 0, hi = PFX_TILE, tiles = 1, rows = PFX_TILE, wide = 0;      // (of the dry round)
             if (!dry) {
-                ok = warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
+                ok = pfx_warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
                 if (!ok) break;
                 const PfxItem& it = ctl.item[j];
                 if (!it.valid) break;
@@ -603,7 +618,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
             float m_true = NEG_INF, m_ref = NEG_INF, l = 0.f;      // the maximum, and the one the weights refer to (raw logits)
             for (int i = 0; i < tiles; ++i) {
                 if (!dry) {
-                    ok = warp_wait(&ctl.s_full[s], ns & 1u, abort_flag);
+                    ok = pfx_warp_wait(&ctl.s_full[s], ns & 1u, abort_flag);
                     if (!ok) break;
                     ++ns;
                 }
@@ -619,8 +634,14 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                     tmem_ld_wait();
                     if (edge) {                                    // columns outside the slice or of refused pages
 #pragma unroll
-                        for (int u = 0; u < PFX_TILE; ++u)
-                            if (u < c_lo || u >= c_hi || ((bad >> (u >> 4)) & 1u)) x[u] = NEG_INF;
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t out = ((bad >> (2 * c)) & 1u ? 0xffffu : 0u) | ((bad >> (2 * c + 1)) & 1u ? 0xffff0000u : 0u);
+                            const int below = c_lo - c * 32, in = c_hi - c * 32;
+                            out |= below >= 32 ? ~0u : (below > 0 ? (1u << below) - 1u : 0u);
+                            out |= in <= 0 ? ~0u : (in < 32 ? ~0u << in : 0u);
+#pragma unroll
+                            for (int u = 0; u < 32; ++u) x[c * 32 + u] = (out >> u) & 1u ? NEG_INF : x[c * 32 + u];
+                        }
                     }
                     const float mx = row_max<PFX_TILE>(x);
                     m_true = fmaxf(m_true, mx);
@@ -684,7 +705,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                 continue;
             }
             if (ok && tiles > 0) {
-                ok = warp_wait(&ctl.o_full[s], no & 1u, abort_flag);
+                ok = pfx_warp_wait(&ctl.o_full[s], no & 1u, abort_flag);
                 if (!ok) break;
                 ++no;
                 tc_fence_after_sync();
@@ -733,15 +754,15 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                 for (int x = max(0, issued - S); x < issued; ++x) {
                     int none = 0;
                     const int seq = 2 * x + (warp == PFX_K_WARP ? 0 : 1);
-                    mbar_wait(&ctl.full[seq % S], (uint32_t)(seq / S) & 1u, &none);
+                    pfx_wait(&ctl.full[seq % S], (uint32_t)(seq / S) & 1u, &none);
                 }
                 int none = 0;
-                if (edge_open) mbar_wait(&ctl.edge, edges & 1u, &none);
+                if (edge_open) pfx_wait(&ctl.edge, edges & 1u, &none);
             }
         }
         if (warp == PFX_Q_WARP && lane == 0 && q_issued > 0) {
             int none = 0;
-            mbar_wait(&ctl.q_full, (uint32_t)(q_issued - 1) & 1u, &none);
+            pfx_wait(&ctl.q_full, (uint32_t)(q_issued - 1) & 1u, &none);
         }
         if (tid == 0 && p.status) atomicOr(p.status, HG_DEV_WAIT_TIMEOUT);
     }
