@@ -91,6 +91,7 @@ constexpr int PFX_REGS_SOFTMAX = 200, PFX_REGS_OTHER = 56;     // 256 threads ea
 constexpr int PFX_MAX_SLOTS = 10;
 constexpr int PFX_MAX_GROUPS = 512;
 constexpr uint32_t PFX_S_COL = 0, PFX_O_COL = 256;      // tensor memory: S / P of the streams, 128 columns each, then their O
+constexpr uint32_t PFX_THIRD_COL = 64;                  // behind O where that has 64 columns: third terms of P
 
 template <int D> __host__ __device__ constexpr int pfx_tile_bytes() { return PFX_TILE * D * 2; }
 template <int D> __host__ __device__ constexpr int pfx_slots() { return D == 128 ? 5 : 10; }
@@ -147,6 +148,13 @@ __device__ __forceinline__ void split2(float2 w, uint32_t& hi, uint32_t& lo) {
     lo = pack2<BF16>(rest.x, rest.y);
 }
 
+template <bool BF16>
+__device__ __forceinline__ uint32_t split_third(float2 w, uint32_t hi, uint32_t lo) {      // what hi and lo left
+    const float2 minus = make_float2(-1.f, -1.f);
+    const float2 rest = fma2(unpack2<BF16>(lo), minus, fma2(unpack2<BF16>(hi), minus, w));
+    return pack2<BF16>(rest.x, rest.y);
+}
+
 // A whole 32-byte sector.
 __device__ __forceinline__ void st_global_hint8(float* addr, const float (&v)[8], uint64_t policy) {
     asm volatile("st.global.L2::cache_hint.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8}, %9;"
@@ -192,6 +200,9 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
     // its components contiguous (N-major), N = D
     constexpr uint32_t IDESC_S = (1u << 4) | (FMT << 7) | (FMT << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
     constexpr uint32_t IDESC_O = (1u << 4) | (FMT << 7) | (FMT << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
+    // bf16 weights lose up to 2^-18 in two terms (1.1e-6 of a result of 2 000 tokens); with 64 components tensor memory has
+    // room for a third one beside O, which leaves 2^-24
+    constexpr bool THIRD = BF16 && D == 64;
     const float NEG_INF = __int_as_float(0xff800000);
 
     extern __shared__ __align__(1024) uint8_t pfx_raw[];
@@ -490,6 +501,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                         const uint32_t ac = a + (kk >> 1) * 32 + (kk & 1) * 8;
                         tc_mma_f16_ts(acc, ac, b + (uint32_t)(kk * 2048 >> 4), IDESC_O, kk ? 1u : (i ? 1u : 0u));
                         tc_mma_f16_ts(acc, ac + 16, b + (uint32_t)(kk * 2048 >> 4), IDESC_O, 1u);
+                        if constexpr (THIRD) tc_mma_f16_ts(acc, acc + PFX_THIRD_COL + kk * 8, b + (uint32_t)(kk * 2048 >> 4), IDESC_O, 1u);
                     }
                 }
                 ++np[s];
@@ -678,7 +690,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                     };
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        uint32_t w[32];
+                        uint32_t w[32], w3[16];
 #pragma unroll
                         for (int u = 0; u < 16; ++u) {
                             float2 e = fma2(make_float2(x[c * 32 + 2 * u], x[c * 32 + 2 * u + 1]), sc2, off2);
@@ -686,9 +698,13 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
                             e.y = fast_exp2(e.y);
                             sum[u & 1] = add2(sum[u & 1], e);
                             split2<BF16>(e, w[u], w[16 + u]);
+                            if constexpr (THIRD) w3[u] = split_third<BF16>(e, w[u], w[16 + u]);
                         }
                         if (c > 0) hand_over(c - 1);
-                        if (!dry) tmem_st_32x32(s_tmem + c * 32, w);
+                        if (!dry) {
+                            tmem_st_32x32(s_tmem + c * 32, w);
+                            if constexpr (THIRD) tmem_st_32x16(o_tmem + PFX_THIRD_COL + c * 16, w3);
+                        }
                     }
                     hand_over(3);
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
