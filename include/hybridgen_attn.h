@@ -417,7 +417,8 @@ hg_status hg_kv_evict_finish(const int32_t* src_begin, const int32_t* n_moved, i
  * one of its members, whose first pages every member's row lists too (hg_kv_fork makes such rows).  Ranges are read on
  * the device and clamped to the row (HG_DEV_RANGE when that cuts something off, or when group_row lies outside the
  * table: such a group is empty).  The chunk grid is that of hg_attn_desc, with its own chunk size: chunk_tokens a multiple
- * of 128 and of page_size; num_chunks must be >= every group's number of chunks.
+ * of 128 and of page_size; num_chunks must be >= every group's number of chunks (a longer slice is truncated to its first
+ * num_chunks chunks).
  */
 #define HG_MAX_GROUPS 512
 typedef struct hg_prefix_desc {
@@ -440,8 +441,10 @@ typedef struct hg_prefix_desc {
  *   o_part, m_part, l_part   dev float [B][Hq][NC][D] / [B][Hq][NC], NC = prefix->num_chunks: as in hg_attn_partial; a
  *           sequence without a group, and slots beyond a group's chunks, are empty (HG_FLAG_SPARSE_EMPTY applies);
  *           o_part 32-byte aligned
- * Of desc: batch, heads, head_dim, dtype, the KV addressing, scale, flags and status are used.  Accumulation is fp32 and P is
- * carried as a two-term (hi + lo) 16-bit expansion, as in hg_attn_partial.
+ * Of desc: batch, heads, head_dim, dtype, the KV addressing, scale, flags and status are used (its chunk fields are not).
+ * Accumulation is fp32 and P is carried as a two-term (hi + lo) 16-bit expansion, as in hg_attn_partial: a weight is off
+ * by at most 2^-18 of itself with bf16 (with 64 components a third term makes that 2^-24), by 2^-24 of the chunk's largest
+ * with fp16.
  */
 hg_status hg_attn_prefix_partial(const void* q, const void* k_cache, const void* v_cache, float* o_part, float* m_part, float* l_part,
                                  void* stream, const hg_attn_desc* desc, const hg_prefix_desc* prefix);
@@ -464,7 +467,8 @@ size_t hg_attn_shared_workspace_bytes(const hg_attn_desc* desc, const hg_prefix_
  * result is attention over all of them together; a token that lies in both a group's slice and a member's own counts
  * twice, so tok_begin[b] is usually the group's end.  A sequence without a group simply has all its tokens in
  * [tok_begin, tok_end).  workspace: dev, 256-byte aligned, at least hg_attn_shared_workspace_bytes(); it holds the work
- * counter too, which the call clears on its way in any case.
+ * counter too, which the call clears on its way in any case; not shared by calls that may overlap on the GPU (captured
+ * graphs replayed on different streams among them).
  */
 hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* v_cache, const int32_t* seq_lens,
                                 const int32_t* tok_begin, const int32_t* tok_end, const hg_partial_src* host_partials,
@@ -495,7 +499,7 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
  *                   it.  copy_src[b] / copy_dst[b] (dev int32 [B]): the page whose first copy_rows[b] token rows
  *                   (copy_rows may be NULL) have to be copied before the sequence is read or appended to, or -1 - the
  *                   list hg_kv_copy_pages takes.  n_ready[b] (may be NULL): how many of the n_new[b] positions are
- *                   writable; fewer where the pool ran out of pages (HG_DEV_NO_PAGE; the slot stays as it was), where
+ *                   writable (not n_new or seq_lens itself); fewer where the pool ran out of pages (HG_DEV_NO_PAGE; the slot stays as it was), where
  *                   the block-table row ends (HG_DEV_RANGE) or meets an entry outside the pool (HG_DEV_BAD_PAGE), and
  *                   beyond 262144 slots in one call.  Append no more than that.  Batches up to 16384.
  *   hg_kv_release   takes one reference off every page of a list (dev int32 [n]; negative entries are skipped) whose

@@ -484,15 +484,16 @@ def _check_groups(desc: HgAttnDesc, prefix: HgPrefixDesc) -> None:
     seq_group = prefix._keep[0]
     if seq_group.numel() < desc.batch:
         raise ValueError(f"seq_group has {seq_group.numel()} elements, the batch {desc.batch}")
-    if seq_group.device.index != torch.cuda.current_device():
-        raise ValueError(f"seq_group is on {seq_group.device}, the current device is cuda:{torch.cuda.current_device()}")
+    for t, name in zip(prefix._keep, ("seq_group", "group_row", "group_begin", "group_end")):
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
 def hg_attn_prefix_partial(q, k_cache, v_cache, o_part, m_part, l_part, desc: HgAttnDesc, prefix: HgPrefixDesc, stream=None) -> None:
     """Chunk partials (o, m, l) of the groups' shared prefixes; one more source for ``hg_attn_merge``."""
     _check_groups(desc, prefix)
     n = desc.batch * desc.num_q_heads * prefix.num_chunks
-    st = lib().hg_attn_prefix_partial(_here(q, "q"), _pool(k_cache, "k_cache"), _pool(v_cache, "v_cache"),
+    st = lib().hg_attn_prefix_partial(_here(q, "q", None, desc.batch * desc.num_q_heads * desc.head_dim), _pool(k_cache, "k_cache"), _pool(v_cache, "v_cache"),
                                       _here(o_part, "o_part", torch.float32, n * desc.head_dim),
                                       _here(m_part, "m_part", torch.float32, n), _here(l_part, "l_part", torch.float32, n),
                                       _stream(stream), C.byref(desc), C.byref(prefix))
@@ -519,7 +520,8 @@ def _decode_shared_args(q, k_cache, v_cache, seq_lens, tok_begin, tok_end, parti
     _check_groups(desc, prefix)
     B, rows = desc.batch, desc.batch * desc.num_q_heads
     arr = _src_array(partials, host=False)
-    return (_here(q, "q"), _pool(k_cache, "k_cache"), _pool(v_cache, "v_cache"), _here(seq_lens, "seq_lens", torch.int32, B),
+    return (_here(q, "q", None, rows * desc.head_dim), _pool(k_cache, "k_cache"), _pool(v_cache, "v_cache"),
+            _here(seq_lens, "seq_lens", torch.int32, B),
             _here(tok_begin, "tok_begin", torch.int32, B), _here(tok_end, "tok_end", torch.int32, B), arr, len(partials),
             _here(out, "out", torch.float32, rows * desc.head_dim), _here(lse, "lse", torch.float32, rows),
             _here(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream), C.byref(desc),

@@ -81,9 +81,8 @@ hg_status hg_kv_fork(const int32_t* src_row, int32_t* ref_count, int32_t* seq_le
     p.vec[0] = seq_lens; p.vec[1] = tok_begin; p.vec[2] = tok_end;
     p.status = desc->status; p.B = desc->batch; p.max_pages = desc->max_pages; p.num_pages = desc->num_pages;
     // a cluster of 8 CTAs shares a tile's rows once there is work for it (1024 rows of 64 entries: 4.1 us instead of 10.2; 256
-    // rows of 502: 5.7 instead of 4.2); 32 columns (128-byte row pieces) a tile where that
-    // leaves two CTAs for every SM, down to 8 (one 32-byte sector) for short tables, and fewer only where the rows of the
-    // batch fill the shared memory
+    // rows of 502: 5.7 instead of 4.2); 32 columns (128-byte row pieces) a tile where that leaves two CTAs for every SM, down
+    // to 8 (one 32-byte sector) for short tables, and fewer only where the rows of the batch fill the shared memory
     const int cluster = p.B >= 512 ? 8 : 1;
     const size_t rows = ((size_t)p.B + cluster - 1) / cluster;
     int shift = 5;
@@ -115,6 +114,7 @@ hg_status hg_kv_reserve(const int32_t* seq_lens, const int32_t* n_new, int32_t* 
     hg_status st = check_table(desc);
     if (st != HG_OK) return st;
     if (!seq_lens || !ref_count || !copy_src || !copy_dst || !aligned16(ref_count)) return HG_ERR_INVALID_ARG;
+    if (n_ready && (n_ready == n_new || n_ready == seq_lens)) return HG_ERR_INVALID_ARG;       // written while others still read
     if (desc->batch > RESERVE_MAX_BATCH) return HG_ERR_UNSUPPORTED;
     ReserveParams p;
     p.seq_lens = seq_lens; p.n_new = n_new; p.table = const_cast<int32_t*>(desc->block_table); p.ref = ref_count;

@@ -14,8 +14,9 @@
 
 namespace hg {
 
-static hg_status check_prefix(const hg_attn_desc* d, const hg_prefix_desc* x) {
-    hg_status st = check_desc(d, true);
+// `own`: the description's own chunk fields are used too
+static hg_status check_prefix(const hg_attn_desc* d, const hg_prefix_desc* x, bool own) {
+    hg_status st = own ? check_desc(d, true) : check_pool(d);
     if (st != HG_OK) return st;
     if (!x || x->struct_size < sizeof(hg_prefix_desc)) return HG_ERR_INVALID_ARG;
     if (x->num_groups < 1 || x->chunk_tokens < 1 || x->num_chunks < 1) return HG_ERR_INVALID_ARG;
@@ -153,7 +154,7 @@ extern "C" {
 
 hg_status hg_attn_prefix_partial(const void* q, const void* k_cache, const void* v_cache, float* o_part, float* m_part, float* l_part,
                                  void* stream, const hg_attn_desc* desc, const hg_prefix_desc* prefix) {
-    hg_status st = check_prefix(desc, prefix);
+    hg_status st = check_prefix(desc, prefix, false);
     if (st != HG_OK) return st;
     if (!q || !k_cache || !v_cache || !o_part || !m_part || !l_part) return HG_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || (reinterpret_cast<uintptr_t>(o_part) & 31u)) return HG_ERR_INVALID_ARG;
@@ -193,7 +194,7 @@ int32_t hg_attn_prefix_suggest_chunk(int64_t shared_tokens, int32_t num_groups, 
 }
 
 size_t hg_attn_shared_workspace_bytes(const hg_attn_desc* desc, const hg_prefix_desc* prefix) {
-    if (check_prefix(desc, prefix) != HG_OK) return 0;
+    if (check_prefix(desc, prefix, true) != HG_OK) return 0;
     return plan_shared(desc, prefix).total;
 }
 
@@ -201,7 +202,7 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
                                 const int32_t* tok_begin, const int32_t* tok_end, const hg_partial_src* host_partials,
                                 int32_t n_host_src, float* out, float* lse, void* workspace, size_t workspace_bytes, void* stream,
                                 const hg_attn_desc* desc, const hg_prefix_desc* prefix) {
-    hg_status st = check_prefix(desc, prefix);
+    hg_status st = check_prefix(desc, prefix, true);
     if (st != HG_OK) return st;
     if (!q || !k_cache || !v_cache || !seq_lens || !tok_begin || !tok_end || !out) return HG_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache)) return HG_ERR_INVALID_ARG;

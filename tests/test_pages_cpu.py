@@ -129,15 +129,18 @@ def test_table_operations_refuse_identity_paging_and_huge_tables(lib, name):
     d = good_desc()
     assert CALLS[name](lib, C.byref(d), lambda i: FAKE) == hg.HG_ERR_INVALID_ARG
     d = table_desc(batch=65535, max_pages=40000, num_pages=2 ** 31 - 1)
-    assert CALLS[name](lib, C.byref(d), lambda i: FAKE) == hg.HG_ERR_UNSUPPORTED
+    assert CALLS[name](lib, C.byref(d), lambda i: FAKE + 64 * i) == hg.HG_ERR_UNSUPPORTED
 
 
 def test_batch_limits_alignment_and_counts(lib):
     good = lambda i: FAKE   # noqa: E731
     d = table_desc(batch=16385, max_pages=2)
-    assert CALLS["hg_kv_reserve"](lib, C.byref(d), good) == hg.HG_ERR_UNSUPPORTED
+    assert CALLS["hg_kv_reserve"](lib, C.byref(d), lambda i: FAKE + 64 * i) == hg.HG_ERR_UNSUPPORTED
     d = table_desc()
     assert CALLS["hg_kv_reserve"](lib, C.byref(d), lambda i: FAKE + 4 * (i == 1)) == hg.HG_ERR_INVALID_ARG
+    distinct = lambda i: FAKE + 64 * i   # noqa: E731
+    for same in (0, 8):                                             # n_ready is written while seq_lens and n_new are read
+        assert CALLS["hg_kv_reserve"](lib, C.byref(d), lambda i: distinct(same if i == 10 else i)) == hg.HG_ERR_INVALID_ARG
     assert CALLS["hg_kv_compact"](lib, C.byref(d), lambda i: FAKE + 4 * (i == 0)) == hg.HG_ERR_INVALID_ARG
     assert CALLS["hg_kv_copy_pages"](lib, C.byref(d), lambda i: FAKE + 8 * (i == 2)) == hg.HG_ERR_INVALID_ARG
     assert lib.hg_kv_compact(FAKE, FAKE, FAKE, FAKE, 0, FAKE, None, C.byref(d)) == hg.HG_ERR_INVALID_ARG

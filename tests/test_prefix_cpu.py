@@ -63,6 +63,7 @@ def test_bad_descriptions_and_pointers_are_refused(lib):
         assert partial(lib, C.byref(d), C.byref(x), **{name: None}) == hg.HG_ERR_INVALID_ARG
     for name in "qkvo":
         assert partial(lib, C.byref(d), C.byref(x), **{name: FAKE + 8}) == hg.HG_ERR_INVALID_ARG
+    assert partial(lib, C.byref(d), C.byref(x), o=FAKE + 16) == hg.HG_ERR_INVALID_ARG          # rows are stored 32 bytes at a time
     assert partial(lib, None, C.byref(x)) == hg.HG_ERR_INVALID_ARG and partial(lib, C.byref(d), None) == hg.HG_ERR_INVALID_ARG
 
 

@@ -383,9 +383,31 @@ def test_page_offsets_past_32_bits():
     check_step(b)
 
 
+def test_more_rows_per_sequence_than_an_item_has():
+    check_step(Batch([0, 0, -1, 0], [300], [20, 0, 5, 131], Hq=300, Hkv=1, seed=12))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("own_chunk", [64, 192, 320])
+def test_own_chunks_that_begin_inside_a_tile(own_chunk, D):
+    b = Batch([0, 0, -1], [200], [330, 1, 700], seed=3, D=D)
+    b.desc.chunk_tokens, b.desc.num_chunks = own_chunk, 700 // own_chunk + 2
+    check_step(b)
+
+
+def test_the_partials_do_not_use_the_own_chunk_fields():
+    b = Batch([0, 0], [300], [5, 5], seed=9)
+    want = b.partial()
+    b.desc.chunk_tokens = b.desc.num_chunks = 0
+    for x, y in zip(b.partial(), want):
+        assert torch.equal(x, y)
+
+
 def test_refused_by_the_binding():
     b = Batch([0, 0], [100], [5, 5], seed=2)
     o, m, l = b.partial()
+    with pytest.raises(ValueError):
+        pkg.hg_attn_prefix_partial(b.q[:1].contiguous(), b.k, b.v, o, m, l, b.desc, b.prefix)
     with pytest.raises(ValueError):
         pkg.hg_attn_prefix_partial(b.q, b.k, b.v, o, m[:1].contiguous(), l, b.desc, b.prefix)
     with pytest.raises(ValueError):
