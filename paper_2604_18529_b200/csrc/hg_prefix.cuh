@@ -22,7 +22,7 @@
 //
 // Bounds, measured (K and V larger than the L2).  128 sequences, 64/8 heads of 128, 65 536 tokens, bf16, chunks of 2432: 316 us,
 // 1.25 of the products' time at the measured 1613 TFLOP/s; a tile takes 4100 cycles where its products (2 of S, 4 of P V)
-// take 3072: a stream's S - row - weights - P V chain is longer than that, and the other stream covers only a part of it (the
+// take 3100: a stream's S - row - weights - P V chain is longer than that, and the other stream covers only a part of it (the
 // exponentials of both need 2048 cycles of the special-function units).  32 sequences, 131 072 tokens: 176 us.  16
 // sequences, 56/56 heads, 16 384 tokens (16 rows a KV head): 87 us for 470 MB, 5.4 TB/s.  4 sequences, 512 tokens: 9.3 us.
 // Tiles of 64 tokens with two S buffers a stream, so that the next S never waits for P: 361 instead of 316 us.
