@@ -142,10 +142,11 @@ hg_status hg_kv_compact(int32_t* ref_count, int32_t* remap, int32_t* move_src, i
     CompactParams p;
     p.ref = ref_count; p.remap = remap; p.move_src = move_src; p.move_dst = move_dst; p.n_moves = n_moves;
     p.num_pages = desc->num_pages; p.max_moves = max_moves;
-    st = desc->num_pages <= 8192 ? launch_pages(kv_compact_kernel<1>, 1, PG_THREADS, 0, 1, stream, p)
-                                 : launch_pages(kv_compact_kernel<8>, 8, PG_THREADS, 0, 8, stream, p);
-    if (st != HG_OK) return st;
     const size_t n = (size_t)desc->batch * desc->max_pages;
+    const bool one = desc->num_pages <= 8192, renames = one && n <= COMPACT_RENAMES;
+    p.table = const_cast<int32_t*>(desc->block_table); p.n_table = renames ? (int)n : 0;
+    st = one ? launch_pages(kv_compact_kernel<1>, 1, PG_THREADS, 0, 1, stream, p) : launch_pages(kv_compact_kernel<8>, 8, PG_THREADS, 0, 8, stream, p);
+    if (st != HG_OK || renames) return st;
     const size_t want = (n + 1023) / 1024, most = (size_t)sms * 8;
     return launch_pages(kv_rename_kernel, (unsigned)(want < most ? want : most), 256, 0, 1, stream, const_cast<int32_t*>(desc->block_table), n,
                         const_cast<const int32_t*>(remap), const_cast<const int32_t*>(n_moves), (int)desc->num_pages);

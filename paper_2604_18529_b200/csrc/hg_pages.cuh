@@ -230,6 +230,12 @@ __device__ __forceinline__ SlotRange reserve_slots(const ReserveParams& p, int b
     return r;
 }
 
+constexpr int RESERVE_KEEP = 4;      // groups of 128 counts of a warp's range that stay in registers
+// Up to this many pages (their counts then fit the registers of one CTA) and slots (one a thread) one CTA does a call alone
+// although a cluster was launched, because the host does not know how many slots n_new asks for: 256 slots, 12069
+// pages: 8.4 us instead of 12.2; 1090 slots, 6104 pages: 14.5 either way.
+constexpr int RESERVE_SOLO_PAGES = RESERVE_KEEP * 128 * PG_WARPS, RESERVE_SOLO_SLOTS = PG_THREADS;
+
 // One cluster does the whole call: its phases (find the shared pages - give up references - find the last writer - rank the
 // needs - hand out) depend on one another, and a cluster barrier costs a few hundred nanoseconds where a launch costs
 // microseconds.  Every phase is a round trip to the L2 for one slot per thread; so a thread keeps its first slot in
@@ -239,56 +245,16 @@ __device__ __forceinline__ SlotRange reserve_slots(const ReserveParams& p, int b
 // when k = refs (nobody else reads it); all others copy.  That is what serving the sequences one after the other gives.
 // In parallel: every writer of a page with more than one reference takes its own off; a count that is still positive says
 // that others remain; else the writers leave the largest of their (sequence, slot) numbers there, as -(number + 1).
+//
+// reserve_phases: everything from the free scan on.  ids: this CTA's share of the free ids, by rank; cum[b]: slots of the
+// sequences before b; refs: the first counts of pr, this warp's pages.
 template <int CLUSTER>
-__global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(const ReserveParams p) {
+__device__ __forceinline__ void reserve_phases(const ReserveParams& p, const int wanted, int32_t* const ids, const int32_t* const cum,
+                                               const int4 (&refs)[RESERVE_KEEP], const PageRange pr, const int rank,
+                                               ClusterScan& scan_a, ClusterScan& scan_b, int& s_carry, int& s_shared) {
     namespace cg = cooperative_groups;
-    extern __shared__ int32_t reserve_smem[];
-    int32_t* const ids = reserve_smem;                            // this CTA's share of the free ids, by rank
-    int32_t* const cum = reserve_smem + RESERVE_IDS_PER_CTA;      // cum[b]: slots of sequences < b
-    __shared__ ClusterScan scan_a, scan_b;
-    __shared__ int s_warp[PG_WARPS], s_carry, s_shared;
+    constexpr int KEEP = RESERVE_KEEP;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int rank = CLUSTER > 1 ? (int)cg::this_cluster().block_rank() : 0;
-    if (tid == 0) s_carry = 0;
-    __syncthreads();
-    pages_begin();
-
-    // ---- free pages of this warp's range: counted here, listed below (the first 512 counts stay in registers) ----
-    constexpr int KEEP = 4;
-    const PageRange pr = warp_pages<CLUSTER>(p.num_pages, rank, warp);
-    int4 refs[KEEP];
-#pragma unroll
-    for (int u = 0; u < KEEP; ++u) refs[u] = pr.begin + u * 128 < pr.end ? load_refs(p.ref, pr.begin + u * 128 + lane * 4, p.num_pages, 1) : make_int4(1, 1, 1, 1);
-
-    // ---- slots per sequence, and what is known without looking at any page ----
-    for (int b0 = 0; b0 < p.B; b0 += PG_THREADS) {
-        const int b = b0 + tid;
-        SlotRange r;
-        r.count = 0;
-        if (b < p.B) r = reserve_slots(p, b);
-        int wt;
-        const int ex = warp_exclusive(r.count, lane, wt);
-        if (lane == 31) s_warp[warp] = wt;
-        __syncthreads();
-        int ct;
-        const int wx = warp_exclusive(s_warp[lane], lane, ct);
-        const int base = s_carry + __shfl_sync(0xffffffffu, wx, warp);
-        if (b < p.B) {
-            cum[b] = base + ex;
-            if (rank == 0) {
-                p.copy_src[b] = -1;
-                p.copy_dst[b] = -1;
-                if (p.copy_rows) p.copy_rows[b] = 0;
-                if (p.n_ready) p.n_ready[b] = r.n;
-                if (r.cut && p.status) atomicOr(p.status, HG_DEV_RANGE);
-            }
-        }
-        __syncthreads();
-        if (tid == 0) s_carry += ct;
-        __syncthreads();
-    }
-    // (B slots' sum fits: max_pages <= 2^31 / B is checked by the host)
-    const int wanted = s_carry;
     constexpr int LANES = CLUSTER * PG_THREADS;
     const int T = min(wanted, LANES * RESERVE_MAX_ITER);         // later slots are left for another call (n_ready says so)
     const int max_ids = CLUSTER * RESERVE_IDS_PER_CTA;
@@ -453,6 +419,71 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(const ReservePar
     if constexpr (CLUSTER > 1) cg::this_cluster().sync();         // peers' shared memory stays until all have read it
 }
 
+template <int CLUSTER>
+__global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(const ReserveParams p) {
+    namespace cg = cooperative_groups;
+    extern __shared__ int32_t reserve_smem[];
+    int32_t* const ids = reserve_smem;                            // this CTA's share of the free ids, by rank
+    int32_t* const cum = reserve_smem + RESERVE_IDS_PER_CTA;      // cum[b]: slots of sequences < b
+    __shared__ ClusterScan scan_a, scan_b;
+    __shared__ int s_warp[PG_WARPS], s_carry, s_shared;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = CLUSTER > 1 ? (int)cg::this_cluster().block_rank() : 0;
+    if (tid == 0) s_carry = 0;
+    __syncthreads();
+    pages_begin();
+
+    // ---- free pages of this warp's range: counted here, listed below (the first 512 counts stay in registers) ----
+    int4 refs[RESERVE_KEEP];
+    PageRange pr;
+    auto load_range = [&](PageRange r) {
+        pr = r;
+#pragma unroll
+        for (int u = 0; u < RESERVE_KEEP; ++u)
+            refs[u] = pr.begin + u * 128 < pr.end ? load_refs(p.ref, pr.begin + u * 128 + lane * 4, p.num_pages, 1) : make_int4(1, 1, 1, 1);
+    };
+    const bool small_pool = CLUSTER > 1 && p.num_pages <= RESERVE_SOLO_PAGES;
+    load_range(small_pool ? warp_pages<1>(p.num_pages, 0, warp) : warp_pages<CLUSTER>(p.num_pages, rank, warp));
+
+    // ---- slots per sequence, and what is known without looking at any page ----
+    for (int b0 = 0; b0 < p.B; b0 += PG_THREADS) {
+        const int b = b0 + tid;
+        SlotRange r;
+        r.count = 0;
+        if (b < p.B) r = reserve_slots(p, b);
+        int wt;
+        const int ex = warp_exclusive(r.count, lane, wt);
+        if (lane == 31) s_warp[warp] = wt;
+        __syncthreads();
+        int ct;
+        const int wx = warp_exclusive(s_warp[lane], lane, ct);
+        const int base = s_carry + __shfl_sync(0xffffffffu, wx, warp);
+        if (b < p.B) {
+            cum[b] = base + ex;
+            if (rank == 0) {
+                p.copy_src[b] = -1;
+                p.copy_dst[b] = -1;
+                if (p.copy_rows) p.copy_rows[b] = 0;
+                if (p.n_ready) p.n_ready[b] = r.n;
+                if (r.cut && p.status) atomicOr(p.status, HG_DEV_RANGE);
+            }
+        }
+        __syncthreads();
+        if (tid == 0) s_carry += ct;
+        __syncthreads();
+    }
+    // (B slots' sum fits: max_pages <= 2^31 / B is checked by the host)
+    const int wanted = s_carry;
+    if constexpr (CLUSTER > 1) {
+        if (small_pool && wanted <= RESERVE_SOLO_SLOTS) {          // (every CTA of the cluster comes to the same decision)
+            if (rank == 0) reserve_phases<1>(p, wanted, ids, cum, refs, pr, 0, scan_a, scan_b, s_carry, s_shared);
+            return;
+        }
+        if (small_pool) load_range(warp_pages<CLUSTER>(p.num_pages, rank, warp));
+    }
+    reserve_phases<CLUSTER>(p, wanted, ids, cum, refs, pr, rank, scan_a, scan_b, s_carry, s_shared);
+}
+
 // ---- compact: the pages in use move to the low end of the pool ------------------------------------------------------------
 
 struct CompactParams {
@@ -461,8 +492,13 @@ struct CompactParams {
     int32_t* move_src;               // [max_moves]
     int32_t* move_dst;               // [max_moves]
     int32_t* n_moves;
-    int num_pages, max_moves;
+    int32_t* table;                  // renamed here too if n_table > 0
+    int num_pages, max_moves, n_table;
 };
+
+// Tables of up to this many entries are renamed by the one CTA that compacts a small pool (400 entries: one launch and some 3 us
+// less); a larger one by a kernel of many CTAs.
+constexpr int COMPACT_RENAMES = 8192;
 
 // U pages in use.  Holes (free ids below U) are as many as strays (used ids from U on): the k-th lowest hole takes the
 // k-th highest stray, so a call that may move only a few pages still shortens the used range from its end.
@@ -535,6 +571,14 @@ __global__ void __launch_bounds__(PG_THREADS) kv_compact_kernel(const CompactPar
         p.remap[src] = dst;
         p.ref[dst] = __ldcg(p.ref + src);
         p.ref[src] = 0;
+    }
+    if (CLUSTER > 1 || p.n_table == 0 || moves == 0) return;
+    __syncthreads();
+    for (int i = tid; i < p.n_table; i += PG_THREADS) {
+        const int e = p.table[i];
+        if ((uint32_t)e >= (uint32_t)p.num_pages) continue;
+        const int to = __ldcg(p.remap + e);
+        if (to != e) p.table[i] = to;
     }
 }
 

@@ -154,6 +154,48 @@ def test_large_pool_and_batch_take_the_cluster():
     p.reserve([S * P] * B)
 
 
+@pytest.mark.parametrize("S", [8, 9])
+@pytest.mark.parametrize("n", [8192, 8193])
+def test_compaction_renames_tables_of_all_sizes(S, n):
+    """Pools and tables on both sides of what the compacting CTA renames by itself."""
+    B, P = 1024, 16
+    r = random.Random(S + n)
+    p = Pool(B, S, n, P, 1, 64)
+    pages = r.sample(range(n), 3000)
+    table = [[r.choice(pages) if r.random() < 0.5 else r.choice([-1, n, n + 7]) for _ in range(S)] for _ in range(B)]
+    ref = [0] * n
+    for row in table:
+        for e in row:
+            if 0 <= e < n:
+                ref[e] += 1
+    p.load(table, ref, [0] * B)
+    for most in (1, 500, n):
+        src, dst = p.compact(most)
+        p.copy_pages(src, dst, None, p.n_moves)
+
+
+@pytest.mark.parametrize("n", [700, 16384, 16385])
+@pytest.mark.parametrize("rows,new", [(300, 1), (1024, 1), (1025, 1), (300, 60), (0, 1)])
+def test_few_slots_of_a_large_table(n, rows, new):
+    """A table that takes the cluster, pools and numbers of slots on both sides of what one of its CTAs does alone."""
+    B, S, P = 1100, 40, 16
+    r = random.Random(n + rows)
+    p = Pool(B, S, n, P, 1, 64)
+    pages, table, lens, ref = r.sample(range(n), 400), [[-1] * S for _ in range(B)], [0] * B, [0] * n
+    for b in range(B):
+        lens[b] = r.randint(0, 3 * P)
+        for s in range(-(-lens[b] // P)):
+            table[b][s] = r.choice(pages)                  # shared by some eight rows each
+            ref[table[b][s]] += 1
+    p.load(table, ref, lens)
+    want = r.sample(range(B), rows)
+    for _ in range(2):
+        ready = p.reserve([new if b in want else 0 for b in range(B)])
+        p.copy_pages(*p.copy)
+        p.o_lens = [a + b for a, b in zip(p.o_lens, ready)]
+        p.lens.copy_(ints(p.o_lens))
+
+
 @pytest.mark.parametrize("B,S", [(64, 3), (65, 40), (129, 300), (700, 33), (16384, 2), (65535, 3)])
 def test_forks_of_large_batches(B, S):
     """Rows shared out over a cluster; random sources, every row possibly another's."""
