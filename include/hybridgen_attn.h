@@ -443,8 +443,8 @@ typedef struct hg_prefix_desc {
  *           o_part 32-byte aligned
  * Of desc: batch, heads, head_dim, dtype, the KV addressing, scale, flags and status are used (its chunk fields are not).
  * Accumulation is fp32 and P is carried as a two-term (hi + lo) 16-bit expansion, as in hg_attn_partial: a weight is off
- * by at most 2^-18 of itself with bf16 (with 64 components a third term makes that 2^-24), by 2^-24 of the chunk's largest
- * with fp16.
+ * by at most 2^-17 of itself with bf16 (with 64 components a third term makes that 2^-24), with fp16 by 2^-22 of itself or
+ * 2^-25 of the chunk's largest.
  */
 hg_status hg_attn_prefix_partial(const void* q, const void* k_cache, const void* v_cache, float* o_part, float* m_part, float* l_part,
                                  void* stream, const hg_attn_desc* desc, const hg_prefix_desc* prefix);

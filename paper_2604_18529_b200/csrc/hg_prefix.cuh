@@ -146,8 +146,8 @@ __device__ __forceinline__ int pfx_tile_index(const PfxItem& it, int s, int i) {
 }
 __device__ __forceinline__ int pfx_total_tiles(const PfxItem& it) { return it.wide ? it.tiles(0) : it.tiles(0) + it.tiles(1); }
 
-// Two weights -> packed hi terms (rounded) and packed lo terms (what that left, rounded): at most 2^-18 (bf16) or 2^-24
-// (fp16) of a weight is lost.
+// Two weights -> packed hi terms (rounded) and packed lo terms (what that left, rounded): at most 2^-17 (bf16) or 2^-22
+// (fp16, or 2^-25 outright: its smallest steps) of a weight is lost.
 template <bool BF16>
 __device__ __forceinline__ void split2(float2 w, uint32_t& hi, uint32_t& lo) {
     hi = pack2<BF16>(w.x, w.y);
@@ -207,8 +207,8 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
     // its components contiguous (N-major), N = D
     constexpr uint32_t IDESC_S = (1u << 4) | (FMT << 7) | (FMT << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
     constexpr uint32_t IDESC_O = (1u << 4) | (FMT << 7) | (FMT << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
-    // bf16 weights lose up to 2^-18 in two terms (1.1e-6 of a result of 2 000 tokens); with 64 components tensor memory has
-    // room for a third one beside O, which leaves 2^-24
+    // bf16 weights lose up to 2^-17 in two terms (1.1e-6 of a result of 2 000 tokens); with 64 components tensor memory has
+    // room for a third one beside O, which leaves 2^-24 (with 128 the four tiles of S / P and O fill it)
     constexpr bool THIRD = BF16 && D == 64;
     const float NEG_INF = __int_as_float(0xff800000);
 
