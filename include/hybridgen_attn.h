@@ -491,6 +491,8 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
  *                   the call: src_row[b] = b leaves the row alone, a negative one frees it (entries -1, lengths 0).
  *                   Several rows may take the same one, and rows may take each other's (a beam step).  seq_lens,
  *                   tok_begin and tok_end (the last two may be NULL) move with the rows; counts follow the entries.
+ *                   One array may be given for several of the three and is moved once (tok_end = seq_lens, say); arrays
+ *                   that overlap in part, or that overlap src_row, are refused.
  *                   A value of B or more leaves the row alone and sets HG_DEV_RANGE.
  *   hg_kv_reserve   makes positions [seq_lens[b], seq_lens[b] + n_new[b]) of every row writable (n_new: dev int32 [B],
  *                   or NULL for one each; 0 or less: nothing): a slot without a page gets one, a page that others use

@@ -53,6 +53,12 @@ static hg_status check_table(const hg_attn_desc* d) {
     return HG_OK;
 }
 
+// Two arrays of `bytes` each that share memory.
+static bool overlap(const void* a, const void* b, size_t bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && (x < y ? y - x : x - y) < bytes;
+}
+
 static int sm_count() {
     static std::atomic<int> known[kMaxDevices];
     int dev = 0;
@@ -78,7 +84,18 @@ hg_status hg_kv_fork(const int32_t* src_row, int32_t* ref_count, int32_t* seq_le
     if (!src_row || !ref_count || !seq_lens) return HG_ERR_INVALID_ARG;
     ForkParams p;
     p.src_row = src_row; p.table = const_cast<int32_t*>(desc->block_table); p.ref = ref_count;
-    p.vec[0] = seq_lens; p.vec[1] = tok_begin; p.vec[2] = tok_end;
+    // one array may stand for several (seq_lens for tok_end, where the GPU holds all tokens): it is moved once.  Arrays that
+    // overlap in part, and a src_row that the call would write while it reads it, are refused.
+    int32_t* const vec[3] = {seq_lens, tok_begin, tok_end};
+    const size_t bytes = (size_t)desc->batch * sizeof(int32_t);
+    for (int i = 0; i < 3; ++i) {
+        p.vec[i] = vec[i];
+        if (overlap(src_row, vec[i], bytes)) return HG_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j) {
+            if (vec[j] == vec[i]) p.vec[i] = nullptr;
+            else if (overlap(vec[j], vec[i], bytes)) return HG_ERR_INVALID_ARG;
+        }
+    }
     p.status = desc->status; p.B = desc->batch; p.max_pages = desc->max_pages; p.num_pages = desc->num_pages;
     // a cluster of 8 CTAs shares a tile's rows once there is work for it (1024 rows of 64 entries: 4.1 us instead of 10.2; 256
     // rows of 502: 5.7 instead of 4.2); 32 columns (128-byte row pieces) a tile where that leaves two CTAs for every SM, down

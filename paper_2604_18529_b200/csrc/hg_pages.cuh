@@ -103,7 +103,7 @@ struct ForkParams {
     const int32_t* src_row;          // [B]
     int32_t* table;                  // [B][max_pages]
     int32_t* ref;                    // [num_pages]
-    int32_t* vec[3];                 // seq_lens, tok_begin, tok_end (each may be NULL)
+    int32_t* vec[3];                 // seq_lens, tok_begin, tok_end (NULL: absent, or the same array as one before)
     int32_t* status;
     int B, max_pages, num_pages;
     int cols_shift;                  // log2 of the block-table columns one cluster handles

@@ -150,6 +150,16 @@ def test_batch_limits_alignment_and_counts(lib):
     assert lib.hg_kv_copy_pages(FAKE, FAKE, None, 0, None, FAKE, FAKE, None, C.byref(d)) == hg.HG_OK
 
 
+def test_fork_refuses_arrays_that_overlap(lib):
+    """Whole arrays may be the same; a part of one, and the rows' sources among what is written, may not."""
+    d = table_desc(batch=64)
+    at = lambda **over: [over.get(n, FAKE + 4096 * i) for i, n in enumerate(("src", "ref", "lens", "begin", "end"))]   # noqa: E731
+    lens = FAKE + 4096 * 2
+    for over in (dict(begin=lens + 4), dict(end=lens - 4), dict(end=lens + 252), dict(begin=FAKE + 4096 * 4 + 128), dict(src=lens),
+                 dict(src=lens + 128), dict(src=FAKE + 4096 * 3), dict(src=FAKE + 4096 * 4 - 252)):
+        assert lib.hg_kv_fork(*at(**over), None, C.byref(d)) == hg.HG_ERR_INVALID_ARG, over
+
+
 def test_binding_refuses_host_tensors():
     import torch
     t = torch.zeros(64, dtype=torch.int32)

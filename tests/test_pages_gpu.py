@@ -330,3 +330,31 @@ def test_wrong_tensors_are_refused_by_the_binding():
         pkg.hg_kv_copy_pages(p.copy[0], p.copy[1][:2], None, None, p.k, p.v, p.desc)
     with pytest.raises(hg.HgError):
         pkg.hg_kv_reserve(p.lens, None, torch.zeros(10, dtype=torch.int32, device=DEV)[1:], *p.copy, None, p.desc)  # misaligned
+
+
+@pytest.mark.parametrize("same", ["end", "begin", "begin and end", "all"])
+@pytest.mark.parametrize("B", [6, 300, 700])
+def test_fork_moves_an_array_once_that_it_is_given_twice(B, same):
+    """Callers whose tokens are all on the GPU keep one array for seq_lens and tok_end; rows swap, branch and end."""
+    r = random.Random(B)
+    S, n = 3, 4 * B
+    table = [[r.choice([-1, r.randrange(n)]) for _ in range(S)] for _ in range(B)]
+    ref = [0] * n
+    for row in table:
+        for e in row:
+            if e >= 0:
+                ref[e] += 1
+    lens, begin, end = ([r.randint(1, 48) for _ in range(B)] for _ in range(3))
+    src = [r.randrange(-1, B) for _ in range(B)]
+    src[0], src[1] = 1, 0
+    p = Pool(B, S, n, 16, 1, 64)
+    p.load(table, ref, lens)
+    p.begin.copy_(ints(begin))
+    p.end.copy_(ints(end))
+    args = {"end": (p.lens, p.begin, p.lens), "begin": (p.lens, p.lens, p.end), "begin and end": (p.lens, p.end, p.end),
+            "all": (p.lens, p.lens, p.lens)}[same]
+    p.o_begin, p.o_end = list(begin), list(end)
+    moved = [{id(p.lens): p.o_lens, id(p.begin): p.o_begin, id(p.end): p.o_end}[i] for i in {id(t) for t in args}]
+    pkg.hg_kv_fork(ints(src), p.ref, *args, p.desc)
+    assert p.take_status() == O.fork(p.o_table, p.o_ref, src, *moved)
+    p.check(same)
