@@ -124,11 +124,19 @@ __device__ __forceinline__ int table_reach(const PartialParams& p) {
     return (int)min((long long)p.max_pages << p.page_shift, (long long)INT32_MAX);
 }
 
+// The ranges and the block table are read past the L1, before and after the wait for the kernel in front (below): the guess
+// may fetch them while that kernel (hg_kv_fork, hg_kv_reserve, hg_kv_compact) is writing them, and a line that it left in
+// the L1 must not answer the real read.
+__device__ __forceinline__ int load_shared_state(const int32_t* x) { return __ldcg(x); }
+
 // Clamped slice [tb, te) of sequence b and its number of chunk slots in use.  The slice also ends where the
-// block table's row ends: tokens beyond it have no page to be read from (range_beyond_table() reports them).
-__device__ __forceinline__ int seq_chunks(const PartialParams& p, int b, int& tb, int& te) {
-    tb = max(p.tok_begin[b], 0);
-    te = min(min(p.tok_end[b], p.seq_lens[b]), table_reach(p));
+// block table's row ends: tokens beyond it have no page to be read from; `beyond` is raised then.
+__device__ __forceinline__ int seq_chunks(const PartialParams& p, int b, int& tb, int& te, bool& beyond) {
+    tb = max(load_shared_state(p.tok_begin + b), 0);
+    te = min(load_shared_state(p.tok_end + b), load_shared_state(p.seq_lens + b));
+    const int reach = table_reach(p);
+    beyond |= te > reach && tb < te;
+    te = min(te, reach);
     if (te <= tb) return 0;
     return min(fast_div(te + p.C - 1, p.div_C) - fast_div(tb, p.div_C), p.NC);
 }
@@ -136,11 +144,6 @@ __device__ __forceinline__ int seq_chunks(const PartialParams& p, int b, int& tb
 // Chunk slots in use by a clamped slice [tb, te).
 __device__ __forceinline__ int chunks_of(const PartialParams& p, int tb, int te) {
     return te <= tb ? 0 : min(fast_div(te + p.C - 1, p.div_C) - fast_div(tb, p.div_C), p.NC);
-}
-
-// True when sequence b's slice reaches past the last page its block-table row can name.
-__device__ __forceinline__ bool range_beyond_table(const PartialParams& p, int b) {
-    return min(p.tok_end[b], p.seq_lens[b]) > table_reach(p) && max(p.tok_begin[b], 0) < min(p.tok_end[b], p.seq_lens[b]);
 }
 
 __device__ __forceinline__ void set_range(const PartialParams& p, Item& it, int tb, int te) {
@@ -163,8 +166,9 @@ __device__ __forceinline__ Item decode_item(const PartialParams& p, const Contro
     Item it;
     it.b = lo;
     int tb, te, nc;
+    bool beyond = false;
     if (lo < RANGE_CACHE) { tb = ctl.rng[lo].x; te = ctl.rng[lo].y; nc = max(chunks_of(p, tb, te), 1); }
-    else nc = max(seq_chunks(p, lo, tb, te), 1);
+    else nc = max(seq_chunks(p, lo, tb, te, beyond), 1);
     const int r = i - ctl.cum[lo];
     if (p.head_blocks == 1) {
         it.c = fast_div(r, p.div_Hkv);    // KV heads vary fastest: CTAs that run side by side read the same pages
@@ -239,8 +243,7 @@ __global__ void __launch_bounds__(THREADS, MODE == MODE_GQA ? 3 : 2) partial_ker
         bool beyond = false;
         for (int b = b0; b < b1; ++b) {
             int tb, te;
-            sum += seq_chunks(p, b, tb, te) * Y;
-            beyond |= range_beyond_table(p, b);
+            sum += seq_chunks(p, b, tb, te, beyond) * Y;
             if (b < RANGE_CACHE) ctl.rng[b] = make_int2(tb, te);
         }
         if (report && beyond && p.status && blockIdx.x == 0) atomicOr(p.status, HG_DEV_RANGE);
@@ -257,7 +260,7 @@ __global__ void __launch_bounds__(THREADS, MODE == MODE_GQA ? 3 : 2) partial_ker
         if (tid == 0) ctl.cum[0] = 0;
         for (int b = b0; b < b1; ++b) {
             int tb, te;
-            run += seq_chunks(p, b, tb, te) * Y;
+            run += (b < RANGE_CACHE ? chunks_of(p, ctl.rng[b].x, ctl.rng[b].y) : seq_chunks(p, b, tb, te, beyond)) * Y;
             ctl.cum[b + 1] = run;
         }
         __syncthreads();
@@ -270,7 +273,8 @@ __global__ void __launch_bounds__(THREADS, MODE == MODE_GQA ? 3 : 2) partial_ker
         // on a guess at this CTA's first work item - the ranges and the block table as they look right now, which is
         // what they will be unless that kernel is the one changing them - the item's first K and V boxes are requested
         // into the L2.  These are hints: every index is bounds-checked, nothing is written, no result depends on what
-        // was read here, and everything is read again, for real, after the wait.
+        // was read here, and everything is read again, for real, after the wait - neither time through the L1, which could
+        // answer the second read with what the first one found.
         if (p.spec_prefetch && p.persistent) {
             scan_items(false);
             if (warp == CONSUMER_WARPS && (int)blockIdx.x < ctl.cum[p.B]) {
@@ -284,7 +288,7 @@ __global__ void __launch_bounds__(THREADS, MODE == MODE_GQA ? 3 : 2) partial_ker
                         const int pg = t0j >> p.page_shift;
                         int phys = -1;
                         if (pg >= 0 && pg < p.max_pages)
-                            phys = p.block_table ? __ldg(p.block_table + (size_t)it.b * p.max_pages + pg) : it.b * p.max_pages + pg;
+                            phys = p.block_table ? load_shared_state(p.block_table + (size_t)it.b * p.max_pages + pg) : it.b * p.max_pages + pg;
                         if (phys >= 0 && phys < p.num_pages && g >= 0 && g < p.Hkv)
                             tma_prefetch_5d(isv ? &tmV : &tmK, 0, t0j & (p.page_size - 1), 0, g, phys);
                     }
@@ -317,7 +321,12 @@ __global__ void __launch_bounds__(THREADS, MODE == MODE_GQA ? 3 : 2) partial_ker
         // (CTAs beyond the round-robin width, or any CTA when there is no item at all, still help with the empty
         // chunk slots below before they leave)
     } else {
-        if (tid == 0 && blockIdx.x == 0 && blockIdx.y == 0 && p.status && range_beyond_table(p, blockIdx.z)) atomicOr(p.status, HG_DEV_RANGE);
+        int tb, te;
+        bool beyond = false;
+        if (tid == 0 && blockIdx.x == 0 && blockIdx.y == 0 && p.status) {
+            seq_chunks(p, blockIdx.z, tb, te, beyond);
+            if (beyond) atomicOr(p.status, HG_DEV_RANGE);
+        }
         __syncthreads();
     }
     if (status_at_entry & HG_DEV_WAIT_TIMEOUT) return;   // checked only now: its load overlapped the scan's loads
@@ -329,7 +338,8 @@ __global__ void __launch_bounds__(THREADS, MODE == MODE_GQA ? 3 : 2) partial_ker
         Item it;
         it.b = blockIdx.z; it.y = blockIdx.y; it.c = blockIdx.x;
         int tb, te;
-        seq_chunks(p, it.b, tb, te);
+        bool beyond = false;
+        seq_chunks(p, it.b, tb, te, beyond);
         if (te <= tb) { it.lo = it.hi = it.tile0 = it.ntiles = 0; } else set_range(p, it, tb, te);
         return it;
     };
@@ -383,7 +393,7 @@ __global__ void __launch_bounds__(THREADS, MODE == MODE_GQA ? 3 : 2) partial_ker
         // (the value is only loaded here; check_page() validates it once it is needed)
         auto lookup = [&](const Item& it, int pg) -> int {
             if ((pg << p.page_shift) < it.hi && ((pg + 1) << p.page_shift) > it.lo && pg < p.max_pages)
-                return p.block_table ? __ldg(p.block_table + (size_t)it.b * p.max_pages + pg) : it.b * p.max_pages + pg;
+                return p.block_table ? load_shared_state(p.block_table + (size_t)it.b * p.max_pages + pg) : it.b * p.max_pages + pg;
             return -2;                                   // no token of the item on this page
         };
         auto check_page = [&](int phys) -> int {

@@ -358,3 +358,64 @@ def test_fork_moves_an_array_once_that_it_is_given_twice(B, same):
     pkg.hg_kv_fork(ints(src), p.ref, *args, p.desc)
     assert p.take_status() == O.fork(p.o_table, p.o_ref, src, *moved)
     p.check(same)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,P", [(8, 2, 64, 16), (4, 4, 128, 16), (32, 2, 128, 64)])
+def test_attention_directly_behind_table_operations(Hq, Hkv, D, P):
+    """Attention launched as a programmatic dependent of the kernel that changes its table and ranges (few chunk slots, no
+    counter to clear), the stream backed up so that it starts early: the bits of a run that waits after every call."""
+    B, S, n, NC, rounds = 6, 8, 40, max(8 * P // 64, 1) + 1, 30
+
+    def run(waits):
+        r = random.Random(D + P)
+        p = Pool(B, S, n, P, Hkv, D, seed=D)
+        for i, x in enumerate((p.k, p.v)):
+            g = torch.Generator(device=DEV)
+            g.manual_seed(i)
+            x.copy_(torch.randn(x.shape, generator=g, device=DEV))
+        p.desc.num_q_heads, p.desc.num_chunks = Hq, NC
+        p.desc.tune = 4 if waits else 0                       # HG_TUNE_NO_PDL for the side that is waited for
+        q = torch.randn(B, Hq, D, generator=g, device=DEV).half()
+        ws = torch.empty(pkg.hg_attn_workspace_bytes(p.desc, 0), dtype=torch.uint8, device=DEV)
+        outs = [[torch.zeros(B, Hq, D, device=DEV), torch.zeros(B, Hq, device=DEV), torch.zeros(B, Hq, NC, D, device=DEV),
+                 torch.zeros(B, Hq, NC, device=DEV), torch.zeros(B, Hq, NC, device=DEV)] for _ in range(4 * rounds)]
+        srcs = [ints([r.randrange(-1, B) if r.random() < 0.7 else b for b in range(B)]) for _ in range(2 * rounds)]
+        news = [ints([r.choice([0, 1, P, 3 * P + 5]) for _ in range(B)]) for _ in range(rounds)]
+        most = [r.randint(1, n) for _ in range(rounds)]
+        torch.cuda.synchronize()
+        if not waits:
+            torch.cuda._sleep(100_000_000)                    # some 50 ms: the calls below queue up behind it
+        at = iter(outs)
+
+        def call(f, *a):
+            f(*a, p.desc)
+            if waits:
+                torch.cuda.synchronize()
+
+        def attend(whole):
+            out, lse, o, m, l = next(at)
+            if whole:
+                call(pkg.hg_attn_decode, q, p.k, p.v, p.lens, p.begin, p.end, [], out, lse, ws)
+            else:
+                call(pkg.hg_attn_partial, q, p.k, p.v, p.lens, p.begin, p.end, o, m, l)
+
+        for i in range(rounds):
+            call(pkg.hg_kv_fork, srcs[2 * i], p.ref, p.lens, p.begin, p.end)
+            attend(i % 2)
+            call(pkg.hg_kv_reserve, p.lens, news[i], p.ref, *p.copy, p.ready)
+            call(pkg.hg_kv_copy_pages, *p.copy, None, p.k, p.v)
+            attend((i + 1) % 2)
+            p.lens.add_(p.ready)
+            p.end.copy_(p.lens)
+            call(pkg.hg_kv_compact, p.ref, p.remap, p.moves[0][:most[i]], p.moves[1][:most[i]], p.n_moves)
+            call(pkg.hg_kv_copy_pages, p.moves[0][:most[i]], p.moves[1][:most[i]], None, p.n_moves, p.k, p.v)
+            attend(i % 2)
+            call(pkg.hg_kv_fork, srcs[2 * i + 1], p.ref, p.lens, p.begin, p.end)
+            attend((i + 1) % 2)
+        torch.cuda.synchronize()
+        return [t for o in outs for t in o] + [p.table, p.ref, p.lens, p.status]
+
+    want, got = run(True), run(False)
+    assert sum(int(t.count_nonzero()) for t in want[:-4]) > 0
+    for i, (x, y) in enumerate(zip(got, want)):
+        assert torch.equal(x, y), i
