@@ -16,7 +16,9 @@
 namespace hg {
 
 // The kernels below are launched as programmatic dependents of whatever precedes them in the stream: the launch
-// itself overlaps the predecessor, nothing is read or written before this returns.
+// itself overlaps the predecessor, nothing is read or written before this returns.  Since a predecessor may still be writing
+// what they read, none of their arrays is declared read-only (const with __restrict__): such loads might go through the
+// non-coherent path or be moved in front of the wait.
 __device__ __forceinline__ void pages_begin() {
     cudaTriggerProgrammaticLaunchCompletion();
     cudaGridDependencySynchronize();
@@ -24,8 +26,7 @@ __device__ __forceinline__ void pages_begin() {
 
 // ---- release: one reference less for every listed page ---------------------------------------------------------------
 
-__global__ void __launch_bounds__(256) kv_release_kernel(const int32_t* __restrict__ ids, int n, int32_t* ref, int num_pages,
-                                                          int32_t* status) {
+__global__ void __launch_bounds__(256) kv_release_kernel(const int32_t* ids, int n, int32_t* ref, int num_pages, int32_t* status) {
     pages_begin();
     for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
         const int p = ids[i];
@@ -583,8 +584,7 @@ __global__ void __launch_bounds__(PG_THREADS) kv_compact_kernel(const CompactPar
 }
 
 // Renames the entries of the block table.
-__global__ void __launch_bounds__(256) kv_rename_kernel(int32_t* table, size_t n, const int32_t* __restrict__ remap,
-                                                         const int32_t* __restrict__ n_moves, int num_pages) {
+__global__ void __launch_bounds__(256) kv_rename_kernel(int32_t* table, size_t n, const int32_t* remap, const int32_t* n_moves, int num_pages) {
     pages_begin();
     if (*n_moves == 0) return;
     const size_t step = (size_t)gridDim.x * 256;
@@ -602,9 +602,8 @@ constexpr int COPY_THREADS = 256;
 
 // A warp per (pair, tensor, KV head): the head's block of a page, 2 to 64 KB, in 16-byte vectors, eight in flight a lane.
 // Bound by HBM: 401 MB of 16-token pages in 120 us, read and written (6.7 TB/s; a plain copy here: 6.54).
-__global__ void __launch_bounds__(COPY_THREADS) kv_copy_pages_kernel(KvPoolView pv, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
-                                                                      const int32_t* __restrict__ rows, int n,
-                                                                      const int32_t* __restrict__ n_dev, int32_t* status) {
+__global__ void __launch_bounds__(COPY_THREADS) kv_copy_pages_kernel(KvPoolView pv, const int32_t* src, const int32_t* dst,
+                                                                      const int32_t* rows, int n, const int32_t* n_dev, int32_t* status) {
     pages_begin();
     const int pairs = n_dev ? max(0, min(*n_dev, n)) : n;
     const int lane = threadIdx.x & 31;
