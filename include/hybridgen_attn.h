@@ -466,7 +466,7 @@ size_t hg_attn_shared_workspace_bytes(const hg_attn_desc* desc, const hg_prefix_
  * tokens [tok_begin, tok_end), and the merge of both with n_host_src (at most HG_MAX_MERGE_SRC - 2) further sources.  The
  * result is attention over all of them together; a token that lies in both a group's slice and a member's own counts
  * twice, so tok_begin[b] is usually the group's end.  A sequence without a group simply has all its tokens in
- * [tok_begin, tok_end).  workspace: dev, 256-byte aligned, at least hg_attn_shared_workspace_bytes(); it holds the work
+ * [tok_begin, tok_end).  A slice that needs more than desc's num_chunks chunks is truncated to them, as in hg_attn_partial.  workspace: dev, 256-byte aligned, at least hg_attn_shared_workspace_bytes(); it holds the work
  * counter too, which the call clears on its way in any case; not shared by calls that may overlap on the GPU (captured
  * graphs replayed on different streams among them).
  */

@@ -85,10 +85,13 @@ static hg_status launch_prefix(const CUtensorMap& tq, const CUtensorMap& tk, con
     return HG_OK;
 }
 
-// The own slices as further items of the shared launch (all pointers set), or not.
+// The own slices of a joined step: further items of the shared launch, or only cut (where `cut` is given) for the launch behind it.
 struct OwnSlices {
     const int32_t *seq_lens, *tok_begin, *tok_end;
     float *o, *m, *l;
+    bool items;
+    int32_t* cut;
+    int cut_C, cut_NC;
 };
 
 static hg_status run_prefix(const void* q, const void* k, const void* v, float* o_part, float* m_part, float* l_part, int32_t* zero,
@@ -102,7 +105,8 @@ static hg_status run_prefix(const void* q, const void* k, const void* v, float* 
     p.group_begin = x->group_begin; p.group_end = x->group_end;
     p.o_part = o_part; p.m_part = m_part; p.l_part = l_part; p.status = d->status; p.zero = zero;
     if (own) {
-        p.own = 1; p.own_NC = d->num_chunks; p.own_C = d->chunk_tokens;
+        p.own = own->items; p.own_NC = d->num_chunks; p.own_C = d->chunk_tokens;
+        p.cut = own->cut; p.cut_C = own->cut_C; p.cut_NC = own->cut_NC;
         p.seq_lens = own->seq_lens; p.tok_begin = own->tok_begin; p.tok_end = own->tok_end;
         p.own_o = own->o; p.own_m = own->m; p.own_l = own->l;
     }
@@ -129,7 +133,7 @@ static bool own_in_shared_launch(const hg_attn_desc* d) {
 }
 
 // Workspace of the joined step: the shared partials in front, behind them what hg_attn_decode's partial half needs.
-struct SharedWorkspace { size_t po, pm, pl, o, m, l, sched, total; };
+struct SharedWorkspace { size_t po, pm, pl, o, m, l, sched, cut, total; };
 
 static SharedWorkspace plan_shared(const hg_attn_desc* d, const hg_prefix_desc* x) {
     SharedWorkspace w;
@@ -142,6 +146,7 @@ static SharedWorkspace plan_shared(const hg_attn_desc* d, const hg_prefix_desc* 
     w.m = off; off += up256(rows * d->num_chunks * sizeof(float));
     w.l = off; off += up256(rows * d->num_chunks * sizeof(float));
     w.sched = off; off += 256;
+    w.cut = off; off += up256((size_t)d->batch * sizeof(int32_t));
     w.total = off;
     return w;
 }
@@ -222,22 +227,25 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
     dd.flags |= HG_FLAG_SPARSE_EMPTY;                                  // the partials are private to this call and its merge
     dd.sched_counter = reinterpret_cast<int32_t*>(ws + w.sched);
     // The chunks of the own slices are private to this call: where there are many, 256 tokens are better than fewer (with
-    // 4000 to 5400 chunk slots of 128 tokens hg_attn_partial takes 26, 32 and 36 us instead of 31, 37 and 40)
+    // 4000 to 5400 chunk slots of 128 tokens hg_attn_partial takes 26, 32 and 36 us instead of 31, 37 and 40).  A slice is
+    // still cut where the caller's chunk slots end: the shared kernel writes the ends that hg_attn_partial reads.
     const int coarse = 256;
+    int32_t* cut = nullptr;
     const int64_t slots = ((int64_t)dd.num_chunks * dd.chunk_tokens + coarse - 1) / coarse + 1;
     if (dd.chunk_tokens < coarse && slots <= dd.num_chunks && (int64_t)dd.batch * dd.num_kv_heads * dd.num_chunks >= 1024) {
+        cut = reinterpret_cast<int32_t*>(ws + w.cut);
         dd.chunk_tokens = coarse;
         dd.num_chunks = (int32_t)slots;
     }
-    const OwnSlices own = {seq_lens, tok_begin, tok_end, at(w.o), at(w.m), at(w.l)};
-    const bool one_launch = own_in_shared_launch(&dd);
+    const bool one_launch = !cut && own_in_shared_launch(&dd);
+    const OwnSlices own = {seq_lens, tok_begin, tok_end, at(w.o), at(w.m), at(w.l), one_launch, cut, desc->chunk_tokens, desc->num_chunks};
     // where the own partials get a launch of their own, the shared kernel clears their work counter on its way, so that no
     // clearing stands between the two
-    st = run_prefix(q, k_cache, v_cache, at(w.po), at(w.pm), at(w.pl), one_launch ? nullptr : dd.sched_counter, one_launch ? &own : nullptr, stream, &dd, prefix);
+    st = run_prefix(q, k_cache, v_cache, at(w.po), at(w.pm), at(w.pl), one_launch ? nullptr : dd.sched_counter, &own, stream, &dd, prefix);
     if (st != HG_OK) return st;
     if (!one_launch) {
         dd.flags |= HG_FLAG_COUNTER_CLEAN;
-        st = hg_attn_partial(q, k_cache, v_cache, seq_lens, tok_begin, tok_end, at(w.o), at(w.m), at(w.l), stream, &dd);
+        st = hg_attn_partial(q, k_cache, v_cache, seq_lens, tok_begin, cut ? cut : tok_end, at(w.o), at(w.m), at(w.l), stream, &dd);
         if (st != HG_OK) return st;
     }
     hg_partial_src src[HG_MAX_MERGE_SRC];

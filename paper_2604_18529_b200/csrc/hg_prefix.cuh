@@ -56,6 +56,8 @@ struct PrefixParams {
     float* own_m;
     float* own_l;
     int own, own_NC, own_C;
+    int32_t* cut;                    // [B], or NULL: receives where own slices end that stop with the last of cut_NC chunks of cut_C
+    int cut_C, cut_NC;               // tokens (the launch that follows works on longer chunks)
     int B, Hq, Hkv, G, NG, NC, C;
     int page_size, page_shift, max_pages, num_pages;
     int sparse_empty, test_stall;
@@ -264,6 +266,9 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
           if (g < (uint32_t)p.NG) atomicAdd(&ctl.group_n[g >> 1], (g & 1) ? 0x10000u : 1u);
       }
       if (blockIdx.x == 0 && p.zero && tid < 258) p.zero[tid - 256] = 0;
+      if (p.cut)
+          for (int b = blockIdx.x * 256 + tid - 256; b < p.B; b += gridDim.x * 256)
+              p.cut[b] = (int)min((long long)p.tok_end[b], (max(p.tok_begin[b], 0) / p.cut_C + (long long)p.cut_NC) * p.cut_C);
       asm volatile("bar.sync 1, 256;" ::: "memory");
       if (timed_out()) {
           // an earlier call ran into its limit: no work until the caller has cleared the word

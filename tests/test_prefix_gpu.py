@@ -485,3 +485,19 @@ def test_fork_reserve_append_attend_compact():
         x = (q[b].double()[:, None] @ K.transpose(1, 2))[:, 0] * D ** -0.5
         assert (lse[b].double() - torch.logsumexp(x, 1)).abs().max() <= 1e-4
         assert (out[b].double() - (torch.softmax(x, 1)[:, None] @ V)[:, 0]).abs().max() <= 1e-4 * float(V.abs().max())
+
+
+@pytest.mark.parametrize("own_chunk,slots", [(64, 6), (64, 26), (128, 4), (128, 14), (192, 5), (192, 10)])
+@pytest.mark.parametrize("D,B,Hq", [(128, 96, 8), (64, 70, 4)])
+def test_own_slices_of_several_chunks_in_a_large_batch(own_chunk, slots, D, B, Hq):
+    """Many short own chunks, slices that begin anywhere in one; what does not fit the caller's chunk slots is left out, as
+    hg_attn_partial does it, whatever grid the call works on."""
+    r = np.random.RandomState(own_chunk + slots + D)
+    group = r.randint(-1, 3, B).tolist()
+    b = Batch(group, [77, 300, 515], r.randint(200, 1500, B).tolist(), Hq, 4, D, 16, F16, 256, seed=slots)
+    b.desc.chunk_tokens, b.desc.num_chunks = own_chunk, slots
+    assert B * 4 * slots >= 1024
+    got = b.step()
+    b.total = [min(t, (int(lo) // own_chunk + slots) * own_chunk) for t, lo in zip(b.total, b.tok_begin.tolist())]
+    close(b, got, b.step64())
+    assert int(b.status) == 0
