@@ -266,9 +266,6 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
           if (g < (uint32_t)p.NG) atomicAdd(&ctl.group_n[g >> 1], (g & 1) ? 0x10000u : 1u);
       }
       if (blockIdx.x == 0 && p.zero && tid < 258) p.zero[tid - 256] = 0;
-      if (p.cut)
-          for (int b = blockIdx.x * 256 + tid - 256; b < p.B; b += gridDim.x * 256)
-              p.cut[b] = (int)min((long long)p.tok_end[b], (max(p.tok_begin[b], 0) / p.cut_C + (long long)p.cut_NC) * p.cut_C);
       asm volatile("bar.sync 1, 256;" ::: "memory");
       if (timed_out()) {
           // an earlier call ran into its limit: no work until the caller has cleared the word
@@ -613,6 +610,8 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
         for (int b = blockIdx.x * 8 + warp; b < p.B; b += gridDim.x * 8) {
             const uint32_t g = (uint32_t)p.seq_group[b];
             write_empty(b, g < (uint32_t)p.NG ? group_slice(p, (int)g).nc : 0, p.NC, p.m_part, p.l_part, p.o_part);
+            if (p.cut && lane == 0)
+                p.cut[b] = (int)min((long long)p.tok_end[b], (max(p.tok_begin[b], 0) / p.cut_C + (long long)p.cut_NC) * p.cut_C);
             if (!p.own) continue;
             const GroupSlice sl = own_slice(p, b);
             if (sl.bad && lane == 0 && p.status) atomicOr(p.status, HG_DEV_RANGE);
