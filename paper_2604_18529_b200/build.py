@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libhybridgen_attn.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("hg_attn.cu", "hg_pages.cu", "hg_prefix.cu", "hg_host.cpp")]
 DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("hg_device.cuh", "hg_partial.cuh", "hg_merge.cuh", "hg_logits.cuh", "hg_logits_tc.cuh", "hg_kvcache.cuh", "hg_stage.cuh",
-                                                  "hg_hostutil.h", "hg_poolview.cuh", "hg_pages.cuh", "hg_prefix.cuh", "hg_tcgen05.cuh")] + [
+                                                  "hg_hostutil.h", "hg_poolview.cuh", "hg_ring.h", "hg_pages.cuh", "hg_prefix.cuh", "hg_tcgen05.cuh")] + [
     os.path.join(ROOT, "include", "hybridgen_attn.h"), os.path.join(ROOT, "include", "hybridgen_host.h")]
 
 

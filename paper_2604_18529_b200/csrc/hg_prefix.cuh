@@ -33,6 +33,7 @@
 
 #include "hg_device.cuh"
 #include "hg_partial.cuh"
+#include "hg_ring.h"
 #include "hg_tcgen05.cuh"
 
 namespace hg {
@@ -134,6 +135,7 @@ struct PfxCtl {
     uint8_t stream_bad[2];           // the same for the tile a stream's softmax warps are about to read
     uint16_t members[2][256];        // sequences of the item's rows, in ascending order
     uint32_t group_n[PFX_MAX_GROUPS / 2];      // members per group, two 16-bit numbers a word (a batch has less than 2^16 sequences)
+    int issued[2], q_issued[4];      // tiles, and items' queries, that the loader warps requested (for the unwinding)
 };
 
 template <int D> constexpr size_t pfx_smem_bytes() {
@@ -774,22 +776,26 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) prefix_partial_kernel(const __
         }
     }
     __syncthreads();
-    if (*abort_flag) {
-        if (warp == PFX_K_WARP || warp == PFX_V_WARP) {
-            // unwinding: copies into this CTA's shared memory may still be on their way
-            if (lane == 0) {
-                for (int x = max(0, issued - S); x < issued; ++x) {
-                    int none = 0;
-                    const int seq = 2 * x + (warp == PFX_K_WARP ? 0 : 1);
-                    pfx_wait(&ctl.full[seq % S], (uint32_t)(seq / S) & 1u, &none);
-                }
-                int none = 0;
-                if (edge_open) pfx_wait(&ctl.edge, edges & 1u, &none);
-            }
+    if (*abort_flag) {                                             // (nobody raises it any more: all threads agree)
+        if (lane == 0) {
+            if (warp == PFX_K_WARP || warp == PFX_V_WARP) ctl.issued[warp - PFX_K_WARP] = issued;
+            if (warp >= PFX_Q_WARP) ctl.q_issued[warp - PFX_Q_WARP] = q_issued;
         }
-        if (warp == PFX_Q_WARP && lane == 0 && q_issued > 0) {
+        __syncthreads();
+        // unwinding: copies into this CTA's shared memory may still be on their way.  A warp per slot of the ring and one for
+        // the queries, so that the waits' limits do not add up
+        if (lane == 0) {
             int none = 0;
-            pfx_wait(&ctl.q_full, (uint32_t)(q_issued - 1) & 1u, &none);
+            const int slot = warp < PFX_K_WARP ? warp : warp - 2;      // (the V loader's warp has the edge barrier)
+            if (warp != PFX_K_WARP && warp != PFX_V_WARP && slot < S) {
+                const int n = ring_last_tile(slot, S, ctl.issued[0], ctl.issued[1]);
+                if (n >= 0) pfx_wait(&ctl.full[slot], (uint32_t)(n / S) & 1u, &none);
+            }
+            if (warp == PFX_V_WARP && edge_open) pfx_wait(&ctl.edge, edges & 1u, &none);
+            if (warp == PFX_Q_WARP) {                                  // (the four warps may have stopped an item apart)
+                const int items = max(max(ctl.q_issued[0], ctl.q_issued[1]), max(ctl.q_issued[2], ctl.q_issued[3]));
+                if (items > 0) pfx_wait(&ctl.q_full, (uint32_t)(items - 1) & 1u, &none);
+            }
         }
         if (tid == 0 && p.status) atomicOr(p.status, HG_DEV_WAIT_TIMEOUT);
     }

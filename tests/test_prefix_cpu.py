@@ -101,3 +101,15 @@ def test_suggested_chunks_are_legal():
     for bad in ((-1, 1, 1, 8, 8, 16), (10, 0, 1, 8, 8, 16), (10, 1, -1, 8, 8, 16), (10, 1, 1, 8, 3, 16), (10, 1, 1, 8, 8, 24)):
         with pytest.raises(pkg.HgError):
             pkg.hg_attn_prefix_suggest_chunk(*bad)
+
+
+def test_unwinding_waits_for_the_tiles_on_their_way(tmp_path):
+    """The ring arithmetic of the kernel's unwinding, compiled for the host, against random runs of its loaders."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "ring")
+    subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Werror", "-O1", os.path.join(root, "tests", "c_abi", "ring_unwind.cpp"), "-o", exe,
+                           "-I", os.path.join(root, "paper_2604_18529_b200", "csrc")])
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0 and "ring OK" in run.stdout, run.stderr
