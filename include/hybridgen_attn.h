@@ -517,6 +517,7 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
  *                   negative id are skipped, ids outside the pool too (HG_DEV_BAD_PAGE).  The pairs are copied side by
  *                   side: no page may be a dst twice, or a dst and a src (the lists above never do that).
  * n of hg_kv_release and hg_kv_copy_pages may be 0.
+ * hg_kv_reserve and hg_kv_compact take pools of up to 2^31 - 256 pages.
  */
 hg_status hg_kv_fork(const int32_t* src_row, int32_t* ref_count, int32_t* seq_lens, int32_t* tok_begin, int32_t* tok_end,
                      void* stream, const hg_attn_desc* desc);

@@ -132,7 +132,7 @@ hg_status hg_kv_reserve(const int32_t* seq_lens, const int32_t* n_new, int32_t* 
     if (st != HG_OK) return st;
     if (!seq_lens || !ref_count || !copy_src || !copy_dst || !aligned16(ref_count)) return HG_ERR_INVALID_ARG;
     if (n_ready && (n_ready == n_new || n_ready == seq_lens)) return HG_ERR_INVALID_ARG;       // written while others still read
-    if (desc->batch > RESERVE_MAX_BATCH) return HG_ERR_UNSUPPORTED;
+    if (desc->batch > RESERVE_MAX_BATCH || desc->num_pages > SCAN_MAX_PAGES) return HG_ERR_UNSUPPORTED;
     ReserveParams p;
     p.seq_lens = seq_lens; p.n_new = n_new; p.table = const_cast<int32_t*>(desc->block_table); p.ref = ref_count;
     p.copy_src = copy_src; p.copy_dst = copy_dst; p.copy_rows = copy_rows; p.n_ready = n_ready; p.status = desc->status;
@@ -154,6 +154,7 @@ hg_status hg_kv_compact(int32_t* ref_count, int32_t* remap, int32_t* move_src, i
     hg_status st = check_table(desc);
     if (st != HG_OK) return st;
     if (!ref_count || !remap || !move_src || !move_dst || !n_moves || max_moves < 1 || !aligned16(ref_count)) return HG_ERR_INVALID_ARG;
+    if (desc->num_pages > SCAN_MAX_PAGES) return HG_ERR_UNSUPPORTED;
     const int sms = sm_count();
     if (sms < 1) return HG_ERR_CUDA;
     CompactParams p;

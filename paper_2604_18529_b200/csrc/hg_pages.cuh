@@ -28,7 +28,7 @@ __device__ __forceinline__ void pages_begin() {
 
 __global__ void __launch_bounds__(256) kv_release_kernel(const int32_t* ids, int n, int32_t* ref, int num_pages, int32_t* status) {
     pages_begin();
-    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+    for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < (unsigned)n; i += gridDim.x * 256) {     // (31 bits of entries and a stride)
         const int p = ids[i];
         if (p < 0) continue;
         bool bad = p >= num_pages;
@@ -41,6 +41,8 @@ __global__ void __launch_bounds__(256) kv_release_kernel(const int32_t* ids, int
 
 constexpr int PG_THREADS = 1024;
 constexpr int PG_WARPS = PG_THREADS / 32;
+// The scans go over the counts in groups of 128 whose numbers, one group past the end too, have 31 bits.
+constexpr int SCAN_MAX_PAGES = 0x7fffff00;
 
 // Sum over the 32 lanes of the values of lower lanes.
 __device__ __forceinline__ int warp_exclusive(int v, int lane, int& total) {
@@ -561,7 +563,7 @@ __global__ void __launch_bounds__(PG_THREADS) kv_compact_kernel(const CompactPar
         }
         at += step;
     }
-    for (int i = moves + rank * PG_THREADS + tid; i < p.max_moves; i += CLUSTER * PG_THREADS) {
+    for (unsigned i = moves + rank * PG_THREADS + tid; i < (unsigned)p.max_moves; i += CLUSTER * PG_THREADS) {
         p.move_src[i] = -1;
         p.move_dst[i] = -1;
     }

@@ -160,6 +160,13 @@ def test_fork_refuses_arrays_that_overlap(lib):
         assert lib.hg_kv_fork(*at(**over), None, C.byref(d)) == hg.HG_ERR_INVALID_ARG, over
 
 
+@pytest.mark.parametrize("name", ["hg_kv_reserve", "hg_kv_compact"])
+def test_scans_refuse_pools_whose_last_group_passes_31_bits(lib, name):
+    for n in (2 ** 31 - 255, 2 ** 31 - 1):
+        d = table_desc(num_pages=n)
+        assert CALLS[name](lib, C.byref(d), lambda i: FAKE + (1 << 40) * i) == hg.HG_ERR_UNSUPPORTED, n
+
+
 def test_binding_refuses_host_tensors():
     import torch
     t = torch.zeros(64, dtype=torch.int32)

@@ -419,3 +419,26 @@ def test_attention_directly_behind_table_operations(Hq, Hkv, D, P):
     assert sum(int(t.count_nonzero()) for t in want[:-4]) > 0
     for i, (x, y) in enumerate(zip(got, want)):
         assert torch.equal(x, y), i
+
+
+def test_lists_of_31_bits():
+    """The longest lists that the calls take: every entry is looked at or written, nothing behind them."""
+    n, most = 64, 2 ** 31 - 1
+    p = Pool(2, 3, n, 16, 1, 64)
+    p.load([[5, -1, -1], [9, -1, -1]], [2 if i in (5, 9) else 0 for i in range(n)], [0, 0])
+    ids = torch.full((most,), -1, dtype=torch.int32, device=DEV)
+    ids[most - 1], ids[most - 300000] = 9, 5
+    pkg.hg_kv_release(ids, p.ref, p.desc)
+    assert p.take_status() == 0
+    for e in (5, 9):
+        p.o_ref[e] -= 1
+    p.check("release")
+    lists = [torch.full((most + 1,), 7, dtype=torch.int32, device=DEV) for _ in range(2)]
+    del ids
+    pkg.hg_kv_compact(p.ref, p.remap, lists[0][:most], lists[1][:most], p.n_moves, p.desc)
+    pairs, remap = O.compact(p.o_table, p.o_ref, most)
+    assert int(p.n_moves) == len(pairs) == 2 and p.remap.tolist() == remap
+    p.check("compact")
+    for x, want in zip(lists, zip(*pairs)):
+        assert x[:2].tolist() == list(want) and int(x[most]) == 7
+        assert int(x[2:most].max()) == int(x[2:most].min()) == -1
