@@ -444,7 +444,9 @@ typedef struct hg_prefix_desc {
  * Of desc: batch, heads, head_dim, dtype, the KV addressing, scale, flags and status are used (its chunk fields are not).
  * Accumulation is fp32 and P is carried as a two-term (hi + lo) 16-bit expansion, as in hg_attn_partial: a weight is off
  * by at most 2^-17 of itself with bf16 (with 64 components a third term makes that 2^-24), with fp16 by 2^-22 of itself or
- * 2^-25 of the chunk's largest.
+ * 2^-25 of the chunk's largest.  (hg_attn_partial with one query head per KV head keeps P in fp32.)
+ * q and the K and V rows of the slices must be finite, as in hg_attn_partial: an infinity in V meets both terms of a weight and
+ * may give NaN, and a row of NaN logits counts as empty.  K and V rows outside the slices may hold anything.
  */
 hg_status hg_attn_prefix_partial(const void* q, const void* k_cache, const void* v_cache, float* o_part, float* m_part, float* l_part,
                                  void* stream, const hg_attn_desc* desc, const hg_prefix_desc* prefix);
@@ -493,7 +495,9 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
  *                   tok_begin and tok_end (the last two may be NULL) move with the rows; counts follow the entries.
  *                   One array may be given for several of the three and is moved once (tok_end = seq_lens, say); arrays
  *                   that overlap in part, or that overlap src_row, are refused.
- *                   A value of B or more leaves the row alone and sets HG_DEV_RANGE.
+ *                   A value of B or more leaves the row alone and sets HG_DEV_RANGE.  Tokens that hg_kv_evict has moved to
+ *                   the host are not part of a row: a branch takes its parent's tok_begin and -1 entries, and the caller
+ *                   copies the parent's host rows for it (or gives their partials to both).
  *   hg_kv_reserve   makes positions [seq_lens[b], seq_lens[b] + n_new[b]) of every row writable (n_new: dev int32 [B],
  *                   or NULL for one each; 0 or less: nothing): a slot without a page gets one, a page that others use
  *                   too is replaced by a page of the row's own (copy on write).  Sequences are served as if one after
@@ -516,7 +520,9 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
  *                   dst[i], all heads, K and V, for i < n and, where n_dev (dev) is given, i < *n_dev.  Pairs with a
  *                   negative id are skipped, ids outside the pool too (HG_DEV_BAD_PAGE).  The pairs are copied side by
  *                   side: no page may be a dst twice, or a dst and a src (the lists above never do that).
- * n of hg_kv_release and hg_kv_copy_pages may be 0.
+ * n of hg_kv_release and hg_kv_copy_pages may be 0.  Arrays that a call writes are distinct from its other arrays unless said
+ * otherwise above.  hg_kv_fork, hg_kv_reserve and hg_kv_compact of a table must not run beside a three-step eviction of it: let
+ * them wait for the stream of hg_kv_evict_finish.
  * hg_kv_reserve and hg_kv_compact take pools of up to 2^31 - 256 pages.
  */
 hg_status hg_kv_fork(const int32_t* src_row, int32_t* ref_count, int32_t* seq_lens, int32_t* tok_begin, int32_t* tok_end,

@@ -125,9 +125,10 @@ static hg_status run_prefix(const void* q, const void* k, const void* v, float* 
 }
 
 // Whether a step's own slices run as items of the shared launch instead of in hg_attn_partial's: when there are so few that
-// they find SMs of their own.  (4 sequences, 8 KV heads, 512 shared and 32 own tokens: 16.5 us a step instead of 23.0.  An
-// item costs its SM some 4 us whatever it holds, where hg_attn_partial streams the next one meanwhile: with 512 items of
-// 100 tokens the step takes 40 us instead of 33, with 3584 of 500 tokens 187 instead of 150.)
+// they find SMs of their own.  (Steps in a loop.  4 sequences, 8 KV heads, 512 shared and 32 own tokens: 13.1 us instead of 21.2.
+// An item costs its SM some 4 us whatever it holds, where hg_attn_partial streams the next one meanwhile: 64 sequences, 8 heads
+// of 64, 2048 + 100 tokens: 34 us instead of 28; 16 sequences, 56 heads, 16384 + 500: 156 instead of 139; 96 sequences in 12
+// groups, 8 KV heads: 199 instead of 161.)
 static bool own_in_shared_launch(const hg_attn_desc* d) {
     return (int64_t)d->batch * d->num_kv_heads * ((d->num_chunks + 1) / 2) <= 128;
 }
@@ -178,8 +179,8 @@ int32_t hg_attn_prefix_suggest_chunk(int64_t shared_tokens, int32_t num_groups, 
     // the last round is taken to be one item longer than the average.
     // A chunk is not longer than 2560 tokens (1024 where few rows make short ones cheap): the tensor cores cut their sums off
     // where fp32 arithmetic rounds, so a chunk's error grows with its length (measured: 2.3e-9 of the result per token, 1.7e-5
-    // at 7296 tokens), while the merge of the chunks rounds.  (131072 tokens, 32 sequences of 64/8 heads: 212 us a step at 2432
-    // tokens, 214 at 7296; 65536 tokens, 128 sequences: 402 at 1792, 370 at 7296.)
+    // at 7296 tokens), while the merge of the chunks rounds.  (Steps in a loop.  131072 tokens, 32 sequences of 64/8 heads:
+    // 213 us at 2432 tokens, 200 at 7296; 65536 tokens, 128 sequences: 446 at 1792, 418 at 2432, 373 at 7296.)
     const int64_t unit = page_size > PFX_TILE ? page_size / PFX_TILE : 1;
     int64_t tiles = (shared_tokens / num_groups + PFX_TILE - 1) / PFX_TILE;
     if (tiles < 1) tiles = 1;

@@ -5,8 +5,8 @@
 //     S = Q K^T,   m = row max of scale S,   P = e^{scale S - m},   l = row sum of P,   o = P V
 // is what hg_attn_partial computes for one sequence at a time, with K and V read once instead of once per member.
 // Both products run on tcgen05.mma with their accumulators in tensor memory; P is carried as hi + lo 16-bit terms (two
-// products; three for bf16 with 64 components), so the arithmetic is 1.5 times that of a single-term P: up to about 230 rows
-// per KV head the stream of K and V from HBM is the bound, above that the tensor cores.
+// products; three for bf16 with 64 components), so the arithmetic is 1.5 times (twice) that of the formulas: up to about 164 rows
+// per KV head (123) the stream of K and V from HBM is the bound at the measured rates, above that the tensor cores.
 //
 // One CTA per SM, persistent.  It runs two STREAMS, each with 128 rows: a tile of 128 tokens is S (128 x 128 fp32 in
 // tensor memory), turned by the stream's four softmax warps (a thread owns a row) into P in the same columns (32 columns
@@ -21,8 +21,8 @@
 // members; 12-15 gather the query rows.  Every wait is bounded.
 //
 // Bounds, measured (K and V larger than the L2).  128 sequences, 64/8 heads of 128, 65 536 tokens, bf16, chunks of 2432: 316 us,
-// 1.25 of the products' time at the measured 1613 TFLOP/s; a tile takes 4100 cycles where its products (2 of S, 4 of P V)
-// take 3100: a stream's S - row - weights - P V chain is longer than that, and the other stream covers only a part of it (the
+// 1.24 of the time of its products at the measured 1613 TFLOP/s (1.85 of the formulas', without lo terms); a tile takes 4100
+// cycles where its products (2 of S, 4 of P V) take 3100: a stream's S - row - weights - P V chain is longer than that, and the other stream covers only a part of it (the
 // exponentials of both need 2048 cycles of the special-function units).  32 sequences, 131 072 tokens: 176 us.  16
 // sequences, 56/56 heads, 16 384 tokens (16 rows a KV head): 87 us for 470 MB, 5.4 TB/s.  4 sequences, 512 tokens: 9.3 us.
 // Tiles of 64 tokens with two S buffers a stream, so that the next S never waits for P: 361 instead of 316 us.

@@ -263,7 +263,8 @@ class HybridPipeline:
 class HostKvStore:
     """The host tier of the cache: pinned rows ``k``, ``v`` ``[B][capacity][Hkv][D]`` holding, for every sequence,
     its oldest tokens in original order - row i is absolute token i, ``n[b]`` rows valid - i.e. the prefix
-    ``[0, tok_begin[b])`` that the Eviction Engine (Section 4.2) has moved off the GPU."""
+    ``[0, tok_begin[b])`` that the Eviction Engine (Section 4.2) has moved off the GPU.  ``hg_kv_fork`` does not know of
+    them: a caller who branches a row with host tokens copies its rows and ``n`` here too."""
 
     def __init__(self, batch: int, capacity: int, num_kv_heads: int, head_dim: int, dtype: torch.dtype,
                  k_node: Optional[int] = None, v_node: Optional[int] = None):
