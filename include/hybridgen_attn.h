@@ -505,9 +505,10 @@ hg_status hg_attn_decode_shared(const void* q, const void* k_cache, const void* 
  *                   it.  copy_src[b] / copy_dst[b] (dev int32 [B]): the page whose first copy_rows[b] token rows
  *                   (copy_rows may be NULL) have to be copied before the sequence is read or appended to, or -1 - the
  *                   list hg_kv_copy_pages takes.  n_ready[b] (may be NULL): how many of the n_new[b] positions are
- *                   writable (not n_new or seq_lens itself); fewer where the pool ran out of pages (HG_DEV_NO_PAGE; the slot stays as it was), where
- *                   the block-table row ends (HG_DEV_RANGE) or meets an entry outside the pool (HG_DEV_BAD_PAGE), and
- *                   beyond 262144 slots in one call.  Append no more than that.  Batches up to 16384.
+ *                   writable; fewer where the pool ran out of pages (HG_DEV_NO_PAGE; the slot stays as it was), where the
+ *                   block-table row ends (HG_DEV_RANGE) or meets an entry outside the pool (HG_DEV_BAD_PAGE), and beyond
+ *                   262144 slots in one call.  Append no more than that.  Batches up to 16384.  None of the four
+ *                   written arrays may overlap n_new or seq_lens.
  *   hg_kv_release   takes one reference off every page of a list (dev int32 [n]; negative entries are skipped) whose
  *                   block-table entries are gone already - the list hg_kv_evict leaves in freed_pages.  A page listed
  *                   more often than it is held keeps the count 0 and sets HG_DEV_BAD_PAGE.

@@ -131,8 +131,11 @@ hg_status hg_kv_reserve(const int32_t* seq_lens, const int32_t* n_new, int32_t* 
     hg_status st = check_table(desc);
     if (st != HG_OK) return st;
     if (!seq_lens || !ref_count || !copy_src || !copy_dst || !aligned16(ref_count)) return HG_ERR_INVALID_ARG;
-    if (n_ready && (n_ready == n_new || n_ready == seq_lens)) return HG_ERR_INVALID_ARG;       // written while others still read
     if (desc->batch > RESERVE_MAX_BATCH || desc->num_pages > SCAN_MAX_PAGES) return HG_ERR_UNSUPPORTED;
+    const size_t bytes = (size_t)desc->batch * sizeof(int32_t);
+    const int32_t* const written[4] = {n_ready, copy_src, copy_dst, copy_rows};                 // while others still read these two
+    for (const int32_t* w : written)
+        if (overlap(w, n_new, bytes) || overlap(w, seq_lens, bytes)) return HG_ERR_INVALID_ARG;
     ReserveParams p;
     p.seq_lens = seq_lens; p.n_new = n_new; p.table = const_cast<int32_t*>(desc->block_table); p.ref = ref_count;
     p.copy_src = copy_src; p.copy_dst = copy_dst; p.copy_rows = copy_rows; p.n_ready = n_ready; p.status = desc->status;

@@ -160,6 +160,15 @@ def test_fork_refuses_arrays_that_overlap(lib):
         assert lib.hg_kv_fork(*at(**over), None, C.byref(d)) == hg.HG_ERR_INVALID_ARG, over
 
 
+def test_reserve_refuses_to_write_what_it_reads(lib):
+    d = table_desc(batch=64)
+    for i in (2, 3, 9, 10):                                         # copy_src, copy_dst, copy_rows, n_ready
+        for j in (0, 8):                                            # seq_lens, n_new
+            for off in (0, 4, -4, 252, -252):
+                at = lambda x: FAKE + 4096 * (j if x == i else x) + (off if x == i else 0)   # noqa: E731
+                assert CALLS["hg_kv_reserve"](lib, C.byref(d), at) == hg.HG_ERR_INVALID_ARG, (i, j, off)
+
+
 @pytest.mark.parametrize("name", ["hg_kv_reserve", "hg_kv_compact"])
 def test_scans_refuse_pools_whose_last_group_passes_31_bits(lib, name):
     for n in (2 ** 31 - 255, 2 ** 31 - 1):
