@@ -454,6 +454,13 @@ def _here(t: Optional[torch.Tensor], name: str, dtype=None, numel: int = 0) -> O
     return p
 
 
+def _count(t: torch.Tensor, name: str) -> int:
+    """The length of a list, which the C ABI takes as an int32 (ctypes would drop the bits above)."""
+    if t.numel() > 0x7fffffff:
+        raise ValueError(f"{name} has {t.numel()} entries, a call takes 2^31 - 1")
+    return t.numel()
+
+
 def _pool(t: torch.Tensor, name: str) -> int:
     """A KV pool, or a view of one: addressed through the description's strides, so it need not be contiguous."""
     if not t.is_cuda:
@@ -585,13 +592,14 @@ def prepare_kv_reserve(seq_lens, n_new, ref_count, copy_src, copy_dst, copy_rows
 
 def hg_kv_release(page_ids, ref_count, desc: HgAttnDesc, stream=None) -> None:
     """One reference less for every page id of the list (negative ones are skipped), as ``hg_kv_evict`` leaves it."""
-    _check(lib().hg_kv_release(_here(page_ids, "page_ids", torch.int32), page_ids.numel(),
+    n = _count(page_ids, "page_ids")
+    _check(lib().hg_kv_release(_here(page_ids, "page_ids", torch.int32), n,
                                _here(ref_count, "ref_count", torch.int32, desc.num_pages), _stream(stream), C.byref(desc)),
            "hg_kv_release")
 
 
 def _kv_compact_args(ref_count, remap, move_src, move_dst, n_moves, desc: HgAttnDesc, stream):
-    n = move_src.numel()
+    n = _count(move_src, "move_src")
     return (_here(ref_count, "ref_count", torch.int32, desc.num_pages), _here(remap, "remap", torch.int32, desc.num_pages),
             _here(move_src, "move_src", torch.int32), _here(move_dst, "move_dst", torch.int32, n), n,
             _here(n_moves, "n_moves", torch.int32, 1), _stream(stream), C.byref(desc))
@@ -610,7 +618,7 @@ def prepare_kv_compact(ref_count, remap, move_src, move_dst, n_moves, desc: HgAt
 
 
 def _kv_copy_pages_args(src, dst, rows, n_pairs, k_cache, v_cache, desc: HgAttnDesc, stream):
-    n = src.numel()
+    n = _count(src, "src")
     return (_here(src, "src", torch.int32), _here(dst, "dst", torch.int32, n), _here(rows, "rows", torch.int32, n), n,
             _here(n_pairs, "n_pairs", torch.int32, 1), _pool(k_cache, "k_cache"), _pool(v_cache, "v_cache"), _stream(stream),
             C.byref(desc))

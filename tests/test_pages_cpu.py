@@ -169,6 +169,16 @@ def test_reserve_refuses_to_write_what_it_reads(lib):
                 assert CALLS["hg_kv_reserve"](lib, C.byref(d), at) == hg.HG_ERR_INVALID_ARG, (i, j, off)
 
 
+def test_binding_refuses_lists_whose_length_passes_31_bits():
+    import torch
+    d, few, many = good_desc(), torch.empty(4, dtype=torch.int32, device="meta"), torch.empty(2 ** 32 + 4, dtype=torch.int32, device="meta")
+    assert hg._count(few, "x") == 4
+    for call in (lambda: hg.hg_kv_release(many, few, d, stream=0), lambda: hg.hg_kv_compact(few, few, many, many, few, d, stream=0),
+                 lambda: hg.hg_kv_copy_pages(many, many, None, None, few, few, d, stream=0)):
+        with pytest.raises(ValueError, match="entries"):
+            call()
+
+
 @pytest.mark.parametrize("name", ["hg_kv_reserve", "hg_kv_compact"])
 def test_scans_refuse_pools_whose_last_group_passes_31_bits(lib, name):
     for n in (2 ** 31 - 255, 2 ** 31 - 1):
