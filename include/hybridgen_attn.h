@@ -537,6 +537,171 @@ hg_status hg_kv_copy_pages(const int32_t* src, const int32_t* dst, const int32_t
                            void* k_cache, void* v_cache, void* stream, const hg_attn_desc* desc);
 
 /*
+ * Several new tokens of a sequence in one step: drafted tokens that the model verifies together (a chain or a tree of
+ * alternatives behind the cache), prompts, or single tokens beside either.  The paper decodes one token a step; these
+ * operators are one step over any number of them, in the order of their use:
+ *     hg_kv_reserve        pages for the new tokens
+ *     hg_kv_slots          which row of the packed tensors is which token, its position and its place in the pool, masks
+ *     hg_kv_append_rope    (each layer) rotary positions; keys and values to their places
+ *     hg_attn_decode_tree  (each layer) attention over the cache and, masked, over the new tokens
+ *     hg_kv_accept         (each layer) the accepted tokens' rows move together behind the cache, the lengths grow
+ * Rows of the packed tensors are tokens, sequence after sequence: sequence b has the rows [cu[b], cu[b + 1]), its token i
+ * the row cu[b] + i.  Token i lies at position seq_lens[b] + i of the block-table row, whatever its depth in a tree;
+ * seq_lens counts the cached tokens only and grows in hg_kv_accept.
+ */
+#define HG_MAX_TREE_NODES 1024 /* new tokens of a sequence that may have a mask */
+
+/*
+ * Rows, positions, places and masks of a step's new tokens.
+ *
+ *   seq_lens  dev int32 [B]    cached tokens (a negative length counts as 0)
+ *   n_new     dev int32 [B]    new tokens of each sequence (0 or less: none), or NULL for one each
+ *   parent    dev int32 [N]    token i's parent in the tree (an earlier token of the same sequence; negative: the end of
+ *             the cache), in packed rows, or NULL: chains (the parent of token i is token i - 1).  A parent that is not
+ *             earlier counts as negative and sets HG_DEV_RANGE.
+ *   num_rows  N: rows of the packed arrays
+ *   cu_new    dev int32 [B + 1] out: first row of every sequence, and the number of rows in use
+ *   tok_seq   dev int32 [N]    out: sequence of the row
+ *   tok_pos   dev int32 [N]    out: its position for rotary embeddings, seq_lens + (number of ancestors among the new tokens)
+ *   tok_slot  dev int64 [N]    out: its place in the pool, page * page_size + row of the page, for position seq_lens + i; -1
+ *             where the block table has no page (HG_DEV_BAD_PAGE) or ends (HG_DEV_RANGE)
+ *   mask      dev uint32 [N][mask_words] out: bit j of row i (word j / 32, bit j % 32) says that token i sees token j of its
+ *             sequence: itself and its ancestors
+ * cu_new is needed, the other outputs may be NULL.  Rows at and beyond cu_new[B] get tok_seq = -1, tok_pos = 0, tok_slot = -1
+ * and no mask bits, so that the step's other calls can run over all N rows.  Where the sequences have more than N tokens
+ * together the last are cut, and with a parent or a mask each sequence is cut at HG_MAX_TREE_NODES and 32 * mask_words tokens
+ * (HG_DEV_RANGE).  Outputs must not overlap each other or the inputs.  Of desc: batch, page_size, num_pages, the block table
+ * and status (a description of the pool that hg_kv_append takes will do).
+ */
+hg_status hg_kv_slots(const int32_t* seq_lens, const int32_t* n_new, const int32_t* parent, int32_t num_rows, int32_t* cu_new,
+                      int32_t* tok_seq, int32_t* tok_pos, int64_t* tok_slot, uint32_t* mask, int32_t mask_words, void* stream,
+                      const hg_attn_desc* desc);
+
+/* Rotary position embeddings (host struct). */
+#define HG_ROPE_HALF 0        /* component i < rot_dim / 2 turns with component i + rot_dim / 2 */
+#define HG_ROPE_INTERLEAVED 1 /* component 2 i turns with component 2 i + 1 */
+#define HG_ROPE_INVERSE 1u    /* flags: turn back (the transpose: what the gradient of a rotated tensor goes through) */
+typedef struct hg_rope_desc {
+    uint32_t struct_size;  /* sizeof(hg_rope_desc) */
+    int32_t num_rows;      /* N: rows of every array below */
+    int32_t rot_dim;       /* the first rot_dim components of a head turn, the others stay; a multiple of 16, at most head_dim */
+    int32_t layout;        /* HG_ROPE_HALF or HG_ROPE_INTERLEAVED */
+    const double* freq;    /* dev [rot_dim / 2], radians per position of every pair (hg_rope_frequencies) */
+    float magnitude;       /* factor on the turned components; 0 means 1 */
+    uint32_t flags;        /* HG_ROPE_INVERSE */
+    int64_t q_stride;      /* elements between rows of q (x); 0 = contiguous.  All strides are multiples of 8 */
+    int64_t q_out_stride;  /* of q_out (y) */
+    int64_t k_stride;      /* of k_new */
+    int64_t v_stride;      /* of v_new */
+} hg_rope_desc;
+
+/*
+ * y = x turned by its row's position: (a, b) -> magnitude (a cos t - b sin t, b cos t + a sin t), t = pos freq[i], in fp32 and
+ * rounded once; angles in 64 bits, so that far positions lose nothing.
+ *   x, y  dev 16-bit [N][num_heads][head_dim], 16-byte aligned; y may be x with the same stride, but not overlap it otherwise
+ *   pos   dev int32 [N]
+ * head_dim in {64, 128}.
+ */
+hg_status hg_rope(const void* x, void* y, const int32_t* pos, int32_t num_heads, int32_t head_dim, int32_t dtype, void* stream,
+                  const hg_rope_desc* rope);
+
+/*
+ * hg_rope of a step's queries and keys, with the keys and values going to their places in the pool.
+ *   q, q_out      dev 16-bit [N][Hq][D]; both NULL: keys and values only.  q_out may be q with the same stride
+ *   k_new, v_new  dev 16-bit [N][Hkv][D]
+ *   pos           dev int32 [N]
+ *   slot          dev int64 [N] (tok_slot of hg_kv_slots): no place twice; a row with a negative one is not stored, one outside
+ *                 the pool neither (HG_DEV_BAD_PAGE).  Their queries are turned all the same
+ *   k_cache, v_cache  dev pools (written)
+ * All 16-byte aligned.  Lengths are not touched.  Of desc: heads, head_dim, dtype, the pool's shape and status.
+ */
+hg_status hg_kv_append_rope(const void* q, const void* k_new, const void* v_new, const int32_t* pos, const int64_t* slot, void* q_out,
+                            void* k_cache, void* v_cache, void* stream, const hg_attn_desc* desc, const hg_rope_desc* rope);
+
+/*
+ * The frequencies freq[i] = theta^(-2 i / rot_dim), i < rot_dim / 2, changed for contexts longer than the one trained on.
+ *   HG_ROPE_SCALE_NONE    as they are
+ *   HG_ROPE_SCALE_LINEAR  freq / factor (positions interpolated)
+ *   HG_ROPE_SCALE_BASE    theta * factor^(rot_dim / (rot_dim - 2)) in place of theta: the fastest stays, the slowest is divided
+ *                         by factor (rot_dim = 2 has only the fastest)
+ *   HG_ROPE_SCALE_TURNS   a pair that makes `high` turns or more in `context` positions stays, one that makes `low` or fewer is
+ *                         divided by factor, between them the two are blended linearly in the number of turns
+ *   HG_ROPE_SCALE_INDEX   the same with a blend that is linear in i, between the indices (rounded outwards, within the rotated part)
+ *                         at which a pair makes `high` and `low` turns; *magnitude = 1 + 0.1 ln(factor)
+ * *magnitude (may be NULL) is 1 otherwise.  freq: HOST double [rot_dim / 2] (out).  No CUDA call is made.
+ */
+#define HG_ROPE_SCALE_NONE 0
+#define HG_ROPE_SCALE_LINEAR 1
+#define HG_ROPE_SCALE_BASE 2
+#define HG_ROPE_SCALE_TURNS 3
+#define HG_ROPE_SCALE_INDEX 4
+typedef struct hg_rope_scaling {
+    uint32_t struct_size;  /* sizeof(hg_rope_scaling) */
+    int32_t kind;          /* HG_ROPE_SCALE_* */
+    double theta;          /* > 1 */
+    double factor;         /* >= 1 (not used by _NONE) */
+    double low, high;      /* 0 < low < high (_TURNS and _INDEX) */
+    double context;        /* positions trained on, > 0 (_TURNS and _INDEX) */
+} hg_rope_scaling;
+hg_status hg_rope_frequencies(int32_t rot_dim, const hg_rope_scaling* scaling, double* freq, float* magnitude);
+
+/* The new tokens of a batch as hg_attn_decode_tree sees them (host struct, dev arrays). */
+typedef struct hg_tree_desc {
+    uint32_t struct_size;     /* sizeof(hg_tree_desc) */
+    int32_t max_nodes;        /* the most new tokens of a sequence, 1 .. HG_MAX_TREE_NODES */
+    int32_t num_rows;         /* N: rows of q, out, lse, mask and the host partials */
+    int32_t mask_words;       /* 32-bit words per row of mask, at least max_nodes / 32 rounded up; not used without a mask */
+    const int32_t* cu_nodes;  /* dev [B + 1], ascending */
+    const uint32_t* mask;     /* dev [N][mask_words] (hg_kv_slots), or NULL: chains, token i sees tokens 0 .. i.  Any bits will
+                                 do: a token need not see itself, and one that sees nothing at all gets out = 0, lse = -inf */
+    int64_t q_stride;         /* elements between rows of q, a multiple of 8; 0 = Hq * D */
+} hg_tree_desc;
+
+/*
+ * One step's attention for the new tokens of every sequence, each over the cached tokens [tok_begin, seq_len) and over those
+ * of the sequence's new tokens that its mask shows, whose keys and values are in the pool already; joined with n_host_src (at
+ * most HG_MAX_MERGE_SRC) sources of partials for tokens that the host holds.  (The paper's step has one new token per sequence
+ * and needs no mask.)  The result is softmax attention over all of them.
+ *
+ *   q          dev 16-bit [N][Hq][D], 16-byte aligned
+ *   seq_lens   dev int32 [B]  cached tokens, without the new ones
+ *   tok_begin  dev int32 [B]  first cached token that the GPU holds (clipped to [0, seq_len]), or NULL for 0
+ *   host_partials  sources as in hg_attn_merge, with rows in the place of sequences: o [N][Hq][nc][D], m and l [N][Hq][nc]
+ *   out        dev 16-bit [N][Hq][D], 16-byte aligned: dtype as desc->dtype (what the next projection takes)
+ *   lse        dev float [N][Hq] (may be NULL)
+ * Rows beyond cu_nodes[B] are neither read nor written.  A sequence with more than max_nodes tokens, or whose rows do not lie
+ * in [0, N), is cut to what fits; positions beyond the block-table row are left out (HG_DEV_RANGE each).  A page that is
+ * needed and not in the pool is left out (HG_DEV_BAD_PAGE).
+ * Logits, softmax statistics and sums are fp32; the weights enter the product with V rounded to desc->dtype (off by at most half
+ * a step, 2^-8 of themselves with bf16 and 2^-11 with fp16, as out itself is), and their sum is that of the unrounded ones.
+ * Cached rows must be finite.  A new token's K and V may hold anything as far as tokens that do not see it are concerned; one
+ * that sees an infinity or a NaN in a V row gets no finite result in that component, and perhaps in none of the head's.
+ * Of desc: batch, heads, head_dim, dtype, the KV addressing, scale, flags and status (its chunk fields are not used);
+ * num_q_heads / num_kv_heads is at most 128.  workspace: dev, 256-byte aligned, hg_attn_tree_workspace_bytes(); its contents need
+ * no preparation; not shared by calls that may overlap on the GPU (captured graphs replayed on different streams among them).
+ */
+hg_status hg_attn_decode_tree(const void* q, const void* k_cache, const void* v_cache, const int32_t* seq_lens,
+                              const int32_t* tok_begin, const hg_partial_src* host_partials, int32_t n_host_src, void* out, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream, const hg_attn_desc* desc,
+                              const hg_tree_desc* tree);
+
+/* Bytes of device workspace hg_attn_decode_tree needs; 0 for an invalid description. */
+size_t hg_attn_tree_workspace_bytes(const hg_attn_desc* desc, const hg_tree_desc* tree);
+
+/*
+ * Keeps the accepted ones of the new tokens: the K and V rows at positions seq_lens[b] + path[b][j] go to seq_lens[b] + j, for
+ * j < n_accept[b], and new_lens[b] = seq_lens[b] + n_accept[b].
+ *   path      dev int32 [B][max_path], ascending (a token's ancestors come before it): the accepted tokens' numbers
+ *   n_accept  dev int32 [B]  how many of the row count (clamped to [0, max_path])
+ *   new_lens  dev int32 [B] (out): seq_lens itself, an array that does not overlap it, or NULL (in all but the last layer, say)
+ * A path ends early where it does not ascend from 0 on or leaves the block-table row (HG_DEV_RANGE), or where a page is
+ * missing (HG_DEV_BAD_PAGE); new_lens counts what was kept.  Pages that other rows use too are written like any (hg_kv_reserve
+ * has replaced them).  max_path is at most HG_MAX_TREE_NODES.
+ */
+hg_status hg_kv_accept(const int32_t* path, const int32_t* n_accept, int32_t max_path, const int32_t* seq_lens, int32_t* new_lens,
+                       void* k_cache, void* v_cache, void* stream, const hg_attn_desc* desc);
+
+/*
  * Evidence kernel, not part of the attention path: streams the same K and V tiles through the
  * same TMA pipeline as hg_attn_partial and folds them into one 32-bit checksum per work item
  * (sink: dev uint32 [B][Hkv][NC]).  Used to measure the read ceiling of the paged access pattern.

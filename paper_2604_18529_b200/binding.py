@@ -29,6 +29,10 @@ HG_STATIC_SCRATCH_BYTES = 8 << 20
 (HG_TUNE_NO_PERSISTENT, HG_TUNE_NO_DYNAMIC, HG_TUNE_NO_PDL, HG_TUNE_NO_MERGE_CLUSTER, HG_TUNE_NO_MERGE_ROWS,
  HG_TUNE_NO_GQA16, HG_TUNE_NO_HOST_DIRECT, HG_TUNE_NO_SPEC_PREFETCH) = 1, 2, 4, 8, 16, 32, 64, 128
 HG_LOGITS_TUNE_WARP_MMA, HG_LOGITS_TUNE_TCGEN05 = 1, 2
+HG_MAX_TREE_NODES = 1024
+HG_ROPE_HALF, HG_ROPE_INTERLEAVED = 0, 1
+HG_ROPE_INVERSE = 1
+(HG_ROPE_SCALE_NONE, HG_ROPE_SCALE_LINEAR, HG_ROPE_SCALE_BASE, HG_ROPE_SCALE_TURNS, HG_ROPE_SCALE_INDEX) = range(5)
 
 
 class HgError(RuntimeError):
@@ -94,6 +98,46 @@ class HgPrefixDesc(C.Structure):
     ]
 
 
+class HgRopeDesc(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32),
+        ("num_rows", C.c_int32),
+        ("rot_dim", C.c_int32),
+        ("layout", C.c_int32),
+        ("freq", C.c_void_p),
+        ("magnitude", C.c_float),
+        ("flags", C.c_uint32),
+        ("q_stride", C.c_int64),
+        ("q_out_stride", C.c_int64),
+        ("k_stride", C.c_int64),
+        ("v_stride", C.c_int64),
+    ]
+
+
+class HgRopeScaling(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32),
+        ("kind", C.c_int32),
+        ("theta", C.c_double),
+        ("factor", C.c_double),
+        ("low", C.c_double),
+        ("high", C.c_double),
+        ("context", C.c_double),
+    ]
+
+
+class HgTreeDesc(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32),
+        ("max_nodes", C.c_int32),
+        ("num_rows", C.c_int32),
+        ("mask_words", C.c_int32),
+        ("cu_nodes", C.c_void_p),
+        ("mask", C.c_void_p),
+        ("q_stride", C.c_int64),
+    ]
+
+
 class HgPartialSrc(C.Structure):
     _fields_ = [("o", C.c_void_p), ("m", C.c_void_p), ("l", C.c_void_p), ("nc", C.c_int32), ("reserved", C.c_int32)]
 
@@ -155,6 +199,21 @@ def lib():
         L.hg_kv_compact.restype = C.c_int
         L.hg_kv_copy_pages.argtypes = [vp] * 3 + [i32] + [vp] * 4 + [C.POINTER(HgAttnDesc)]
         L.hg_kv_copy_pages.restype = C.c_int
+        L.hg_kv_slots.argtypes = [vp] * 3 + [i32] + [vp] * 5 + [i32, vp, C.POINTER(HgAttnDesc)]
+        L.hg_kv_slots.restype = C.c_int
+        L.hg_rope.argtypes = [vp] * 3 + [i32] * 3 + [vp, C.POINTER(HgRopeDesc)]
+        L.hg_rope.restype = C.c_int
+        L.hg_kv_append_rope.argtypes = [vp] * 9 + [C.POINTER(HgAttnDesc), C.POINTER(HgRopeDesc)]
+        L.hg_kv_append_rope.restype = C.c_int
+        L.hg_rope_frequencies.argtypes = [i32, C.POINTER(HgRopeScaling), C.POINTER(C.c_double), C.POINTER(C.c_float)]
+        L.hg_rope_frequencies.restype = C.c_int
+        L.hg_attn_decode_tree.argtypes = [vp] * 5 + [C.POINTER(HgPartialSrc), i32, vp, vp, vp, C.c_size_t, vp, C.POINTER(HgAttnDesc),
+                                                     C.POINTER(HgTreeDesc)]
+        L.hg_attn_decode_tree.restype = C.c_int
+        L.hg_attn_tree_workspace_bytes.argtypes = [C.POINTER(HgAttnDesc), C.POINTER(HgTreeDesc)]
+        L.hg_attn_tree_workspace_bytes.restype = C.c_size_t
+        L.hg_kv_accept.argtypes = [vp, vp, i32] + [vp] * 5 + [C.POINTER(HgAttnDesc)]
+        L.hg_kv_accept.restype = C.c_int
         L.hg_kv_read_probe.argtypes = [vp] * 7 + [C.POINTER(HgAttnDesc)]
         L.hg_kv_read_probe.restype = C.c_int
         L.hg_status_string.argtypes = [C.c_int]
@@ -634,6 +693,225 @@ def prepare_kv_copy_pages(src, dst, rows, n_pairs, k_cache, v_cache, desc: HgAtt
     """``hg_kv_copy_pages`` with its arguments marshalled once (see ``prepare_partial``)."""
     return _prepared(lib().hg_kv_copy_pages, _kv_copy_pages_args(src, dst, rows, n_pairs, k_cache, v_cache, desc, stream),
                      (src, dst, rows, n_pairs, k_cache, v_cache, desc), "hg_kv_copy_pages")
+
+
+def _rows(t: Optional[torch.Tensor], name: str, desc_dtype: int, heads: int, head_dim: int, n: int) -> Tuple[Optional[int], int]:
+    """Pointer and row stride of a packed tensor [N][heads][head_dim] whose rows are contiguous but may lie apart (a part of a
+    fused projection's output)."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, head_dim) or t.shape[0] < n:
+        raise ValueError(f"{name} must be [{n}][{heads}][{head_dim}], got {tuple(t.shape)}")
+    if _DTYPES.get(t.dtype) != desc_dtype:
+        raise ValueError(f"{name} has another type than the description: {t.dtype}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim) or (t.shape[0] > 1 and t.stride(0) < heads * head_dim):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap, got strides {t.stride()}")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _kv_slots_args(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, num_rows, desc: HgAttnDesc, stream):
+    B = desc.batch
+    outputs = [t for t in (tok_seq, tok_pos, tok_slot, mask) if t is not None]
+    if num_rows is None:
+        if not outputs:
+            raise ValueError("num_rows is needed where no row's output is given")
+        num_rows = outputs[0].shape[0]
+    if num_rows > 0x7fffffff:
+        raise ValueError(f"{num_rows} rows, a call takes 2^31 - 1")
+    words = 0 if mask is None else mask.shape[1]
+    return (_here(seq_lens, "seq_lens", torch.int32, B), _here(n_new, "n_new", torch.int32, B),
+            _here(parent, "parent", torch.int32, num_rows), num_rows, _here(cu_new, "cu_new", torch.int32, B + 1),
+            _here(tok_seq, "tok_seq", torch.int32, num_rows), _here(tok_pos, "tok_pos", torch.int32, num_rows),
+            _here(tok_slot, "tok_slot", torch.int64, num_rows), _here(mask, "mask", torch.int32, num_rows * words), words,
+            _stream(stream), C.byref(desc))
+
+
+def hg_kv_slots(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, desc: HgAttnDesc, num_rows: Optional[int] = None,
+                stream=None) -> None:
+    """Rows, positions, places in the pool and masks of a step's new tokens, n_new[b] (None: one) of each sequence; ``parent``
+    (packed, None: chains) makes trees of them.  ``mask`` is int32 [N][words] (bits); rows behind the last token get -1 and 0."""
+    _check(lib().hg_kv_slots(*_kv_slots_args(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, num_rows, desc, stream)),
+           "hg_kv_slots")
+
+
+def prepare_kv_slots(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, desc: HgAttnDesc, num_rows: Optional[int] = None,
+                     stream=None):
+    """``hg_kv_slots`` with its arguments marshalled once (see ``prepare_partial``)."""
+    return _prepared(lib().hg_kv_slots,
+                     _kv_slots_args(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, num_rows, desc, stream),
+                     (seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, desc), "hg_kv_slots")
+
+
+_ROPE_LAYOUTS = {"half": HG_ROPE_HALF, "interleaved": HG_ROPE_INTERLEAVED}
+_ROPE_SCALES = {"none": HG_ROPE_SCALE_NONE, "linear": HG_ROPE_SCALE_LINEAR, "base": HG_ROPE_SCALE_BASE, "turns": HG_ROPE_SCALE_TURNS,
+                "index": HG_ROPE_SCALE_INDEX}
+
+
+def hg_rope_frequencies(rot_dim: int, theta: float = 10000.0, scale: str = "none", factor: float = 1.0, low: float = 1.0,
+                        high: float = 32.0, context: float = 0.0) -> Tuple[torch.Tensor, float]:
+    """Radians per position (float64 [rot_dim / 2], on the host) and the magnitude of a rotary embedding; ``scale`` is "none",
+    "linear", "base", "turns" or "index" (``HG_ROPE_SCALE_*``)."""
+    s = HgRopeScaling()
+    s.struct_size = C.sizeof(HgRopeScaling)
+    s.kind, s.theta, s.factor, s.low, s.high, s.context = _ROPE_SCALES[scale], theta, factor, low, high, context
+    freq, magnitude = torch.empty(max(1, rot_dim // 2), dtype=torch.float64), C.c_float(0)
+    _check(lib().hg_rope_frequencies(rot_dim, C.byref(s), C.cast(freq.data_ptr(), C.POINTER(C.c_double)), C.byref(magnitude)),
+           "hg_rope_frequencies")
+    return freq, float(magnitude.value)
+
+
+def rope_desc(*, rot_dim: int, freq: torch.Tensor, layout: str = "half", magnitude: float = 1.0, inverse: bool = False) -> HgRopeDesc:
+    """Fill an ``hg_rope_desc`` (``freq``: float64 CUDA [rot_dim / 2], kept alive); rows and strides come from the call's tensors."""
+    d = HgRopeDesc()
+    d.struct_size = C.sizeof(HgRopeDesc)
+    d.rot_dim, d.layout, d.magnitude = rot_dim, _ROPE_LAYOUTS[layout], magnitude
+    d.freq = _dev(freq, "freq", torch.float64)
+    if freq.numel() < rot_dim // 2:
+        raise ValueError(f"freq has {freq.numel()} elements, {rot_dim // 2} are needed")
+    d.flags = HG_ROPE_INVERSE if inverse else 0
+    d._keep = (freq,)
+    return d
+
+
+def _rope_rows(rope: HgRopeDesc, n: int, **strides) -> HgRopeDesc:
+    """The description with a call's own rows and strides."""
+    if n > 0x7fffffff:
+        raise ValueError(f"{n} rows, a call takes 2^31 - 1")
+    _here(rope._keep[0], "freq")
+    d = HgRopeDesc.from_buffer_copy(rope)
+    d.num_rows = n
+    for name, stride in strides.items():
+        setattr(d, name, stride)
+    return d
+
+
+def _rope_args(x, y, pos, rope: HgRopeDesc, stream):
+    n, heads, D = x.shape
+    dtype = _DTYPES.get(x.dtype, -1)
+    px, sx = _rows(x, "x", dtype, heads, D, n)
+    py, sy = _rows(y, "y", dtype, heads, D, n)
+    d = _rope_rows(rope, n, q_stride=sx, q_out_stride=sy)
+    return (px, py, _here(pos, "pos", torch.int32, n), heads, D, dtype, _stream(stream), C.byref(d)), d
+
+
+def hg_rope(x, y, pos, rope: HgRopeDesc, stream=None) -> None:
+    """y = x [N][heads][D] turned by its rows' positions (``rope_desc(inverse=True)``: turned back, the gradient's way)."""
+    args, _ = _rope_args(x, y, pos, rope, stream)
+    _check(lib().hg_rope(*args), "hg_rope")
+
+
+def prepare_rope(x, y, pos, rope: HgRopeDesc, stream=None):
+    """``hg_rope`` with its arguments marshalled once (see ``prepare_partial``)."""
+    args, d = _rope_args(x, y, pos, rope, stream)
+    return _prepared(lib().hg_rope, args, (x, y, pos, rope, d), "hg_rope")
+
+
+def _kv_append_rope_args(q, k_new, v_new, pos, slot, q_out, k_cache, v_cache, desc: HgAttnDesc, rope: HgRopeDesc, stream):
+    n, D, dtype = k_new.shape[0], desc.head_dim, desc.dtype
+    pq, sq = _rows(q, "q", dtype, desc.num_q_heads, D, n)
+    po, so = _rows(q_out, "q_out", dtype, desc.num_q_heads, D, n)
+    pk, sk = _rows(k_new, "k_new", dtype, desc.num_kv_heads, D, n)
+    pv, sv = _rows(v_new, "v_new", dtype, desc.num_kv_heads, D, n)
+    d = _rope_rows(rope, n, q_stride=sq, q_out_stride=so, k_stride=sk, v_stride=sv)
+    return (pq, pk, pv, _here(pos, "pos", torch.int32, n), _here(slot, "slot", torch.int64, n), po, _pool(k_cache, "k_cache"),
+            _pool(v_cache, "v_cache"), _stream(stream), C.byref(desc), C.byref(d)), d
+
+
+def hg_kv_append_rope(q, k_new, v_new, pos, slot, q_out, k_cache, v_cache, desc: HgAttnDesc, rope: HgRopeDesc, stream=None) -> None:
+    """Rotary positions of a step's queries (q to q_out, which may be q; None: no queries) and keys; keys and values go to their
+    places ``slot`` in the pool (a negative one: nowhere)."""
+    args, _ = _kv_append_rope_args(q, k_new, v_new, pos, slot, q_out, k_cache, v_cache, desc, rope, stream)
+    _check(lib().hg_kv_append_rope(*args), "hg_kv_append_rope")
+
+
+def prepare_kv_append_rope(q, k_new, v_new, pos, slot, q_out, k_cache, v_cache, desc: HgAttnDesc, rope: HgRopeDesc, stream=None):
+    """``hg_kv_append_rope`` with its arguments marshalled once (see ``prepare_partial``)."""
+    args, d = _kv_append_rope_args(q, k_new, v_new, pos, slot, q_out, k_cache, v_cache, desc, rope, stream)
+    return _prepared(lib().hg_kv_append_rope, args, (q, k_new, v_new, pos, slot, q_out, k_cache, v_cache, desc, rope, d), "hg_kv_append_rope")
+
+
+def tree_desc(*, cu_nodes: torch.Tensor, max_nodes: int, num_rows: int, mask: Optional[torch.Tensor] = None) -> HgTreeDesc:
+    """Fill an ``hg_tree_desc``: ``cu_nodes`` (int32 CUDA [B + 1]) and ``mask`` (int32 CUDA [num_rows][words], bits; None: chains) are
+    kept alive by the returned object."""
+    d = HgTreeDesc()
+    d.struct_size = C.sizeof(HgTreeDesc)
+    d.max_nodes, d.num_rows = max_nodes, num_rows
+    d.cu_nodes = _dev(cu_nodes, "cu_nodes", torch.int32)
+    d.mask = _dev(mask, "mask", torch.int32)
+    if mask is not None:
+        if mask.dim() != 2 or mask.shape[0] < num_rows:
+            raise ValueError(f"mask must be [{num_rows}][words], got {tuple(mask.shape)}")
+        d.mask_words = mask.shape[1]
+    d._keep = (cu_nodes, mask)
+    return d
+
+
+def hg_attn_tree_workspace_bytes(desc: HgAttnDesc, tree: HgTreeDesc) -> int:
+    n = int(lib().hg_attn_tree_workspace_bytes(C.byref(desc), C.byref(tree)))
+    if n == 0:
+        raise HgError(HG_ERR_INVALID_ARG, "hg_attn_tree_workspace_bytes")
+    return n
+
+
+def _decode_tree_args(q, k_cache, v_cache, seq_lens, tok_begin, partials, out, lse, workspace, desc: HgAttnDesc, tree: HgTreeDesc, stream):
+    B, N = desc.batch, tree.num_rows
+    _here(tree._keep[0], "cu_nodes", None, B + 1)
+    _here(tree._keep[1], "mask")
+    pq, sq = _rows(q, "q", desc.dtype, desc.num_q_heads, desc.head_dim, N)
+    if _DTYPES.get(out.dtype) != desc.dtype:
+        raise ValueError(f"out has another type than the description: {out.dtype}")
+    for o, m, _ in partials:
+        if m.numel() < N * desc.num_q_heads * m.shape[-1] or o.shape[-1] != desc.head_dim:
+            raise ValueError("partial source shapes must be o [N][Hq][nc][D], m and l [N][Hq][nc]")
+        _here(o, "partial o")
+    arr = _src_array(partials, host=False)
+    d = HgTreeDesc.from_buffer_copy(tree)
+    d.q_stride = sq
+    return (pq, _pool(k_cache, "k_cache"), _pool(v_cache, "v_cache"), _here(seq_lens, "seq_lens", torch.int32, B),
+            _here(tok_begin, "tok_begin", torch.int32, B), arr, len(partials),
+            _here(out, "out", None, N * desc.num_q_heads * desc.head_dim), _here(lse, "lse", torch.float32, N * desc.num_q_heads),
+            _here(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream), C.byref(desc), C.byref(d)), d
+
+
+def hg_attn_decode_tree(q, k_cache, v_cache, seq_lens, tok_begin, host_partials, out, lse, workspace, desc: HgAttnDesc, tree: HgTreeDesc,
+                        stream=None) -> None:
+    """Attention of a step's new tokens q [N][Hq][D] over the cached tokens [tok_begin, seq_lens) (None: from 0), over those new ones
+    that their mask shows, and over ``host_partials`` (o [N][Hq][nc][D], m and l [N][Hq][nc]); out is 16-bit like q."""
+    args, _ = _decode_tree_args(q, k_cache, v_cache, seq_lens, tok_begin, host_partials, out, lse, workspace, desc, tree, stream)
+    _check(lib().hg_attn_decode_tree(*args), "hg_attn_decode_tree")
+
+
+def prepare_decode_tree(q, k_cache, v_cache, seq_lens, tok_begin, host_partials, out, lse, workspace, desc: HgAttnDesc, tree: HgTreeDesc,
+                        stream=None):
+    """``hg_attn_decode_tree`` with its arguments marshalled once (see ``prepare_partial``)."""
+    args, d = _decode_tree_args(q, k_cache, v_cache, seq_lens, tok_begin, host_partials, out, lse, workspace, desc, tree, stream)
+    keep = (q, k_cache, v_cache, seq_lens, tok_begin, host_partials, out, lse, workspace, desc, tree, d)
+    return _prepared(lib().hg_attn_decode_tree, args, keep, "hg_attn_decode_tree")
+
+
+def _kv_accept_args(path, n_accept, seq_lens, new_lens, k_cache, v_cache, desc: HgAttnDesc, stream):
+    B = desc.batch
+    if path.dim() != 2:
+        raise ValueError(f"path must be [B][max_path], got {tuple(path.shape)}")
+    return (_here(path, "path", torch.int32, B * path.shape[1]), _here(n_accept, "n_accept", torch.int32, B), path.shape[1],
+            _here(seq_lens, "seq_lens", torch.int32, B), _here(new_lens, "new_lens", torch.int32, B), _pool(k_cache, "k_cache"),
+            _pool(v_cache, "v_cache"), _stream(stream), C.byref(desc))
+
+
+def hg_kv_accept(path, n_accept, seq_lens, new_lens, k_cache, v_cache, desc: HgAttnDesc, stream=None) -> None:
+    """The K and V rows of the accepted new tokens path[b][:n_accept[b]] move together behind the cache; new_lens (seq_lens itself,
+    another array or None) gets the grown lengths."""
+    _check(lib().hg_kv_accept(*_kv_accept_args(path, n_accept, seq_lens, new_lens, k_cache, v_cache, desc, stream)), "hg_kv_accept")
+
+
+def prepare_kv_accept(path, n_accept, seq_lens, new_lens, k_cache, v_cache, desc: HgAttnDesc, stream=None):
+    """``hg_kv_accept`` with its arguments marshalled once (see ``prepare_partial``)."""
+    return _prepared(lib().hg_kv_accept, _kv_accept_args(path, n_accept, seq_lens, new_lens, k_cache, v_cache, desc, stream),
+                     (path, n_accept, seq_lens, new_lens, k_cache, v_cache, desc), "hg_kv_accept")
 
 
 def hg_kv_read_probe(k_cache, v_cache, seq_lens, tok_begin, tok_end, sink, desc: HgAttnDesc, stream=None) -> None:
