@@ -84,6 +84,12 @@ __device__ __forceinline__ uint64_t l2_evict_first_policy() {
     return pol;
 }
 
+__device__ __forceinline__ uint64_t l2_evict_normal_policy() {
+    uint64_t pol;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
+    return pol;
+}
+
 // Partials are scratch that the merge reads back within microseconds and the next step overwrites in place: stores
 // and loads of them ask the L2 to keep their lines while K and V stream through (which ask to be evicted first), so
 // that they neither go out to DRAM between the two kernels nor have to be allocated again by the next step.

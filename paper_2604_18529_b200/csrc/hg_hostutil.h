@@ -86,6 +86,27 @@ inline EncodeTiledFn encode_fn() {
     return fn;
 }
 
+// The pool as in hg_attn_partial, {d within a 64-element half, token in page, half, head, page}, but ONE half a box: the
+// tensor cores want the token rows of a tile's half at one stride, whatever the page size.
+inline hg_status make_tile_maps(const hg_attn_desc* d, const void* k, const void* v, int tile, CUtensorMap* tk, CUtensorMap* tv) {
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return HG_ERR_CUDA;
+    cuuint64_t dims[5] = {64, (cuuint64_t)d->page_size, (cuuint64_t)(d->head_dim / 64), (cuuint64_t)d->num_kv_heads, (cuuint64_t)d->num_pages};
+    cuuint64_t strides[4] = {(cuuint64_t)d->tok_stride * 2u, 128u, (cuuint64_t)d->head_stride * 2u, (cuuint64_t)d->page_stride * 2u};
+    if (d->num_kv_heads == 1) strides[2] = strides[0];     // unused dimensions still need a legal stride
+    if (d->num_pages == 1) strides[3] = strides[0];
+    cuuint32_t box[5] = {64, (cuuint32_t)(d->page_size < tile ? d->page_size : tile), 1, 1, 1};
+    cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    const CUtensorMapDataType dt = d->dtype == HG_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const void* base[2] = {k, v};
+    CUtensorMap* out[2] = {tk, tv};
+    for (int i = 0; i < 2; ++i)
+        if (enc(out[i], dt, 5, const_cast<void*>(base[i]), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return HG_ERR_UNSUPPORTED;   // a stride pattern the TMA unit cannot express
+    return HG_OK;
+}
+
 // The optional tuning fields (all defaults when the caller's struct ends before them).
 struct Tune {
     uint32_t bits;

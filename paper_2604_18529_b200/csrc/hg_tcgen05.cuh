@@ -132,4 +132,36 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// A whole 32-byte sector.
+__device__ __forceinline__ void st_global_hint8(float* addr, const float (&v)[8], uint64_t policy) {
+    asm volatile("st.global.L2::cache_hint.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8}, %9;"
+                 ::"l"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "l"(policy)
+                 : "memory");
+}
+template <int N>
+__device__ __forceinline__ float row_max(const float* x) {
+    float m[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) m[c] = fmaxf(x[2 * c], x[2 * c + 1]);
+#pragma unroll
+    for (int u = 8; u < N; u += 8)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) m[c] = max3(m[c], x[u + 2 * c], x[u + 2 * c + 1]);
+    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+}
+// mbar_wait / warp_wait with less code around them: the kernels on tensor memory have some twenty waits, and their roles share
+// the instruction cache.  The limit is counted in clock cycles (2 to 3 s).
+constexpr long long PFX_WAIT_CYCLES = 4000000000ll;
+__device__ __forceinline__ bool pfx_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity))
+        if (*abort_flag || clock64() - t0 > PFX_WAIT_CYCLES) { *abort_flag = 1; return false; }
+    return true;
+}
+__device__ __forceinline__ bool pfx_warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    const bool ok = pfx_wait(bar, parity, abort_flag);
+    return __all_sync(0xffffffffu, ok);
+}
+
 }  // namespace hg

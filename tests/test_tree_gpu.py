@@ -411,6 +411,18 @@ def test_offsets_beyond_32_bits():
     s.check()
 
 
+def test_a_wait_that_runs_out_is_reported():
+    s = Step([500, 90], [6, 40], flags=hg.HG_FLAG_TEST_STALL)
+    s.call()
+    torch.cuda.synchronize()
+    assert int(s.status) & hg.HG_DEV_WAIT_TIMEOUT
+    s.desc.flags = 0
+    s.call()                                                                # skipped while the word is set
+    torch.cuda.synchronize()
+    s.status.zero_()
+    s.check()
+
+
 def test_the_binding_refuses_wrong_tensors():
     s = Step([20], [3])
     ok = dict(q=s.q, out=s.out, lse=s.lse, ws=s.ws, host=[])
