@@ -55,11 +55,11 @@ static TreePlan plan_tree(int head_dim, int ctas) {
     return w;
 }
 
-template <int D, bool BF16>
+template <int D, bool BF16, int ROWS>
 static hg_status launch_tree(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const TreeParams& p, int ctas, cudaStream_t st, bool pdl) {
     static std::atomic<uint64_t> done;                     // a bit per device: the shared-memory opt-in is in force
-    auto kern = tree_kernel<D, BF16>;
-    constexpr size_t smem = tree_smem_bytes<D>();
+    auto kern = tree_kernel<D, BF16, ROWS>;
+    constexpr size_t smem = tree_smem_bytes<D, ROWS>();
     static_assert(smem <= 227 * 1024, "shared memory of one SM");
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return HG_ERR_CUDA; }
@@ -78,6 +78,16 @@ static hg_status launch_tree(const CUtensorMap& tq, const CUtensorMap& tk, const
     cfg.gridDim = dim3((unsigned)ctas, TREE_MERGE_SPLITS); cfg.blockDim = dim3(TREE_MERGE_THREADS); cfg.dynamicSmemBytes = 0;
     if (cudaLaunchKernelEx(&cfg, tree_merge_kernel<D, BF16>, p) != cudaSuccess) { cudaGetLastError(); return HG_ERR_CUDA; }
     return HG_OK;
+}
+
+template <int D, bool BF16>
+static hg_status launch_tree_rows(int rows, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const TreeParams& p, int ctas, cudaStream_t st, bool pdl) {
+    switch (rows) {
+        case 16: return launch_tree<D, BF16, 16>(tq, tk, tv, p, ctas, st, pdl);
+        case 32: return launch_tree<D, BF16, 32>(tq, tk, tv, p, ctas, st, pdl);
+        case 64: return launch_tree<D, BF16, 64>(tq, tk, tv, p, ctas, st, pdl);
+        default: return launch_tree<D, BF16, 0>(tq, tk, tv, p, ctas, st, pdl);
+    }
 }
 
 static int device_sms() {
@@ -119,6 +129,8 @@ hg_status hg_attn_decode_tree(const void* q, const void* k_cache, const void* v_
     if (workspace_bytes < hg_attn_tree_workspace_bytes(desc, tree)) return HG_ERR_WORKSPACE;
     TreeParams p;
     memset(&p, 0, sizeof p);
+    p.v = static_cast<const uint16_t*>(v_cache);
+    p.page_stride = desc->page_stride; p.head_stride = desc->head_stride; p.tok_stride = desc->tok_stride;
     p.block_table = desc->block_table; p.seq_lens = seq_lens; p.tok_begin = tok_begin; p.cu = tree->cu_nodes; p.mask = tree->mask;
     p.out = static_cast<uint16_t*>(out); p.lse = lse; p.status = desc->status;
     p.src.n = n_host_src;
@@ -127,7 +139,8 @@ hg_status hg_attn_decode_tree(const void* q, const void* k_cache, const void* v_
     }
     p.B = desc->batch; p.Hq = desc->num_q_heads; p.Hkv = desc->num_kv_heads; p.G = p.Hq / p.Hkv;
     p.N = tree->num_rows; p.max_nodes = tree->max_nodes; p.words = tree->mask_words;
-    p.nodes = 128 / p.G;
+    const int most = tree->max_nodes < 128 ? tree->max_nodes * p.G : 128, rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 ? 64 : 0;
+    p.nodes = (rows ? rows : 128) / p.G;
     p.page_size = desc->page_size; p.page_shift = ilog2_exact(desc->page_size); p.max_pages = desc->max_pages; p.num_pages = desc->num_pages;
     p.scale = desc->scale > 0.f ? desc->scale : 1.0f / sqrtf((float)desc->head_dim);
     p.div_G = make_fast_div((uint32_t)p.G);
@@ -136,6 +149,7 @@ hg_status hg_attn_decode_tree(const void* q, const void* k_cache, const void* v_
     p.test_stall = (desc->flags & HG_FLAG_TEST_STALL) ? 1 : 0;
     const int sms = device_sms(), ctas = sms < HG_TREE_CTAS ? sms : HG_TREE_CTAS;
     if (sms < 1) return HG_ERR_CUDA;
+    p.inv_ctas = ctas > 1 ? ~0ull / (unsigned)ctas + 1ull : 0ull;      // (one CTA: its stretch begins at 0)
     const TreePlan w = plan_tree(desc->head_dim, HG_TREE_CTAS);
     char* ws = static_cast<char*>(workspace);
     p.ws.cut = reinterpret_cast<TreeCut*>(ws); p.ws.valid = reinterpret_cast<int32_t*>(ws + w.valid);
@@ -147,8 +161,8 @@ hg_status hg_attn_decode_tree(const void* q, const void* k_cache, const void* v_
     if (st != HG_OK) return st;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     const bool bf16 = desc->dtype == HG_DTYPE_BF16, pdl = !desc_tune(desc).off(HG_TUNE_NO_PDL);
-    if (desc->head_dim == 128) return bf16 ? launch_tree<128, true>(tq, tk, tv, p, ctas, cs, pdl) : launch_tree<128, false>(tq, tk, tv, p, ctas, cs, pdl);
-    return bf16 ? launch_tree<64, true>(tq, tk, tv, p, ctas, cs, pdl) : launch_tree<64, false>(tq, tk, tv, p, ctas, cs, pdl);
+    if (desc->head_dim == 128) return bf16 ? launch_tree_rows<128, true>(rows, tq, tk, tv, p, ctas, cs, pdl) : launch_tree_rows<128, false>(rows, tq, tk, tv, p, ctas, cs, pdl);
+    return bf16 ? launch_tree_rows<64, true>(rows, tq, tk, tv, p, ctas, cs, pdl) : launch_tree_rows<64, false>(rows, tq, tk, tv, p, ctas, cs, pdl);
 }
 
 }  // extern "C"

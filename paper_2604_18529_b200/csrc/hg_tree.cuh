@@ -6,21 +6,25 @@
 // with S = -inf where a token is not seen.  K and V are read once for up to 256 rows: below about 120 rows a KV head their stream
 // from HBM is the bound at the measured rates, above that the tensor cores.
 //
-// Both products run on tcgen05.mma with accumulators in tensor memory, two STREAMS of 128 rows per CTA, tiles of 128 tokens: a
-// stream's four softmax warps (a thread owns a row) turn S into P, 16-bit in half of S's columns, the A operand of P V.  P is
-// rounded to the inputs' type: a weight is off by at most half a step, as the result itself is; l is the sum of the unrounded
-// weights.  A UNIT is (sequence, KV head, whole new tokens with up to 256 rows):
-//   wide    more than 128 rows: the streams take 128 rows each and share every K and V tile;
-//   narrow  up to 128 rows: the streams take alternate tiles and are joined at the end, both in the lanes of tensor memory that
-//           the same row has in either.
+// Both products run on tcgen05.mma with accumulators in tensor memory, tiles of 128 tokens in two STREAMS per CTA, each with four
+// softmax warps.  P is rounded to the inputs' type: a weight is off by at most half a step, as the result itself is; l is the sum
+// of the unrounded weights.  Two forms:
+//   many rows (ROWS = 0)   the rows are the products' M: S = Q K^T is 128 x 128, a thread owns a row, P goes back to tensor memory
+//           as the A operand of P V.  A UNIT is (sequence, KV head, whole new tokens with up to 256 rows): wide, more than 128
+//           rows, where the streams take 128 rows each and share every K and V tile; or narrow, up to 128 rows, where the streams
+//           take alternate tiles.
+//   few rows (ROWS = 16, 32, 64: the most of a unit)   the tokens are M: S^T = K Q^T is 128 x ROWS, a thread owns a token, so the
+//           exponentials are ROWS a tile and thread instead of 128 whatever the number of rows; P^T goes to shared memory as the
+//           B operand of O^T = V^T P^T.  All units are narrow.
+// A narrow unit's streams are joined at its end, both in the lanes of tensor memory that the same row (component) has in either.
 //
 // Work is dealt by cost: the units' tiles stand in a row, and each of the persistent CTAs (one per SM) takes an equal stretch of
 // it.  So long and short sequences balance by themselves; a CTA finishes the units that lie wholly in its stretch, the host's
 // partials included, and leaves softmax partials of the at most two that its ends cut, which tree_merge_kernel joins.
 //
-// Roles: warps 0-7 softmax and epilogue; 8 and 9 load K and V tiles (TMA, a ring of tiles that alternates the two); 10 issues the
-// products; 11 finds the CTA's stretch, publishes its pieces and loads the queries (TMA, a box of G heads by whole tokens).
-// Every wait is bounded.
+// Roles: warps 0-7 softmax and epilogue; 8 and 9 load K and V tiles (TMA, a ring each; one warp for both would leave free slots
+// waiting behind taken ones: 204 instead of 168 us at one new token, 8 sequences, 64/8 heads, 32 768 tokens); 10 issues the products; 11 finds the CTA's stretch, publishes its pieces up to four ahead and loads their queries (TMA,
+// a box of G heads by whole tokens).  Every wait is bounded.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -28,7 +32,6 @@
 
 #include "hg_device.cuh"
 #include "hg_partial.cuh"
-#include "hg_ring.h"
 #include "hg_tcgen05.cuh"
 
 namespace hg {
@@ -36,15 +39,22 @@ namespace hg {
 constexpr int TREE_TILE = 128;                // tokens per tile, rows per stream
 constexpr int TREE_THREADS = 384;
 constexpr int TREE_K_WARP = 8, TREE_V_WARP = 9, TREE_MMA_WARP = 10, TREE_ITEM_WARP = 11;
-constexpr int TREE_REGS_SOFTMAX = 208, TREE_REGS_OTHER = 72;   // of the 384 x 168 of the launch
-constexpr int TREE_MAX_SLOTS = 10;
-constexpr uint32_t TREE_S_COL = 0, TREE_O_COL = 256;           // tensor memory: S of the streams, 128 columns each, then their O
-constexpr uint32_t TREE_P_COL = 384;                           // ... and with 64 components P beside them, 64 columns each
-// Costs of a unit and of its tiles, for the dealing: what starting a unit takes, a tile for two streams and for one.
-constexpr int TREE_COST_UNIT = 6, TREE_COST_WIDE = 4, TREE_COST_NARROW = 3;
+constexpr int TREE_REGS_SOFTMAX = 200, TREE_REGS_OTHER = 96;   // (many rows) of the 384 x 168 of the launch
+constexpr int TREE_ITEMS = 4;                 // pieces published ahead
+// Costs for the dealing: a tile, and a unit on top of its tiles (start, first tile, end).  Measured at 2, 4, 6, 8, 12 and 16 tiles a
+// unit: 16 sequences, 56 heads, 5 new tokens, up to 16 384 tokens: 310 (2), 285 us (from 4 on); 48 sequences, 32/8 heads, up to
+// 32 and 16 384: 299 (2 to 6), 302, 305, 309; 128 sequences, 8 heads of 64, 2 and 1 500: 70, 62, 63, 63, 65, 64.
+constexpr int TREE_COST_TILE = 4, TREE_COST_UNIT = 16;
 
 template <int D> __host__ __device__ constexpr int tree_tile_bytes() { return TREE_TILE * D * 2; }
-template <int D> __host__ __device__ constexpr int tree_slots() { return D == 128 ? 5 : 10; }
+// Ring slots for K and V tiles: what shared memory has room for.  K and V have rings of their own: the S products run ahead of the
+// P V products, so that in a common ring a slot's use before the last might be unfinished when its next one is waited for, and a
+// barrier's parity does not tell the two apart.
+template <int D, int ROWS> __host__ __device__ constexpr int tree_k_slots() { return D == 128 ? (ROWS == 16 || ROWS == 32 ? 3 : 2) : ROWS == 64 ? 5 : 6; }
+template <int D, int ROWS> __host__ __device__ constexpr int tree_v_slots() { return D == 128 ? 3 : 6; }
+// Queries of a stream (two buffers), weights of a stream (two buffers; many rows have them in tensor memory).
+template <int D, int ROWS> __host__ __device__ constexpr int tree_q_bytes() { return (ROWS ? ROWS : TREE_TILE) * D * 2; }
+template <int ROWS> __host__ __device__ constexpr int tree_p_bytes() { return ROWS * TREE_TILE * 2; }
 
 struct TreeSources {
     const float* o[HG_MAX_MERGE_SRC];
@@ -67,6 +77,8 @@ struct TreeWorkspace {
 
 struct TreeParams {
     const int32_t* block_table;      // [B][max_pages], or NULL: identity paging
+    const uint16_t* v;               // (for the look at single rows)
+    int64_t page_stride, head_stride, tok_stride;
     const int32_t* seq_lens;
     const int32_t* tok_begin;        // or NULL
     const int32_t* cu;
@@ -77,11 +89,12 @@ struct TreeParams {
     TreeWorkspace ws;
     TreeSources src;
     int B, Hq, Hkv, G, N, max_nodes, words;
-    int nodes;                       // new tokens of a stream's rows: 128 / G
+    int nodes;                       // new tokens of a stream's rows: 128 (ROWS) / G
     int page_size, page_shift, max_pages, num_pages;
     int reread, test_stall;          // reread: several units of a KV head read the same tiles
     float scale, scale_log2;
     FastDiv div_G;
+    uint64_t inv_ctas;               // 2^64 / CTAs, rounded up
 };
 
 // What a sequence has to do.
@@ -104,23 +117,27 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
     s.narrow = rest > 0 && rest <= p.nodes ? rest : 0;
     return s;
 }
-__device__ __forceinline__ long long tree_unit_cost(const TreeSeq& s, bool wide) {
-    return TREE_COST_UNIT + (long long)s.tiles * (wide ? TREE_COST_WIDE : TREE_COST_NARROW);
+__device__ __forceinline__ long long tree_cost(const TreeSeq& s) { return TREE_COST_UNIT + (long long)s.tiles * TREE_COST_TILE; }   // of a unit
+__device__ __forceinline__ long long tree_head_cost(const TreeSeq& s) { return (s.wides + (s.narrow ? 1 : 0)) * tree_cost(s); }
+// Quotients of numbers that nearly always have 32 bits.
+__device__ __forceinline__ long long tree_div(long long a, long long b) {
+    return ((unsigned long long)(a | b) >> 32) ? a / b : (long long)((uint32_t)a / (uint32_t)b);
 }
-__device__ __forceinline__ long long tree_head_cost(const TreeSeq& s) {
-    return s.wides * tree_unit_cost(s, true) + (s.narrow ? tree_unit_cost(s, false) : 0);
+// Where the stretch of CTA c begins: floor(total c / ctas), by a product (inv_ctas = 2^64 / ctas rounded up: exact below 2^56).
+__device__ __forceinline__ long long tree_stretch(const TreeParams& p, long long total, int c) {
+    return (long long)__umul64hi((unsigned long long)total * (unsigned)c, p.inv_ctas);
 }
-// Where the stretch of CTA c of n begins; the CTA that a place belongs to.
-__device__ __forceinline__ long long tree_stretch(long long total, int c, int n) { return total / n * c + total % n * c / n; }
-__device__ __forceinline__ int tree_cta_of(long long place, long long total, int n) {
-    int c = (int)min((long long)n - 1, (long long)((double)place / (double)total * n));
-    while (c > 0 && tree_stretch(total, c, n) > place) --c;
-    while (c + 1 < n && tree_stretch(total, c + 1, n) <= place) ++c;
+// The CTA that a place belongs to.
+__device__ __forceinline__ int tree_cta_of(const TreeParams& p, long long place, long long total, int ctas) {
+    int c = (int)min((long long)ctas - 1, (long long)((double)place / (double)total * ctas));
+    while (c > 0 && tree_stretch(p, total, c) > place) --c;
+    while (c + 1 < ctas && tree_stretch(p, total, c + 1) <= place) ++c;
     return c;
 }
-// A unit's tile t stands at TREE_COST_UNIT + t * cost behind the unit's begin; how many stand in front of a place.
-__device__ __forceinline__ int tree_tiles_before(long long place, int cost, int tiles) {
-    return place <= TREE_COST_UNIT ? 0 : (int)min((long long)tiles, (place - TREE_COST_UNIT + cost - 1) / cost);
+// A unit's tile t stands at TREE_COST_UNIT + t * TREE_COST_TILE behind the unit's begin; how many stand in front of a place in it.
+__device__ __forceinline__ int tree_tiles_before(int place, int tiles) {
+    const int x = place - TREE_COST_UNIT;
+    return x <= 0 ? 0 : min(tiles, (x + TREE_COST_TILE - 1) / TREE_COST_TILE);
 }
 
 // Which new tokens 32 w .. 32 w + 31 token i (packed row `row`) sees.
@@ -138,63 +155,151 @@ struct TreeItem {
     int n, len, lo, hi;              // the sequence's new tokens, position of the first, tokens in the pool
     int first, tiles;                // first token of the first tile, tiles
     int whole, slot;                 // all of the unit's tiles, else where the partials go
+    int q;                           // buffer of the queries (wide: both)
 };
 
+template <int D, int ROWS>
 struct TreeCtl {
-    uint64_t full[TREE_MAX_SLOTS], empty[TREE_MAX_SLOTS];
+    static constexpr int S = tree_k_slots<D, ROWS>() + tree_v_slots<D, ROWS>();
+    uint64_t full[S], empty[S];      // K slots, then V slots
     uint64_t s_full[2], s_read[2], p_free[2], p_full[2][4], o_full[2];   // p_full: the quarters of a tile's tokens
-    uint64_t edge, q_full, q_free, drain;
-    uint64_t join_sync[4];           // the two warps that share 32 rows of a narrow unit
-    uint64_t item_full[2], item_empty[2];
-    TreeItem item[2];
+    uint64_t q_full[2], q_free[2], drain;
+    uint64_t join_sync[4];           // the warps that join a narrow unit's streams
+    uint64_t vote[2];                // (few rows) a stream's warps
+    uint64_t item_full[TREE_ITEMS], item_empty[TREE_ITEMS];
+    TreeItem item[TREE_ITEMS];
+    int poisoned[TREE_ITEMS];        // something in the V rows of the item's new tokens is not finite
     uint32_t tmem;
     int abort;
     uint8_t bad[16];                 // per tile, in load order: 16-token pieces of the tile whose page was refused
     uint8_t stream_bad[2];           // the same for the tile a stream's softmax warps are about to read
-    uint32_t poison[2][HG_MAX_TREE_NODES / 32];    // new tokens of an item with something not finite in their V rows
-    float2 join[2][TREE_TILE];       // per stream, rows' reference and sum (narrow)
+    int moved[3][2];                 // (few rows) in turns: the last tile, counted, in which a stream's references had to move
+    // many rows: per stream, rows' reference and sum.  Few rows: per stream, rows' references as the exponents' summand, and, in
+    // turns, the maxima of a tile as ordered integers
+    union __align__(16) {
+        float2 join[2][ROWS ? 1 : TREE_TILE];
+        struct { float off[2][ROWS ? ROWS : 1]; uint32_t top[3][2][ROWS ? ROWS : 1]; } col;
+    };
     long long part[4];
     long long start_base;
     int start_b;
-    int issued[2], q_issued, edge_open;      // tiles, items' queries and edge tiles that were requested (for the unwinding)
+    int issued[2], q_issued[2];      // tiles of K and V, and items' queries by buffer, that were requested (for the unwinding)
 };
 
-template <int D> constexpr size_t tree_smem_bytes() { return (size_t)(2 + tree_slots<D>()) * tree_tile_bytes<D>() + sizeof(TreeCtl); }
+template <int D, int ROWS> constexpr size_t tree_smem_bytes() {
+    return (size_t)TreeCtl<D, ROWS>::S * tree_tile_bytes<D>() + 2 * tree_q_bytes<D, ROWS>() + 2 * tree_p_bytes<ROWS>() + sizeof(TreeCtl<D, ROWS>);
+}
 
 // Tiles of a stream; number of its tile i in load order.
 __device__ __forceinline__ int tree_stream_tiles(const TreeItem& it, int s) { return it.wide ? it.tiles : (it.tiles + 1 - s) / 2; }
 __device__ __forceinline__ int tree_tile_index(const TreeItem& it, int s, int i) { return it.wide ? i : 2 * i + s; }
 
+// Eight 16-bit numbers: bits 15 or 31 of the result tell that one of them is not finite (all exponent bits set).
 template <bool BF16>
-__device__ __forceinline__ bool not_finite(uint4 x) {
-    constexpr uint32_t E = BF16 ? 0x7f807f80u : 0x7c007c00u;
-    bool any = false;
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int u = 0; u < 4; ++u) any = any || (w[u] & E & 0xffffu) == (E & 0xffffu) || (w[u] & E & 0xffff0000u) == (E & 0xffff0000u);
-    return any;
+__device__ __forceinline__ uint32_t not_finite(uint4 x) {
+    constexpr uint32_t ONE = BF16 ? 0x00800080u : 0x04000400u;     // carries out of the exponent exactly then
+    return ((x.x & 0x7fff7fffu) + ONE) | ((x.y & 0x7fff7fffu) + ONE) | ((x.z & 0x7fff7fffu) + ONE) | ((x.w & 0x7fff7fffu) + ONE);
 }
 
+// Whether a row sees a new token, among the piece's, with something in its V row that is not finite.  (Looked at only where one
+// has been met.)
 template <int D, bool BF16>
+__device__ __forceinline__ bool tree_poisoned(const TreeParams& p, const TreeItem& it, int row, int node) {
+    const int first = max(it.first - it.len, 0), last = min(min(it.hi, it.first + it.tiles * TREE_TILE) - it.len, it.n);
+#pragma unroll 1
+    for (int j = first; j < last; ++j) {
+        if (!((tree_word(p, row, node, j >> 5) >> (j & 31)) & 1u)) continue;
+        const int t = it.len + j;
+        const size_t e = (size_t)it.b * p.max_pages + (t >> p.page_shift);
+        const long long page = p.block_table ? p.block_table[e] : (long long)e;
+        if (page < 0 || page >= p.num_pages) continue;
+        const uint4* const v = reinterpret_cast<const uint4*>(p.v + page * p.page_stride + it.h * p.head_stride + (t & (p.page_size - 1)) * p.tok_stride);
+        for (int c = 0; c < D / 8; ++c)
+            if (not_finite<BF16>(v[c]) & 0x80008000u) return true;
+    }
+    return false;
+}
+
+// Floats as integers of the same order (NaN aside); 0 is below all of them.
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+
+// N values a lane, over the lanes that differ in the bits of N - 1: lane i gets the maximum (sum) of value i mod N.
+template <int N, bool MAX>
+__device__ __forceinline__ float lanes_fold(const float* x, int lane) {
+    if constexpr (N == 1) return x[0];
+    else {
+        constexpr int H = N / 2;
+        float v[H];
+        const bool up = lane & H;
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+            const float keep = up ? x[i + H] : x[i], give = up ? x[i] : x[i + H], got = __shfl_xor_sync(0xffffffffu, give, H);
+            v[i] = MAX ? fmaxf(keep, got) : keep + got;
+        }
+        return lanes_fold<H, MAX>(v, lane);
+    }
+}
+// ... over all 32 lanes.
+template <int N, bool MAX>
+__device__ __forceinline__ float across_lanes(const float* x, int lane) {
+    float r = lanes_fold<N, MAX>(x, lane);
+    if constexpr (N == 16) {
+        const float got = __shfl_xor_sync(0xffffffffu, r, 16);
+        r = MAX ? fmaxf(r, got) : r + got;
+    }
+    return r;
+}
+
+// What the host's partials make of a row's own (m, l): the maximum of all, the sum of weights.  Returns the factor on the row's own.
+__device__ __forceinline__ float tree_join_host(const TreeParams& p, size_t orow, float m, float& l, float& top) {
+    constexpr float LOG2E = 1.4426950408889634f;
+    const float none = __int_as_float(0xff800000);
+    top = m;
+    for (int x = 0; x < p.src.n; ++x)
+        for (int c = 0; c < p.src.nc[x]; ++c) top = fmaxf(top, p.src.m[x][orow * p.src.nc[x] + c]);
+    const float own = m == none ? 0.f : fast_exp2((m - top) * LOG2E);
+    l *= own;
+    for (int x = 0; x < p.src.n; ++x)
+        for (int c = 0; c < p.src.nc[x]; ++c) {
+            const float hm = p.src.m[x][orow * p.src.nc[x] + c];
+            if (hm != none) l += p.src.l[x][orow * p.src.nc[x] + c] * fast_exp2((hm - top) * LOG2E);
+        }
+    return own;
+}
+
+template <int D, bool BF16, int ROWS>
 __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                                                                const __grid_constant__ CUtensorMap tmV, const __grid_constant__ TreeParams p) {
-    constexpr int S = tree_slots<D>();
-    constexpr int TILE_BYTES = tree_tile_bytes<D>();
+    constexpr bool FEW = ROWS > 0;
+    constexpr int KS = tree_k_slots<D, ROWS>(), VS = tree_v_slots<D, ROWS>(), S = KS + VS;
+    constexpr int TILE_BYTES = tree_tile_bytes<D>(), Q_BYTES = tree_q_bytes<D, ROWS>(), P_BYTES = tree_p_bytes<ROWS>();
     constexpr int HALVES = D / 64;
-    constexpr uint32_t HALF_BYTES = TREE_TILE * 128;
+    constexpr uint32_t HALF_BYTES = TREE_TILE * 128, Q_HALF_BYTES = Q_BYTES / HALVES;
     constexpr uint32_t FMT = BF16 ? 1u : 0u;
-    // instruction descriptors: fp32 accumulator, 16-bit A and B, M = 128; S: both K-major, N = 128 tokens; O: B (V) with
-    // its components contiguous (N-major), N = D
-    constexpr uint32_t IDESC_S = (1u << 4) | (FMT << 7) | (FMT << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
-    constexpr uint32_t IDESC_O = (1u << 4) | (FMT << 7) | (FMT << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
-    // with 64 components tensor memory has room for P beside S: the next S is computed while the weights of this one are
-    constexpr bool BESIDE = D == 64;
-    constexpr uint32_t P_COL = BESIDE ? TREE_P_COL : TREE_S_COL, P_STRIDE = BESIDE ? 64 : 128, O_STRIDE = BESIDE ? 64 : 128;
+    // instruction descriptors: fp32 accumulator, 16-bit A and B.  Many rows: M = 128; S: both K-major, N = 128 tokens; O: B (V)
+    // with its components contiguous (N-major), N = D.  Few rows: S^T: both K-major, M = 128 tokens, N = ROWS; O^T: A (V) with its
+    // components contiguous (M-major), M = D, and B (P) with a token's rows contiguous (N-major)
+    constexpr uint32_t IDESC = (1u << 4) | (FMT << 7) | (FMT << 10);
+    constexpr uint32_t IDESC_S = IDESC | (((FEW ? (uint32_t)ROWS : 128u) >> 3) << 17) | ((128u >> 4) << 24);
+    constexpr uint32_t IDESC_O = FEW ? IDESC | (1u << 15) | (1u << 16) | (((uint32_t)ROWS >> 3) << 17) | (((uint32_t)D >> 4) << 24)
+                                     : IDESC | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
+    // many rows with 128 components fill tensor memory, and P takes the place of half of S; else P lies beside S, and the next S is
+    // computed while the weights of this one are
+    constexpr bool BESIDE = FEW || D == 64;
+    constexpr uint32_t S_STRIDE = FEW ? ROWS : 128, O_COL = 2 * S_STRIDE, O_STRIDE = FEW ? ROWS : D;
+    constexpr uint32_t P_COL = BESIDE ? 384 : 0, P_STRIDE = BESIDE ? 64 : 128;     // (many rows)
+    constexpr uint32_t TMEM_COLS = FEW ? 4 * ROWS : 512;
     const float NEG_INF = __int_as_float(0xff800000);
 
     extern __shared__ __align__(1024) uint8_t tree_raw[];
-    uint8_t* const ring = tree_raw + 2 * TILE_BYTES;               // Q of the two streams in front
-    TreeCtl& ctl = *reinterpret_cast<TreeCtl*>(tree_raw + (2 + S) * TILE_BYTES);
+    uint8_t* const q_smem = tree_raw;
+    uint8_t* const p_smem = tree_raw + 2 * Q_BYTES;
+    uint8_t* const ring = p_smem + 2 * P_BYTES;
+    TreeCtl<D, ROWS>& ctl = *reinterpret_cast<TreeCtl<D, ROWS>*>(ring + S * TILE_BYTES);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int* const abort_flag = &ctl.abort;
 
@@ -209,19 +314,21 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
             mbar_init(&ctl.p_free[s], 1);
             for (int c = 0; c < 4; ++c) mbar_init(&ctl.p_full[s][c], 4);
             mbar_init(&ctl.o_full[s], 1);
-            mbar_init(&ctl.item_full[s], 1);
-            mbar_init(&ctl.item_empty[s], 8 + 3);
+            mbar_init(&ctl.q_full[s], 1);
+            mbar_init(&ctl.q_free[s], 1);
+            mbar_init(&ctl.vote[s], 4);
         }
-        for (int i = 0; i < 4; ++i) mbar_init(&ctl.join_sync[i], 2);
-        mbar_init(&ctl.q_full, 1);
-        mbar_init(&ctl.q_free, 1);
+        for (int i = 0; i < TREE_ITEMS; ++i) { mbar_init(&ctl.item_full[i], 1); mbar_init(&ctl.item_empty[i], 8 + 3); }
+        for (int i = 0; i < 4; ++i) mbar_init(&ctl.join_sync[i], FEW ? 8 : 2);
         mbar_init(&ctl.drain, 1);
-        mbar_init(&ctl.edge, 1);
         ctl.abort = 0;
         fence_barrier_init();
     }
+    if (FEW)
+        for (int i = tid; i < 6 * (FEW ? ROWS : 1); i += TREE_THREADS) (&ctl.col.top[0][0][0])[i] = 0;
+    if (tid < 6) (&ctl.moved[0][0])[tid] = 0;
     if (warp == TREE_MMA_WARP) {
-        tmem_alloc(&ctl.tmem, 512);
+        tmem_alloc(&ctl.tmem, TMEM_COLS);
         tmem_relinquish();
     }
     tc_fence_before_sync();
@@ -229,61 +336,63 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
     tc_fence_after_sync();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&ctl.tmem);
 
-    int issued = 0, q_issued = 0;                                  // (loaders) tiles, (item warp) queries requested so far
-    uint32_t edges = 0;                                            // (V loader) tiles that went over the edge barrier
-    bool edge_open = false;                                        // ... and one that is still on its way
+    int issued = 0;                                                // (loader) tiles requested so far
+    uint32_t q_armed[2] = {0, 0};                                  // (item warp) queries requested, by barrier
     cudaTriggerProgrammaticLaunchCompletion();
     auto timed_out = [&]() { return p.status && (*reinterpret_cast<volatile int32_t*>(p.status) & HG_DEV_WAIT_TIMEOUT); };
     if (warp >= 8) {
-      reg_shrink<TREE_REGS_OTHER>();
+      if constexpr (!FEW) reg_shrink<TREE_REGS_OTHER>();
       cudaGridDependencySynchronize();
-      // ---- the sequences' costs, and where this CTA's stretch begins: 128 threads, a run of sequences each ----
       const int me = tid - 256, cta = blockIdx.x, ctas = gridDim.x;
       if (me < 2) p.ws.valid[2 * cta + me] = 0;
       if (me == 2) p.ws.cut[cta].nodes = 0;
-      if (me == 3) ctl.start_b = -1;
-      const int run = (p.B + 127) / 128, b_first = min(p.B, me * run), b_last = min(p.B, b_first + run);
-      long long mine = 0;
-      bool trouble = false;
-      for (int b = b_first; b < b_last; ++b) {
-          const TreeSeq s = tree_seq(p, b);
-          mine += tree_head_cost(s) * p.Hkv;
-          trouble = trouble || s.bad;
-      }
-      if (trouble && cta == 0 && p.status) atomicOr(p.status, HG_DEV_RANGE);
-      long long upto = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-          const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-          if (lane >= o) upto += y;
-      }
-      if (lane == 31) ctl.part[warp - 8] = upto;
-      asm volatile("bar.sync 1, 128;" ::: "memory");
       long long total = 0;
-      for (int w = 0; w < 4; ++w) {
-          if (w < warp - 8) upto += ctl.part[w];
-          total += ctl.part[w];
-      }
-      const long long from = tree_stretch(total, cta, ctas), to = tree_stretch(total, cta + 1, ctas);
-      if (from < to && from >= upto - mine && from < upto) {
-          long long base = upto - mine;
+      if (p.B > 32) {
+          // ---- the sequences' costs, and where this CTA's stretch begins: 128 threads, a run of sequences each.  (The item warp
+          // alone does it where its lanes have room for all sequences) ----
+          if (me == 3) ctl.start_b = -1;
+          const int run = (p.B + 127) / 128, b_first = min(p.B, me * run), b_last = min(p.B, b_first + run);
+          long long mine = 0;
+          bool trouble = false;
           for (int b = b_first; b < b_last; ++b) {
-              const long long cost = tree_head_cost(tree_seq(p, b)) * p.Hkv;
-              if (from < base + cost) { ctl.start_b = b; ctl.start_base = base; break; }
-              base += cost;
+              const TreeSeq s = tree_seq(p, b);
+              mine += tree_head_cost(s) * p.Hkv;
+              trouble = trouble || s.bad;
           }
+          if (trouble && cta == 0 && p.status) atomicOr(p.status, HG_DEV_RANGE);
+          long long upto = mine;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+              const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+              if (lane >= o) upto += y;
+          }
+          if (lane == 31) ctl.part[warp - 8] = upto;
+          asm volatile("bar.sync 1, 128;" ::: "memory");
+          for (int w = 0; w < 4; ++w) {
+              if (w < warp - 8) upto += ctl.part[w];
+              total += ctl.part[w];
+          }
+          const long long from = tree_stretch(p, total, cta);
+          if (from >= upto - mine && from < upto) {
+              long long base = upto - mine;
+              for (int b = b_first; b < b_last; ++b) {
+                  const long long cost = tree_head_cost(tree_seq(p, b)) * p.Hkv;
+                  if (from < base + cost) { ctl.start_b = b; ctl.start_base = base; break; }
+                  base += cost;
+              }
+          }
+          asm volatile("bar.sync 1, 128;" ::: "memory");
       }
-      asm volatile("bar.sync 1, 128;" ::: "memory");
       if (warp == TREE_ITEM_WARP) {
-        // =============================== item warp: the stretch's pieces, one ahead, and their queries ===============================
-        long long at = from, base = ctl.start_base;                // place in the row of tiles; that of the lanes' first sequence
-        int ub = ctl.start_b < 0 ? p.B : ctl.start_b;              // first of the 32 sequences in the lanes
-        // (after an earlier call that ran into its limit there is no work until the caller has cleared the word)
-        if (ub == p.B || __any_sync(0xffffffffu, timed_out())) at = to;
+        // =============================== item warp: the stretch's pieces, some ahead, and their queries ===============================
+        int ub = 0;                                                // first of the 32 sequences in the lanes
+        long long base = 0;                                        // ... its place in the row of tiles
+        if (p.B > 32) { ub = ctl.start_b < 0 ? p.B : ctl.start_b; base = ctl.start_base; }
         TreeSeq sq;
         long long cost = 0, before = 0, block = 0;
         auto load_sequences = [&]() {
             sq.n = 0;
+            sq.bad = false;
             cost = 0;
             if (ub + lane < p.B) {
                 sq = tree_seq(p, ub + lane);
@@ -299,12 +408,22 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
             block = __shfl_sync(0xffffffffu, x, 31);
         };
         load_sequences();
+        if (p.B <= 32) {
+            total = block;
+            if (sq.bad && cta == 0 && p.status) atomicOr(p.status, HG_DEV_RANGE);
+        }
+        long long at = tree_stretch(p, total, cta);                // place in the row of tiles
+        const long long to = cta + 1 < ctas ? tree_stretch(p, total, cta + 1) : total;
+        // (after an earlier call that ran into its limit there is no work until the caller has cleared the word)
+        if (ub == p.B || __any_sync(0xffffffffu, timed_out())) at = to;
         bool ok = true;
-        int k = 0;
+        int last_q = 1;
+        uint32_t q_uses[2] = {0, 0};                               // of the buffers
         const int row_bytes = p.G * p.nodes * 128;                 // a query box
-        while (ok) {
+        for (int k = 0; ok; ++k) {
             TreeItem it;
             it.valid = 0;
+            long long last_place = 0;
             while (at < to) {                                      // the next piece with a tile in it
                 while (at >= base + block && ub < p.B) { base += block; ub += 32; load_sequences(); }
                 if (ub >= p.B) { at = to; break; }
@@ -315,15 +434,14 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                 s.hi = __shfl_sync(0xffffffffu, sq.hi, src); s.tiles = __shfl_sync(0xffffffffu, sq.tiles, src);
                 s.wides = __shfl_sync(0xffffffffu, sq.wides, src); s.narrow = __shfl_sync(0xffffffffu, sq.narrow, src);
                 const long long begin = base + __shfl_sync(0xffffffffu, before, src);
-                const long long head = tree_head_cost(s), wide = tree_unit_cost(s, true);
-                const int h = (int)((at - begin) / head);
+                const long long head = tree_head_cost(s), unit_cost = tree_cost(s);
+                const int h = (int)tree_div(at - begin, head);
                 const long long in_head = (at - begin) - head * h;
-                const int u = (int)min((long long)s.wides, in_head / wide);
+                const int u = s.wides == 0 ? 0 : (int)tree_div(in_head, unit_cost);
                 const bool is_wide = u < s.wides;
-                const long long unit = begin + head * h + wide * u, unit_cost = tree_unit_cost(s, is_wide);
-                const int tile_cost = is_wide ? TREE_COST_WIDE : TREE_COST_NARROW;
-                const int t0 = tree_tiles_before(at - unit, tile_cost, s.tiles);
-                const int t1 = to >= unit + unit_cost ? s.tiles : tree_tiles_before(to - unit, tile_cost, s.tiles);
+                const long long unit = begin + head * h + unit_cost * u;
+                const int t0 = tree_tiles_before((int)(at - unit), s.tiles);
+                const int t1 = to >= unit + unit_cost ? s.tiles : tree_tiles_before((int)(to - unit), s.tiles);
                 at = min(to, unit + unit_cost);
                 if (t0 >= t1) continue;
                 it.valid = 1;
@@ -336,38 +454,45 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                 it.tiles = t1 - t0;
                 it.whole = t0 == 0 && t1 == s.tiles;
                 it.slot = 2 * cta + (t0 == 0 ? 1 : 0);
-                if (!it.whole && lane == 0) {
-                    p.ws.valid[it.slot] = 1;
-                    if (t0 == 0) {
-                        const int last = tree_cta_of(unit + TREE_COST_UNIT + (long long)(s.tiles - 1) * tile_cost, total, ctas);
-                        *reinterpret_cast<int4*>(&p.ws.cut[cta]) = make_int4(it.row0, it.nodes, h, last);
-                    }
-                }
+                it.q = is_wide ? 0 : last_q ^ 1;
+                last_q = is_wide ? 1 : it.q;
+                // (of the unit's last tile, for the merge)
+                last_place = unit + TREE_COST_UNIT + (long long)(s.tiles - 1) * TREE_COST_TILE;
                 break;
             }
-            const int j = k & 1;
-            if (k >= 2) ok = pfx_warp_wait(&ctl.item_empty[j], (uint32_t)((k - 2) >> 1) & 1u, abort_flag);
+            const int j = k % TREE_ITEMS;
+            if (k >= TREE_ITEMS) ok = pfx_warp_wait(&ctl.item_empty[j], (uint32_t)(k / TREE_ITEMS - 1) & 1u, abort_flag);
             if (!ok) break;
             if (lane == 0) {
                 ctl.item[j] = it;
+                ctl.poisoned[j] = 0;
                 mbar_arrive(&ctl.item_full[j]);
             }
             __syncwarp();
             if (!it.valid) break;
-            if (k >= 1) ok = pfx_warp_wait(&ctl.q_free, (uint32_t)(k - 1) & 1u, abort_flag);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (!it.wide && x != it.q) continue;
+                if (ok && q_uses[x] > 0) ok = pfx_warp_wait(&ctl.q_free[x], (q_uses[x] - 1) & 1u, abort_flag);
+                ++q_uses[x];
+            }
             if (!ok) break;
-            if (lane == 0) {
+            if (lane == 0) {                                       // (wide: both buffers, on the first one's barrier)
                 const int boxes = HALVES * (it.wide ? 2 : 1);
-                mbar_arrive_expect_tx(&ctl.q_full, (uint32_t)(boxes * row_bytes));
+                mbar_arrive_expect_tx(&ctl.q_full[it.q], (uint32_t)(boxes * row_bytes));
                 for (int x = 0; x < boxes; ++x) {
                     const int s = x / HALVES, half = x % HALVES;
-                    tma_load_3d(tree_raw + s * TILE_BYTES + half * HALF_BYTES, &tmQ, &ctl.q_full, half * 64, it.h * p.G, it.row0 + s * p.nodes);
+                    tma_load_3d(q_smem + (it.q + s) * Q_BYTES + half * Q_HALF_BYTES, &tmQ, &ctl.q_full[it.q], half * 64, it.h * p.G, it.row0 + s * p.nodes);
                 }
             }
-            q_issued = ++k;
+            if (it.q) ++q_armed[1]; else ++q_armed[0];
+            if (!it.whole && lane == 0) {
+                p.ws.valid[it.slot] = 1;
+                if (it.slot & 1) *reinterpret_cast<int4*>(&p.ws.cut[cta]) = make_int4(it.row0, it.nodes, it.h, tree_cta_of(p, last_place, total, ctas));
+            }
         }
       } else if (warp == TREE_K_WARP || warp == TREE_V_WARP) {
-        // =============================== loaders: K tiles and V tiles, alternately in the ring ===============================
+        // =============================== loaders of K tiles and of V tiles ===============================
         const bool is_k = warp == TREE_K_WARP;
         const CUtensorMap* const tm = is_k ? &tmK : &tmV;
         const uint64_t policy = p.reread ? l2_evict_normal_policy() : l2_evict_first_policy();
@@ -376,73 +501,50 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
         bool ok = true;
         int n = 0;                                                 // tiles of earlier items
         for (int k = 0; ok; ++k) {
-            const int j = k & 1;
-            ok = pfx_warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
+            const int j = k % TREE_ITEMS;
+            ok = pfx_warp_wait(&ctl.item_full[j], (uint32_t)(k / TREE_ITEMS) & 1u, abort_flag);
             if (!ok) break;
             const TreeItem it = ctl.item[j];
-            if (!is_k && it.valid && lane < HG_MAX_TREE_NODES / 32) ctl.poison[j][lane] = 0;
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl.item_empty[j]);
             if (!it.valid) break;
-            // the block-table entry of this lane's box of tile x, as it comes: nothing looks at it before its tile's turn, so the
-            // look-up, two tiles ahead, is not waited for
-            struct Box { int e; bool want; };
-            auto look_up = [&](int x) -> Box {
-                Box v;
-                const int t = it.first + x * TREE_TILE + piece * box_rows;
-                v.want = lane < boxes && x < it.tiles && t < it.hi && t + box_rows > it.lo;
-                v.e = it.b * p.max_pages + (t >> p.page_shift);
-                if (v.want && p.block_table) v.e = p.block_table[(size_t)it.b * p.max_pages + (t >> p.page_shift)];
-                return v;
+            // block-table entries of 32 pages in the lanes, the next 32 on their way (a tile's pages never straddle the two)
+            const int page0 = it.first >> p.page_shift, pages = p.page_size < TREE_TILE ? TREE_TILE >> p.page_shift : 1;
+            auto look_up = [&](int from) {
+                const int pg = from + lane;
+                if (pg > (it.hi - 1) >> p.page_shift || pg < it.lo >> p.page_shift || it.hi <= it.lo) return -1;
+                const long long e = (long long)it.b * p.max_pages + pg;
+                return p.block_table ? p.block_table[e] : (int)e;
             };
-            Box b0 = look_up(0), b1 = look_up(1);
+            int base = page0, now = look_up(base), next = look_up(base + 32);
             for (int x = 0; x < it.tiles; ++x) {
-                const int t_x = it.first + x * TREE_TILE, row = (t_x + piece * box_rows) & (p.page_size - 1);
-                const int e = !b0.want ? -1 : ((uint32_t)b0.e < (uint32_t)p.num_pages ? b0.e : -2);      // -1: not wanted, -2: refused
-                b0 = b1;
-                b1 = look_up(x + 2);
-                const int seq = 2 * (n + x) + (is_k ? 0 : 1), slot = seq % S;
+                const int t_x = it.first + x * TREE_TILE, t_box = t_x + piece * box_rows, row = t_box & (p.page_size - 1);
+                if ((t_x >> p.page_shift) + pages > base + 32) {
+                    base += 32;
+                    now = next;
+                    next = look_up(base + 32);
+                }
+                const int entry = __shfl_sync(0xffffffffu, now, (t_box >> p.page_shift) - base);
+                const bool want = lane < boxes && t_box < it.hi && t_box + box_rows > it.lo;
+                const int e = !want ? -1 : ((uint32_t)entry < (uint32_t)p.num_pages ? entry : -2);      // -1: not wanted, -2: refused
+                const int y = n + x, use = is_k ? y / KS : y / VS, slot = is_k ? y % KS : KS + y % VS;
                 const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, e >= 0)) * (uint32_t)box_rows * 128u;
                 uint32_t bad = 0;
-                if (__any_sync(0xffffffffu, e == -2)) {
+                if (is_k && __any_sync(0xffffffffu, e == -2)) {
                     if (e == -2) {
                         bad = ((1u << (box_rows >> 4)) - 1u) << (piece * (box_rows >> 4));
-                        if (p.status && is_k) atomicOr(p.status, HG_DEV_BAD_PAGE);
+                        if (p.status) atomicOr(p.status, HG_DEV_BAD_PAGE);
                     }
                     bad = __reduce_or_sync(0xffffffffu, bad);
                 }
-                if (seq >= S) ok = pfx_warp_wait(&ctl.empty[slot], (uint32_t)(seq / S - 1) & 1u, abort_flag);
+                if (use > 0) ok = pfx_warp_wait(&ctl.empty[slot], (uint32_t)(use - 1) & 1u, abort_flag);
                 if (!ok || p.test_stall) break;
-                // V rows outside the slice, and of refused pages, hold anything (NaN patterns among it) and meet weights of 0, and
-                // so do rows of new tokens with those that do not see them: such a tile lands on a barrier of its own and is handed
-                // on when those rows are cleared
-                const int c_lo = max(it.lo - t_x, 0), c_hi = min(it.hi - t_x, TREE_TILE), c_new = max(min(it.len - t_x, TREE_TILE), c_lo);
-                const bool edge = !is_k && (c_lo > 0 || c_hi < TREE_TILE || c_new < TREE_TILE || bad);
-                uint64_t* const landed = edge ? &ctl.edge : &ctl.full[slot];
-                uint8_t* const tile = ring + slot * TILE_BYTES;
                 if (lane == 0) {
                     if (is_k) ctl.bad[(n + x) & 15] = (uint8_t)bad;
-                    mbar_arrive_expect_tx(landed, bytes);
+                    mbar_arrive_expect_tx(&ctl.full[slot], bytes);
                 }
-                if (e >= 0) tma_load_5d(tile + half * HALF_BYTES + piece * box_rows * 128, tm, landed, 0, row, half, it.h, e, policy);
-                if (edge) {
-                    ok = pfx_warp_wait(&ctl.edge, edges & 1u, abort_flag);
-                    if (!ok) { edge_open = true; break; }
-                    ++edges;
-                    for (int u = lane; u < TREE_TILE * HALVES * 8; u += 32) {     // whole 128-byte rows: the swizzle does not matter
-                        const int r = (u >> 3) % TREE_TILE, hf = (u >> 3) / TREE_TILE;
-                        const uint32_t a = smem_u32(tile) + hf * HALF_BYTES + r * 128 + (u & 7) * 16;
-                        if (r < c_lo || r >= c_hi || ((bad >> (r >> 4)) & 1u)) sts128_zero(a);
-                        else if (r >= c_new && not_finite<BF16>(lds128(a))) {
-                            const int node = t_x + r - it.len;
-                            atomicOr(&ctl.poison[j][node >> 5], 1u << (node & 31));
-                            sts128_zero(a);
-                        }
-                    }
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&ctl.full[slot]);
-                }
+                __syncwarp();
+                if (e >= 0) tma_load_5d(ring + slot * TILE_BYTES + half * HALF_BYTES + piece * box_rows * 128, tm, &ctl.full[slot], 0, row, half, it.h, e, policy);
                 issued = n + x + 1;
             }
             n += it.tiles;
@@ -453,65 +555,86 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
         if (elect_one()) {
             bool ok = true;
             int n = 0, prev_n = 0;                                 // tiles before this item, and before the previous one
-            uint32_t np[2] = {0, 0}, nsc[2] = {0, 0};              // P tiles taken, S tiles computed per stream
+            uint32_t np[2] = {0, 0}, nsc[2] = {0, 0}, nq[2] = {0, 0};      // P tiles taken, S tiles computed per stream; queries per buffer
             bool held = false;                                     // stream 1's last products of the item before are still to come
             TreeItem it, prev;
-            const uint64_t q_desc = tc_smem_desc(smem_u32(tree_raw), 16u, 1024u, 2u);
+            const uint64_t q_desc = tc_smem_desc(smem_u32(q_smem), 16u, 1024u, 2u);
             const uint64_t k_desc = tc_smem_desc(smem_u32(ring), 16u, 1024u, 2u);
             const uint64_t v_desc = tc_smem_desc(smem_u32(ring), HALF_BYTES, 1024u, 2u);
-            auto scores = [&](int s, int i, bool last) {           // S = Q K^T of a stream's tile
-                const int x = n + tree_tile_index(it, s, i), seq = 2 * x, slot = seq % S;
-                ok = pfx_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
+            const uint64_t p_desc = tc_smem_desc(smem_u32(p_smem), 128u, 2048u, 0u);       // 8 tokens 128 bytes apart, 8 rows 2048
+            auto scores = [&](int s, int i, bool last) {           // S = Q K^T (S^T = K Q^T) of a stream's tile
+                const int x = n + tree_tile_index(it, s, i), slot = x % KS;
+                ok = pfx_wait(&ctl.full[slot], (uint32_t)(x / KS) & 1u, abort_flag);
                 if (BESIDE && ok && nsc[s] > 0) ok = pfx_wait(&ctl.s_read[s], (nsc[s] - 1) & 1u, abort_flag);
                 if (!ok) return;
                 ++nsc[s];
                 ctl.stream_bad[s] = ctl.bad[x & 15];
                 tc_fence_after_sync();
-                const uint64_t a = q_desc + (uint32_t)((it.wide ? s : 0) * (TILE_BYTES >> 4)), b = k_desc + (uint32_t)(slot * (TILE_BYTES >> 4));
-                const uint32_t acc = tmem + TREE_S_COL + s * 128;
+                const uint64_t a = q_desc + (uint32_t)((it.wide ? s : it.q) * (Q_BYTES >> 4)), b = k_desc + (uint32_t)(slot * (TILE_BYTES >> 4));
+                const uint32_t acc = tmem + s * S_STRIDE;
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {              // 16 components: 32 bytes of a 128-byte row, halves apart
-                    const uint32_t off = (uint32_t)((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4;
-                    tc_mma_f16_ss(acc, a + off, b + off, IDESC_S, kk ? 1u : 0u);
+                    const uint32_t off_k = (uint32_t)((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4;
+                    const uint32_t off_q = (uint32_t)((kk >> 2) * Q_HALF_BYTES + (kk & 3) * 32) >> 4;
+                    if constexpr (FEW) tc_mma_f16_ss(acc, b + off_k, a + off_q, IDESC_S, kk ? 1u : 0u);
+                    else tc_mma_f16_ss(acc, a + off_q, b + off_k, IDESC_S, kk ? 1u : 0u);
                 }
                 tc_commit(&ctl.s_full[s]);
                 if (!it.wide || s == 1) tc_commit(&ctl.empty[slot]);
-                if (last) tc_commit(&ctl.q_free);
+                if (last && (it.wide || it.q == 0)) tc_commit(&ctl.q_free[0]);
+                if (last && (it.wide || it.q == 1)) tc_commit(&ctl.q_free[1]);
                 mbar_arrive(&ctl.s_full[s]);
             };
             auto values = [&](const TreeItem& im, int n0, int s, int i) {     // O += P V of a stream's tile, quarter by quarter
-                const int x = n0 + tree_tile_index(im, s, i), seq = 2 * x + 1, slot = seq % S;
-                ok = pfx_wait(&ctl.full[slot], (uint32_t)(seq / S) & 1u, abort_flag);
+                const int x = n0 + tree_tile_index(im, s, i), slot = KS + x % VS;
+                ok = pfx_wait(&ctl.full[slot], (uint32_t)(x / VS) & 1u, abort_flag);
                 const uint64_t b = v_desc + (uint32_t)(slot * (TILE_BYTES >> 4));
-                const uint32_t acc = tmem + TREE_O_COL + s * O_STRIDE, a = tmem + P_COL + s * P_STRIDE;
-#pragma unroll
-                for (int part = 0; part < 4; ++part) {
-                    ok = ok && pfx_wait(&ctl.p_full[s][part], np[s] & 1u, abort_flag);
+                const uint32_t acc = tmem + O_COL + s * O_STRIDE;
+                if constexpr (FEW) {                               // O^T += V^T P^T
+                    const uint64_t w = p_desc + (uint32_t)(s * (P_BYTES >> 4));
+                    ok = ok && pfx_wait(&ctl.p_full[s][0], np[s] & 1u, abort_flag);
                     if (!ok) return;
                     tc_fence_after_sync();
 #pragma unroll
-                    for (int kk = part * 2; kk < part * 2 + 2; ++kk)           // 16 tokens: 8 columns of P
-                        tc_mma_f16_ts(acc, a + kk * 8, b + (uint32_t)(kk * 2048 >> 4), IDESC_O, kk ? 1u : (i ? 1u : 0u));
+                    for (int kk = 0; kk < 8; ++kk)                 // 16 tokens
+                        tc_mma_f16_ss(acc, b + (uint32_t)(kk * 2048 >> 4), w + (uint32_t)(kk * 256 >> 4), IDESC_O, kk ? 1u : (i ? 1u : 0u));
+                } else {
+                    const uint32_t a = tmem + P_COL + s * P_STRIDE;
+#pragma unroll
+                    for (int part = 0; part < 4; ++part) {
+                        ok = ok && pfx_wait(&ctl.p_full[s][part], np[s] & 1u, abort_flag);
+                        if (!ok) return;
+                        tc_fence_after_sync();
+#pragma unroll
+                        for (int kk = part * 2; kk < part * 2 + 2; ++kk)       // 16 tokens: 8 columns of P
+                            tc_mma_f16_ts(acc, a + kk * 8, b + (uint32_t)(kk * 2048 >> 4), IDESC_O, kk ? 1u : (i ? 1u : 0u));
+                    }
                 }
                 ++np[s];
                 if (!im.wide || s == 1) tc_commit(&ctl.empty[slot]);
                 if (BESIDE) tc_commit(&ctl.p_free[s]);
                 if (i == tree_stream_tiles(im, s) - 1) tc_commit(&ctl.o_full[s]);
             };
+            auto release = [&]() {                                 // the held products, where there is nothing to put in front of them
+                if (held) values(prev, prev_n, 1, tree_stream_tiles(prev, 1) - 1);
+                held = false;
+            };
             for (int k = 0; ok; ++k) {
-                const int j = k & 1;
-                ok = pfx_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
+                const int j = k % TREE_ITEMS;
+                if (!mbar_test(&ctl.item_full[j], (uint32_t)(k / TREE_ITEMS) & 1u)) release();
+                ok = ok && pfx_wait(&ctl.item_full[j], (uint32_t)(k / TREE_ITEMS) & 1u, abort_flag);
                 if (!ok) break;
                 it = ctl.item[j];
                 mbar_arrive(&ctl.item_empty[j]);
                 if (!it.valid) break;
-                ok = pfx_wait(&ctl.q_full, (uint32_t)k & 1u, abort_flag);
+                const uint32_t q_parity = (it.q ? nq[1]++ : nq[0]++) & 1u;
+                if (!mbar_test(&ctl.q_full[it.q], q_parity) || !mbar_test(&ctl.full[n % KS], (uint32_t)(n / KS) & 1u)) release();
+                ok = ok && pfx_wait(&ctl.q_full[it.q], q_parity, abort_flag);
                 if (!ok) break;
                 const int n0 = tree_stream_tiles(it, 0), n1 = tree_stream_tiles(it, 1);      // n0 >= n1, n0 >= 1
                 int left = n0 + n1;                                // score products still to issue
                 scores(0, 0, --left == 0);
-                if (ok && held) values(prev, prev_n, 1, tree_stream_tiles(prev, 1) - 1);
-                held = false;
+                if (ok) release();
                 if (ok && n1 > 0) scores(1, 0, --left == 0);
                 for (int i = 0; i < n0 && ok; ++i) {
                     if (BESIDE && i + 1 < n0) scores(0, i + 1, --left == 0);
@@ -527,7 +650,7 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                 prev_n = n;
                 n += it.tiles;
             }
-            if (ok && held) values(prev, prev_n, 1, tree_stream_tiles(prev, 1) - 1);
+            if (ok) release();
             int none = 0;                                          // nothing is in flight when the tensor memory is given back
             tc_commit(&ctl.drain);
             pfx_wait(&ctl.drain, 0u, &none);
@@ -535,259 +658,484 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
         __syncwarp();
       }
     } else {
-        reg_grow<TREE_REGS_SOFTMAX>();
+        if constexpr (!FEW) reg_grow<TREE_REGS_SOFTMAX>();
         // =============================== softmax warps: S -> P, epilogue ===============================
-        const int s = warp >> 2, w4 = warp & 3;                    // stream, quarter of its rows
+        const int s = warp >> 2, w4 = warp & 3;                    // stream, quarter of its lanes
         const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
-        const uint32_t s_tmem = tmem + TREE_S_COL + s * 128 + lanes, p_tmem = tmem + P_COL + s * P_STRIDE + lanes;
-        const uint32_t o_tmem = tmem + TREE_O_COL + s * O_STRIDE + lanes;
-        const int r = w4 * 32 + lane;                              // row of the stream
-        const int r_node = fast_div(r, p.div_G), r_head = r - r_node * p.G;
+        const uint32_t s_tmem = tmem + s * S_STRIDE + lanes, o_tmem = tmem + O_COL + lanes;     // (o_tmem: of stream 0)
+        const int r = w4 * 32 + lane;                              // row of the stream (token of the tile)
         const float sc = p.scale_log2;
         const uint64_t keep = l2_evict_last_policy();
         bool ok = true;
         uint32_t ns = 0, no1 = 0, nj = 0;                          // tiles of this stream, items with tiles of stream 1, joins so far
-        auto join_sync = [&]() {                                   // with the other stream's warp of these rows
+        auto join_sync = [&]() {                                   // with the other warps that join the streams
+            uint64_t* const bar = &ctl.join_sync[FEW ? 0 : w4];
             __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl.join_sync[w4]);
-            return pfx_warp_wait(&ctl.join_sync[w4], nj++ & 1u, abort_flag);
+            if (lane == 0) mbar_arrive(bar);
+            return pfx_warp_wait(bar, nj++ & 1u, abort_flag);
         };
-        // Round -1 runs a tile's code on whatever stands in tensor memory and hands nothing on, before the wait for the
-        // kernel in front of this one: the tile's instructions are in the caches when the first S is there
-        for (int k = -1; ok; ++k) {
-            const int j = k & 1;
-            const bool dry = k < 0;
-            int tiles = 1, tiles1 = 0;
-            bool exists = true;
-            TreeItem it;
-            it.wide = 0; it.first = 0; it.lo = 0; it.hi = it.len = TREE_TILE; it.nodes = p.nodes; it.i0 = it.row0 = 0;      // (of the dry round)
-            if (!dry) {
-                ok = pfx_warp_wait(&ctl.item_full[j], (uint32_t)(k >> 1) & 1u, abort_flag);
-                if (!ok) break;
-                it = ctl.item[j];
-                if (!it.valid) break;
-                tiles = tree_stream_tiles(it, s);
-                tiles1 = tree_stream_tiles(it, 1);
-            }
-            const int at = (it.wide ? s * p.nodes : 0) + r_node;    // this row's new token in the unit
-            exists = r_node < p.nodes && at < it.nodes;
-            const bool live = __any_sync(0xffffffffu, exists);     // some row of this warp exists
-            const int node = it.i0 + at, row = it.row0 + at;
-            float m_true = NEG_INF, m_ref = NEG_INF, l = 0.f;      // the maximum, and the one the weights refer to (raw logits)
-            for (int i = 0; i < tiles; ++i) {
-                if (!dry) {
+        // V rows outside the slice, and of refused pages, hold anything (NaN patterns among it) and meet weights of 0, and so do rows
+        // of new tokens with those that do not see them.  They are cleared before the tile's weights are handed over: thread r looks
+        // at token r.  (Where the streams share a tile both do, and write the same.)
+        auto clear_v = [&](int x, bool clear, bool look, int j) {  // x: the tile's number
+            if (!__any_sync(0xffffffffu, clear || look)) return true;
+            const int slot = KS + x % VS;
+            if (!pfx_warp_wait(&ctl.full[slot], (uint32_t)(x / VS) & 1u, abort_flag)) return false;
+            if (clear || look)
+#pragma unroll 1
+                for (int hf = 0; hf < HALVES; ++hf) {              // whole 128-byte rows: the swizzle does not matter
+                    const uint32_t a = smem_u32(ring) + slot * TILE_BYTES + hf * HALF_BYTES + r * 128;
+                    bool zero = clear;
+                    if (!clear) {
+                        uint32_t found = 0;
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) found |= not_finite<BF16>(lds128(a + ((u + lane) & 7) * 16));
+                        zero = found & 0x80008000u;
+                        if (zero) *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) = 1;
+                    }
+                    if (zero)
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) sts128_zero(a + ((u + lane) & 7) * 16);
+                }
+            fence_proxy_async();
+            return true;
+        };
+        int n = 0;                                                 // tiles of earlier items
+        cudaGridDependencySynchronize();
+        for (int k = 0; ok; ++k) {
+            const int j = k % TREE_ITEMS;
+            ok = pfx_warp_wait(&ctl.item_full[j], (uint32_t)(k / TREE_ITEMS) & 1u, abort_flag);
+            if (!ok) break;
+            const TreeItem it = ctl.item[j];
+            if (!it.valid) break;
+            const int tiles = tree_stream_tiles(it, s), tiles1 = tree_stream_tiles(it, 1);
+            if constexpr (FEW) {
+                // ---- a thread is a token.  Lane i speaks for rows i (and 32 + i) of the unit, their references being the same in
+                // all warps of the stream ----
+                constexpr int V = ROWS == 64 ? 2 : 1, N = ROWS == 16 ? 16 : 32;
+                const int rows = it.nodes * p.G;
+                float ref[V], l[V];                                // of this lane's rows; l: over the warp's tokens
+#pragma unroll
+                for (int v = 0; v < V; ++v) { ref[v] = NEG_INF; l[v] = 0.f; }
+                for (int i = 0; i < tiles; ++i) {
                     ok = pfx_warp_wait(&ctl.s_full[s], ns & 1u, abort_flag);
                     if (!ok) break;
                     ++ns;
-                }
-                tc_fence_after_sync();
-                if (live) {
+                    tc_fence_after_sync();
                     const int t = it.first + tree_tile_index(it, s, i) * TREE_TILE;
-                    const int c_lo = max(it.lo - t, 0), c_hi = min(it.hi - t, TREE_TILE);
-                    const uint32_t bad = dry ? 0u : *reinterpret_cast<volatile uint8_t*>(&ctl.stream_bad[s]);
-                    const bool tail = t + TREE_TILE > it.len, edge = c_lo > 0 || c_hi < TREE_TILE || tail || bad;
-                    float x[TREE_TILE];
+                    const uint32_t bad = *reinterpret_cast<volatile uint8_t*>(&ctl.stream_bad[s]);
+                    float x[ROWS];
+                    if constexpr (ROWS == 16) tmem_ld_32x16(s_tmem, *reinterpret_cast<uint32_t(*)[16]>(&x[0]));
+                    else
 #pragma unroll
-                    for (int c0 = 0; c0 < TREE_TILE; c0 += 32) tmem_ld_32x32(s_tmem + c0, *reinterpret_cast<uint32_t(*)[32]>(&x[c0]));
+                        for (int c0 = 0; c0 < ROWS; c0 += 32) tmem_ld_32x32(s_tmem + c0, *reinterpret_cast<uint32_t(*)[32]>(&x[c0]));
                     tmem_ld_wait();
-                    if (BESIDE) {
-                        tc_fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0 && !dry) mbar_arrive(&ctl.s_read[s]);
-                    }
-                    if (edge) {                                    // columns outside the slice, of refused pages, of tokens not seen
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t out = ((bad >> (2 * c)) & 1u ? 0xffffu : 0u) | ((bad >> (2 * c + 1)) & 1u ? 0xffff0000u : 0u);
-                            const int below = c_lo - c * 32, in = c_hi - c * 32;
-                            out |= below >= 32 ? ~0u : (below > 0 ? (1u << below) - 1u : 0u);
-                            out |= in <= 0 ? ~0u : (in < 32 ? ~0u << in : 0u);
-                            const int d0 = t + c * 32 - it.len;    // the new token at the first of these columns
-                            if (tail && exists && d0 > -32) {
-                                const int w = max(d0, 0) >> 5;
-                                const uint32_t a = tree_word(p, row, node, w);
-                                if (d0 < 0) out |= ~a << -d0;
-                                else out |= ~__funnelshift_r(a, (d0 & 31) ? tree_word(p, row, node, w + 1) : 0u, d0 & 31);
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&ctl.s_read[s]);
+                    if (t < it.lo || t + TREE_TILE > min(it.hi, it.len) || bad) {      // tokens outside the slice, of refused pages, not seen
+                        uint64_t hide = t + r < it.lo || t + r >= it.hi || ((bad >> (r >> 4)) & 1u) ? ~0ull : 0ull;
+                        const int d = t + r - it.len;              // which new token this is
+                        ok = clear_v(n + tree_tile_index(it, s, i), hide != 0, d >= 0, j);
+                        if (!ok) break;
+                        if (d >= 0 && hide == 0) {
+                            if (!p.mask) hide = d * p.G >= 64 ? ~0ull : (1ull << (d * p.G)) - 1ull;      // tokens in front of it
+                            else {
+                                const uint64_t group = p.G >= 64 ? ~0ull : (1ull << p.G) - 1ull;
+                                const uint32_t* const words = p.mask + (size_t)it.row0 * p.words + (d >> 5);
+#pragma unroll 2
+                                for (int u = 0; u < it.nodes; ++u)
+                                    if (!((words[(size_t)u * p.words] >> (d & 31)) & 1u)) hide |= group << (u * p.G);
                             }
-#pragma unroll
-                            for (int u = 0; u < 32; ++u) x[c * 32 + u] = (out >> u) & 1u ? NEG_INF : x[c * 32 + u];
                         }
+#pragma unroll
+                        for (int c = 0; c < ROWS; ++c) x[c] = (hide >> c) & 1u ? NEG_INF : x[c];
                     }
-                    const float mx = row_max<TREE_TILE>(x);
-                    m_true = fmaxf(m_true, mx);
-                    // a row's sums follow its maximum only when that has moved by more than 2^8 (then the weights would leave
-                    // the 16-bit types' comfortable range); the difference is put right at the end.  Each row decides by
-                    // itself, so its result does not depend on its neighbours (rows that do not exist among them)
-                    const bool moved = (m_true - m_ref) * sc > 8.f;
-                    if (BESIDE && !dry && ns > 1) {                // the last tile's weights are used up, and its products in O
+                    // a row's reference moves only when a logit is more than 2^8 above it (then the weights would leave the 16-bit
+                    // types' comfortable range), and at a unit's first tile.  The four warps find out by a vote
+                    float mx[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) mx[v] = across_lanes<N, true>(&x[v * 32], lane);
+                    bool up = i == 0;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) up = up || ((mx[v] - ref[v]) * sc > 8.f && v * 32 + (lane & (N - 1)) < rows);
+                    up = __any_sync(0xffffffffu, up);
+                    const int turn = (int)(ns % 3);
+                    if (up) {
+                        if (lane < N)
+#pragma unroll
+                            for (int v = 0; v < V; ++v) atomicMax(&ctl.col.top[turn][s][v * 32 + lane], ordered(mx[v]));
+                        if (lane == 0) *reinterpret_cast<volatile int*>(&ctl.moved[turn][s]) = (int)ns;
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&ctl.vote[s]);
+                    ok = pfx_warp_wait(&ctl.vote[s], (ns - 1) & 1u, abort_flag);
+                    if (!ok) break;
+                    // the last turn's maxima have been read by all: cleared for the one after the next
+                    if (w4 == 0 && lane < N)
+#pragma unroll
+                        for (int v = 0; v < V; ++v) ctl.col.top[(ns + 2) % 3][s][v * 32 + lane] = 0;
+                    if (ns > 1) {                              // the last tile's weights are used up, and its products in O
                         ok = pfx_warp_wait(&ctl.p_free[s], (ns - 2) & 1u, abort_flag);
                         if (!ok) break;
                         tc_fence_after_sync();
                     }
-                    if (__any_sync(0xffffffffu, moved && exists)) {
-                        const float f = !moved ? 1.f : m_ref == NEG_INF ? 0.f : fast_exp2((m_ref - m_true) * sc);
-                        if (moved) m_ref = m_true;
+                    if (*reinterpret_cast<volatile int*>(&ctl.moved[turn][s]) == (int)ns) {
+                        float f[V];
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            const int c = v * 32 + (lane & (N - 1));
+                            const uint32_t m = *reinterpret_cast<volatile uint32_t*>(&ctl.col.top[turn][s][c]);
+                            const float now = fmaxf(ref[v], m ? unordered(m) : NEG_INF);
+                            f[v] = ref[v] == NEG_INF ? 0.f : fast_exp2((ref[v] - now) * sc);
+                            ref[v] = now;
+                            l[v] *= f[v];
+                            ctl.col.off[s][c] = now == NEG_INF ? NEG_INF : -now * sc;      // (the same from all warps)
+                        }
+                        __syncwarp();
                         if (i > 0) {
-                            l *= f;
 #pragma unroll 1
-                            for (int c0 = 0; c0 < D; c0 += 8) {
+                            for (int c0 = 0; c0 < ROWS; c0 += 8) {
                                 uint32_t y[8];
-                                tmem_ld_32x8(o_tmem + c0, y);
+                                tmem_ld_32x8(o_tmem + s * O_STRIDE + c0, y);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int u = 0; u < 8; ++u) y[u] = __float_as_uint(__uint_as_float(y[u]) * f);
-                                tmem_st_32x8(o_tmem + c0, y);
+                                for (int u = 0; u < 8; ++u)
+                                    y[u] = __float_as_uint(__uint_as_float(y[u]) * __shfl_sync(0xffffffffu, c0 + u < 32 ? f[0] : f[V - 1], (c0 + u) & 31));
+                                tmem_st_32x8(o_tmem + s * O_STRIDE + c0, y);
                             }
+                            tmem_st_wait();
                         }
                     }
-                    const float off = m_ref == NEG_INF ? 0.f : -m_ref * sc;
-                    const float2 sc2 = make_float2(sc, sc), off2 = make_float2(off, off);
-                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                    // a quarter of the tokens at a time; each is handed over when the next one's weights are computed (a store
-                    // into tensor memory takes some 300 cycles to complete while the tensor cores work)
-                    auto hand_over = [&](int c) {
-                        tmem_st_wait();
-                        tc_fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0 && !dry) mbar_arrive(&ctl.p_full[s][c]);
-                    };
+                    const float2 sc2 = make_float2(sc, sc);
+                    uint8_t* const dst = p_smem + s * P_BYTES + r * 16;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t w[16];
+                    for (int c = 0; c < ROWS; c += 8) {
+                        const float4 a = *reinterpret_cast<const float4*>(&ctl.col.off[s][c]), b = *reinterpret_cast<const float4*>(&ctl.col.off[s][c + 4]);
+                        const float2 off[4] = {make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)};
+                        uint32_t w[4];
 #pragma unroll
-                        for (int u = 0; u < 16; ++u) {
-                            float2 e = fma2(make_float2(x[c * 32 + 2 * u], x[c * 32 + 2 * u + 1]), sc2, off2);
+                        for (int u = 0; u < 4; ++u) {
+                            float2 e = fma2(make_float2(x[c + 2 * u], x[c + 2 * u + 1]), sc2, off[u]);
                             e.x = fast_exp2(e.x);
                             e.y = fast_exp2(e.y);
-                            sum[u & 1] = add2(sum[u & 1], e);
+                            x[c + 2 * u] = e.x;
+                            x[c + 2 * u + 1] = e.y;
                             w[u] = pack2<BF16>(e.x, e.y);
                         }
-                        if (c > 0) hand_over(c - 1);
-                        if (!dry) tmem_st_32x16(p_tmem + c * 16, w);
+                        *reinterpret_cast<uint4*>(dst + (c / 8) * 2048) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
-                    hand_over(3);
-                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                } else {
+                    fence_proxy_async();                           // the tensor core reads P through the asynchronous proxy
                     tc_fence_before_sync();
                     __syncwarp();
-                    if (BESIDE && lane == 0) mbar_arrive(&ctl.s_read[s]);
-                    if (BESIDE && ns > 1) ok = pfx_warp_wait(&ctl.p_free[s], (ns - 2) & 1u, abort_flag);
-                    if (!ok) break;
-                    if (lane < 4) mbar_arrive(&ctl.p_full[s][lane]);
+                    if (lane == 0) mbar_arrive(&ctl.p_full[s][0]);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) l[v] += across_lanes<N, false>(&x[v * 32], lane);
                 }
-            }
-            if (dry) {
-                cudaGridDependencySynchronize();
-                continue;
-            }
-            if (!ok) break;
-            // ---- the piece's end.  Stream 0 has a tile always; where the streams share their rows, each takes half of the
-            // components of both streams' sums ----
-            if (it.wide ? s == 0 : true) ok = pfx_warp_wait(&ctl.o_full[0], (uint32_t)k & 1u, abort_flag);
-            if (ok && tiles1 > 0 && (it.wide ? s == 1 : true)) ok = pfx_warp_wait(&ctl.o_full[1], no1 & 1u, abort_flag);
-            if (!ok) break;
-            if (tiles1 > 0) ++no1;
-            tc_fence_after_sync();
-            if (live) {
-                // sums refer to m_ref, at most 2^8 below the maximum: as good a reference as the maximum itself
-                float m_raw = m_ref, f0 = 1.f, f1 = 0.f;           // factors on the two sums
-                bool both = false;
-                uint32_t o0 = o_tmem, o1 = o_tmem;
-                int c_begin = 0, c_end = D;
-                if (!it.wide) {
-                    ctl.join[s][r] = make_float2(m_ref, l);
-                    ok = join_sync();
-                    if (!ok) break;
-                    const float2 other = ctl.join[s ^ 1][r];
-                    m_raw = fmaxf(m_ref, other.x);
-                    const float a = m_ref == NEG_INF ? 0.f : fast_exp2((m_ref - m_raw) * sc), b = other.x == NEG_INF ? 0.f : fast_exp2((other.x - m_raw) * sc);
-                    l = l * a + other.y * b;
-                    f0 = s == 0 ? a : b;
-                    f1 = s == 0 ? b : a;
-                    both = tiles1 > 0;
-                    o0 = tmem + TREE_O_COL + lanes;
-                    o1 = o0 + O_STRIDE;
-                    c_begin = s * (D / 2);
-                    c_end = c_begin + D / 2;
-                } else if (m_ref == NEG_INF) f0 = 0.f;
-                const int head = it.h * p.G + r_head;
-                const size_t orow = (size_t)row * p.Hq + head;
+                if (!ok) break;
+                // ---- the piece's end: each stream takes half of the rows, all of their components ----
+                ok = pfx_warp_wait(&ctl.o_full[0], (uint32_t)k & 1u, abort_flag);
+                if (ok && tiles1 > 0) ok = pfx_warp_wait(&ctl.o_full[1], no1 & 1u, abort_flag);
+                if (!ok) break;
+                if (tiles1 > 0) ++no1;
+                tc_fence_after_sync();
+                float* const sums = reinterpret_cast<float*>(p_smem + s * P_BYTES);      // (the weights there are used up) [4 warps + 1][ROWS]
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    if (lane < N) {
+                        sums[w4 * ROWS + v * 32 + lane] = l[v];
+                        if (w4 == 0) sums[4 * ROWS + v * 32 + lane] = ref[v];
+                    }
+                }
+                ok = join_sync();
+                if (!ok) break;
+                constexpr int H = ROWS / 2;
+                const int c = s * H + (lane & (H - 1)), node = fast_div(c, p.div_G);      // this lane's row
+                const bool exists = c < rows, both = tiles1 > 0;
+                const float* const sums0 = reinterpret_cast<const float*>(p_smem);
+                const float* const sums1 = reinterpret_cast<const float*>(p_smem + P_BYTES);
+                const float ref0 = sums0[4 * ROWS + c], ref1 = sums1[4 * ROWS + c], m_raw = fmaxf(ref0, ref1);
+                float f0 = ref0 == NEG_INF ? 0.f : fast_exp2((ref0 - m_raw) * sc), f1 = ref1 == NEG_INF || !both ? 0.f : fast_exp2((ref1 - m_raw) * sc);
+                float lsum = (sums0[c] + sums0[ROWS + c] + sums0[2 * ROWS + c] + sums0[3 * ROWS + c]) * f0 +
+                             (sums1[c] + sums1[ROWS + c] + sums1[2 * ROWS + c] + sums1[3 * ROWS + c]) * f1;
+                const int row = it.row0 + node;
+                const size_t orow = (size_t)row * p.Hq + it.h * p.G + (c - node * p.G);
+                const size_t prow = (size_t)it.slot * 256 + c;
                 const float m = m_raw == NEG_INF ? NEG_INF : m_raw * p.scale;
-                float top = m;
-                const bool last_word = it.wide || s == 0;          // who writes the row's single numbers
-                // tokens that this row sees and whose V rows are not finite: no finite result
-                if (it.hi > it.len && it.first + it.tiles * TREE_TILE > it.len && exists) {
-                    for (int w = 0; w * 32 < it.n; ++w) {
-                        const uint32_t bad = *reinterpret_cast<volatile uint32_t*>(&ctl.poison[j][w]);
-                        if (bad && (bad & tree_word(p, row, node, w))) { f0 = __int_as_float(0x7fc00000); both = false; }
-                    }
+                if (exists && *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) && tree_poisoned<D, BF16>(p, it, row, it.i0 + node)) {
+                    f0 = __int_as_float(0x7fc00000);
+                    f1 = 0.f;
                 }
-                float scale0 = f0, scale1 = f1, unit = 1.f;
+                float top = m, inv = 1.f;
                 if (it.whole && exists) {
-                    for (int x = 0; x < p.src.n; ++x)
-                        for (int c = 0; c < p.src.nc[x]; ++c) top = fmaxf(top, p.src.m[x][orow * p.src.nc[x] + c]);
-                    unit = m == NEG_INF ? 0.f : fast_exp2((m - top) * 1.4426950408889634f);
-                    l *= unit;
-                    for (int x = 0; x < p.src.n; ++x)
-                        for (int c = 0; c < p.src.nc[x]; ++c) {
-                            const size_t q = orow * p.src.nc[x] + c;
-                            const float hm = p.src.m[x][q];
-                            if (hm != NEG_INF) l += p.src.l[x][q] * fast_exp2((hm - top) * 1.4426950408889634f);
-                        }
-                    if (p.lse && last_word) p.lse[orow] = l == 0.f ? NEG_INF : top + logf(l);
-                    unit = l == 0.f ? 0.f : 1.f / l;
-                    const float mine_f = m == NEG_INF ? 0.f : fast_exp2((m - top) * 1.4426950408889634f);
-                    scale0 = f0 * mine_f * unit;
-                    scale1 = f1 * mine_f * unit;
+                    const float own = tree_join_host(p, orow, m, lsum, top);
+                    inv = lsum == 0.f ? 0.f : 1.f / lsum;
+                    f0 *= own * inv;
+                    f1 *= own * inv;
+                    if (p.lse && w4 == 0 && lane < H) p.lse[orow] = lsum == 0.f ? NEG_INF : top + logf(lsum);
                 }
-                const size_t prow = (size_t)it.slot * 256 + (it.wide ? s * TREE_TILE : 0) + r;
-                if (!it.whole && exists && last_word) { p.ws.m[prow] = m; p.ws.l[prow] = l; }
+                if (!it.whole && exists && w4 == 0 && lane < H) { p.ws.m[prow] = m; p.ws.l[prow] = lsum; }
+                // lane l of tensor memory holds component l of the rows (128 components), or, for M = 64 products, lane 32 w + i
+                // holds component 16 w + i (i < 16; lanes 16-31 of each quarter unused)
+                const int d = D == 128 ? r : w4 * 16 + lane;
+                const bool holds = D == 128 || lane < 16;
+                const int to_row = (int)orow;
 #pragma unroll 1
-                for (int c0 = c_begin; c0 < c_end; c0 += 32) {
-                    float y[32];
-                    tmem_ld_32x32(o0 + c0, *reinterpret_cast<uint32_t(*)[32]>(&y[0]));
+                for (int c0 = 0; c0 < H && s * H + c0 < rows; c0 += 8) {
+                    uint32_t y0[8], y1[8];
+                    tmem_ld_32x8(o_tmem + s * H + c0, y0);
+                    tmem_ld_32x8(o_tmem + (both ? O_STRIDE : 0) + s * H + c0, y1);
                     tmem_ld_wait();
+                    float y[8];
 #pragma unroll
-                    for (int u = 0; u < 32; ++u) y[u] = scale0 == 0.f ? 0.f : y[u] * scale0;
-                    if (both) {
-                        float z[32];
-                        tmem_ld_32x32(o1 + c0, *reinterpret_cast<uint32_t(*)[32]>(&z[0]));
+                    for (int u = 0; u < 8; ++u) {
+                        const float g0 = __shfl_sync(0xffffffffu, f0, c0 + u), g1 = __shfl_sync(0xffffffffu, f1, c0 + u);
+                        y[u] = g0 == 0.f ? 0.f : __uint_as_float(y0[u]) * g0;
+                        if (g1 != 0.f) y[u] = fmaf(__uint_as_float(y1[u]), g1, y[u]);
+                    }
+                    const int left = min(8, rows - s * H - c0);
+                    if (it.whole) {
+                        for (int z = 0; z < p.src.n; ++z)
+#pragma unroll 1
+                            for (int e = 0; e < p.src.nc[z]; ++e) {          // (an empty partial's o row is not read)
+                                float w = 0.f;
+                                if (exists) {
+                                    const float hm = p.src.m[z][orow * p.src.nc[z] + e];
+                                    if (hm != NEG_INF) w = fast_exp2((hm - top) * 1.4426950408889634f) * inv;
+                                }
+#pragma unroll
+                                for (int u = 0; u < 8; ++u) {
+                                    const float wu = __shfl_sync(0xffffffffu, w, c0 + u);
+                                    const size_t q = (size_t)__shfl_sync(0xffffffffu, to_row, c0 + u) * p.src.nc[z] + e;
+                                    if (wu != 0.f && u < left && holds) y[u] = fmaf(p.src.o[z][q * D + d], wu, y[u]);
+                                }
+                            }
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            const size_t q = (size_t)__shfl_sync(0xffffffffu, to_row, c0 + u);
+                            if (u < left && holds) p.out[q * D + d] = (uint16_t)pack2<BF16>(y[u], 0.f);
+                        }
+                    } else {
+                        float* const dst = p.ws.o + ((size_t)it.slot * 256 + s * H + c0) * D + d;
+#pragma unroll
+                        for (int u = 0; u < 8; ++u)
+                            if (u < left && holds) st_global_hint(dst + u * D, y[u], keep);
+                    }
+                }
+                tc_fence_before_sync();
+                ok = join_sync();                                  // both streams' sums are read: either may begin anew
+                if (!ok) break;
+            } else {
+                // ---- a thread is a row ----
+                const uint32_t p_tmem = tmem + P_COL + s * P_STRIDE + lanes;
+                const int r_node = fast_div(r, p.div_G);
+                const int at = (it.wide ? s * p.nodes : 0) + r_node;    // this row's new token in the unit
+                const bool exists = r_node < p.nodes && at < it.nodes;
+                const bool live = __any_sync(0xffffffffu, exists); // some row of this warp exists
+                const int node = it.i0 + at, row = it.row0 + at;
+                float m_true = NEG_INF, m_ref = NEG_INF, l = 0.f;  // the maximum, and the one the weights refer to (raw logits)
+                for (int i = 0; i < tiles; ++i) {
+                    ok = pfx_warp_wait(&ctl.s_full[s], ns & 1u, abort_flag);
+                    if (!ok) break;
+                    ++ns;
+                    tc_fence_after_sync();
+                    if (live) {
+                        const int t = it.first + tree_tile_index(it, s, i) * TREE_TILE;
+                        const int c_lo = max(it.lo - t, 0), c_hi = min(it.hi - t, TREE_TILE);
+                        const uint32_t bad = *reinterpret_cast<volatile uint8_t*>(&ctl.stream_bad[s]);
+                        const bool tail = t + TREE_TILE > it.len, edge = c_lo > 0 || c_hi < TREE_TILE || tail || bad;
+                        float x[TREE_TILE];
+#pragma unroll
+                        for (int c0 = 0; c0 < TREE_TILE; c0 += 32) tmem_ld_32x32(s_tmem + c0, *reinterpret_cast<uint32_t(*)[32]>(&x[c0]));
                         tmem_ld_wait();
+                        if (BESIDE) {
+                            tc_fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&ctl.s_read[s]);
+                        }
+                        if (edge) {                                // columns outside the slice, of refused pages, of tokens not seen
+                            ok = clear_v(n + tree_tile_index(it, s, i), r < c_lo || r >= c_hi || ((bad >> (r >> 4)) & 1u), t + r >= it.len, j);
+                            if (!ok) break;
 #pragma unroll
-                        for (int u = 0; u < 32; ++u) y[u] = scale1 == 0.f ? y[u] : fmaf(z[u], scale1, y[u]);
-                    }
-                    if (!exists) continue;
-                    if (!it.whole) {
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t out = ((bad >> (2 * c)) & 1u ? 0xffffu : 0u) | ((bad >> (2 * c + 1)) & 1u ? 0xffff0000u : 0u);
+                                const int below = c_lo - c * 32, in = c_hi - c * 32;
+                                out |= below >= 32 ? ~0u : (below > 0 ? (1u << below) - 1u : 0u);
+                                out |= in <= 0 ? ~0u : (in < 32 ? ~0u << in : 0u);
+                                const int d0 = t + c * 32 - it.len;    // the new token at the first of these columns
+                                if (tail && exists && d0 > -32) {
+                                    const int w = max(d0, 0) >> 5;
+                                    const uint32_t a = tree_word(p, row, node, w);
+                                    if (d0 < 0) out |= ~a << -d0;
+                                    else out |= ~__funnelshift_r(a, (d0 & 31) ? tree_word(p, row, node, w + 1) : 0u, d0 & 31);
+                                }
 #pragma unroll
-                        for (int u = 0; u < 32; u += 8) st_global_hint8(p.ws.o + prow * D + c0 + u, *reinterpret_cast<const float(*)[8]>(&y[u]), keep);
-                        continue;
-                    }
-                    for (int x = 0; x < p.src.n; ++x)
-                        for (int c = 0; c < p.src.nc[x]; ++c) {
-                            const size_t q = orow * p.src.nc[x] + c;
-                            const float hm = p.src.m[x][q];
-                            if (hm == NEG_INF) continue;           // (its o row is not read)
-                            const float w = fast_exp2((hm - top) * 1.4426950408889634f) * unit;
-                            const float4* const ho = reinterpret_cast<const float4*>(p.src.o[x] + q * D + c0);
-#pragma unroll
-                            for (int u = 0; u < 8; ++u) {
-                                const float4 v = ho[u];
-                                y[4 * u] = fmaf(v.x, w, y[4 * u]); y[4 * u + 1] = fmaf(v.y, w, y[4 * u + 1]);
-                                y[4 * u + 2] = fmaf(v.z, w, y[4 * u + 2]); y[4 * u + 3] = fmaf(v.w, w, y[4 * u + 3]);
+                                for (int u = 0; u < 32; ++u) x[c * 32 + u] = (out >> u) & 1u ? NEG_INF : x[c * 32 + u];
                             }
                         }
-                    uint4* const dst = reinterpret_cast<uint4*>(p.out + orow * D + c0);
+                        const float mx = row_max<TREE_TILE>(x);
+                        m_true = fmaxf(m_true, mx);
+                        // a row's sums follow its maximum only when that has moved by more than 2^8 (then the weights would leave
+                        // the 16-bit types' comfortable range).  Each row decides by itself, so its result does not depend on its
+                        // neighbours (rows that do not exist among them)
+                        const bool moved = (m_true - m_ref) * sc > 8.f;
+                        if (BESIDE && ns > 1) {            // the last tile's weights are used up, and its products in O
+                            ok = pfx_warp_wait(&ctl.p_free[s], (ns - 2) & 1u, abort_flag);
+                            if (!ok) break;
+                            tc_fence_after_sync();
+                        }
+                        if (__any_sync(0xffffffffu, moved && exists)) {
+                            const float f = !moved ? 1.f : m_ref == NEG_INF ? 0.f : fast_exp2((m_ref - m_true) * sc);
+                            if (moved) m_ref = m_true;
+                            if (i > 0) {
+                                l *= f;
+#pragma unroll 1
+                                for (int c0 = 0; c0 < D; c0 += 8) {
+                                    uint32_t y[8];
+                                    tmem_ld_32x8(o_tmem + s * O_STRIDE + c0, y);
+                                    tmem_ld_wait();
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        dst[u] = make_uint4(pack2<BF16>(y[8 * u], y[8 * u + 1]), pack2<BF16>(y[8 * u + 2], y[8 * u + 3]),
-                                            pack2<BF16>(y[8 * u + 4], y[8 * u + 5]), pack2<BF16>(y[8 * u + 6], y[8 * u + 7]));
+                                    for (int u = 0; u < 8; ++u) y[u] = __float_as_uint(__uint_as_float(y[u]) * f);
+                                    tmem_st_32x8(o_tmem + s * O_STRIDE + c0, y);
+                                }
+                            }
+                        }
+                        const float off = m_ref == NEG_INF ? 0.f : -m_ref * sc;
+                        const float2 sc2 = make_float2(sc, sc), off2 = make_float2(off, off);
+                        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                        // a quarter of the tokens at a time; each is handed over when the next one's weights are computed (a store
+                        // into tensor memory takes some 300 cycles to complete while the tensor cores work)
+                        auto hand_over = [&](int c) {
+                            tmem_st_wait();
+                            tc_fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&ctl.p_full[s][c]);
+                        };
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t w[16];
+#pragma unroll
+                            for (int u = 0; u < 16; ++u) {
+                                float2 e = fma2(make_float2(x[c * 32 + 2 * u], x[c * 32 + 2 * u + 1]), sc2, off2);
+                                e.x = fast_exp2(e.x);
+                                e.y = fast_exp2(e.y);
+                                sum[u & 1] = add2(sum[u & 1], e);
+                                w[u] = pack2<BF16>(e.x, e.y);
+                            }
+                            if (c > 0) hand_over(c - 1);
+                            tmem_st_32x16(p_tmem + c * 16, w);
+                        }
+                        hand_over(3);
+                        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                    } else {
+                        const int t = it.first + tree_tile_index(it, s, i) * TREE_TILE;
+                        const uint32_t bad = *reinterpret_cast<volatile uint8_t*>(&ctl.stream_bad[s]);
+                        if (t < it.lo || t + TREE_TILE > min(it.hi, it.len) || bad)
+                            ok = clear_v(n + tree_tile_index(it, s, i), t + r < it.lo || t + r >= it.hi || ((bad >> (r >> 4)) & 1u), t + r >= it.len, j);
+                        if (!ok) break;
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (BESIDE && lane == 0) mbar_arrive(&ctl.s_read[s]);
+                        if (BESIDE && ns > 1) ok = pfx_warp_wait(&ctl.p_free[s], (ns - 2) & 1u, abort_flag);
+                        if (!ok) break;
+                        if (lane < 4) mbar_arrive(&ctl.p_full[s][lane]);
+                    }
                 }
-                if (!it.wide) {                                    // both streams' sums are read: either may begin anew
-                    tc_fence_before_sync();
-                    ok = join_sync();
-                    if (!ok) break;
+                if (!ok) break;
+                // ---- the piece's end.  Stream 0 has a tile always; where the streams share their rows, each takes half of the
+                // components of both streams' sums ----
+                if (it.wide ? s == 0 : true) ok = pfx_warp_wait(&ctl.o_full[0], (uint32_t)k & 1u, abort_flag);
+                if (ok && tiles1 > 0 && (it.wide ? s == 1 : true)) ok = pfx_warp_wait(&ctl.o_full[1], no1 & 1u, abort_flag);
+                if (!ok) break;
+                if (tiles1 > 0) ++no1;
+                tc_fence_after_sync();
+                if (live) {
+                    // sums refer to m_ref, at most 2^8 below the maximum: as good a reference as the maximum itself
+                    float m_raw = m_ref, f0 = m_ref == NEG_INF ? 0.f : 1.f, f1 = 0.f;      // factors on the two sums
+                    bool both = false;
+                    uint32_t o0 = o_tmem + s * O_STRIDE, o1 = o0;
+                    int c_begin = 0, c_end = D;
+                    if (!it.wide) {
+                        ctl.join[s][r] = make_float2(m_ref, l);
+                        ok = join_sync();
+                        if (!ok) break;
+                        const float2 other = ctl.join[s ^ 1][r];
+                        m_raw = fmaxf(m_ref, other.x);
+                        const float a = m_ref == NEG_INF ? 0.f : fast_exp2((m_ref - m_raw) * sc), b = other.x == NEG_INF ? 0.f : fast_exp2((other.x - m_raw) * sc);
+                        l = l * a + other.y * b;
+                        f0 = s == 0 ? a : b;
+                        f1 = s == 0 ? b : a;
+                        both = tiles1 > 0;
+                        o0 = o_tmem;
+                        o1 = o0 + O_STRIDE;
+                        c_begin = s * (D / 2);
+                        c_end = c_begin + D / 2;
+                    }
+                    const size_t orow = (size_t)row * p.Hq + it.h * p.G + (r - r_node * p.G);
+                    const float m = m_raw == NEG_INF ? NEG_INF : m_raw * p.scale;
+                    const bool last_word = it.wide || s == 0;      // who writes the row's single numbers
+                    if (exists && *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) && tree_poisoned<D, BF16>(p, it, row, node)) {
+                        f0 = __int_as_float(0x7fc00000);
+                        both = false;
+                    }
+                    float top = m, inv = 1.f;
+                    if (it.whole && exists) {
+                        const float own = tree_join_host(p, orow, m, l, top);
+                        inv = l == 0.f ? 0.f : 1.f / l;
+                        f0 *= own * inv;
+                        f1 *= own * inv;
+                        if (p.lse && last_word) p.lse[orow] = l == 0.f ? NEG_INF : top + logf(l);
+                    }
+                    const size_t prow = (size_t)it.slot * 256 + (it.wide ? s * TREE_TILE : 0) + r;
+                    if (!it.whole && exists && last_word) { p.ws.m[prow] = m; p.ws.l[prow] = l; }
+#pragma unroll 1
+                    for (int c0 = c_begin; c0 < c_end; c0 += 32) {
+                        float y[32];
+                        tmem_ld_32x32(o0 + c0, *reinterpret_cast<uint32_t(*)[32]>(&y[0]));
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int u = 0; u < 32; ++u) y[u] = f0 == 0.f ? 0.f : y[u] * f0;
+                        if (both) {
+                            float z[32];
+                            tmem_ld_32x32(o1 + c0, *reinterpret_cast<uint32_t(*)[32]>(&z[0]));
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int u = 0; u < 32; ++u) y[u] = f1 == 0.f ? y[u] : fmaf(z[u], f1, y[u]);
+                        }
+                        if (!exists) continue;
+                        if (!it.whole) {
+#pragma unroll
+                            for (int u = 0; u < 32; u += 8) st_global_hint8(p.ws.o + prow * D + c0 + u, *reinterpret_cast<const float(*)[8]>(&y[u]), keep);
+                            continue;
+                        }
+                        for (int x = 0; x < p.src.n; ++x)
+                            for (int c = 0; c < p.src.nc[x]; ++c) {
+                                const size_t q = orow * p.src.nc[x] + c;
+                                const float hm = p.src.m[x][q];
+                                if (hm == NEG_INF) continue;       // (its o row is not read)
+                                const float w = fast_exp2((hm - top) * 1.4426950408889634f) * inv;
+                                const float4* const ho = reinterpret_cast<const float4*>(p.src.o[x] + q * D + c0);
+#pragma unroll
+                                for (int u = 0; u < 8; ++u) {
+                                    const float4 v = ho[u];
+                                    y[4 * u] = fmaf(v.x, w, y[4 * u]); y[4 * u + 1] = fmaf(v.y, w, y[4 * u + 1]);
+                                    y[4 * u + 2] = fmaf(v.z, w, y[4 * u + 2]); y[4 * u + 3] = fmaf(v.w, w, y[4 * u + 3]);
+                                }
+                            }
+                        uint4* const dst = reinterpret_cast<uint4*>(p.out + orow * D + c0);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            dst[u] = make_uint4(pack2<BF16>(y[8 * u], y[8 * u + 1]), pack2<BF16>(y[8 * u + 2], y[8 * u + 3]),
+                                                pack2<BF16>(y[8 * u + 4], y[8 * u + 5]), pack2<BF16>(y[8 * u + 6], y[8 * u + 7]));
+                    }
+                    if (!it.wide) {                                // both streams' sums are read: either may begin anew
+                        tc_fence_before_sync();
+                        ok = join_sync();
+                        if (!ok) break;
+                    }
                 }
             }
+            n += it.tiles;
             tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl.item_empty[j]);
@@ -797,27 +1145,26 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
     if (*abort_flag) {                                             // (nobody raises it any more: all threads agree)
         if (lane == 0) {
             if (warp == TREE_K_WARP || warp == TREE_V_WARP) ctl.issued[warp - TREE_K_WARP] = issued;
-            if (warp == TREE_V_WARP) ctl.edge_open = edge_open ? (int)(edges & 1u) : -1;
-            if (warp == TREE_ITEM_WARP) ctl.q_issued = q_issued;
+            if (warp == TREE_ITEM_WARP) { ctl.q_issued[0] = (int)q_armed[0]; ctl.q_issued[1] = (int)q_armed[1]; }
         }
         __syncthreads();
-        // unwinding: copies into this CTA's shared memory may still be on their way.  A warp per slot of the ring, one for the edge
-        // barrier and one for the queries, so that the waits' limits do not add up
+        // unwinding: copies into this CTA's shared memory may still be on their way.  A warp per slot of the ring and per buffer of
+        // the queries, so that the waits' limits do not add up
         if (lane == 0) {
             int none = 0;
             if (warp < S) {
-                const int n = ring_last_tile(warp, S, ctl.issued[0], ctl.issued[1]);
-                if (n >= 0) pfx_wait(&ctl.full[warp], (uint32_t)(n / S) & 1u, &none);
+                // the last tile requested into the slot is the only one that can still be coming
+                const int slots = warp < KS ? KS : VS, at = warp < KS ? warp : warp - KS, tiles = ctl.issued[warp < KS ? 0 : 1];
+                if (tiles > at) pfx_wait(&ctl.full[warp], (uint32_t)((tiles - 1 - at) / slots) & 1u, &none);
             }
-            if (warp == TREE_MMA_WARP && ctl.edge_open >= 0) pfx_wait(&ctl.edge, (uint32_t)ctl.edge_open, &none);
-            if (warp == TREE_ITEM_WARP && ctl.q_issued > 0) pfx_wait(&ctl.q_full, (uint32_t)(ctl.q_issued - 1) & 1u, &none);
+            if (warp >= 10 && ctl.q_issued[warp - 10] > 0) pfx_wait(&ctl.q_full[warp - 10], (uint32_t)(ctl.q_issued[warp - 10] - 1) & 1u, &none);
         }
         if (tid == 0 && p.status) atomicOr(p.status, HG_DEV_WAIT_TIMEOUT);
     }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    if (warp == TREE_MMA_WARP) tmem_dealloc(tmem, 512);
+    if (warp == TREE_MMA_WARP) tmem_dealloc(tmem, TMEM_COLS);
 }
 
 // Joins the pieces of the units that the ends of the CTAs' stretches cut, and the host's partials.  Grid (CTAs of the kernel in
