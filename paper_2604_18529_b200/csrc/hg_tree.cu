@@ -75,7 +75,8 @@ static hg_status launch_tree(const CUtensorMap& tq, const CUtensorMap& tk, const
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = pdl ? 1 : 0;
     if (cudaLaunchKernelEx(&cfg, kern, tq, tk, tv, p) != cudaSuccess) { cudaGetLastError(); return HG_ERR_CUDA; }
-    cfg.gridDim = dim3((unsigned)ctas, TREE_MERGE_SPLITS); cfg.blockDim = dim3(TREE_MERGE_THREADS); cfg.dynamicSmemBytes = 0;
+    // (a row of a cut unit for a warp; with many rows two)
+    cfg.gridDim = dim3((unsigned)ctas, ROWS ? ROWS / 8 : 16); cfg.blockDim = dim3(TREE_MERGE_THREADS); cfg.dynamicSmemBytes = 0;
     if (cudaLaunchKernelEx(&cfg, tree_merge_kernel<D, BF16>, p) != cudaSuccess) { cudaGetLastError(); return HG_ERR_CUDA; }
     return HG_OK;
 }
@@ -85,7 +86,6 @@ static hg_status launch_tree_rows(int rows, const CUtensorMap& tq, const CUtenso
     switch (rows) {
         case 16: return launch_tree<D, BF16, 16>(tq, tk, tv, p, ctas, st, pdl);
         case 32: return launch_tree<D, BF16, 32>(tq, tk, tv, p, ctas, st, pdl);
-        case 64: return launch_tree<D, BF16, 64>(tq, tk, tv, p, ctas, st, pdl);
         default: return launch_tree<D, BF16, 0>(tq, tk, tv, p, ctas, st, pdl);
     }
 }
@@ -139,7 +139,7 @@ hg_status hg_attn_decode_tree(const void* q, const void* k_cache, const void* v_
     }
     p.B = desc->batch; p.Hq = desc->num_q_heads; p.Hkv = desc->num_kv_heads; p.G = p.Hq / p.Hkv;
     p.N = tree->num_rows; p.max_nodes = tree->max_nodes; p.words = tree->mask_words;
-    const int most = tree->max_nodes < 128 ? tree->max_nodes * p.G : 128, rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 ? 64 : 0;
+    const int most = tree->max_nodes < 128 ? tree->max_nodes * p.G : 128, rows = most <= 16 ? 16 : most <= 32 ? 32 : 0;
     p.nodes = (rows ? rows : 128) / p.G;
     p.page_size = desc->page_size; p.page_shift = ilog2_exact(desc->page_size); p.max_pages = desc->max_pages; p.num_pages = desc->num_pages;
     p.scale = desc->scale > 0.f ? desc->scale : 1.0f / sqrtf((float)desc->head_dim);

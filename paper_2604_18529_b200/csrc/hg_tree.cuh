@@ -13,7 +13,7 @@
 //           as the A operand of P V.  A UNIT is (sequence, KV head, whole new tokens with up to 256 rows): wide, more than 128
 //           rows, where the streams take 128 rows each and share every K and V tile; or narrow, up to 128 rows, where the streams
 //           take alternate tiles.
-//   few rows (ROWS = 16, 32, 64: the most of a unit)   the tokens are M: S^T = K Q^T is 128 x ROWS, a thread owns a token, so the
+//   few rows (ROWS = 16, 32: the most of a unit)   the tokens are M: S^T = K Q^T is 128 x ROWS, a thread owns a token, so the
 //           exponentials are ROWS a tile and thread instead of 128 whatever the number of rows; P^T goes to shared memory as the
 //           B operand of O^T = V^T P^T.  All units are narrow.
 // A narrow unit's streams are joined at its end, both in the lanes of tensor memory that the same row (component) has in either.
@@ -45,12 +45,13 @@ constexpr int TREE_ITEMS = 4;                 // pieces published ahead
 // unit: 16 sequences, 56 heads, 5 new tokens, up to 16 384 tokens: 310 (2), 285 us (from 4 on); 48 sequences, 32/8 heads, up to
 // 32 and 16 384: 299 (2 to 6), 302, 305, 309; 128 sequences, 8 heads of 64, 2 and 1 500: 70, 62, 63, 63, 65, 64.
 constexpr int TREE_COST_TILE = 4, TREE_COST_UNIT = 16;
+constexpr int TREE_MIN_STRETCH = 8;
 
 template <int D> __host__ __device__ constexpr int tree_tile_bytes() { return TREE_TILE * D * 2; }
 // Ring slots for K and V tiles: what shared memory has room for.  K and V have rings of their own: the S products run ahead of the
 // P V products, so that in a common ring a slot's use before the last might be unfinished when its next one is waited for, and a
 // barrier's parity does not tell the two apart.
-template <int D, int ROWS> __host__ __device__ constexpr int tree_k_slots() { return D == 128 ? (ROWS == 16 || ROWS == 32 ? 3 : 2) : ROWS == 64 ? 5 : 6; }
+template <int D, int ROWS> __host__ __device__ constexpr int tree_k_slots() { return D == 64 ? 6 : ROWS ? 3 : 2; }
 template <int D, int ROWS> __host__ __device__ constexpr int tree_v_slots() { return D == 128 ? 3 : 6; }
 // Queries of a stream (two buffers), weights of a stream (two buffers; many rows have them in tensor memory).
 template <int D, int ROWS> __host__ __device__ constexpr int tree_q_bytes() { return (ROWS ? ROWS : TREE_TILE) * D * 2; }
@@ -123,15 +124,21 @@ __device__ __forceinline__ long long tree_head_cost(const TreeSeq& s) { return (
 __device__ __forceinline__ long long tree_div(long long a, long long b) {
     return ((unsigned long long)(a | b) >> 32) ? a / b : (long long)((uint32_t)a / (uint32_t)b);
 }
-// Where the stretch of CTA c begins: floor(total c / ctas), by a product (inv_ctas = 2^64 / ctas rounded up: exact below 2^56).
-__device__ __forceinline__ long long tree_stretch(const TreeParams& p, long long total, int c) {
-    return (long long)__umul64hi((unsigned long long)total * (unsigned)c, p.inv_ctas);
+// Where the stretch of CTA c of n begins: floor(total c / n).  For all CTAs of the launch by a product (inv_ctas = 2^64 / CTAs
+// rounded up: exact below 2^56).
+__device__ __forceinline__ long long tree_stretch(const TreeParams& p, long long total, int c, int n) {
+    if (n == (int)gridDim.x) return (long long)__umul64hi((unsigned long long)total * (unsigned)c, p.inv_ctas);
+    return tree_div(total * c, n);
+}
+// How many CTAs share the work: where there is little, stretches have a tile for each stream.
+__device__ __forceinline__ int tree_ctas(long long total) {
+    return total >= (long long)TREE_MIN_STRETCH * gridDim.x ? (int)gridDim.x : max(1, (int)total / TREE_MIN_STRETCH);
 }
 // The CTA that a place belongs to.
-__device__ __forceinline__ int tree_cta_of(const TreeParams& p, long long place, long long total, int ctas) {
-    int c = (int)min((long long)ctas - 1, (long long)((double)place / (double)total * ctas));
-    while (c > 0 && tree_stretch(p, total, c) > place) --c;
-    while (c + 1 < ctas && tree_stretch(p, total, c + 1) <= place) ++c;
+__device__ __forceinline__ int tree_cta_of(const TreeParams& p, long long place, long long total, int n) {
+    int c = (int)min((long long)n - 1, (long long)((double)place / (double)total * n));
+    while (c > 0 && tree_stretch(p, total, c, n) > place) --c;
+    while (c + 1 < n && tree_stretch(p, total, c + 1, n) <= place) ++c;
     return c;
 }
 // A unit's tile t stands at TREE_COST_UNIT + t * TREE_COST_TILE behind the unit's begin; how many stand in front of a place in it.
@@ -343,7 +350,7 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
     if (warp >= 8) {
       if constexpr (!FEW) reg_shrink<TREE_REGS_OTHER>();
       cudaGridDependencySynchronize();
-      const int me = tid - 256, cta = blockIdx.x, ctas = gridDim.x;
+      const int me = tid - 256, cta = blockIdx.x;
       if (me < 2) p.ws.valid[2 * cta + me] = 0;
       if (me == 2) p.ws.cut[cta].nodes = 0;
       long long total = 0;
@@ -372,7 +379,8 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
               if (w < warp - 8) upto += ctl.part[w];
               total += ctl.part[w];
           }
-          const long long from = tree_stretch(p, total, cta);
+          const int n = tree_ctas(total);
+          const long long from = cta < n ? tree_stretch(p, total, cta, n) : total;
           if (from >= upto - mine && from < upto) {
               long long base = upto - mine;
               for (int b = b_first; b < b_last; ++b) {
@@ -385,6 +393,8 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
       }
       if (warp == TREE_ITEM_WARP) {
         // =============================== item warp: the stretch's pieces, some ahead, and their queries ===============================
+        // (after an earlier call that ran into its limit there is no work until the caller has cleared the word)
+        const bool skip = timed_out();
         int ub = 0;                                                // first of the 32 sequences in the lanes
         long long base = 0;                                        // ... its place in the row of tiles
         if (p.B > 32) { ub = ctl.start_b < 0 ? p.B : ctl.start_b; base = ctl.start_base; }
@@ -412,10 +422,10 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
             total = block;
             if (sq.bad && cta == 0 && p.status) atomicOr(p.status, HG_DEV_RANGE);
         }
-        long long at = tree_stretch(p, total, cta);                // place in the row of tiles
-        const long long to = cta + 1 < ctas ? tree_stretch(p, total, cta + 1) : total;
-        // (after an earlier call that ran into its limit there is no work until the caller has cleared the word)
-        if (ub == p.B || __any_sync(0xffffffffu, timed_out())) at = to;
+        const int sharing = tree_ctas(total);
+        long long at = cta < sharing ? tree_stretch(p, total, cta, sharing) : total;       // place in the row of tiles
+        const long long to = cta + 1 < sharing ? tree_stretch(p, total, cta + 1, sharing) : total;
+        if (ub == p.B || skip) at = to;
         bool ok = true;
         int last_q = 1;
         uint32_t q_uses[2] = {0, 0};                               // of the buffers
@@ -488,7 +498,7 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
             if (it.q) ++q_armed[1]; else ++q_armed[0];
             if (!it.whole && lane == 0) {
                 p.ws.valid[it.slot] = 1;
-                if (it.slot & 1) *reinterpret_cast<int4*>(&p.ws.cut[cta]) = make_int4(it.row0, it.nodes, it.h, tree_cta_of(p, last_place, total, ctas));
+                if (it.slot & 1) *reinterpret_cast<int4*>(&p.ws.cut[cta]) = make_int4(it.row0, it.nodes, it.h, tree_cta_of(p, last_place, total, sharing));
             }
         }
       } else if (warp == TREE_K_WARP || warp == TREE_V_WARP) {
@@ -710,13 +720,12 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
             if (!it.valid) break;
             const int tiles = tree_stream_tiles(it, s), tiles1 = tree_stream_tiles(it, 1);
             if constexpr (FEW) {
-                // ---- a thread is a token.  Lane i speaks for rows i (and 32 + i) of the unit, their references being the same in
-                // all warps of the stream ----
-                constexpr int V = ROWS == 64 ? 2 : 1, N = ROWS == 16 ? 16 : 32;
+                // ---- a thread is a token.  Lane i speaks for row i mod ROWS of the unit, the rows' references being the same in all
+                // warps of the stream ----
                 const int rows = it.nodes * p.G;
-                float ref[V], l[V];                                // of this lane's rows; l: over the warp's tokens
+                float ref = NEG_INF, l[ROWS];                      // of this lane's row; over this thread's tokens
 #pragma unroll
-                for (int v = 0; v < V; ++v) { ref[v] = NEG_INF; l[v] = 0.f; }
+                for (int c = 0; c < ROWS; ++c) l[c] = 0.f;
                 for (int i = 0; i < tiles; ++i) {
                     ok = pfx_warp_wait(&ctl.s_full[s], ns & 1u, abort_flag);
                     if (!ok) break;
@@ -724,24 +733,22 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                     tc_fence_after_sync();
                     const int t = it.first + tree_tile_index(it, s, i) * TREE_TILE;
                     const uint32_t bad = *reinterpret_cast<volatile uint8_t*>(&ctl.stream_bad[s]);
-                    float x[ROWS];
+                    float x[ROWS], e[ROWS];
                     if constexpr (ROWS == 16) tmem_ld_32x16(s_tmem, *reinterpret_cast<uint32_t(*)[16]>(&x[0]));
-                    else
-#pragma unroll
-                        for (int c0 = 0; c0 < ROWS; c0 += 32) tmem_ld_32x32(s_tmem + c0, *reinterpret_cast<uint32_t(*)[32]>(&x[c0]));
+                    else tmem_ld_32x32(s_tmem, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
                     tmem_ld_wait();
                     tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&ctl.s_read[s]);
                     if (t < it.lo || t + TREE_TILE > min(it.hi, it.len) || bad) {      // tokens outside the slice, of refused pages, not seen
-                        uint64_t hide = t + r < it.lo || t + r >= it.hi || ((bad >> (r >> 4)) & 1u) ? ~0ull : 0ull;
+                        uint32_t hide = t + r < it.lo || t + r >= it.hi || ((bad >> (r >> 4)) & 1u) ? ~0u : 0u;
                         const int d = t + r - it.len;              // which new token this is
                         ok = clear_v(n + tree_tile_index(it, s, i), hide != 0, d >= 0, j);
                         if (!ok) break;
                         if (d >= 0 && hide == 0) {
-                            if (!p.mask) hide = d * p.G >= 64 ? ~0ull : (1ull << (d * p.G)) - 1ull;      // tokens in front of it
+                            if (!p.mask) hide = d * p.G >= 32 ? ~0u : (1u << (d * p.G)) - 1u;          // tokens in front of it
                             else {
-                                const uint64_t group = p.G >= 64 ? ~0ull : (1ull << p.G) - 1ull;
+                                const uint32_t group = p.G >= 32 ? ~0u : (1u << p.G) - 1u;
                                 const uint32_t* const words = p.mask + (size_t)it.row0 * p.words + (d >> 5);
 #pragma unroll 2
                                 for (int u = 0; u < it.nodes; ++u)
@@ -751,20 +758,25 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
 #pragma unroll
                         for (int c = 0; c < ROWS; ++c) x[c] = (hide >> c) & 1u ? NEG_INF : x[c];
                     }
+                    auto exponents = [&]() {                       // scale (x - reference), in powers of 2
+                        const float2 sc2 = make_float2(sc, sc);
+#pragma unroll
+                        for (int c = 0; c < ROWS; c += 4) {
+                            const float4 a = *reinterpret_cast<const float4*>(&ctl.col.off[s][c]);
+                            const float2 lo = fma2(make_float2(x[c], x[c + 1]), sc2, make_float2(a.x, a.y));
+                            const float2 hi = fma2(make_float2(x[c + 2], x[c + 3]), sc2, make_float2(a.z, a.w));
+                            e[c] = lo.x; e[c + 1] = lo.y; e[c + 2] = hi.x; e[c + 3] = hi.y;
+                        }
+                    };
+                    exponents();
                     // a row's reference moves only when a logit is more than 2^8 above it (then the weights would leave the 16-bit
-                    // types' comfortable range), and at a unit's first tile.  The four warps find out by a vote
-                    float mx[V];
-#pragma unroll
-                    for (int v = 0; v < V; ++v) mx[v] = across_lanes<N, true>(&x[v * 32], lane);
-                    bool up = i == 0;
-#pragma unroll
-                    for (int v = 0; v < V; ++v) up = up || ((mx[v] - ref[v]) * sc > 8.f && v * 32 + (lane & (N - 1)) < rows);
-                    up = __any_sync(0xffffffffu, up);
+                    // types' comfortable range), and at a unit's first tile.  The four warps find out by a vote; those that want
+                    // to move leave their maxima
+                    const bool up = i == 0 || __any_sync(0xffffffffu, row_max<ROWS>(e) > 8.f);
                     const int turn = (int)(ns % 3);
                     if (up) {
-                        if (lane < N)
-#pragma unroll
-                            for (int v = 0; v < V; ++v) atomicMax(&ctl.col.top[turn][s][v * 32 + lane], ordered(mx[v]));
+                        const float mx = across_lanes<ROWS, true>(x, lane);
+                        if (lane < ROWS) atomicMax(&ctl.col.top[turn][s][lane], ordered(mx));
                         if (lane == 0) *reinterpret_cast<volatile int*>(&ctl.moved[turn][s]) = (int)ns;
                     }
                     __syncwarp();
@@ -772,65 +784,54 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                     ok = pfx_warp_wait(&ctl.vote[s], (ns - 1) & 1u, abort_flag);
                     if (!ok) break;
                     // the last turn's maxima have been read by all: cleared for the one after the next
-                    if (w4 == 0 && lane < N)
-#pragma unroll
-                        for (int v = 0; v < V; ++v) ctl.col.top[(ns + 2) % 3][s][v * 32 + lane] = 0;
-                    if (ns > 1) {                              // the last tile's weights are used up, and its products in O
+                    if (w4 == 0 && lane < ROWS) ctl.col.top[(ns + 2) % 3][s][lane] = 0;
+                    if (ns > 1) {                                  // the last tile's weights are used up, and its products in O
                         ok = pfx_warp_wait(&ctl.p_free[s], (ns - 2) & 1u, abort_flag);
                         if (!ok) break;
                         tc_fence_after_sync();
                     }
                     if (*reinterpret_cast<volatile int*>(&ctl.moved[turn][s]) == (int)ns) {
-                        float f[V];
-#pragma unroll
-                        for (int v = 0; v < V; ++v) {
-                            const int c = v * 32 + (lane & (N - 1));
-                            const uint32_t m = *reinterpret_cast<volatile uint32_t*>(&ctl.col.top[turn][s][c]);
-                            const float now = fmaxf(ref[v], m ? unordered(m) : NEG_INF);
-                            f[v] = ref[v] == NEG_INF ? 0.f : fast_exp2((ref[v] - now) * sc);
-                            ref[v] = now;
-                            l[v] *= f[v];
-                            ctl.col.off[s][c] = now == NEG_INF ? NEG_INF : -now * sc;      // (the same from all warps)
-                        }
+                        const int c = lane & (ROWS - 1);
+                        const uint32_t m = *reinterpret_cast<volatile uint32_t*>(&ctl.col.top[turn][s][c]);
+                        const float now = fmaxf(ref, m ? unordered(m) : NEG_INF), f = ref == NEG_INF ? 0.f : fast_exp2((ref - now) * sc);
+                        ref = now;
+                        // the exponents' summand (the same from all warps): for a row that has not seen anything yet one that lifts any
+                        // finite logit over the limit, for one that does not exist one that lifts none
+                        ctl.col.off[s][c] = c >= rows ? NEG_INF : now == NEG_INF ? 1e30f : -now * sc;
                         __syncwarp();
+                        exponents();
                         if (i > 0) {
+#pragma unroll
+                            for (int u = 0; u < ROWS; ++u) l[u] *= __shfl_sync(0xffffffffu, f, u);
 #pragma unroll 1
                             for (int c0 = 0; c0 < ROWS; c0 += 8) {
                                 uint32_t y[8];
                                 tmem_ld_32x8(o_tmem + s * O_STRIDE + c0, y);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int u = 0; u < 8; ++u)
-                                    y[u] = __float_as_uint(__uint_as_float(y[u]) * __shfl_sync(0xffffffffu, c0 + u < 32 ? f[0] : f[V - 1], (c0 + u) & 31));
+                                for (int u = 0; u < 8; ++u) y[u] = __float_as_uint(__uint_as_float(y[u]) * __shfl_sync(0xffffffffu, f, c0 + u));
                                 tmem_st_32x8(o_tmem + s * O_STRIDE + c0, y);
                             }
                             tmem_st_wait();
                         }
                     }
-                    const float2 sc2 = make_float2(sc, sc);
                     uint8_t* const dst = p_smem + s * P_BYTES + r * 16;
 #pragma unroll
                     for (int c = 0; c < ROWS; c += 8) {
-                        const float4 a = *reinterpret_cast<const float4*>(&ctl.col.off[s][c]), b = *reinterpret_cast<const float4*>(&ctl.col.off[s][c + 4]);
-                        const float2 off[4] = {make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)};
                         uint32_t w[4];
 #pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            float2 e = fma2(make_float2(x[c + 2 * u], x[c + 2 * u + 1]), sc2, off[u]);
-                            e.x = fast_exp2(e.x);
-                            e.y = fast_exp2(e.y);
-                            x[c + 2 * u] = e.x;
-                            x[c + 2 * u + 1] = e.y;
-                            w[u] = pack2<BF16>(e.x, e.y);
+                        for (int u = 0; u < 8; ++u) {
+                            e[c + u] = fast_exp2(e[c + u]);
+                            l[c + u] += e[c + u];
                         }
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) w[u] = pack2<BF16>(e[c + 2 * u], e[c + 2 * u + 1]);
                         *reinterpret_cast<uint4*>(dst + (c / 8) * 2048) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                     fence_proxy_async();                           // the tensor core reads P through the asynchronous proxy
                     tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&ctl.p_full[s][0]);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) l[v] += across_lanes<N, false>(&x[v * 32], lane);
                 }
                 if (!ok) break;
                 // ---- the piece's end: each stream takes half of the rows, all of their components ----
@@ -840,12 +841,10 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                 if (tiles1 > 0) ++no1;
                 tc_fence_after_sync();
                 float* const sums = reinterpret_cast<float*>(p_smem + s * P_BYTES);      // (the weights there are used up) [4 warps + 1][ROWS]
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    if (lane < N) {
-                        sums[w4 * ROWS + v * 32 + lane] = l[v];
-                        if (w4 == 0) sums[4 * ROWS + v * 32 + lane] = ref[v];
-                    }
+                const float sum = across_lanes<ROWS, false>(l, lane);
+                if (lane < ROWS) {
+                    sums[w4 * ROWS + lane] = sum;
+                    if (w4 == 0) sums[4 * ROWS + lane] = ref;
                 }
                 ok = join_sync();
                 if (!ok) break;
@@ -883,6 +882,7 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
 #pragma unroll 1
                 for (int c0 = 0; c0 < H && s * H + c0 < rows; c0 += 8) {
                     uint32_t y0[8], y1[8];
+                    __syncwarp();                                  // (tensor memory is read by whole warps)
                     tmem_ld_32x8(o_tmem + s * H + c0, y0);
                     tmem_ld_32x8(o_tmem + (both ? O_STRIDE : 0) + s * H + c0, y1);
                     tmem_ld_wait();
@@ -1076,7 +1076,7 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                     const bool last_word = it.wide || s == 0;      // who writes the row's single numbers
                     if (exists && *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) && tree_poisoned<D, BF16>(p, it, row, node)) {
                         f0 = __int_as_float(0x7fc00000);
-                        both = false;
+                        f1 = 0.f;
                     }
                     float top = m, inv = 1.f;
                     if (it.whole && exists) {
@@ -1091,6 +1091,7 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
 #pragma unroll 1
                     for (int c0 = c_begin; c0 < c_end; c0 += 32) {
                         float y[32];
+                        __syncwarp();                              // (tensor memory is read by whole warps)
                         tmem_ld_32x32(o0 + c0, *reinterpret_cast<uint32_t(*)[32]>(&y[0]));
                         tmem_ld_wait();
 #pragma unroll
@@ -1169,7 +1170,7 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
 
 // Joins the pieces of the units that the ends of the CTAs' stretches cut, and the host's partials.  Grid (CTAs of the kernel in
 // front, splits of a unit's rows), a warp per row.
-constexpr int TREE_MERGE_THREADS = 256, TREE_MERGE_SPLITS = 16;
+constexpr int TREE_MERGE_THREADS = 256;
 
 template <int D, bool BF16>
 __global__ void __launch_bounds__(TREE_MERGE_THREADS) tree_merge_kernel(const __grid_constant__ TreeParams p) {
@@ -1178,48 +1179,78 @@ __global__ void __launch_bounds__(TREE_MERGE_THREADS) tree_merge_kernel(const __
     const float NEG_INF = __int_as_float(0xff800000);
     cudaTriggerProgrammaticLaunchCompletion();
     cudaGridDependencySynchronize();
-    if (p.status && (*reinterpret_cast<volatile int32_t*>(p.status) & HG_DEV_WAIT_TIMEOUT)) return;
     const int4 cut = *reinterpret_cast<const int4*>(&p.ws.cut[blockIdx.x]);       // row0, nodes, h, last
-    if (cut.y <= 0) return;
+    const int bits = p.status ? *reinterpret_cast<volatile int32_t*>(p.status) : 0;
+    if (cut.y <= 0 || (bits & HG_DEV_WAIT_TIMEOUT)) return;
     const int lane = threadIdx.x & 31, first = blockIdx.x, pieces = cut.w - first + 1, stream_rows = p.nodes * p.G;
     for (int x = blockIdx.y * (TREE_MERGE_THREADS / 32) + (threadIdx.x >> 5); x < cut.y * p.G; x += gridDim.y * (TREE_MERGE_THREADS / 32)) {
         const int node = fast_div(x, p.div_G), s = x >= stream_rows ? 1 : 0;
         const size_t orow = (size_t)(cut.x + node) * p.Hq + cut.z * p.G + (x - node * p.G);
         const int r = s * TREE_TILE + x - s * stream_rows;
+        // a lane holds a piece's (m, l), of 32 pieces at a time; most units have fewer
         auto slot_of = [&](int e) { return e == 0 ? 2 * first + 1 : 2 * (first + e); };
-        float top = NEG_INF;
-        for (int e = lane; e < pieces; e += 32)
-            if (p.ws.valid[slot_of(e)]) top = fmaxf(top, p.ws.m[(size_t)slot_of(e) * 256 + r]);
+        auto load = [&](int e, float& m, float& pl) {
+            m = NEG_INF;
+            pl = 0.f;
+            if (e >= pieces) return;
+            const size_t q = (size_t)slot_of(e) * 256 + r;
+            const int valid = p.ws.valid[slot_of(e)];
+            const float pm = p.ws.m[q];
+            pl = p.ws.l[q];
+            if (valid) m = pm;
+        };
+        float m0, l0, top, l = 0.f, acc[W];
+        load(lane, m0, l0);
+        top = m0;
+        for (int e = lane + 32; e < pieces; e += 32) {
+            float m, pl;
+            load(e, m, pl);
+            top = fmaxf(top, m);
+        }
         for (int y = 0; y < p.src.n; ++y)
             for (int c = lane; c < p.src.nc[y]; c += 32) top = fmaxf(top, p.src.m[y][orow * p.src.nc[y] + c]);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        float l = 0.f, acc[W];
 #pragma unroll
         for (int u = 0; u < W; ++u) acc[u] = 0.f;
-        auto add = [&](float m, float pl, const float* o) {
-            if (m == NEG_INF) return;                              // (its o row is not read)
-            const float w = fast_exp2((m - top) * LOG2E);
-            l = fmaf(pl, w, l);
-            if constexpr (W == 4) {
-                const float4 v = *reinterpret_cast<const float4*>(o + lane * 4);
-                acc[0] = fmaf(v.x, w, acc[0]); acc[1] = fmaf(v.y, w, acc[1]); acc[2] = fmaf(v.z, w, acc[2]); acc[3] = fmaf(v.w, w, acc[3]);
-            } else {
-                const float2 v = *reinterpret_cast<const float2*>(o + lane * 2);
-                acc[0] = fmaf(v.x, w, acc[0]); acc[1] = fmaf(v.y, w, acc[1]);
+        // adds up `n` partials whose weights the lanes hold, eight rows of sums requested at a time (one of weight 0 is not read)
+        auto add = [&](float m, float pl, int n, auto row_of) {
+            const float w = m == NEG_INF ? 0.f : fast_exp2((m - top) * LOG2E);
+            l = m == NEG_INF ? l : fmaf(pl, w, l);
+            for (int e0 = 0; e0 < n; e0 += 8) {
+                __align__(16) float v[8][W];
+                float we[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    we[u] = __shfl_sync(0xffffffffu, w, (e0 + u) & 31);
+                    if (e0 + u >= n) we[u] = 0.f;
+                    const float* const o = row_of(e0 + u) + lane * W;
+#pragma unroll
+                    for (int z = 0; z < W; ++z) v[u][z] = 0.f;
+                    if (we[u] != 0.f) {
+                        if constexpr (W == 4) *reinterpret_cast<float4*>(v[u]) = *reinterpret_cast<const float4*>(o);
+                        else *reinterpret_cast<float2*>(v[u]) = *reinterpret_cast<const float2*>(o);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+#pragma unroll
+                    for (int z = 0; z < W; ++z) acc[z] = fmaf(v[u][z], we[u], acc[z]);
             }
         };
-#pragma unroll 4
-        for (int e = 0; e < pieces; ++e) {
-            const int slot = slot_of(e);
-            const size_t q = (size_t)slot * 256 + r;
-            if (p.ws.valid[slot]) add(p.ws.m[q], p.ws.l[q], p.ws.o + q * D);
+        for (int e0 = 0; e0 < pieces; e0 += 32) {
+            if (e0 > 0) load(e0 + lane, m0, l0);
+            add(m0, l0, min(32, pieces - e0), [&](int e) { return p.ws.o + ((size_t)slot_of(e0 + e) * 256 + r) * D; });
         }
         for (int y = 0; y < p.src.n; ++y)
-            for (int c = 0; c < p.src.nc[y]; ++c) {
-                const size_t q = orow * p.src.nc[y] + c;
-                add(p.src.m[y][q], p.src.l[y][q], p.src.o[y] + q * D);
+            for (int c0 = 0; c0 < p.src.nc[y]; c0 += 32) {
+                const size_t q = orow * p.src.nc[y] + c0;
+                const bool is = c0 + lane < p.src.nc[y];
+                add(is ? p.src.m[y][q + lane] : NEG_INF, is ? p.src.l[y][q + lane] : 0.f, min(32, p.src.nc[y] - c0),
+                    [&](int e) { return p.src.o[y] + (q + e) * D; });
             }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
         const float inv = l == 0.f ? 0.f : 1.f / l;
         if (lane == 0 && p.lse) p.lse[orow] = l == 0.f ? NEG_INF : top + logf(l);
         uint32_t w[W / 2];

@@ -255,30 +255,32 @@ def test_wide_masks_and_spare_bits():
 
 @pytest.mark.parametrize("bad", [float("nan"), INF, -INF])
 @pytest.mark.parametrize("dtype,D", [(F16, 128), (BF16, 64)])
-def test_what_masked_tokens_hold_does_not_matter(bad, dtype, D):
+@pytest.mark.parametrize("Hkv", [1, 4])                                       # 80 and 20 rows a KV head
+def test_what_masked_tokens_hold_does_not_matter(bad, dtype, D, Hkv):
     """Token 3 of each sequence overflows; nobody but token 6 sees it"""
     sees = [[i] if i != 6 else [3, 6] for i in range(20)]
-    s = Step([130, 9], [20, 7], masks=[sees, sees[:7]], dtype=dtype, D=D, Hq=4, Hkv=2)
+    s = Step([130, 9], [20, 7], masks=[sees, sees[:7]], dtype=dtype, D=D, Hq=4, Hkv=Hkv)
     s.call()
     want, want_lse = s.out.clone(), s.lse.clone()
     for b in range(2):
         t = s.lens[b] + 3
         page = int(s.table[b, t // s.P])
         s.k[page, :, t % s.P] = bad
-        s.v[page, 1, t % s.P, 5] = bad
+        s.v[page, Hkv - 1, t % s.P, 5] = bad
     s.out.fill_(-77)
     s.call()
     torch.cuda.synchronize()
     others = [r for r in range(27) if r not in (3, 6, 20 + 3, 20 + 6)]       # (token 3 sees itself)
     assert torch.equal(s.out[others], want[others]) and torch.equal(s.lse[others], want_lse[others])
-    s2 = Step([130, 9], [20, 7], masks=[sees, sees[:7]], dtype=dtype, D=D, Hq=4, Hkv=2)
+    s2 = Step([130, 9], [20, 7], masks=[sees, sees[:7]], dtype=dtype, D=D, Hq=4, Hkv=Hkv)
     for b in range(2):                                                      # only V: the logits of token 6 stay
         t = s2.lens[b] + 3
-        s2.v[int(s2.table[b, t // s2.P]), 1, t % s2.P, 5] = bad
+        s2.v[int(s2.table[b, t // s2.P]), Hkv - 1, t % s2.P, 5] = bad
     s2.call()
     torch.cuda.synchronize()
     seers = [3, 6, 23, 26]
-    assert not torch.isfinite(s2.out[seers, 2:, 5]).any() and torch.equal(s2.out[seers, :2], want[seers, :2])      # heads of KV head 1, and of 0
+    first = 4 - 4 // Hkv                                                    # of the heads that read the last KV head
+    assert not torch.isfinite(s2.out[seers, first:, 5]).any() and torch.equal(s2.out[seers, :first], want[seers, :first])
     assert torch.equal(s2.out[others], want[others]) and torch.equal(s2.lse[:27], want_lse[:27])
 
 
