@@ -66,7 +66,7 @@ static hg_status run_rope(RopeParams& p, int heads, int kv_heads, int head_dim, 
     p.div_head = make_fast_div((uint32_t)p.head_units);
     // a row's units go to several CTAs where there are few rows
     const int step = ROPE_THREADS * ROPE_UNROLL, chunks = (p.units + step - 1) / step;
-    const dim3 grid((unsigned)r->num_rows, (unsigned)(r->num_rows >= 512 ? 1 : chunks < 65535 ? chunks : 65535));
+    const dim3 grid((unsigned)r->num_rows, (unsigned)(r->num_rows >= 2048 ? 1 : chunks < 65535 ? chunks : 65535));
     if (half) return bf16 ? launch_draft(kv_append_rope_kernel<true, true>, grid, ROPE_THREADS, 0, stream, p)
                           : launch_draft(kv_append_rope_kernel<false, true>, grid, ROPE_THREADS, 0, stream, p);
     return bf16 ? launch_draft(kv_append_rope_kernel<true, false>, grid, ROPE_THREADS, 0, stream, p)
@@ -102,12 +102,18 @@ hg_status hg_kv_slots(const int32_t* seq_lens, const int32_t* n_new, const int32
     p.B = desc->batch; p.N = num_rows; p.words = mask ? mask_words : 0;
     p.cut = !parent && !mask ? 0x7fffffff : mask && mask_words * 32 < HG_MAX_TREE_NODES ? mask_words * 32 : HG_MAX_TREE_NODES;
     p.page_shift = ilog2_exact(desc->page_size); p.max_pages = desc->max_pages; p.num_pages = desc->num_pages;
-    // about four CTAs of 256 rows' threads for every SM at most: ranges of sequences, and splits of their rows where there are more
-    // rows than that
+    if (desc->batch <= SLOTS_SCAN) {
+        const bool quads = !parent && !mask && aligned16(tok_seq) && aligned16(tok_pos) && aligned16(tok_slot);
+        const long long per_cta = SLOTS_THREADS * (quads ? 4 : 1), ctas = ((long long)num_rows + per_cta - 1) / per_cta;
+        const dim3 grid((unsigned)(ctas < 888 ? ctas : 888));      // (what 148 SMs hold at a time)
+        return quads ? launch_draft(kv_slots_kernel<true>, grid, SLOTS_THREADS, 0, stream, p)
+                     : launch_draft(kv_slots_kernel<false>, grid, SLOTS_THREADS, 0, stream, p);
+    }
+    // ranges of sequences, and splits of their rows
     const int ranges = desc->batch < 592 ? desc->batch : 592;
     p.per = (desc->batch + ranges - 1) / ranges;
-    const long long per_range = ((long long)num_rows + ranges - 1) / ranges, splits = (per_range + 1023) / 1024, most = 592 / ranges;
-    return launch_draft(kv_slots_kernel, dim3((unsigned)ranges, (unsigned)(splits < most ? splits : most)), SLOTS_THREADS, 0, stream, p);
+    const long long per_range = ((long long)num_rows + ranges - 1) / ranges, splits = (per_range + 511) / 512, most = 1184 / ranges;
+    return launch_draft(kv_slots_many_kernel, dim3((unsigned)ranges, (unsigned)(splits < most ? splits : most)), SLOTS_THREADS, 0, stream, p);
 }
 
 hg_status hg_rope(const void* x, void* y, const int32_t* pos, int32_t num_heads, int32_t head_dim, int32_t dtype, void* stream,

@@ -23,6 +23,7 @@ __device__ __forceinline__ void draft_begin() {
 // ---- slots: rows, positions, places, masks -----------------------------------------------------------------------------
 
 constexpr int SLOTS_THREADS = 256;
+constexpr int SLOTS_SCAN = 2048;           // sequences that every CTA can scan
 
 struct SlotsParams {
     const int32_t* seq_lens;
@@ -54,10 +55,159 @@ __device__ __forceinline__ void block_sum2(long long& a, long long& b, long long
     for (int w = 0; w < (int)blockDim.x / 32; ++w) { a += part[w][0]; b += part[w][1]; }
 }
 
-// Grid (sequence ranges, splits of a range's rows).  A CTA sums the lengths in front of its range (reading them takes less
-// than a second launch would: 65 535 lengths are 256 KB from the L2), scans its own 256 at a time and fills their rows, a
-// thread a row.
+// Up the tree from token i of the sequence whose rows begin at `first`: the number of its ancestors, and their bits (and its own),
+// which come in descending order.
+__device__ __forceinline__ int slots_ancestors(const SlotsParams& p, int first, int i, uint32_t* bits, int& trouble) {
+    int depth = 0, w = i >> 5, node = i;
+    uint32_t word = 1u << (i & 31);
+    if (bits) for (int z = p.words - 1; z > w; --z) bits[z] = 0;
+    for (;;) {
+        const int up = p.parent[first + node];
+        if (up >= node) trouble |= HG_DEV_RANGE;
+        if (up < 0 || up >= node) break;
+        ++depth;
+        if (bits && (up >> 5) != w) {
+            bits[w] = word;
+            for (--w; w > (up >> 5); --w) bits[w] = 0;
+            word = 0;
+        }
+        word |= 1u << (up & 31);
+        node = up;
+    }
+    if (bits) {
+        bits[w] = word;
+        for (--w; w >= 0; --w) bits[w] = 0;
+    }
+    return depth;
+}
+
+// What a row gets: token i of sequence b, whose rows begin at `first` and whose cache has `len` tokens; `entry`: the block-table
+// entry of its page, -1 where the table ends.
+__device__ __forceinline__ void slots_row(const SlotsParams& p, int r, int b, int first, int len, int entry, int& trouble) {
+    const int i = r - first;
+    int depth = i;
+    uint32_t* const bits = p.mask ? p.mask + (size_t)r * p.words : nullptr;
+    if (p.parent) depth = slots_ancestors(p, first, i, bits, trouble);
+    else if (bits)
+        for (int w = 0; w < p.words; ++w) {
+            const int last = i - w * 32;
+            bits[w] = last >= 31 ? 0xffffffffu : last < 0 ? 0u : (2u << last) - 1u;
+        }
+    if (p.seq) p.seq[r] = b;
+    if (p.pos) p.pos[r] = len + depth;
+    if (p.slot) {
+        const int in_page = (len + i) & ((1 << p.page_shift) - 1);
+        if (entry == -2) trouble |= HG_DEV_BAD_PAGE;
+        p.slot[r] = entry < 0 ? -1ll : ((long long)entry << p.page_shift) + in_page;
+    }
+}
+__device__ __forceinline__ int slots_entry(const SlotsParams& p, int b, long long t, int& trouble) {
+    const long long page = t >> p.page_shift;
+    if (page >= p.max_pages) { trouble |= HG_DEV_RANGE; return -1; }
+    const long long e = (long long)b * p.max_pages + page;
+    const int entry = p.table ? p.table[e] : (int)e;
+    return (unsigned)entry < (unsigned)p.num_pages ? entry : -2;
+}
+
+// Up to SLOTS_SCAN sequences: every CTA scans all the lengths, which costs less than handing them on, and takes rows in turn, so
+// that long and short sequences balance.  Sums are cut at N, which leaves them associative.  QUADS: a thread takes four rows in a
+// row (no masks to write, arrays aligned for vectors), else one.  600 000 rows of 300 sequences: 6.4 us; one row a thread 9.5.
+template <bool QUADS>
 __global__ void __launch_bounds__(SLOTS_THREADS) kv_slots_kernel(SlotsParams p) {
+    __shared__ unsigned warp_total[SLOTS_THREADS / 32];
+    __shared__ int start[SLOTS_SCAN + 1], cached[SLOTS_SCAN];
+    draft_begin();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, run = (p.B + SLOTS_THREADS - 1) / SLOTS_THREADS;
+    const unsigned N = (unsigned)p.N;
+    int trouble = 0;
+    unsigned sum = 0;
+    for (int b = tid; b < p.B; b += SLOTS_THREADS) {
+        cached[b] = max(p.seq_lens[b], 0);
+        start[b] = max(p.n_new ? p.n_new[b] : 1, 0);               // (as asked, for now)
+    }
+    __syncthreads();
+    const int b0 = min(p.B, tid * run), b1 = min(p.B, b0 + run);
+    for (int b = b0; b < b1; ++b) sum = min(sum + (unsigned)min(start[b], p.cut), N);
+    unsigned x = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x = min(x + y, N);
+    }
+    if (lane == 31) warp_total[warp] = x;
+    unsigned upto = __shfl_up_sync(0xffffffffu, x, 1);
+    if (lane == 0) upto = 0;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) upto = min(upto + warp_total[w], N);
+    for (int b = b0; b < b1; ++b) {
+        const int asked = start[b];
+        const unsigned next = min(upto + (unsigned)min(asked, p.cut), N);
+        start[b] = (int)upto;
+        if (next - upto < (unsigned)asked && blockIdx.x == 0) trouble |= HG_DEV_RANGE;
+        upto = next;
+        if (b == p.B - 1) start[p.B] = (int)next;
+    }
+    __syncthreads();
+    if (blockIdx.x == 0) for (int b = tid; b <= p.B; b += SLOTS_THREADS) p.cu[b] = start[b];
+    const int total = start[p.B];
+    constexpr int ROWS = QUADS ? 4 : 1;
+    for (long long r0 = ((long long)blockIdx.x * SLOTS_THREADS + tid) * ROWS; r0 < p.N; r0 += (long long)gridDim.x * SLOTS_THREADS * ROWS) {
+        int k = 0;
+        if (r0 < total)
+            for (int above = p.B; above - k > 1;) {                // the last sequence that starts at or before the row
+                const int mid = (k + above) >> 1;
+                if (start[mid] <= (int)r0) k = mid; else above = mid;
+            }
+        if constexpr (QUADS) {
+            __align__(16) int seq[4], pos[4];
+            __align__(16) long long slot[4];
+            int entry[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                seq[u] = -1; pos[u] = 0; slot[u] = -1;
+                if (r0 + u >= total) continue;
+                const int r = (int)r0 + u;
+                while (start[k + 1] <= r) ++k;
+                seq[u] = k;
+                pos[u] = cached[k] + (r - start[k]);
+                if (p.slot) entry[u] = slots_entry(p, k, (long long)cached[k] + (r - start[k]), trouble);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (!p.slot || seq[u] < 0) continue;
+                if (entry[u] == -2) trouble |= HG_DEV_BAD_PAGE;
+                if (entry[u] >= 0) slot[u] = ((long long)entry[u] << p.page_shift) + (pos[u] & ((1 << p.page_shift) - 1));
+            }
+            if (r0 + 4 <= p.N) {
+                if (p.seq) *reinterpret_cast<int4*>(p.seq + r0) = *reinterpret_cast<const int4*>(seq);
+                if (p.pos) *reinterpret_cast<int4*>(p.pos + r0) = *reinterpret_cast<const int4*>(pos);
+                if (p.slot) {
+                    *reinterpret_cast<longlong2*>(p.slot + r0) = *reinterpret_cast<const longlong2*>(slot);
+                    *reinterpret_cast<longlong2*>(p.slot + r0 + 2) = *reinterpret_cast<const longlong2*>(slot + 2);
+                }
+            } else
+                for (int u = 0; r0 + u < p.N; ++u) {
+                    if (p.seq) p.seq[r0 + u] = u == 0 ? seq[0] : u == 1 ? seq[1] : seq[2];
+                    if (p.pos) p.pos[r0 + u] = u == 0 ? pos[0] : u == 1 ? pos[1] : pos[2];
+                    if (p.slot) p.slot[r0 + u] = u == 0 ? slot[0] : u == 1 ? slot[1] : slot[2];
+                }
+        } else if (r0 < total) {
+            const int r = (int)r0, entry = p.slot ? slots_entry(p, k, (long long)cached[k] + (r - start[k]), trouble) : -1;
+            slots_row(p, r, k, start[k], cached[k], entry, trouble);
+        } else {                                                   // behind the last token
+            if (p.seq) p.seq[r0] = -1;
+            if (p.pos) p.pos[r0] = 0;
+            if (p.slot) p.slot[r0] = -1;
+            if (p.mask) for (int w = 0; w < p.words; ++w) p.mask[(size_t)r0 * p.words + w] = 0;
+        }
+    }
+    if (trouble && p.status) atomicOr(p.status, trouble);
+}
+
+// More sequences than that.  Grid (sequence ranges, splits of a range's rows).  A CTA sums the lengths in front of its range
+// (reading them takes less than a second launch would: 65 535 lengths are 256 KB from the L2), scans its own 256 at a time and
+// fills their rows, a thread a row.
+__global__ void __launch_bounds__(SLOTS_THREADS) kv_slots_many_kernel(SlotsParams p) {
     __shared__ long long part[SLOTS_THREADS / 32][2];
     __shared__ long long warp_total[SLOTS_THREADS / 32];
     __shared__ int first_row[SLOTS_THREADS], length[SLOTS_THREADS];
@@ -107,50 +257,8 @@ __global__ void __launch_bounds__(SLOTS_THREADS) kv_slots_kernel(SlotsParams p) 
                 const int mid = (k + above) >> 1;
                 if (first_row[mid] <= r) k = mid; else above = mid;
             }
-            const int i = r - first_row[k];
-            int depth = i;
-            uint32_t* const bits = p.mask ? p.mask + (size_t)r * p.words : nullptr;
-            if (p.parent) {                                        // up the tree; ancestors come in descending order
-                depth = 0;
-                int w = i >> 5, node = i;
-                uint32_t word = 1u << (i & 31);
-                if (bits) for (int z = p.words - 1; z > w; --z) bits[z] = 0;
-                for (;;) {
-                    const int up = p.parent[first_row[k] + node];
-                    if (up >= node) trouble |= HG_DEV_RANGE;
-                    if (up < 0 || up >= node) break;
-                    ++depth;
-                    if (bits && (up >> 5) != w) {
-                        bits[w] = word;
-                        for (--w; w > (up >> 5); --w) bits[w] = 0;
-                        word = 0;
-                    }
-                    word |= 1u << (up & 31);
-                    node = up;
-                }
-                if (bits) {
-                    bits[w] = word;
-                    for (--w; w >= 0; --w) bits[w] = 0;
-                }
-            } else if (bits) {
-                for (int w = 0; w < p.words; ++w) {
-                    const int last = i - w * 32;
-                    bits[w] = last >= 31 ? 0xffffffffu : last < 0 ? 0u : (2u << last) - 1u;
-                }
-            }
-            if (p.seq) p.seq[r] = q0 + k;
-            if (p.pos) p.pos[r] = length[k] + depth;
-            if (p.slot) {
-                const long long t = (long long)length[k] + i, page = t >> p.page_shift;
-                long long at = -1;
-                if (page >= p.max_pages) trouble |= HG_DEV_RANGE;
-                else {
-                    const long long e = (long long)(q0 + k) * p.max_pages + page, id = p.table ? p.table[e] : e;
-                    if (id < 0 || id >= p.num_pages) trouble |= HG_DEV_BAD_PAGE;
-                    else at = (id << p.page_shift) + (t & ((1 << p.page_shift) - 1));
-                }
-                p.slot[r] = at;
-            }
+            const int entry = p.slot ? slots_entry(p, q0 + k, (long long)length[k] + (r - first_row[k]), trouble) : -1;
+            slots_row(p, r, q0 + k, first_row[k], length[k], entry, trouble);
         }
     }
     // rows behind the last token
@@ -277,7 +385,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) kv_append_rope_kernel(RopeParams
 
 // ---- accepted rows ---------------------------------------------------------------------------------------------------------
 
-constexpr int ACCEPT_THREADS = 256, ACCEPT_UNROLL = 8, ACCEPT_MAX_PATH = 1024;
+constexpr int ACCEPT_THREADS = 256, ACCEPT_UNROLL = 4, ACCEPT_MAX_PATH = 1024;
 
 struct AcceptParams {
     KvPoolView pv;
@@ -303,31 +411,28 @@ __global__ void __launch_bounds__(ACCEPT_THREADS) kv_accept_kernel(AcceptParams 
     const KvPoolView& pv = p.pv;
     const int len = max(p.seq_lens[b], 0), n = min(p.n_accept[b], p.max_path);
     int trouble = 0;
-    auto place = [&](long long t, int64_t& at) {                   // of position t: 0, or what is wrong with it
+    auto entry = [&](long long t) {                                // of position t: a page, or, negative, what is wrong with it
         const long long page = t >> pv.page_shift;
-        if (page >= pv.max_pages) return HG_DEV_RANGE;
+        if (page >= pv.max_pages) return -HG_DEV_RANGE;
         const long long e = (long long)b * pv.max_pages + page;
-        const long long id = pv.block_table ? pv.block_table[e] : e;
-        if (id < 0 || id >= pv.num_pages) return HG_DEV_BAD_PAGE;
-        at = id * pv.page_stride + (t & (pv.page_size - 1)) * pv.tok_stride;
-        return 0;
+        const int id = pv.block_table ? pv.block_table[e] : (int)e;
+        return (unsigned)id < (unsigned)pv.num_pages ? id : -HG_DEV_BAD_PAGE;
     };
     int last = p.max_path;                                         // this thread's first bad step
     for (int j = tid; j < n; j += ACCEPT_THREADS) {
         const int x = p.path[(size_t)b * p.max_path + j], above = j > 0 ? p.path[(size_t)b * p.max_path + j - 1] : -1;
-        int wrong = x > above && x >= j ? 0 : HG_DEV_RANGE;
-        int64_t f = 0, t = 0;
-        if (!wrong) wrong = place((long long)len + x, f);
-        if (!wrong) wrong = place((long long)len + j, t);
-        from[j] = f;
-        to[j] = t;
+        const bool ascends = x > above && x >= j;
+        const long long f = (long long)len + (ascends ? x : j), t = (long long)len + j;
+        const int fe = entry(f), te = entry(t), wrong = !ascends ? HG_DEV_RANGE : fe < 0 ? -fe : te < 0 ? -te : 0;
+        from[j] = fe * pv.page_stride + (f & (pv.page_size - 1)) * pv.tok_stride;
+        to[j] = te * pv.page_stride + (t & (pv.page_size - 1)) * pv.tok_stride;
         if (wrong && j < last) { last = j; trouble = wrong; }
     }
     if (last < p.max_path) atomicMin(&kept, last);
     __syncthreads();
     const int keep = max(0, min(n, kept));
     if (trouble && last == keep && p.status) atomicOr(p.status, trouble);
-    cluster.sync();                                                // every CTA has read the length, which may be overwritten
+    if (p.new_lens == p.seq_lens) cluster.sync();                  // every CTA has read the length before it is overwritten
     if (p.new_lens && rank == 0 && tid == 0) p.new_lens[b] = len + keep;
     const int vecs = pv.D / 8, columns = pv.Hkv * vecs;
     for (int c = rank * ACCEPT_THREADS + tid; c < 2 * columns; c += ranks * ACCEPT_THREADS) {
