@@ -69,7 +69,7 @@ static hg_status launch_tree(const CUtensorMap& tq, const CUtensorMap& tk, const
     }
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
-    cfg.gridDim = dim3((unsigned)ctas); cfg.blockDim = dim3(TREE_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)ctas); cfg.blockDim = dim3(tree_threads<ROWS>()); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;

@@ -37,9 +37,11 @@
 namespace hg {
 
 constexpr int TREE_TILE = 128;                // tokens per tile, rows per stream
-constexpr int TREE_THREADS = 384;
-constexpr int TREE_K_WARP = 8, TREE_V_WARP = 9, TREE_MMA_WARP = 10, TREE_ITEM_WARP = 11;
-constexpr int TREE_REGS_SOFTMAX = 200, TREE_REGS_OTHER = 96;   // (many rows) of the 384 x 168 of the launch
+template <int ROWS> __host__ __device__ constexpr int tree_threads() { return ROWS ? 512 : 384; }
+constexpr int TREE_K_WARP = 8, TREE_V_WARP = 9, TREE_MMA_WARP = 10, TREE_ITEM_WARP = 11, TREE_END_WARP = 12;
+// registers of the softmax warps and of the others: together the 384 x 168 (many rows) or 512 x 128 (few rows) of the launch
+template <int ROWS> __host__ __device__ constexpr int tree_regs_softmax() { return ROWS ? 160 : 200; }
+constexpr int TREE_REGS_OTHER = 96;
 constexpr int TREE_ITEMS = 4;                 // pieces published ahead
 // Costs for the dealing: a tile, and a unit on top of its tiles (start, first tile, end).  Measured at 2, 4, 6, 8, 12 and 16 tiles a
 // unit: 16 sequences, 56 heads, 5 new tokens, up to 16 384 tokens: 310 (2), 285 us (from 4 on); 48 sequences, 32/8 heads, up to
@@ -169,10 +171,12 @@ template <int D, int ROWS>
 struct TreeCtl {
     static constexpr int S = tree_k_slots<D, ROWS>() + tree_v_slots<D, ROWS>();
     uint64_t full[S], empty[S];      // K slots, then V slots
-    uint64_t s_full[2], s_read[2], p_free[2], p_full[2][4], o_full[2];   // p_full: the quarters of a tile's tokens
+    uint64_t s_full[2], s_read[2], p_free[2], p_full[2][ROWS ? 1 : 4];   // p_full: (many rows) the quarters of a tile's tokens
+    uint64_t o_full[2][2];           // per stream, with few rows for even and odd pieces
     uint64_t q_full[2], q_free[2], drain;
-    uint64_t join_sync[4];           // the warps that join a narrow unit's streams
+    uint64_t join_sync[ROWS ? 1 : 4];        // (many rows) the two warps that join 32 rows of a narrow unit's streams
     uint64_t vote[2];                // (few rows) a stream's warps
+    uint64_t sums_full, sums_free, o_free[2];      // (few rows) the pieces' way to the warps that finish them
     uint64_t item_full[TREE_ITEMS], item_empty[TREE_ITEMS];
     TreeItem item[TREE_ITEMS];
     int poisoned[TREE_ITEMS];        // something in the V rows of the item's new tokens is not finite
@@ -185,7 +189,11 @@ struct TreeCtl {
     // turns, the maxima of a tile as ordered integers
     union __align__(16) {
         float2 join[2][ROWS ? 1 : TREE_TILE];
-        struct { float off[2][ROWS ? ROWS : 1]; uint32_t top[3][2][ROWS ? ROWS : 1]; } col;
+        struct {
+            float off[2][ROWS ? ROWS : 1];
+            uint32_t top[3][2][ROWS ? ROWS : 1];
+            float sums[2][4][ROWS ? ROWS : 1], ref[2][ROWS ? ROWS : 1];      // of a piece: per stream and warp, and references
+        } col;
     };
     long long part[4];
     long long start_base;
@@ -279,7 +287,7 @@ __device__ __forceinline__ float tree_join_host(const TreeParams& p, size_t orow
 }
 
 template <int D, bool BF16, int ROWS>
-__global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+__global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                                                                const __grid_constant__ CUtensorMap tmV, const __grid_constant__ TreeParams p) {
     constexpr bool FEW = ROWS > 0;
     constexpr int KS = tree_k_slots<D, ROWS>(), VS = tree_v_slots<D, ROWS>(), S = KS + VS;
@@ -299,7 +307,7 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
     constexpr bool BESIDE = FEW || D == 64;
     constexpr uint32_t S_STRIDE = FEW ? ROWS : 128, O_COL = 2 * S_STRIDE, O_STRIDE = FEW ? ROWS : D;
     constexpr uint32_t P_COL = BESIDE ? 384 : 0, P_STRIDE = BESIDE ? 64 : 128;     // (many rows)
-    constexpr uint32_t TMEM_COLS = FEW ? 4 * ROWS : 512;
+    constexpr uint32_t TMEM_COLS = FEW ? 8 * ROWS : 512;           // (few rows: S, and O for even and odd pieces, 6 * ROWS of them)
     const float NEG_INF = __int_as_float(0xff800000);
 
     extern __shared__ __align__(1024) uint8_t tree_raw[];
@@ -319,20 +327,24 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
             mbar_init(&ctl.s_full[s], 2);                          // the products' completion, and the tile's description
             mbar_init(&ctl.s_read[s], 4);
             mbar_init(&ctl.p_free[s], 1);
-            for (int c = 0; c < 4; ++c) mbar_init(&ctl.p_full[s][c], 4);
-            mbar_init(&ctl.o_full[s], 1);
+            for (int c = 0; c < (FEW ? 1 : 4); ++c) mbar_init(&ctl.p_full[s][c], 4);
+            mbar_init(&ctl.o_full[s][0], 1);
+            mbar_init(&ctl.o_full[s][1], 1);
+            mbar_init(&ctl.o_free[s], 4);
             mbar_init(&ctl.q_full[s], 1);
             mbar_init(&ctl.q_free[s], 1);
             mbar_init(&ctl.vote[s], 4);
         }
-        for (int i = 0; i < TREE_ITEMS; ++i) { mbar_init(&ctl.item_full[i], 1); mbar_init(&ctl.item_empty[i], 8 + 3); }
-        for (int i = 0; i < 4; ++i) mbar_init(&ctl.join_sync[i], FEW ? 8 : 2);
+        for (int i = 0; i < TREE_ITEMS; ++i) { mbar_init(&ctl.item_full[i], 1); mbar_init(&ctl.item_empty[i], FEW ? 8 + 3 + 4 : 8 + 3); }
+        for (int i = 0; i < (FEW ? 1 : 4); ++i) mbar_init(&ctl.join_sync[i], 2);
+        mbar_init(&ctl.sums_full, 8);
+        mbar_init(&ctl.sums_free, 4);
         mbar_init(&ctl.drain, 1);
         ctl.abort = 0;
         fence_barrier_init();
     }
     if (FEW)
-        for (int i = tid; i < 6 * (FEW ? ROWS : 1); i += TREE_THREADS) (&ctl.col.top[0][0][0])[i] = 0;
+        for (int i = tid; i < 6 * (FEW ? ROWS : 1); i += tree_threads<ROWS>()) (&ctl.col.top[0][0][0])[i] = 0;
     if (tid < 6) (&ctl.moved[0][0])[tid] = 0;
     if (warp == TREE_MMA_WARP) {
         tmem_alloc(&ctl.tmem, TMEM_COLS);
@@ -347,8 +359,8 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
     uint32_t q_armed[2] = {0, 0};                                  // (item warp) queries requested, by barrier
     cudaTriggerProgrammaticLaunchCompletion();
     auto timed_out = [&]() { return p.status && (*reinterpret_cast<volatile int32_t*>(p.status) & HG_DEV_WAIT_TIMEOUT); };
-    if (warp >= 8) {
-      if constexpr (!FEW) reg_shrink<TREE_REGS_OTHER>();
+    if (warp >= 8 && warp < TREE_END_WARP) {
+      reg_shrink<TREE_REGS_OTHER>();
       cudaGridDependencySynchronize();
       const int me = tid - 256, cta = blockIdx.x;
       if (me < 2) p.ws.valid[2 * cta + me] = 0;
@@ -510,29 +522,33 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
         const int piece = lane / HALVES, half = lane % HALVES;     // this lane's box: a page (or part of one) and a half
         bool ok = true;
         int n = 0;                                                 // tiles of earlier items
+        // block-table entries of 32 pages in the lanes, from page `from` on of a row whose tokens are [lo, hi)
+        auto look_up = [&](int b, int lo, int hi, int from) {
+            const int pg = from + lane;
+            if (pg > (hi - 1) >> p.page_shift || pg < lo >> p.page_shift || hi <= lo) return -1;
+            const long long e = (long long)b * p.max_pages + pg;
+            return p.block_table ? p.block_table[e] : (int)e;
+        };
+        // those at the beginning of the item behind this one are requested as soon as it is published: a unit of a few tiles would
+        // wait for them as long as it takes
+        int ahead = 0;
+        bool looked = false;
         for (int k = 0; ok; ++k) {
             const int j = k % TREE_ITEMS;
             ok = pfx_warp_wait(&ctl.item_full[j], (uint32_t)(k / TREE_ITEMS) & 1u, abort_flag);
             if (!ok) break;
             const TreeItem it = ctl.item[j];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl.item_empty[j]);
             if (!it.valid) break;
-            // block-table entries of 32 pages in the lanes, the next 32 on their way (a tile's pages never straddle the two)
             const int page0 = it.first >> p.page_shift, pages = p.page_size < TREE_TILE ? TREE_TILE >> p.page_shift : 1;
-            auto look_up = [&](int from) {
-                const int pg = from + lane;
-                if (pg > (it.hi - 1) >> p.page_shift || pg < it.lo >> p.page_shift || it.hi <= it.lo) return -1;
-                const long long e = (long long)it.b * p.max_pages + pg;
-                return p.block_table ? p.block_table[e] : (int)e;
-            };
-            int base = page0, now = look_up(base), next = look_up(base + 32);
+            // (a tile's pages never straddle the 32 in the lanes and the next 32)
+            int base = page0, now = looked ? ahead : look_up(it.b, it.lo, it.hi, base), next = look_up(it.b, it.lo, it.hi, base + 32);
+            looked = false;
             for (int x = 0; x < it.tiles; ++x) {
                 const int t_x = it.first + x * TREE_TILE, t_box = t_x + piece * box_rows, row = t_box & (p.page_size - 1);
                 if ((t_x >> p.page_shift) + pages > base + 32) {
                     base += 32;
                     now = next;
-                    next = look_up(base + 32);
+                    next = look_up(it.b, it.lo, it.hi, base + 32);
                 }
                 const int entry = __shfl_sync(0xffffffffu, now, (t_box >> p.page_shift) - base);
                 const bool want = lane < boxes && t_box < it.hi && t_box + box_rows > it.lo;
@@ -556,15 +572,23 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                 __syncwarp();
                 if (e >= 0) tma_load_5d(ring + slot * TILE_BYTES + half * HALF_BYTES + piece * box_rows * 128, tm, &ctl.full[slot], 0, row, half, it.h, e, policy);
                 issued = n + x + 1;
+                const int j1 = (k + 1) % TREE_ITEMS;
+                if (!looked && __all_sync(0xffffffffu, mbar_test(&ctl.item_full[j1], (uint32_t)((k + 1) / TREE_ITEMS) & 1u))) {
+                    const TreeItem& it1 = ctl.item[j1];
+                    if (it1.valid) ahead = look_up(it1.b, it1.lo, it1.hi, it1.first >> p.page_shift);
+                    looked = true;
+                }
             }
             n += it.tiles;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.item_empty[j]);
             if (p.test_stall) break;
         }
       } else {
         // =============================== tensor-core warp: one thread issues all products ===============================
         if (elect_one()) {
             bool ok = true;
-            int n = 0, prev_n = 0;                                 // tiles before this item, and before the previous one
+            int n = 0, prev_n = 0, prev_odd = 0;                   // tiles before this item, and before the previous one; its parity
             uint32_t np[2] = {0, 0}, nsc[2] = {0, 0}, nq[2] = {0, 0};      // P tiles taken, S tiles computed per stream; queries per buffer
             bool held = false;                                     // stream 1's last products of the item before are still to come
             TreeItem it, prev;
@@ -595,11 +619,12 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                 if (last && (it.wide || it.q == 1)) tc_commit(&ctl.q_free[1]);
                 mbar_arrive(&ctl.s_full[s]);
             };
-            auto values = [&](const TreeItem& im, int n0, int s, int i) {     // O += P V of a stream's tile, quarter by quarter
+            // O += P V of a stream's tile, quarter by quarter; `odd`: the piece's parity
+            auto values = [&](const TreeItem& im, int n0, int odd, int s, int i) {
                 const int x = n0 + tree_tile_index(im, s, i), slot = KS + x % VS;
                 ok = pfx_wait(&ctl.full[slot], (uint32_t)(x / VS) & 1u, abort_flag);
                 const uint64_t b = v_desc + (uint32_t)(slot * (TILE_BYTES >> 4));
-                const uint32_t acc = tmem + O_COL + s * O_STRIDE;
+                const uint32_t acc = tmem + O_COL + ((FEW ? odd * 2 : 0) + s) * O_STRIDE;
                 if constexpr (FEW) {                               // O^T += V^T P^T
                     const uint64_t w = p_desc + (uint32_t)(s * (P_BYTES >> 4));
                     ok = ok && pfx_wait(&ctl.p_full[s][0], np[s] & 1u, abort_flag);
@@ -623,10 +648,10 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                 ++np[s];
                 if (!im.wide || s == 1) tc_commit(&ctl.empty[slot]);
                 if (BESIDE) tc_commit(&ctl.p_free[s]);
-                if (i == tree_stream_tiles(im, s) - 1) tc_commit(&ctl.o_full[s]);
+                if (i == tree_stream_tiles(im, s) - 1) tc_commit(&ctl.o_full[s][FEW ? odd : 0]);
             };
             auto release = [&]() {                                 // the held products, where there is nothing to put in front of them
-                if (held) values(prev, prev_n, 1, tree_stream_tiles(prev, 1) - 1);
+                if (held) values(prev, prev_n, prev_odd, 1, tree_stream_tiles(prev, 1) - 1);
                 held = false;
             };
             for (int k = 0; ok; ++k) {
@@ -648,16 +673,18 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                 if (ok && n1 > 0) scores(1, 0, --left == 0);
                 for (int i = 0; i < n0 && ok; ++i) {
                     if (BESIDE && i + 1 < n0) scores(0, i + 1, --left == 0);
-                    if (ok) values(it, n, 0, i);
+                    if (FEW && i == 0 && k >= 2) ok = ok && pfx_wait(&ctl.o_free[k & 1], (uint32_t)(k / 2 - 1) & 1u, abort_flag);      // the sums of the piece before the last are read
+                    if (ok) values(it, n, k & 1, 0, i);
                     if (!BESIDE && ok && i + 1 < n0) scores(0, i + 1, --left == 0);
                     if (!ok || i >= n1) break;
                     if (i + 1 == n0) { held = true; break; }       // behind the next item's first scores
                     if (BESIDE && i + 1 < n1) scores(1, i + 1, --left == 0);
-                    if (ok) values(it, n, 1, i);
+                    if (ok) values(it, n, k & 1, 1, i);
                     if (!BESIDE && ok && i + 1 < n1) scores(1, i + 1, --left == 0);
                 }
                 prev = it;
                 prev_n = n;
+                prev_odd = k & 1;
                 n += it.tiles;
             }
             if (ok) release();
@@ -667,8 +694,8 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
         }
         __syncwarp();
       }
-    } else {
-        if constexpr (!FEW) reg_grow<TREE_REGS_SOFTMAX>();
+    } else if (warp < 8) {
+        reg_grow<tree_regs_softmax<ROWS>()>();
         // =============================== softmax warps: S -> P, epilogue ===============================
         const int s = warp >> 2, w4 = warp & 3;                    // stream, quarter of its lanes
         const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
@@ -679,7 +706,7 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
         bool ok = true;
         uint32_t ns = 0, no1 = 0, nj = 0;                          // tiles of this stream, items with tiles of stream 1, joins so far
         auto join_sync = [&]() {                                   // with the other warps that join the streams
-            uint64_t* const bar = &ctl.join_sync[FEW ? 0 : w4];
+            uint64_t* const bar = &ctl.join_sync[w4];
             __syncwarp();
             if (lane == 0) mbar_arrive(bar);
             return pfx_warp_wait(bar, nj++ & 1u, abort_flag);
@@ -806,11 +833,11 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
 #pragma unroll 1
                             for (int c0 = 0; c0 < ROWS; c0 += 8) {
                                 uint32_t y[8];
-                                tmem_ld_32x8(o_tmem + s * O_STRIDE + c0, y);
+                                tmem_ld_32x8(o_tmem + ((k & 1) * 2 + s) * O_STRIDE + c0, y);
                                 tmem_ld_wait();
 #pragma unroll
                                 for (int u = 0; u < 8; ++u) y[u] = __float_as_uint(__uint_as_float(y[u]) * __shfl_sync(0xffffffffu, f, c0 + u));
-                                tmem_st_32x8(o_tmem + s * O_STRIDE + c0, y);
+                                tmem_st_32x8(o_tmem + ((k & 1) * 2 + s) * O_STRIDE + c0, y);
                             }
                             tmem_st_wait();
                         }
@@ -834,97 +861,16 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                     if (lane == 0) mbar_arrive(&ctl.p_full[s][0]);
                 }
                 if (!ok) break;
-                // ---- the piece's end: each stream takes half of the rows, all of their components ----
-                ok = pfx_warp_wait(&ctl.o_full[0], (uint32_t)k & 1u, abort_flag);
-                if (ok && tiles1 > 0) ok = pfx_warp_wait(&ctl.o_full[1], no1 & 1u, abort_flag);
-                if (!ok) break;
-                if (tiles1 > 0) ++no1;
-                tc_fence_after_sync();
-                float* const sums = reinterpret_cast<float*>(p_smem + s * P_BYTES);      // (the weights there are used up) [4 warps + 1][ROWS]
+                // ---- the piece's end: its references and sums of weights go to the warps that finish it ----
                 const float sum = across_lanes<ROWS, false>(l, lane);
+                if (k >= 1) ok = pfx_warp_wait(&ctl.sums_free, (uint32_t)(k - 1) & 1u, abort_flag);
+                if (!ok) break;
                 if (lane < ROWS) {
-                    sums[w4 * ROWS + lane] = sum;
-                    if (w4 == 0) sums[4 * ROWS + lane] = ref;
+                    ctl.col.sums[s][w4][lane] = sum;
+                    if (w4 == 0) ctl.col.ref[s][lane] = ref;
                 }
-                ok = join_sync();
-                if (!ok) break;
-                constexpr int H = ROWS / 2;
-                const int c = s * H + (lane & (H - 1)), node = fast_div(c, p.div_G);      // this lane's row
-                const bool exists = c < rows, both = tiles1 > 0;
-                const float* const sums0 = reinterpret_cast<const float*>(p_smem);
-                const float* const sums1 = reinterpret_cast<const float*>(p_smem + P_BYTES);
-                const float ref0 = sums0[4 * ROWS + c], ref1 = sums1[4 * ROWS + c], m_raw = fmaxf(ref0, ref1);
-                float f0 = ref0 == NEG_INF ? 0.f : fast_exp2((ref0 - m_raw) * sc), f1 = ref1 == NEG_INF || !both ? 0.f : fast_exp2((ref1 - m_raw) * sc);
-                float lsum = (sums0[c] + sums0[ROWS + c] + sums0[2 * ROWS + c] + sums0[3 * ROWS + c]) * f0 +
-                             (sums1[c] + sums1[ROWS + c] + sums1[2 * ROWS + c] + sums1[3 * ROWS + c]) * f1;
-                const int row = it.row0 + node;
-                const size_t orow = (size_t)row * p.Hq + it.h * p.G + (c - node * p.G);
-                const size_t prow = (size_t)it.slot * 256 + c;
-                const float m = m_raw == NEG_INF ? NEG_INF : m_raw * p.scale;
-                if (exists && *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) && tree_poisoned<D, BF16>(p, it, row, it.i0 + node)) {
-                    f0 = __int_as_float(0x7fc00000);
-                    f1 = 0.f;
-                }
-                float top = m, inv = 1.f;
-                if (it.whole && exists) {
-                    const float own = tree_join_host(p, orow, m, lsum, top);
-                    inv = lsum == 0.f ? 0.f : 1.f / lsum;
-                    f0 *= own * inv;
-                    f1 *= own * inv;
-                    if (p.lse && w4 == 0 && lane < H) p.lse[orow] = lsum == 0.f ? NEG_INF : top + logf(lsum);
-                }
-                if (!it.whole && exists && w4 == 0 && lane < H) { p.ws.m[prow] = m; p.ws.l[prow] = lsum; }
-                // lane l of tensor memory holds component l of the rows (128 components), or, for M = 64 products, lane 32 w + i
-                // holds component 16 w + i (i < 16; lanes 16-31 of each quarter unused)
-                const int d = D == 128 ? r : w4 * 16 + lane;
-                const bool holds = D == 128 || lane < 16;
-                const int to_row = (int)orow;
-#pragma unroll 1
-                for (int c0 = 0; c0 < H && s * H + c0 < rows; c0 += 8) {
-                    uint32_t y0[8], y1[8];
-                    __syncwarp();                                  // (tensor memory is read by whole warps)
-                    tmem_ld_32x8(o_tmem + s * H + c0, y0);
-                    tmem_ld_32x8(o_tmem + (both ? O_STRIDE : 0) + s * H + c0, y1);
-                    tmem_ld_wait();
-                    float y[8];
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        const float g0 = __shfl_sync(0xffffffffu, f0, c0 + u), g1 = __shfl_sync(0xffffffffu, f1, c0 + u);
-                        y[u] = g0 == 0.f ? 0.f : __uint_as_float(y0[u]) * g0;
-                        if (g1 != 0.f) y[u] = fmaf(__uint_as_float(y1[u]), g1, y[u]);
-                    }
-                    const int left = min(8, rows - s * H - c0);
-                    if (it.whole) {
-                        for (int z = 0; z < p.src.n; ++z)
-#pragma unroll 1
-                            for (int e = 0; e < p.src.nc[z]; ++e) {          // (an empty partial's o row is not read)
-                                float w = 0.f;
-                                if (exists) {
-                                    const float hm = p.src.m[z][orow * p.src.nc[z] + e];
-                                    if (hm != NEG_INF) w = fast_exp2((hm - top) * 1.4426950408889634f) * inv;
-                                }
-#pragma unroll
-                                for (int u = 0; u < 8; ++u) {
-                                    const float wu = __shfl_sync(0xffffffffu, w, c0 + u);
-                                    const size_t q = (size_t)__shfl_sync(0xffffffffu, to_row, c0 + u) * p.src.nc[z] + e;
-                                    if (wu != 0.f && u < left && holds) y[u] = fmaf(p.src.o[z][q * D + d], wu, y[u]);
-                                }
-                            }
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            const size_t q = (size_t)__shfl_sync(0xffffffffu, to_row, c0 + u);
-                            if (u < left && holds) p.out[q * D + d] = (uint16_t)pack2<BF16>(y[u], 0.f);
-                        }
-                    } else {
-                        float* const dst = p.ws.o + ((size_t)it.slot * 256 + s * H + c0) * D + d;
-#pragma unroll
-                        for (int u = 0; u < 8; ++u)
-                            if (u < left && holds) st_global_hint(dst + u * D, y[u], keep);
-                    }
-                }
-                tc_fence_before_sync();
-                ok = join_sync();                                  // both streams' sums are read: either may begin anew
-                if (!ok) break;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl.sums_full);
             } else {
                 // ---- a thread is a row ----
                 const uint32_t p_tmem = tmem + P_COL + s * P_STRIDE + lanes;
@@ -1044,8 +990,8 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
                 if (!ok) break;
                 // ---- the piece's end.  Stream 0 has a tile always; where the streams share their rows, each takes half of the
                 // components of both streams' sums ----
-                if (it.wide ? s == 0 : true) ok = pfx_warp_wait(&ctl.o_full[0], (uint32_t)k & 1u, abort_flag);
-                if (ok && tiles1 > 0 && (it.wide ? s == 1 : true)) ok = pfx_warp_wait(&ctl.o_full[1], no1 & 1u, abort_flag);
+                if (it.wide ? s == 0 : true) ok = pfx_warp_wait(&ctl.o_full[0][0], (uint32_t)k & 1u, abort_flag);
+                if (ok && tiles1 > 0 && (it.wide ? s == 1 : true)) ok = pfx_warp_wait(&ctl.o_full[1][0], no1 & 1u, abort_flag);
                 if (!ok) break;
                 if (tiles1 > 0) ++no1;
                 tc_fence_after_sync();
@@ -1140,6 +1086,111 @@ __global__ void __launch_bounds__(TREE_THREADS, 1) tree_kernel(const __grid_cons
             tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl.item_empty[j]);
+        }
+    } else if constexpr (FEW) {
+        if (warp >= TREE_END_WARP) {
+        reg_shrink<TREE_REGS_OTHER>();
+        // =============================== (few rows) the pieces' ends: sums of both streams, the host's partials, the result ===============================
+        cudaGridDependencySynchronize();
+        const int w4 = warp & 3, r = w4 * 32 + lane;
+        const float sc = p.scale_log2;
+        const uint64_t keep = l2_evict_last_policy();
+        uint32_t no1[2] = {0, 0};                                  // even and odd pieces with tiles of stream 1 so far
+        bool ok = true;
+        for (int k = 0; ok; ++k) {
+            const int j = k % TREE_ITEMS;
+            ok = pfx_warp_wait(&ctl.item_full[j], (uint32_t)(k / TREE_ITEMS) & 1u, abort_flag);
+            if (!ok) break;
+            const TreeItem it = ctl.item[j];
+            if (!it.valid) break;
+            const int tiles1 = tree_stream_tiles(it, 1), rows = it.nodes * p.G;
+            const uint32_t o_tmem = tmem + O_COL + (k & 1) * 2 * O_STRIDE + ((uint32_t)(w4 * 32) << 16);      // of stream 0
+            ok = pfx_warp_wait(&ctl.sums_full, (uint32_t)k & 1u, abort_flag);
+            if (!ok) break;
+            const int c = lane & (ROWS - 1), node = fast_div(c, p.div_G);       // this lane's row
+            const bool exists = c < rows, both = tiles1 > 0;
+            const float ref0 = ctl.col.ref[0][c], ref1 = ctl.col.ref[1][c], m_raw = fmaxf(ref0, ref1);
+            float f0 = ref0 == NEG_INF ? 0.f : fast_exp2((ref0 - m_raw) * sc), f1 = ref1 == NEG_INF || !both ? 0.f : fast_exp2((ref1 - m_raw) * sc);
+            float lsum = (ctl.col.sums[0][0][c] + ctl.col.sums[0][1][c] + ctl.col.sums[0][2][c] + ctl.col.sums[0][3][c]) * f0 +
+                         (ctl.col.sums[1][0][c] + ctl.col.sums[1][1][c] + ctl.col.sums[1][2][c] + ctl.col.sums[1][3][c]) * f1;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.sums_free);
+            const int row = it.row0 + node;
+            const size_t orow = (size_t)row * p.Hq + it.h * p.G + (c - node * p.G);
+            const size_t prow = (size_t)it.slot * 256 + c;
+            const float m = m_raw == NEG_INF ? NEG_INF : m_raw * p.scale;
+            if (exists && *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) && tree_poisoned<D, BF16>(p, it, row, it.i0 + node)) {
+                f0 = __int_as_float(0x7fc00000);
+                f1 = 0.f;
+            }
+            float top = m, inv = 1.f;
+            if (it.whole && exists) {
+                const float own = tree_join_host(p, orow, m, lsum, top);
+                inv = lsum == 0.f ? 0.f : 1.f / lsum;
+                f0 *= own * inv;
+                f1 *= own * inv;
+                if (p.lse && w4 == 0 && lane < ROWS) p.lse[orow] = lsum == 0.f ? NEG_INF : top + logf(lsum);
+            }
+            if (!it.whole && exists && w4 == 0 && lane < ROWS) { p.ws.m[prow] = m; p.ws.l[prow] = lsum; }
+            // lane l of tensor memory holds component l of the rows (128 components), or, for M = 64 products, lane 32 w + i
+            // holds component 16 w + i (i < 16; lanes 16-31 of each quarter unused)
+            const int d = D == 128 ? r : w4 * 16 + lane;
+            const bool holds = D == 128 || lane < 16;
+            const int to_row = (int)orow;
+            ok = pfx_warp_wait(&ctl.o_full[0][k & 1], (uint32_t)(k / 2) & 1u, abort_flag);
+            if (ok && both) ok = pfx_warp_wait(&ctl.o_full[1][k & 1], ((k & 1 ? no1[1]++ : no1[0]++)) & 1u, abort_flag);
+            if (!ok) break;
+            tc_fence_after_sync();
+#pragma unroll 1
+            for (int c0 = 0; c0 < rows; c0 += 8) {
+                uint32_t y0[8], y1[8];
+                __syncwarp();                                  // (tensor memory is read by whole warps)
+                tmem_ld_32x8(o_tmem + c0, y0);
+                tmem_ld_32x8(o_tmem + (both ? O_STRIDE : 0) + c0, y1);
+                tmem_ld_wait();
+                float y[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const float g0 = __shfl_sync(0xffffffffu, f0, c0 + u), g1 = __shfl_sync(0xffffffffu, f1, c0 + u);
+                    y[u] = g0 == 0.f ? 0.f : __uint_as_float(y0[u]) * g0;
+                    if (g1 != 0.f) y[u] = fmaf(__uint_as_float(y1[u]), g1, y[u]);
+                }
+                const int left = min(8, rows - c0);
+                if (it.whole) {
+                    for (int z = 0; z < p.src.n; ++z)
+#pragma unroll 1
+                        for (int e = 0; e < p.src.nc[z]; ++e) {          // (an empty partial's o row is not read)
+                            float w = 0.f;
+                            if (exists) {
+                                const float hm = p.src.m[z][orow * p.src.nc[z] + e];
+                                if (hm != NEG_INF) w = fast_exp2((hm - top) * 1.4426950408889634f) * inv;
+                            }
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) {
+                                const float wu = __shfl_sync(0xffffffffu, w, c0 + u);
+                                const size_t q = (size_t)__shfl_sync(0xffffffffu, to_row, c0 + u) * p.src.nc[z] + e;
+                                if (wu != 0.f && u < left && holds) y[u] = fmaf(p.src.o[z][q * D + d], wu, y[u]);
+                            }
+                        }
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const size_t q = (size_t)__shfl_sync(0xffffffffu, to_row, c0 + u);
+                        if (u < left && holds) p.out[q * D + d] = (uint16_t)pack2<BF16>(y[u], 0.f);
+                    }
+                } else {
+                    float* const dst = p.ws.o + ((size_t)it.slot * 256 + c0) * D + d;
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+                        if (u < left && holds) st_global_hint(dst + u * D, y[u], keep);
+                }
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&ctl.o_free[k & 1]);
+                mbar_arrive(&ctl.item_empty[j]);
+            }
+        }
         }
     }
     __syncthreads();
