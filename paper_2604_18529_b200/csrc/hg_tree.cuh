@@ -22,13 +22,21 @@
 // it.  So long and short sequences balance by themselves; a CTA finishes the units that lie wholly in its stretch, the host's
 // partials included, and leaves softmax partials of the at most two that its ends cut, which tree_merge_kernel joins.
 //
-// Roles: warps 0-7 softmax and epilogue; 8 and 9 load K and V tiles (TMA, a ring each; one warp for both would leave free slots
-// waiting behind taken ones: 204 instead of 168 us at one new token, 8 sequences, 64/8 heads, 32 768 tokens); 10 issues the products; 11 finds the CTA's stretch, publishes its pieces up to four ahead and loads their queries (TMA,
-// a box of G heads by whole tokens).  Every wait is bounded.
+// Roles: warps 0-7 softmax and (many rows) epilogue; 8 and 9 load K and V tiles (TMA, a ring each; one warp for both would leave
+// free slots waiting behind taken ones: 204 instead of 168 us at one new token, 8 sequences, 64/8 heads, 32 768 tokens); 10 issues
+// the products; 11 finds the CTA's stretch, publishes its pieces up to four ahead and loads their queries (TMA, a box of G heads by
+// whole tokens); 12-15 (few rows) finish the pieces while the softmax warps are at the next.  Every wait is bounded.
+//
+// Measured (K and V larger than the L2), us, in a loop / the floor at the measured rates: one new token, 8 sequences, 64/8 heads,
+// 32 768 tokens: 168 / 167; the same with 64 components and twice the tokens: 168 / 167; 8 new tokens: 182 / 167, 16: 186 / 168
+// (many rows); 32 and 131 072 tokens, one sequence: 157 / 84 (bound by the exponentials and products of a pair of tiles, 3400
+// cycles where the products take 2048, at 1.55 GHz under the power cap).
 #pragma once
 
 #include <cuda_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "hg_device.cuh"
 #include "hg_partial.cuh"
@@ -198,6 +206,7 @@ struct TreeCtl {
     long long part[4];
     long long start_base;
     int start_b;
+    int left[TREE_ITEMS];            // (few rows) products of S still to issue, by item
     int issued[2], q_issued[2];      // tiles of K and V, and items' queries by buffer, that were requested (for the unwinding)
 };
 
@@ -586,17 +595,110 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
         }
       } else {
         // =============================== tensor-core warp: one thread issues all products ===============================
-        if (elect_one()) {
+        if constexpr (FEW) {
+          if (elect_one()) {
+            // Few rows: whatever is ready next, looked for in turn.  Each stream goes from tile to tile and from item to item without
+            // a stop: S^T as soon as K and Q are there and the S before is read, at most two tiles ahead of O^T, which needs P and V
+            struct Stream {
+                int k, i, tiles, total, base;      // next to score: item, tile; the item's tiles of this stream and of both, its first tile
+                bool loaded, end;
+                uint32_t scored, valued;           // tiles so far
+                int x0, x1;                        // the tiles scored and not valued (even and odd ones): number in load order,
+                uint32_t about0, about1;           // and bit 0: first of its item, 1: last, from 2 on the item
+            };
+            Stream st0 = {0, 0, 0, 0, 0, false, false, 0, 0, 0, 0, 0, 0}, st1 = st0;
+            uint32_t seen = 0;                                     // items loaded by one stream (bits)
+            const uint64_t q_desc = tc_smem_desc(smem_u32(q_smem), 16u, 1024u, 2u), k_desc = tc_smem_desc(smem_u32(ring), 16u, 1024u, 2u);
+            const uint64_t v_desc = tc_smem_desc(smem_u32(ring), HALF_BYTES, 1024u, 2u);
+            const uint64_t p_desc = tc_smem_desc(smem_u32(p_smem), 128u, 2048u, 0u);       // 8 tokens 128 bytes apart, 8 rows 2048
+            // A barrier's phase is looked at only when the one before is known to be over: a ring slot's use before last may be the
+            // other stream's, so a stream is never a whole ring ahead of the other
+            auto step = [&](auto which) -> bool {                  // one product of a stream, if there is one to issue
+                constexpr int s = decltype(which)::value;
+                Stream& t = s ? st1 : st0;
+                const Stream& u = s ? st0 : st1;
+                const int u_score = u.end ? 0x7fffffff : u.loaded ? u.base + 2 * u.i + (1 - s) : u.base;     // the other's next tiles
+                const int u_value = u.valued == u.scored ? u_score : u.valued & 1 ? u.x1 : u.x0;
+                if (t.valued != t.scored) {                        // O^T += V^T P^T
+                    const int x = t.valued & 1 ? t.x1 : t.x0, slot = KS + x % VS;
+                    const uint32_t about = t.valued & 1 ? t.about1 : t.about0;
+                    const int item = (int)(about >> 2);
+                    if (x - u_value < VS && mbar_test(&ctl.p_full[s][0], t.valued & 1u) && mbar_test(&ctl.full[slot], (uint32_t)(x / VS) & 1u) &&
+                        (!(about & 1u) || item < 2 || mbar_test(&ctl.o_free[item & 1], (uint32_t)(item / 2 - 1) & 1u))) {
+                        tc_fence_after_sync();
+                        const uint64_t v = v_desc + (uint32_t)(slot * (TILE_BYTES >> 4)), w = p_desc + (uint32_t)(s * (P_BYTES >> 4));
+                        const uint32_t acc = tmem + O_COL + ((item & 1) * 2 + s) * O_STRIDE;
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk)             // 16 tokens
+                            tc_mma_f16_ss(acc, v + (uint32_t)(kk * 2048 >> 4), w + (uint32_t)(kk * 256 >> 4), IDESC_O, kk || !(about & 1u) ? 1u : 0u);
+                        tc_commit(&ctl.empty[slot]);
+                        tc_commit(&ctl.p_free[s]);
+                        if (about & 2u) tc_commit(&ctl.o_full[s][item & 1]);
+                        ++t.valued;
+                        return true;
+                    }
+                }
+                while (!t.loaded && !t.end) {                      // the next item with a tile for this stream, if it is published
+                    const int j = t.k % TREE_ITEMS;
+                    if (!mbar_test(&ctl.item_full[j], (uint32_t)(t.k / TREE_ITEMS) & 1u)) break;
+                    const volatile TreeItem& it = ctl.item[j];
+                    if (!it.valid) { t.end = true; break; }
+                    t.total = it.tiles;
+                    t.tiles = (t.total + 1 - s) / 2;
+                    t.i = 0;
+                    if ((seen >> j) & 1u) mbar_arrive(&ctl.item_empty[j]);       // both streams have it
+                    else ctl.left[j] = t.total;
+                    seen ^= 1u << j;
+                    if (t.tiles > 0) t.loaded = true;
+                    else { t.base += t.total; ++t.k; }
+                }
+                if (!t.loaded || t.scored - t.valued >= 2) return false;
+                const int x = t.base + 2 * t.i + s, slot = x % KS, j = t.k % TREE_ITEMS;
+                // (x against u_value: the softmax warps may look at the tile's V slot)
+                if (x - u_score >= KS || x - u_value >= VS || (t.scored > 0 && !mbar_test(&ctl.s_read[s], (t.scored - 1) & 1u)) ||
+                    !mbar_test(&ctl.full[slot], (uint32_t)(x / KS) & 1u)) return false;
+                // (items take the two Q buffers in turn; the one before last is over when the other stream is at most one behind)
+                if (t.i == 0 && ((!u.end && t.k - u.k >= 2) || !mbar_test(&ctl.q_full[t.k & 1], (uint32_t)(t.k / 2) & 1u))) return false;
+                ctl.stream_bad[s] = ctl.bad[x & 15];               // S^T = K Q^T
+                tc_fence_after_sync();
+                const uint64_t kd = k_desc + (uint32_t)(slot * (TILE_BYTES >> 4)), qd = q_desc + (uint32_t)((t.k & 1) * (Q_BYTES >> 4));
+                const uint32_t acc = tmem + s * S_STRIDE;
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk)                // 16 components: 32 bytes of a 128-byte row, halves apart
+                    tc_mma_f16_ss(acc, kd + ((uint32_t)((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4), qd + ((uint32_t)((kk >> 2) * Q_HALF_BYTES + (kk & 3) * 32) >> 4),
+                                  IDESC_S, kk ? 1u : 0u);
+                tc_commit(&ctl.s_full[s]);
+                tc_commit(&ctl.empty[slot]);
+                if (--ctl.left[j] == 0) tc_commit(&ctl.q_free[t.k & 1]);
+                mbar_arrive(&ctl.s_full[s]);
+                const uint32_t about = (t.i == 0 ? 1u : 0u) | (t.i == t.tiles - 1 ? 2u : 0u) | (uint32_t)t.k << 2;
+                if (t.scored & 1) { t.x1 = x; t.about1 = about; }
+                else { t.x0 = x; t.about0 = about; }
+                ++t.scored;
+                if (++t.i == t.tiles) { t.loaded = false; t.base += t.total; ++t.k; }
+                return true;
+            };
+            long long since = clock64();
+            for (;;) {
+                const bool first = step(std::integral_constant<int, 0>()), second = step(std::integral_constant<int, 1>());
+                if (st0.end && st1.end && st0.valued == st0.scored && st1.valued == st1.scored) break;
+                if (first || second) since = clock64();
+                else if (*abort_flag || clock64() - since > PFX_WAIT_CYCLES) { *abort_flag = 1; break; }
+            }
+            int none = 0;                                          // nothing is in flight when the tensor memory is given back
+            tc_commit(&ctl.drain);
+            pfx_wait(&ctl.drain, 0u, &none);
+          }
+        } else if (elect_one()) {
             bool ok = true;
-            int n = 0, prev_n = 0, prev_odd = 0;                   // tiles before this item, and before the previous one; its parity
+            int n = 0, prev_n = 0;                                 // tiles before this item, and before the previous one
             uint32_t np[2] = {0, 0}, nsc[2] = {0, 0}, nq[2] = {0, 0};      // P tiles taken, S tiles computed per stream; queries per buffer
             bool held = false;                                     // stream 1's last products of the item before are still to come
             TreeItem it, prev;
             const uint64_t q_desc = tc_smem_desc(smem_u32(q_smem), 16u, 1024u, 2u);
             const uint64_t k_desc = tc_smem_desc(smem_u32(ring), 16u, 1024u, 2u);
             const uint64_t v_desc = tc_smem_desc(smem_u32(ring), HALF_BYTES, 1024u, 2u);
-            const uint64_t p_desc = tc_smem_desc(smem_u32(p_smem), 128u, 2048u, 0u);       // 8 tokens 128 bytes apart, 8 rows 2048
-            auto scores = [&](int s, int i, bool last) {           // S = Q K^T (S^T = K Q^T) of a stream's tile
+            auto scores = [&](int s, int i, bool last) {           // S = Q K^T of a stream's tile
                 const int x = n + tree_tile_index(it, s, i), slot = x % KS;
                 ok = pfx_wait(&ctl.full[slot], (uint32_t)(x / KS) & 1u, abort_flag);
                 if (BESIDE && ok && nsc[s] > 0) ok = pfx_wait(&ctl.s_read[s], (nsc[s] - 1) & 1u, abort_flag);
@@ -610,8 +712,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                 for (int kk = 0; kk < D / 16; ++kk) {              // 16 components: 32 bytes of a 128-byte row, halves apart
                     const uint32_t off_k = (uint32_t)((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4;
                     const uint32_t off_q = (uint32_t)((kk >> 2) * Q_HALF_BYTES + (kk & 3) * 32) >> 4;
-                    if constexpr (FEW) tc_mma_f16_ss(acc, b + off_k, a + off_q, IDESC_S, kk ? 1u : 0u);
-                    else tc_mma_f16_ss(acc, a + off_q, b + off_k, IDESC_S, kk ? 1u : 0u);
+                    tc_mma_f16_ss(acc, a + off_q, b + off_k, IDESC_S, kk ? 1u : 0u);
                 }
                 tc_commit(&ctl.s_full[s]);
                 if (!it.wide || s == 1) tc_commit(&ctl.empty[slot]);
@@ -619,39 +720,28 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                 if (last && (it.wide || it.q == 1)) tc_commit(&ctl.q_free[1]);
                 mbar_arrive(&ctl.s_full[s]);
             };
-            // O += P V of a stream's tile, quarter by quarter; `odd`: the piece's parity
-            auto values = [&](const TreeItem& im, int n0, int odd, int s, int i) {
+            auto values = [&](const TreeItem& im, int n0, int s, int i) {     // O += P V of a stream's tile, quarter by quarter
                 const int x = n0 + tree_tile_index(im, s, i), slot = KS + x % VS;
                 ok = pfx_wait(&ctl.full[slot], (uint32_t)(x / VS) & 1u, abort_flag);
                 const uint64_t b = v_desc + (uint32_t)(slot * (TILE_BYTES >> 4));
-                const uint32_t acc = tmem + O_COL + ((FEW ? odd * 2 : 0) + s) * O_STRIDE;
-                if constexpr (FEW) {                               // O^T += V^T P^T
-                    const uint64_t w = p_desc + (uint32_t)(s * (P_BYTES >> 4));
-                    ok = ok && pfx_wait(&ctl.p_full[s][0], np[s] & 1u, abort_flag);
+                const uint32_t acc = tmem + O_COL + s * O_STRIDE;
+                const uint32_t a = tmem + P_COL + s * P_STRIDE;
+#pragma unroll
+                for (int part = 0; part < 4; ++part) {
+                    ok = ok && pfx_wait(&ctl.p_full[s][part], np[s] & 1u, abort_flag);
                     if (!ok) return;
                     tc_fence_after_sync();
 #pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)                 // 16 tokens
-                        tc_mma_f16_ss(acc, b + (uint32_t)(kk * 2048 >> 4), w + (uint32_t)(kk * 256 >> 4), IDESC_O, kk ? 1u : (i ? 1u : 0u));
-                } else {
-                    const uint32_t a = tmem + P_COL + s * P_STRIDE;
-#pragma unroll
-                    for (int part = 0; part < 4; ++part) {
-                        ok = ok && pfx_wait(&ctl.p_full[s][part], np[s] & 1u, abort_flag);
-                        if (!ok) return;
-                        tc_fence_after_sync();
-#pragma unroll
-                        for (int kk = part * 2; kk < part * 2 + 2; ++kk)       // 16 tokens: 8 columns of P
-                            tc_mma_f16_ts(acc, a + kk * 8, b + (uint32_t)(kk * 2048 >> 4), IDESC_O, kk ? 1u : (i ? 1u : 0u));
-                    }
+                    for (int kk = part * 2; kk < part * 2 + 2; ++kk)       // 16 tokens: 8 columns of P
+                        tc_mma_f16_ts(acc, a + kk * 8, b + (uint32_t)(kk * 2048 >> 4), IDESC_O, kk ? 1u : (i ? 1u : 0u));
                 }
                 ++np[s];
                 if (!im.wide || s == 1) tc_commit(&ctl.empty[slot]);
                 if (BESIDE) tc_commit(&ctl.p_free[s]);
-                if (i == tree_stream_tiles(im, s) - 1) tc_commit(&ctl.o_full[s][FEW ? odd : 0]);
+                if (i == tree_stream_tiles(im, s) - 1) tc_commit(&ctl.o_full[s][0]);
             };
             auto release = [&]() {                                 // the held products, where there is nothing to put in front of them
-                if (held) values(prev, prev_n, prev_odd, 1, tree_stream_tiles(prev, 1) - 1);
+                if (held) values(prev, prev_n, 1, tree_stream_tiles(prev, 1) - 1);
                 held = false;
             };
             for (int k = 0; ok; ++k) {
@@ -673,18 +763,16 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                 if (ok && n1 > 0) scores(1, 0, --left == 0);
                 for (int i = 0; i < n0 && ok; ++i) {
                     if (BESIDE && i + 1 < n0) scores(0, i + 1, --left == 0);
-                    if (FEW && i == 0 && k >= 2) ok = ok && pfx_wait(&ctl.o_free[k & 1], (uint32_t)(k / 2 - 1) & 1u, abort_flag);      // the sums of the piece before the last are read
-                    if (ok) values(it, n, k & 1, 0, i);
+                    if (ok) values(it, n, 0, i);
                     if (!BESIDE && ok && i + 1 < n0) scores(0, i + 1, --left == 0);
                     if (!ok || i >= n1) break;
                     if (i + 1 == n0) { held = true; break; }       // behind the next item's first scores
                     if (BESIDE && i + 1 < n1) scores(1, i + 1, --left == 0);
-                    if (ok) values(it, n, k & 1, 1, i);
+                    if (ok) values(it, n, 1, i);
                     if (!BESIDE && ok && i + 1 < n1) scores(1, i + 1, --left == 0);
                 }
                 prev = it;
                 prev_n = n;
-                prev_odd = k & 1;
                 n += it.tiles;
             }
             if (ok) release();
