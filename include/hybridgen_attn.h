@@ -55,8 +55,8 @@ typedef enum hg_dtype { HG_DTYPE_F16 = 0, HG_DTYPE_BF16 = 1 } hg_dtype;
 
 /* bits of hg_attn_desc.flags */
 #define HG_FLAG_NONE 0u
-#define HG_FLAG_TEST_STALL 1u /* testing aid: the loader of hg_attn_partial, hg_attn_prefix_partial or
-                                 hg_kv_read_probe never fills a
+#define HG_FLAG_TEST_STALL 1u /* testing aid: the loader of hg_attn_partial, hg_attn_prefix_partial,
+                                 hg_attn_decode_tree or hg_kv_read_probe never fills a
                                  stage, so every wait runs into its time limit (about 2 s); the call then
                                  reports HG_DEV_WAIT_TIMEOUT through *status and returns normally */
 
@@ -88,7 +88,9 @@ typedef enum hg_dtype { HG_DTYPE_F16 = 0, HG_DTYPE_BF16 = 1 } hg_dtype;
                                  read and its tokens were left out of the partial, as if they were not resident */
 #define HG_DEV_RANGE 4        /* a slice reached past max_pages * page_size tokens, the end of its block-table row:
                                  it was cut there (the partials cover [tok_begin, max_pages * page_size)).  Of the
-                                 page operations: a row number or a position outside the block table */
+                                 page operations and the operators on several new
+                                 tokens: a row number or a position outside the block
+                                 table, or what their own comments say */
 #define HG_DEV_NO_PAGE 8      /* hg_kv_reserve ran out of free pages (n_ready says what it could serve) */
 
 /*
@@ -607,7 +609,8 @@ hg_status hg_rope(const void* x, void* y, const int32_t* pos, int32_t num_heads,
 
 /*
  * hg_rope of a step's queries and keys, with the keys and values going to their places in the pool.
- *   q, q_out      dev 16-bit [N][Hq][D]; both NULL: keys and values only.  q_out may be q with the same stride
+ *   q, q_out      dev 16-bit [N][Hq][D]; both NULL: keys and values only.  q_out may be q with the same stride, but overlaps no
+ *                 other input (rows of equal strides may lie between one another: parts of a fused projection's output)
  *   k_new, v_new  dev 16-bit [N][Hkv][D]
  *   pos           dev int32 [N]
  *   slot          dev int64 [N] (tok_slot of hg_kv_slots): no place twice; a row with a negative one is not stored, one outside
@@ -667,7 +670,7 @@ typedef struct hg_tree_desc {
  *   seq_lens   dev int32 [B]  cached tokens, without the new ones
  *   tok_begin  dev int32 [B]  first cached token that the GPU holds (clipped to [0, seq_len]), or NULL for 0
  *   host_partials  sources as in hg_attn_merge, with rows in the place of sequences: o [N][Hq][nc][D], m and l [N][Hq][nc]
- *   out        dev 16-bit [N][Hq][D], 16-byte aligned: dtype as desc->dtype (what the next projection takes)
+ *   out        dev 16-bit [N][Hq][D], 16-byte aligned: dtype as desc->dtype (what the next projection takes).  Not q's memory
  *   lse        dev float [N][Hq] (may be NULL)
  * Rows beyond cu_nodes[B] are neither read nor written.  A sequence with more than max_nodes tokens, or whose rows do not lie
  * in [0, N), is cut to what fits; positions beyond the block-table row are left out (HG_DEV_RANGE each).  A page that is

@@ -32,12 +32,6 @@ static hg_status launch_draft(void (*kern)(P), dim3 grid, unsigned threads, int 
     return HG_OK;
 }
 
-// Two arrays that share memory.
-static bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return a && b && a_bytes && b_bytes && x < y + b_bytes && y < x + a_bytes;
-}
-
 static hg_status check_rope(const hg_rope_desc* r, int head_dim) {
     if (!r || r->struct_size < sizeof(hg_rope_desc)) return HG_ERR_INVALID_ARG;
     if (r->num_rows < 1 || r->rot_dim < 2 || r->rot_dim > head_dim || !r->freq) return HG_ERR_INVALID_ARG;
@@ -128,7 +122,9 @@ hg_status hg_rope(const void* x, void* y, const int32_t* pos, int32_t num_heads,
     memset(&p, 0, sizeof p);
     p.q_stride = row_stride(rope->q_stride, num_heads, head_dim);
     p.q_out_stride = row_stride(rope->q_out_stride, num_heads, head_dim);
-    if (p.q_stride < 0 || p.q_out_stride < 0 || (x == y && p.q_stride != p.q_out_stride)) return HG_ERR_INVALID_ARG;
+    if (p.q_stride < 0 || p.q_out_stride < 0) return HG_ERR_INVALID_ARG;
+    const int64_t width = (int64_t)num_heads * head_dim, n = rope->num_rows;
+    if (!(x == y && p.q_stride == p.q_out_stride) && rows_overlap(x, p.q_stride, width, y, p.q_out_stride, width, n)) return HG_ERR_INVALID_ARG;
     p.q = static_cast<const uint16_t*>(x); p.q_out = static_cast<uint16_t*>(y); p.pos = pos;
     return run_rope(p, num_heads, 0, head_dim, dtype == HG_DTYPE_BF16, rope, stream);
 }
@@ -150,8 +146,11 @@ hg_status hg_kv_append_rope(const void* q, const void* k_new, const void* v_new,
     p.q_out_stride = row_stride(rope->q_out_stride, Hq, D);
     p.k_stride = row_stride(rope->k_stride, Hkv, D);
     p.v_stride = row_stride(rope->v_stride, Hkv, D);
-    if (p.q_stride < 0 || p.q_out_stride < 0 || p.k_stride < 0 || p.v_stride < 0 || (q && q == q_out && p.q_stride != p.q_out_stride))
-        return HG_ERR_INVALID_ARG;
+    if (p.q_stride < 0 || p.q_out_stride < 0 || p.k_stride < 0 || p.v_stride < 0) return HG_ERR_INVALID_ARG;
+    const int64_t width = (int64_t)Hq * D, kv_width = (int64_t)Hkv * D, n = rope->num_rows;
+    if (q && ((!(q == q_out && p.q_stride == p.q_out_stride) && rows_overlap(q, p.q_stride, width, q_out, p.q_out_stride, width, n)) ||
+              rows_overlap(k_new, p.k_stride, kv_width, q_out, p.q_out_stride, width, n) ||
+              rows_overlap(v_new, p.v_stride, kv_width, q_out, p.q_out_stride, width, n))) return HG_ERR_INVALID_ARG;
     p.q = static_cast<const uint16_t*>(q); p.q_out = static_cast<uint16_t*>(q_out);
     p.k = static_cast<const uint16_t*>(k_new); p.v = static_cast<const uint16_t*>(v_new);
     p.pv = pool_view(desc, k_cache, v_cache);

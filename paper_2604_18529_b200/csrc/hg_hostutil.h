@@ -68,6 +68,20 @@ inline hg_status check_desc(const hg_attn_desc* d, bool need_kv) {
     return HG_OK;
 }
 
+// Two arrays that share memory.
+inline bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && a_bytes && b_bytes && x < y + b_bytes && y < x + a_bytes;
+}
+// Two packed tensors of n rows, `width` 16-bit elements wide and `stride` apart, that share memory.  Rows of the same stride may lie
+// between one another (parts of a fused projection's output).
+inline bool rows_overlap(const void* a, int64_t a_stride, int64_t a_width, const void* b, int64_t b_stride, int64_t b_width, int64_t n) {
+    if (!overlap(a, (size_t)((n - 1) * a_stride + a_width) * 2, b, (size_t)((n - 1) * b_stride + b_width) * 2)) return false;
+    if (a_stride != b_stride || n == 1) return true;
+    const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a)) / 2, d = (apart % b_stride + b_stride) % b_stride;
+    return d < a_width || d + b_width > b_stride;
+}
+
 // ---- tensor maps -------------------------------------------------------------------------------------
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,

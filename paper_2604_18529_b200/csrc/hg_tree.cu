@@ -127,6 +127,8 @@ hg_status hg_attn_decode_tree(const void* q, const void* k_cache, const void* v_
             return HG_ERR_INVALID_ARG;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HG_ERR_INVALID_ARG;
     if (workspace_bytes < hg_attn_tree_workspace_bytes(desc, tree)) return HG_ERR_WORKSPACE;
+    const int64_t q_width = (int64_t)desc->num_q_heads * desc->head_dim;       // (rows of out are written while others' q is still read)
+    if (rows_overlap(q, tree->q_stride ? tree->q_stride : q_width, q_width, out, q_width, q_width, tree->num_rows)) return HG_ERR_INVALID_ARG;
     TreeParams p;
     memset(&p, 0, sizeof p);
     p.v = static_cast<const uint16_t*>(v_cache);
@@ -155,7 +157,7 @@ hg_status hg_attn_decode_tree(const void* q, const void* k_cache, const void* v_
     p.ws.cut = reinterpret_cast<TreeCut*>(ws); p.ws.valid = reinterpret_cast<int32_t*>(ws + w.valid);
     p.ws.o = reinterpret_cast<float*>(ws + w.o); p.ws.m = reinterpret_cast<float*>(ws + w.m); p.ws.l = reinterpret_cast<float*>(ws + w.l);
     CUtensorMap tq, tk, tv;
-    st = make_query_map(desc, p, tree->q_stride ? tree->q_stride : (int64_t)p.Hq * desc->head_dim, q, &tq);
+    st = make_query_map(desc, p, tree->q_stride ? tree->q_stride : q_width, q, &tq);
     if (st != HG_OK) return st;
     st = make_tile_maps(desc, k_cache, v_cache, TREE_TILE, &tk, &tv);
     if (st != HG_OK) return st;

@@ -55,7 +55,7 @@ def rope(**over):
 
 
 def decode(lib, d, x, src=None, n=0, ws=FAKE, size=1 << 40, **over):
-    a = dict(q=FAKE, k=FAKE, v=FAKE, lens=FAKE, begin=FAKE, out=FAKE)
+    a = dict(q=FAKE, k=FAKE, v=FAKE, lens=FAKE, begin=FAKE, out=FAKE + (1 << 24))
     a.update(over)
     return lib.hg_attn_decode_tree(a["q"], a["k"], a["v"], a["lens"], a["begin"], src, n, a["out"], FAKE, ws, size, None,
                                    d and C.byref(d), x and C.byref(x))
@@ -87,6 +87,9 @@ def test_tree_attention_refuses_what_it_cannot_run(lib):
     assert need > 0
     assert decode(lib, d, x, size=need - 1) == hg.HG_ERR_WORKSPACE
     assert decode(lib, d, x, ws=None) == INVALID and decode(lib, d, x, ws=FAKE + 16) == INVALID
+    # the result in the queries' place: rows of other CTAs' queries would be overwritten before they are read
+    assert decode(lib, d, x, out=FAKE) == INVALID and decode(lib, d, x, q=FAKE + (1 << 24) + 16) == INVALID
+    assert decode(lib, d, tree(q_stride=4096), out=FAKE + (63 * 4096 + d.num_q_heads * d.head_dim) * 2 - 16) == INVALID
     src = (hg.HgPartialSrc * 9)()
     for s in src:
         s.o, s.m, s.l, s.nc = FAKE, FAKE, FAKE, 1
@@ -118,11 +121,13 @@ def test_slots_refuse_bad_arguments(lib):
 
 
 def test_rope_refuses_bad_arguments(lib):
-    def plain(r=None, x=FAKE, y=FAKE + 4096, pos=FAKE, heads=4, dim=128, dtype=0):
+    far = [FAKE + (i << 24) for i in range(4)]
+
+    def plain(r=None, x=FAKE, y=far[1], pos=FAKE, heads=4, dim=128, dtype=0):
         return lib.hg_rope(x, y, pos, heads, dim, dtype, None, C.byref(r or rope()))
 
     def append(r=None, d=None, **over):
-        a = dict(q=FAKE, k=FAKE, v=FAKE, pos=FAKE, slot=FAKE, out=FAKE, kc=FAKE, vc=FAKE)
+        a = dict(q=FAKE, k=far[1], v=far[2], pos=FAKE, slot=FAKE, out=far[3], kc=FAKE, vc=FAKE)
         a.update(over)
         d = d or good_desc()
         return lib.hg_kv_append_rope(a["q"], a["k"], a["v"], a["pos"], a["slot"], a["out"], a["kc"], a["vc"], None, C.byref(d), C.byref(r or rope()))
@@ -139,11 +144,18 @@ def test_rope_refuses_bad_arguments(lib):
     assert plain(x=FAKE + 8) == INVALID and plain(y=FAKE + 8) == INVALID and plain(heads=0) == INVALID and plain(dtype=2) == INVALID
     assert plain(dim=96) == UNSUPPORTED and plain(dim=0) == INVALID
     assert plain(y=FAKE, r=rope(q_out_stride=1024)) == INVALID                       # in place, but with other strides
+    # outputs that overlap an input: five rows of 4 heads of 128 components; the last 16 bytes of one, and rows 1536 elements apart
+    assert plain(y=FAKE + 5 * 1024 - 16) == INVALID and plain(x=far[1] + 5 * 1024 - 16) == INVALID
+    assert plain(rope(q_stride=1536, q_out_stride=1536), y=FAKE + 1008) == INVALID and plain(rope(q_stride=1536, q_out_stride=1536), y=FAKE + 2064) == INVALID
+    assert plain(rope(q_stride=1536), y=FAKE + 1024) == INVALID
     for name in ("k", "v", "pos", "slot", "kc", "vc", "q", "out"):
         assert append(**{name: None}) == INVALID, name
     for name in ("k", "v", "kc", "vc", "q", "out"):
         assert append(**{name: FAKE + 8}) == INVALID, name
     assert append(slot=FAKE + 4) == INVALID and append(d=good_desc(head_dim=96)) == UNSUPPORTED
+    assert append(out=far[1]) == INVALID and append(out=far[2]) == INVALID and append(out=FAKE + 16) == INVALID
+    assert append(rope(q_out_stride=4096), out=FAKE) == INVALID
+    assert append(rope(q_stride=1536, q_out_stride=1536, k_stride=1536), out=FAKE, k=FAKE + 1008) == INVALID
     assert lib.hg_rope(FAKE, FAKE, FAKE, 4, 128, 0, None, None) == INVALID
 
 

@@ -270,6 +270,27 @@ def turned64_grad(x, pos, freq, rot, layout, magnitude):
     return y.index_add(2, rest, x[..., rest])
 
 
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_parts_of_a_fused_projection_in_place_and_beside(layout):
+    """Rows of equal strides that lie between one another are no overlap"""
+    N, Hq, Hkv, D, P = 40, 6, 2, 64, 16
+    rows = torch.randn((N, 2 * Hq + 2 * Hkv, D), device=DEV).half()
+    q, k, v, other = rows.split([Hq, Hkv, Hkv, Hq], 1)
+    freq, _ = freqs(D)
+    pos, slot = torch.arange(N, device=DEV, dtype=torch.int32), torch.arange(N, device=DEV)
+    want, keys = turned64(q, pos, freq, D, layout), turned64(k, pos, freq, D, layout)
+    kc, vc = torch.zeros((2, 3, Hkv, P, D), device=DEV).half()
+    desc, rope = pool_desc(None, P, 3, Hq, Hkv, D, F16, None, kc), hg.rope_desc(rot_dim=D, freq=freq, layout=layout)
+    before = rows.clone()
+    hg.hg_rope(q, other, pos, rope)
+    torch.cuda.synchronize()
+    assert near(other, want, q) and torch.equal(rows[:, :Hq + 2 * Hkv], before[:, :Hq + 2 * Hkv])
+    hg.hg_kv_append_rope(q, k, v, pos, slot, q, kc, vc, desc, rope)
+    torch.cuda.synchronize()
+    assert torch.equal(q, other) and torch.equal(rows[:, Hq:Hq + 2 * Hkv], before[:, Hq:Hq + 2 * Hkv])
+    assert near(kc.transpose(1, 2).reshape(-1, Hkv, D)[:N], keys, k) and torch.equal(vc.transpose(1, 2).reshape(-1, Hkv, D)[:N], v)
+
+
 def test_far_and_negative_positions():
     freq, _ = freqs(128)
     pos = ints([0, -5, 2 ** 31 - 1, -2 ** 31, 10 ** 9, 1])
