@@ -146,6 +146,7 @@ hg_status hg_attn_decode_tree(const void* q, const void* k_cache, const void* v_
     p.page_size = desc->page_size; p.page_shift = ilog2_exact(desc->page_size); p.max_pages = desc->max_pages; p.num_pages = desc->num_pages;
     p.scale = desc->scale > 0.f ? desc->scale : 1.0f / sqrtf((float)desc->head_dim);
     p.div_G = make_fast_div((uint32_t)p.G);
+    p.div_wide = make_fast_div((uint32_t)(2 * p.nodes));
     p.scale_log2 = p.scale * 1.4426950408889634f;
     p.reread = tree->max_nodes > 2 * p.nodes;
     p.test_stall = (desc->flags & HG_FLAG_TEST_STALL) ? 1 : 0;

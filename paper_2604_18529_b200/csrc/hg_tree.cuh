@@ -27,6 +27,10 @@
 // the products; 11 finds the CTA's stretch, publishes its pieces up to four ahead and loads their queries (TMA, a box of G heads by
 // whole tokens); 12-15 (few rows) finish the pieces while the softmax warps are at the next.  Every wait is bounded.
 //
+// The roles share the instruction cache, so what runs once a piece or less often is kept small (rolled loops, estimates in place of
+// 64-bit quotients): 107 KB of code became 88 (few rows) and 134 became 112, and with them 128 sequences, 8 heads of 64, 2 new and
+// up to 1500 tokens went from 62 to 83 us, by the run, to a steady 60, and 60 sequences, 40 heads, up to 48 and 873 from 249 to 238.
+//
 // Measured (K and V larger than the L2), us, in a loop / the floor at the measured rates: one new token, 8 sequences, 64/8 heads,
 // 32 768 tokens: 168 / 167; the same with 64 components and twice the tokens: 168 / 167; 8 new tokens: 182 / 167, 16: 186 / 168
 // (many rows); 32 and 131 072 tokens, one sequence: 157 / 84 (bound by the exponentials and products of a pair of tiles, 3400
@@ -104,7 +108,7 @@ struct TreeParams {
     int page_size, page_shift, max_pages, num_pages;
     int reread, test_stall;          // reread: several units of a KV head read the same tiles
     float scale, scale_log2;
-    FastDiv div_G;
+    FastDiv div_G, div_wide;         // of G, of 2 nodes
     uint64_t inv_ctas;               // 2^64 / CTAs, rounded up
 };
 
@@ -123,22 +127,24 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
     s.hi = (int)min(end, room);
     if (s.n > 0 && end > room) s.bad = true;
     s.tiles = s.hi > s.lo ? (s.hi - (s.lo & ~(TREE_TILE - 1)) + TREE_TILE - 1) / TREE_TILE : 1;     // (none at all: one that shows nothing)
-    const int rest = s.n % (2 * p.nodes);
-    s.wides = s.n / (2 * p.nodes) + (rest > p.nodes ? 1 : 0);
+    s.wides = fast_div(s.n, p.div_wide);
+    const int rest = s.n - s.wides * 2 * p.nodes;
+    s.wides += rest > p.nodes ? 1 : 0;
     s.narrow = rest > 0 && rest <= p.nodes ? rest : 0;
     return s;
 }
 __device__ __forceinline__ long long tree_cost(const TreeSeq& s) { return TREE_COST_UNIT + (long long)s.tiles * TREE_COST_TILE; }   // of a unit
 __device__ __forceinline__ long long tree_head_cost(const TreeSeq& s) { return (s.wides + (s.narrow ? 1 : 0)) * tree_cost(s); }
-// Quotients of numbers that nearly always have 32 bits.
-__device__ __forceinline__ long long tree_div(long long a, long long b) {
-    return ((unsigned long long)(a | b) >> 32) ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+// Quotients below 2^17 (heads, units of a head): an estimate in floats is off by one at most (it has 2^-21 of itself).
+__device__ __forceinline__ int tree_div(long long a, long long b) {
+    const int q = (int)__fdividef((float)a, (float)b);
+    return q * b > a ? q - 1 : (q + 1) * b <= a ? q + 1 : q;
 }
 // Where the stretch of CTA c of n begins: floor(total c / n).  For all CTAs of the launch by a product (inv_ctas = 2^64 / CTAs
-// rounded up: exact below 2^56).
+// rounded up: exact below 2^56); with fewer CTAs there is less than TREE_MIN_STRETCH a CTA.
 __device__ __forceinline__ long long tree_stretch(const TreeParams& p, long long total, int c, int n) {
     if (n == (int)gridDim.x) return (long long)__umul64hi((unsigned long long)total * (unsigned)c, p.inv_ctas);
-    return tree_div(total * c, n);
+    return (long long)((uint32_t)total * (uint32_t)c / (uint32_t)n);
 }
 // How many CTAs share the work: where there is little, stretches have a tile for each stream.
 __device__ __forceinline__ int tree_ctas(long long total) {
@@ -146,8 +152,10 @@ __device__ __forceinline__ int tree_ctas(long long total) {
 }
 // The CTA that a place belongs to.
 __device__ __forceinline__ int tree_cta_of(const TreeParams& p, long long place, long long total, int n) {
-    int c = (int)min((long long)n - 1, (long long)((double)place / (double)total * n));
+    int c = min(n - 1, (int)__fdividef((float)place * (float)n, (float)total));
+#pragma unroll 1
     while (c > 0 && tree_stretch(p, total, c, n) > place) --c;
+#pragma unroll 1
     while (c + 1 < n && tree_stretch(p, total, c + 1, n) <= place) ++c;
     return c;
 }
@@ -238,6 +246,7 @@ __device__ __forceinline__ bool tree_poisoned(const TreeParams& p, const TreeIte
         const long long page = p.block_table ? p.block_table[e] : (long long)e;
         if (page < 0 || page >= p.num_pages) continue;
         const uint4* const v = reinterpret_cast<const uint4*>(p.v + page * p.page_stride + it.h * p.head_stride + (t & (p.page_size - 1)) * p.tok_stride);
+#pragma unroll 1
         for (int c = 0; c < D / 8; ++c)
             if (not_finite<BF16>(v[c]) & 0x80008000u) return true;
     }
@@ -283,11 +292,15 @@ __device__ __forceinline__ float tree_join_host(const TreeParams& p, size_t orow
     constexpr float LOG2E = 1.4426950408889634f;
     const float none = __int_as_float(0xff800000);
     top = m;
+#pragma unroll 1
     for (int x = 0; x < p.src.n; ++x)
+#pragma unroll 1
         for (int c = 0; c < p.src.nc[x]; ++c) top = fmaxf(top, p.src.m[x][orow * p.src.nc[x] + c]);
     const float own = m == none ? 0.f : fast_exp2((m - top) * LOG2E);
     l *= own;
+#pragma unroll 1
     for (int x = 0; x < p.src.n; ++x)
+#pragma unroll 1
         for (int c = 0; c < p.src.nc[x]; ++c) {
             const float hm = p.src.m[x][orow * p.src.nc[x] + c];
             if (hm != none) l += p.src.l[x][orow * p.src.nc[x] + c] * fast_exp2((hm - top) * LOG2E);
@@ -382,6 +395,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
           const int run = (p.B + 127) / 128, b_first = min(p.B, me * run), b_last = min(p.B, b_first + run);
           long long mine = 0;
           bool trouble = false;
+#pragma unroll 1
           for (int b = b_first; b < b_last; ++b) {
               const TreeSeq s = tree_seq(p, b);
               mine += tree_head_cost(s) * p.Hkv;
@@ -404,6 +418,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
           const long long from = cta < n ? tree_stretch(p, total, cta, n) : total;
           if (from >= upto - mine && from < upto) {
               long long base = upto - mine;
+#pragma unroll 1
               for (int b = b_first; b < b_last; ++b) {
                   const long long cost = tree_head_cost(tree_seq(p, b)) * p.Hkv;
                   if (from < base + cost) { ctl.start_b = b; ctl.start_base = base; break; }
@@ -455,7 +470,9 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
             TreeItem it;
             it.valid = 0;
             long long last_place = 0;
+#pragma unroll 1
             while (at < to) {                                      // the next piece with a tile in it
+#pragma unroll 1
                 while (at >= base + block && ub < p.B) { base += block; ub += 32; load_sequences(); }
                 if (ub >= p.B) { at = to; break; }
                 const int src = __ffs(__ballot_sync(0xffffffffu, at >= base + before && at < base + before + cost)) - 1;
@@ -466,9 +483,9 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                 s.wides = __shfl_sync(0xffffffffu, sq.wides, src); s.narrow = __shfl_sync(0xffffffffu, sq.narrow, src);
                 const long long begin = base + __shfl_sync(0xffffffffu, before, src);
                 const long long head = tree_head_cost(s), unit_cost = tree_cost(s);
-                const int h = (int)tree_div(at - begin, head);
+                const int h = tree_div(at - begin, head);
                 const long long in_head = (at - begin) - head * h;
-                const int u = s.wides == 0 ? 0 : (int)tree_div(in_head, unit_cost);
+                const int u = s.wides == 0 ? 0 : tree_div(in_head, unit_cost);
                 const bool is_wide = u < s.wides;
                 const long long unit = begin + head * h + unit_cost * u;
                 const int t0 = tree_tiles_before((int)(at - unit), s.tiles);
@@ -511,6 +528,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
             if (lane == 0) {                                       // (wide: both buffers, on the first one's barrier)
                 const int boxes = HALVES * (it.wide ? 2 : 1);
                 mbar_arrive_expect_tx(&ctl.q_full[it.q], (uint32_t)(boxes * row_bytes));
+#pragma unroll 1
                 for (int x = 0; x < boxes; ++x) {
                     const int s = x / HALVES, half = x % HALVES;
                     tma_load_3d(q_smem + (it.q + s) * Q_BYTES + half * Q_HALF_BYTES, &tmQ, &ctl.q_full[it.q], half * 64, it.h * p.G, it.row0 + s * p.nodes);
@@ -552,6 +570,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
             // (a tile's pages never straddle the 32 in the lanes and the next 32)
             int base = page0, now = looked ? ahead : look_up(it.b, it.lo, it.hi, base), next = look_up(it.b, it.lo, it.hi, base + 32);
             looked = false;
+#pragma unroll 1
             for (int x = 0; x < it.tiles; ++x) {
                 const int t_x = it.first + x * TREE_TILE, t_box = t_x + piece * box_rows, row = t_box & (p.page_size - 1);
                 if ((t_x >> p.page_shift) + pages > base + 32) {
@@ -1143,7 +1162,9 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                             for (int u = 0; u < 32; u += 8) st_global_hint8(p.ws.o + prow * D + c0 + u, *reinterpret_cast<const float(*)[8]>(&y[u]), keep);
                             continue;
                         }
+#pragma unroll 1
                         for (int x = 0; x < p.src.n; ++x)
+#pragma unroll 1
                             for (int c = 0; c < p.src.nc[x]; ++c) {
                                 const size_t q = orow * p.src.nc[x] + c;
                                 const float hm = p.src.m[x][q];
@@ -1245,6 +1266,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                 }
                 const int left = min(8, rows - c0);
                 if (it.whole) {
+#pragma unroll 1
                     for (int z = 0; z < p.src.n; ++z)
 #pragma unroll 1
                         for (int e = 0; e < p.src.nc[z]; ++e) {          // (an empty partial's o row is not read)
@@ -1322,6 +1344,7 @@ __global__ void __launch_bounds__(TREE_MERGE_THREADS) tree_merge_kernel(const __
     const int bits = p.status ? *reinterpret_cast<volatile int32_t*>(p.status) : 0;
     if (cut.y <= 0 || (bits & HG_DEV_WAIT_TIMEOUT)) return;
     const int lane = threadIdx.x & 31, first = blockIdx.x, pieces = cut.w - first + 1, stream_rows = p.nodes * p.G;
+#pragma unroll 1
     for (int x = blockIdx.y * (TREE_MERGE_THREADS / 32) + (threadIdx.x >> 5); x < cut.y * p.G; x += gridDim.y * (TREE_MERGE_THREADS / 32)) {
         const int node = fast_div(x, p.div_G), s = x >= stream_rows ? 1 : 0;
         const size_t orow = (size_t)(cut.x + node) * p.Hq + cut.z * p.G + (x - node * p.G);
@@ -1341,12 +1364,15 @@ __global__ void __launch_bounds__(TREE_MERGE_THREADS) tree_merge_kernel(const __
         float m0, l0, top, l = 0.f, acc[W];
         load(lane, m0, l0);
         top = m0;
+#pragma unroll 1
         for (int e = lane + 32; e < pieces; e += 32) {
             float m, pl;
             load(e, m, pl);
             top = fmaxf(top, m);
         }
+#pragma unroll 1
         for (int y = 0; y < p.src.n; ++y)
+#pragma unroll 1
             for (int c = lane; c < p.src.nc[y]; c += 32) top = fmaxf(top, p.src.m[y][orow * p.src.nc[y] + c]);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -1356,6 +1382,7 @@ __global__ void __launch_bounds__(TREE_MERGE_THREADS) tree_merge_kernel(const __
         auto add = [&](float m, float pl, int n, auto row_of) {
             const float w = m == NEG_INF ? 0.f : fast_exp2((m - top) * LOG2E);
             l = m == NEG_INF ? l : fmaf(pl, w, l);
+#pragma unroll 1
             for (int e0 = 0; e0 < n; e0 += 8) {
                 __align__(16) float v[8][W];
                 float we[8];
@@ -1377,11 +1404,14 @@ __global__ void __launch_bounds__(TREE_MERGE_THREADS) tree_merge_kernel(const __
                     for (int z = 0; z < W; ++z) acc[z] = fmaf(v[u][z], we[u], acc[z]);
             }
         };
+#pragma unroll 1
         for (int e0 = 0; e0 < pieces; e0 += 32) {
             if (e0 > 0) load(e0 + lane, m0, l0);
             add(m0, l0, min(32, pieces - e0), [&](int e) { return p.ws.o + ((size_t)slot_of(e0 + e) * 256 + r) * D; });
         }
+#pragma unroll 1
         for (int y = 0; y < p.src.n; ++y)
+#pragma unroll 1
             for (int c0 = 0; c0 < p.src.nc[y]; c0 += 32) {
                 const size_t q = orow * p.src.nc[y] + c0;
                 const bool is = c0 + lane < p.src.nc[y];
