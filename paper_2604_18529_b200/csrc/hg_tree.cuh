@@ -28,8 +28,8 @@
 // whole tokens); 12-15 (few rows) finish the pieces while the softmax warps are at the next.  Every wait is bounded.
 //
 // The roles share the instruction cache, so what runs once a piece or less often is kept small (rolled loops, estimates in place of
-// 64-bit quotients): 107 KB of code became 88 (few rows) and 134 became 112, and with them 128 sequences, 8 heads of 64, 2 new and
-// up to 1500 tokens went from 62 to 83 us, by the run, to a steady 60, and 60 sequences, 40 heads, up to 48 and 873 from 249 to 238.
+// 64-bit quotients, one place that clears V rows): 107 KB of code became 88 (few rows) and 134 became 107, and with them 128 sequences, 8 heads of 64, 2 new and
+// up to 1500 tokens went from 62 to 83 us, by the run, to a steady 59, and 60 sequences, 40 heads, up to 48 and 873 from 217 to 190.
 //
 // Measured (K and V larger than the L2), us, in a loop / the floor at the measured rates: one new token, 8 sequences, 64/8 heads,
 // 32 768 tokens: 168 / 167; the same with 64 components and twice the tokens: 168 / 167; 8 new tokens: 182 / 167, 16: 186 / 168
@@ -292,6 +292,7 @@ __device__ __forceinline__ float tree_join_host(const TreeParams& p, size_t orow
     constexpr float LOG2E = 1.4426950408889634f;
     const float none = __int_as_float(0xff800000);
     top = m;
+    if (p.src.n == 0) return 1.f;
 #pragma unroll 1
     for (int x = 0; x < p.src.n; ++x)
 #pragma unroll 1
@@ -992,11 +993,15 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                     if (!ok) break;
                     ++ns;
                     tc_fence_after_sync();
+                    const int t = it.first + tree_tile_index(it, s, i) * TREE_TILE;
+                    const int c_lo = max(it.lo - t, 0), c_hi = min(it.hi - t, TREE_TILE);
+                    const uint32_t bad = *reinterpret_cast<volatile uint8_t*>(&ctl.stream_bad[s]);
+                    const bool tail = t + TREE_TILE > it.len, edge = c_lo > 0 || c_hi < TREE_TILE || tail || bad;
+                    auto clear = [&]() { return !edge || clear_v(n + tree_tile_index(it, s, i), r < c_lo || r >= c_hi || ((bad >> (r >> 4)) & 1u), t + r >= it.len, j); };
+                    // (where S may be overwritten early, that comes first; else the row is not in registers yet)
+                    if (!BESIDE) ok = clear();
+                    if (!ok) break;
                     if (live) {
-                        const int t = it.first + tree_tile_index(it, s, i) * TREE_TILE;
-                        const int c_lo = max(it.lo - t, 0), c_hi = min(it.hi - t, TREE_TILE);
-                        const uint32_t bad = *reinterpret_cast<volatile uint8_t*>(&ctl.stream_bad[s]);
-                        const bool tail = t + TREE_TILE > it.len, edge = c_lo > 0 || c_hi < TREE_TILE || tail || bad;
                         float x[TREE_TILE];
 #pragma unroll
                         for (int c0 = 0; c0 < TREE_TILE; c0 += 32) tmem_ld_32x32(s_tmem + c0, *reinterpret_cast<uint32_t(*)[32]>(&x[c0]));
@@ -1006,9 +1011,9 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                             __syncwarp();
                             if (lane == 0) mbar_arrive(&ctl.s_read[s]);
                         }
+                        if (BESIDE) ok = clear();
+                        if (!ok) break;
                         if (edge) {                                // columns outside the slice, of refused pages, of tokens not seen
-                            ok = clear_v(n + tree_tile_index(it, s, i), r < c_lo || r >= c_hi || ((bad >> (r >> 4)) & 1u), t + r >= it.len, j);
-                            if (!ok) break;
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
                                 uint32_t out = ((bad >> (2 * c)) & 1u ? 0xffffu : 0u) | ((bad >> (2 * c + 1)) & 1u ? 0xffff0000u : 0u);
@@ -1081,10 +1086,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                         hand_over(3);
                         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     } else {
-                        const int t = it.first + tree_tile_index(it, s, i) * TREE_TILE;
-                        const uint32_t bad = *reinterpret_cast<volatile uint8_t*>(&ctl.stream_bad[s]);
-                        if (t < it.lo || t + TREE_TILE > min(it.hi, it.len) || bad)
-                            ok = clear_v(n + tree_tile_index(it, s, i), t + r < it.lo || t + r >= it.hi || ((bad >> (r >> 4)) & 1u), t + r >= it.len, j);
+                        if (BESIDE) ok = clear();
                         if (!ok) break;
                         tc_fence_before_sync();
                         __syncwarp();
@@ -1127,7 +1129,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                     const size_t orow = (size_t)row * p.Hq + it.h * p.G + (r - r_node * p.G);
                     const float m = m_raw == NEG_INF ? NEG_INF : m_raw * p.scale;
                     const bool last_word = it.wide || s == 0;      // who writes the row's single numbers
-                    if (exists && *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) && tree_poisoned<D, BF16>(p, it, row, node)) {
+                    if (__builtin_expect(exists && *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) && tree_poisoned<D, BF16>(p, it, row, node), 0)) {
                         f0 = __int_as_float(0x7fc00000);
                         f1 = 0.f;
                     }
@@ -1228,7 +1230,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
             const size_t orow = (size_t)row * p.Hq + it.h * p.G + (c - node * p.G);
             const size_t prow = (size_t)it.slot * 256 + c;
             const float m = m_raw == NEG_INF ? NEG_INF : m_raw * p.scale;
-            if (exists && *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) && tree_poisoned<D, BF16>(p, it, row, it.i0 + node)) {
+            if (__builtin_expect(exists && *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) && tree_poisoned<D, BF16>(p, it, row, it.i0 + node), 0)) {
                 f0 = __int_as_float(0x7fc00000);
                 f1 = 0.f;
             }
