@@ -32,9 +32,11 @@
 // up to 1500 tokens went from 62 to 83 us, by the run, to a steady 59, and 60 sequences, 40 heads, up to 48 and 873 from 217 to 190.
 //
 // Measured (K and V larger than the L2), us, in a loop / the floor at the measured rates: one new token, 8 sequences, 64/8 heads,
-// 32 768 tokens: 168 / 167; the same with 64 components and twice the tokens: 168 / 167; 8 new tokens: 182 / 167, 16: 186 / 168
-// (many rows); 32 and 131 072 tokens, one sequence: 157 / 84 (bound by the exponentials and products of a pair of tiles, 3400
-// cycles where the products take 2048, at 1.55 GHz under the power cap).
+// 32 768 tokens: 169 / 167; the same with 64 components and twice the tokens: 166 / 167; 8 new tokens: 172 / 167, 16: 183 / 168
+// (many rows); 32 and 131 072 tokens, one sequence: 140 / 84 (bound by the exponentials and products of a pair of tiles, 3400
+// cycles where the products take 2048, at 1.55 GHz under the power cap).  Short units cost more than their bytes (first tile, masked
+// last tile, join, some 5000 cycles in all with many rows): 60 sequences, 40/40 heads, up to 873 tokens, up to 32, 48 and 200 new
+// ones: 162 / 85, 192 / 88 and 330 / 115.
 #pragma once
 
 #include <cuda_runtime.h>
