@@ -678,7 +678,8 @@ typedef struct hg_tree_desc {
  * Logits, softmax statistics and sums are fp32; the weights enter the product with V rounded to desc->dtype (off by at most half
  * a step, 2^-8 of themselves with bf16 and 2^-11 with fp16, as out itself is), and their sum is that of the unrounded ones.
  * Cached rows must be finite.  A new token's K and V may hold anything as far as tokens that do not see it are concerned; one
- * that sees an infinity or a NaN in a V row gets no finite result in that component, and perhaps in none of the head's.
+ * that sees an infinity or a NaN in a V row, with a weight above 0, gets no finite result in that component, and perhaps in
+ * none of the head's.
  * Of desc: batch, heads, head_dim, dtype, the KV addressing, scale, flags and status (its chunk fields are not used);
  * num_q_heads / num_kv_heads is at most 128.  workspace: dev, 256-byte aligned, hg_attn_tree_workspace_bytes(); its contents need
  * no preparation; not shared by calls that may overlap on the GPU (captured graphs replayed on different streams among them).

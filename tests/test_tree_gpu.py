@@ -293,6 +293,17 @@ def test_many_short_sequences():
     Step(r.randint(0, 200, 700).tolist(), r.randint(0, 5, 700).tolist(), Hq=4, Hkv=2, D=64).check()
 
 
+@pytest.mark.parametrize("Hq,Hkv,nodes", [(1500, 500, [70, 9, 0]), (600, 600, [300, 1, 40]), (2100, 2100, [2, 1, 3])])
+def test_many_heads(Hq, Hkv, nodes):
+    """Shares of the work that begin at any head, and at any unit of one"""
+    Step([150, 3, 40], nodes, Hq=Hq, Hkv=Hkv, D=64, dtype=BF16).check()
+
+
+def test_many_sequences_of_many_rows():
+    r = np.random.RandomState(5)
+    Step(r.randint(0, 900, 45).tolist(), r.randint(0, 61, 45).tolist(), Hq=24, Hkv=4, kind="any", host=(1,)).check()
+
+
 def test_one_long_sequence():
     Step([70000], [24], Hq=16, Hkv=2, P=64, dtype=BF16).check()
 
