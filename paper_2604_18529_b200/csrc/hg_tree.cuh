@@ -388,8 +388,6 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
       reg_shrink<TREE_REGS_OTHER>();
       cudaGridDependencySynchronize();
       const int me = tid - 256, cta = blockIdx.x;
-      if (me < 2) p.ws.valid[2 * cta + me] = 0;
-      if (me == 2) p.ws.cut[cta].nodes = 0;
       long long total = 0;
       if (p.B > 32) {
           // ---- the sequences' costs, and where this CTA's stretch begins: 128 threads, a run of sequences each.  (The item warp
@@ -434,6 +432,10 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
         // =============================== item warp: the stretch's pieces, some ahead, and their queries ===============================
         // (after an earlier call that ran into its limit there is no work until the caller has cleared the word)
         const bool skip = timed_out();
+        // nothing is cut so far: cleared by the warp that sets these words for the pieces, so that its own order holds for both
+        if (lane < 2) p.ws.valid[2 * cta + lane] = 0;
+        if (lane == 2) p.ws.cut[cta].nodes = 0;
+        __syncwarp();
         int ub = 0;                                                // first of the 32 sequences in the lanes
         long long base = 0;                                        // ... its place in the row of tiles
         if (p.B > 32) { ub = ctl.start_b < 0 ? p.B : ctl.start_b; base = ctl.start_base; }

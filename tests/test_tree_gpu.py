@@ -361,6 +361,24 @@ def test_results_do_not_change_from_call_to_call():
         assert torch.equal(s.out, out) and torch.equal(s.lse, lse)
 
 
+@pytest.mark.parametrize("lens,nodes", [([5000], [9]), ([2000, 700, 3], [40, 1, 17]), ([300] * 32, [4] * 32), ([260] * 33, [3] * 33)])
+def test_calls_behind_one_another_in_one_workspace(lens, nodes):
+    """Each call finds the flags and descriptions of another one's cut units, with up to 32 sequences and with more"""
+    a, b = Step(lens, nodes, Hq=16), Step([1500, 40, 900], [5, 70, 1], Hq=4, Hkv=4, seed=1)
+    a.check()
+    b.check()
+    size = max(a.ws.numel(), b.ws.numel())
+    ws = torch.full((size,), 1, dtype=torch.uint8, device=DEV)
+    results = [[(torch.full_like(s.out, -77), torch.full_like(s.lse, -77)) for s in (a, b)] for _ in range(40)]
+    for pair in results:
+        for s, (out, lse) in zip((a, b), pair):
+            s.call(out=out, lse=lse, ws=ws)
+    torch.cuda.synchronize()
+    for pair in results:
+        for s, (out, lse) in zip((a, b), pair):
+            assert torch.equal(out, s.out) and torch.equal(lse, s.lse)
+
+
 def test_two_streams_and_a_captured_call():
     a, b = Step([3000, 40], [9, 3], seed=1, Hq=16), Step([100, 2500, 7], [30, 2, 5], seed=2, dtype=BF16)
     a.call()
