@@ -1325,7 +1325,8 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                 const int slots = warp < KS ? KS : VS, at = warp < KS ? warp : warp - KS, tiles = ctl.issued[warp < KS ? 0 : 1];
                 if (tiles > at) pfx_wait(&ctl.full[warp], (uint32_t)((tiles - 1 - at) / slots) & 1u, &none);
             }
-            if (warp >= 10 && ctl.q_issued[warp - 10] > 0) pfx_wait(&ctl.q_full[warp - 10], (uint32_t)(ctl.q_issued[warp - 10] - 1) & 1u, &none);
+            const int buffer = warp - TREE_MMA_WARP;               // (two buffers; with few rows there are four more warps)
+            if (buffer >= 0 && buffer < 2 && ctl.q_issued[buffer] > 0) pfx_wait(&ctl.q_full[buffer], (uint32_t)(ctl.q_issued[buffer] - 1) & 1u, &none);
         }
         if (tid == 0 && p.status) atomicOr(p.status, HG_DEV_WAIT_TIMEOUT);
     }

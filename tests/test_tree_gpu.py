@@ -454,6 +454,19 @@ def test_a_wait_that_runs_out_is_reported():
     s.check()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nodes", [[4, 3], [8, 5]])                          # 16 and 32 rows a KV head
+def test_a_wait_that_runs_out_with_few_rows(D, nodes):
+    """The forms whose CTAs have sixteen warps: all of them take part in the unwinding, and the call returns normally"""
+    s = Step([500, 90], nodes, D=D, flags=hg.HG_FLAG_TEST_STALL)
+    s.call()
+    torch.cuda.synchronize()
+    assert int(s.status) & hg.HG_DEV_WAIT_TIMEOUT
+    s.desc.flags = 0
+    s.status.zero_()
+    s.check()
+
+
 def test_the_binding_refuses_wrong_tensors():
     s = Step([20], [3])
     ok = dict(q=s.q, out=s.out, lse=s.lse, ws=s.ws, host=[])
