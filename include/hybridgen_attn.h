@@ -675,8 +675,10 @@ typedef struct hg_tree_desc {
  * Rows beyond cu_nodes[B] are neither read nor written.  A sequence with more than max_nodes tokens, or whose rows do not lie
  * in [0, N), is cut to what fits; positions beyond the block-table row are left out (HG_DEV_RANGE each).  A page that is
  * needed and not in the pool is left out (HG_DEV_BAD_PAGE).
- * Logits, softmax statistics and sums are fp32; the weights enter the product with V rounded to desc->dtype (off by at most half
- * a step, 2^-8 of themselves with bf16 and 2^-11 with fp16, as out itself is), and their sum is that of the unrounded ones.
+ * Logits, softmax statistics and sums are fp32; the weights enter the product with V rounded to desc->dtype, off by at most half a
+ * step, as out itself is: 2^-8 of themselves with bf16; with fp16 2^-11 of themselves, or 2^-32 of the row's largest where that
+ * is more (weights below 2^-21 of it; below 2^-32 some are lost).  Their sum is that of the unrounded ones.  (hg_attn_decode,
+ * whose out is fp32, keeps more: it carries them in two 16-bit terms or in fp32.)
  * Cached rows must be finite.  A new token's K and V may hold anything as far as tokens that do not see it are concerned; one
  * that sees an infinity or a NaN in a V row, with a weight above 0, gets no finite result in that component, and perhaps in
  * none of the head's.

@@ -8,7 +8,9 @@
 //
 // Both products run on tcgen05.mma with accumulators in tensor memory, tiles of 128 tokens in two STREAMS per CTA, each with four
 // softmax warps.  P is rounded to the inputs' type: a weight is off by at most half a step, as the result itself is; l is the sum
-// of the unrounded weights.  Two forms:
+// of the unrounded weights.  With fp16 a half step is 2^-11 of a weight only down to 2^-14, and 2^-25 below, so its weights are
+// 2^7 times as large (up to 2^15, since a reference may lie 2^8 below the maximum): 2^-11 of themselves or 2^-32 of the largest.
+// Two forms:
 //   many rows (ROWS = 0)   the rows are the products' M: S = Q K^T is 128 x 128, a thread owns a row, P goes back to tensor memory
 //           as the A operand of P V.  A UNIT is (sequence, KV head, whole new tokens with up to 256 rows): wide, more than 128
 //           rows, where the streams take 128 rows each and share every K and V tile; or narrow, up to 128 rows, where the streams
@@ -62,6 +64,10 @@ constexpr int TREE_ITEMS = 4;                 // pieces published ahead
 // 32 and 16 384: 299 (2 to 6), 302, 305, 309; 128 sequences, 8 heads of 64, 2 and 1 500: 70, 62, 63, 63, 65, 64.
 constexpr int TREE_COST_TILE = 4, TREE_COST_UNIT = 16;
 constexpr int TREE_MIN_STRETCH = 8;
+
+// Powers of two on the weights: what fp16 has room for above the 2^8 by which a logit may pass its reference.
+constexpr float TREE_PAST = 8.f;
+template <bool BF16> __host__ __device__ constexpr float tree_lift() { return BF16 ? 0.f : 7.f; }
 
 template <int D> __host__ __device__ constexpr int tree_tile_bytes() { return TREE_TILE * D * 2; }
 // Ring slots for K and V tiles: what shared memory has room for.  K and V have rings of their own: the S products run ahead of the
@@ -320,6 +326,8 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
     constexpr int HALVES = D / 64;
     constexpr uint32_t HALF_BYTES = TREE_TILE * 128, Q_HALF_BYTES = Q_BYTES / HALVES;
     constexpr uint32_t FMT = BF16 ? 1u : 0u;
+    // weights are 2^LIFT e^(scale (logit - reference)): as softmax statistics, sums that refer to LIFT ln 2 below the reference
+    constexpr float LIFT = tree_lift<BF16>(), LIFT_LN = LIFT * 0.693147180559945309f;
     // instruction descriptors: fp32 accumulator, 16-bit A and B.  Many rows: M = 128; S: both K-major, N = 128 tokens; O: B (V)
     // with its components contiguous (N-major), N = D.  Few rows: S^T: both K-major, M = 128 tokens, N = ROWS; O^T: A (V) with its
     // components contiguous (M-major), M = D, and B (P) with a token's rows contiguous (N-major)
@@ -897,7 +905,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
 #pragma unroll
                         for (int c = 0; c < ROWS; ++c) x[c] = (hide >> c) & 1u ? NEG_INF : x[c];
                     }
-                    auto exponents = [&]() {                       // scale (x - reference), in powers of 2
+                    auto exponents = [&]() {                       // scale (x - reference), in powers of 2, lifted
                         const float2 sc2 = make_float2(sc, sc);
 #pragma unroll
                         for (int c = 0; c < ROWS; c += 4) {
@@ -911,7 +919,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                     // a row's reference moves only when a logit is more than 2^8 above it (then the weights would leave the 16-bit
                     // types' comfortable range), and at a unit's first tile.  The four warps find out by a vote; those that want
                     // to move leave their maxima
-                    const bool up = i == 0 || __any_sync(0xffffffffu, row_max<ROWS>(e) > 8.f);
+                    const bool up = i == 0 || __any_sync(0xffffffffu, row_max<ROWS>(e) > TREE_PAST + LIFT);
                     const int turn = (int)(ns % 3);
                     if (up) {
                         const float mx = across_lanes<ROWS, true>(x, lane);
@@ -936,7 +944,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                         ref = now;
                         // the exponents' summand (the same from all warps): for a row that has not seen anything yet one that lifts any
                         // finite logit over the limit, for one that does not exist one that lifts none
-                        ctl.col.off[s][c] = c >= rows ? NEG_INF : now == NEG_INF ? 1e30f : -now * sc;
+                        ctl.col.off[s][c] = c >= rows ? NEG_INF : now == NEG_INF ? 1e30f : fmaf(-now, sc, LIFT);
                         __syncwarp();
                         exponents();
                         if (i > 0) {
@@ -1040,7 +1048,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                         // a row's sums follow its maximum only when that has moved by more than 2^8 (then the weights would leave
                         // the 16-bit types' comfortable range).  Each row decides by itself, so its result does not depend on its
                         // neighbours (rows that do not exist among them)
-                        const bool moved = (m_true - m_ref) * sc > 8.f;
+                        const bool moved = (m_true - m_ref) * sc > TREE_PAST;
                         if (BESIDE && ns > 1) {            // the last tile's weights are used up, and its products in O
                             ok = pfx_warp_wait(&ctl.p_free[s], (ns - 2) & 1u, abort_flag);
                             if (!ok) break;
@@ -1062,7 +1070,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                                 }
                             }
                         }
-                        const float off = m_ref == NEG_INF ? 0.f : -m_ref * sc;
+                        const float off = m_ref == NEG_INF ? 0.f : fmaf(-m_ref, sc, LIFT);
                         const float2 sc2 = make_float2(sc, sc), off2 = make_float2(off, off);
                         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                         // a quarter of the tokens at a time; each is handed over when the next one's weights are computed (a store
@@ -1131,7 +1139,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
                         c_end = c_begin + D / 2;
                     }
                     const size_t orow = (size_t)row * p.Hq + it.h * p.G + (r - r_node * p.G);
-                    const float m = m_raw == NEG_INF ? NEG_INF : m_raw * p.scale;
+                    const float m = m_raw == NEG_INF ? NEG_INF : fmaf(m_raw, p.scale, -LIFT_LN);
                     const bool last_word = it.wide || s == 0;      // who writes the row's single numbers
                     if (__builtin_expect(exists && *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) && tree_poisoned<D, BF16>(p, it, row, node), 0)) {
                         f0 = __int_as_float(0x7fc00000);
@@ -1233,7 +1241,7 @@ __global__ void __launch_bounds__(tree_threads<ROWS>(), 1) tree_kernel(const __g
             const int row = it.row0 + node;
             const size_t orow = (size_t)row * p.Hq + it.h * p.G + (c - node * p.G);
             const size_t prow = (size_t)it.slot * 256 + c;
-            const float m = m_raw == NEG_INF ? NEG_INF : m_raw * p.scale;
+            const float m = m_raw == NEG_INF ? NEG_INF : fmaf(m_raw, p.scale, -LIFT_LN);
             if (__builtin_expect(exists && *reinterpret_cast<volatile int*>(&ctl.poisoned[j]) && tree_poisoned<D, BF16>(p, it, row, it.i0 + node), 0)) {
                 f0 = __int_as_float(0x7fc00000);
                 f1 = 0.f;

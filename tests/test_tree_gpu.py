@@ -288,6 +288,73 @@ def test_fused_queries_and_a_scale():
     Step([100, 30], [12, 3], fused=True, scale=0.25).check()
 
 
+def one_logit(lens, nodes, logit, Hq, Hkv, D, dtype=F16, **kw):
+    """A step whose logits are those of ``logit(position)`` (all heads alike, rounded to the type) and whose V are positive"""
+    s = Step(lens, nodes, Hq=Hq, Hkv=Hkv, D=D, dtype=dtype, scale=1.0, **kw)
+    s.q[...] = 0
+    s.q[..., 0] = 4
+    v = torch.rand(s.v.shape, device=DEV) * 500 + 500
+    for b in range(s.B):
+        t = torch.arange(lens[b] + nodes[b], device=DEV)
+        page, row = s.table[b].long()[t // s.P], t % s.P
+        key = torch.zeros((t.numel(), Hkv, D), device=DEV)
+        key[..., 0] = (logit(t) / 4)[:, None]
+        s.k[page, :, row] = key.to(dtype)
+        s.v[page, :, row] = v[page, :, row].to(dtype)
+    return s
+
+
+SHAPES = [(8, 2, 3), (8, 2, 8), (8, 2, 20), (8, 2, 40)]                      # 12, 32, 80 and 160 rows a KV head
+
+
+@pytest.mark.parametrize("depth", [12.0, 15.0, 17.0, 17.5])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,n", SHAPES)
+def test_small_weights_beside_large_ones(depth, D, Hq, Hkv, n):
+    """Every 64th token takes nearly all the weight and has V = 0; out is what the others give, e^-depth of it each.
+
+    A weight is off by u = 2^-11 of itself, or by 2^-32 of the largest where that is more (half a step of the smallest fp16
+    numbers, 2^-25, in weights that are 2^7 times as large), so out, all V being positive, by u of itself and 2^-32 of the sum
+    of V over the sum of weights, one for every 64 tokens at least; the rest is as in the tolerances above."""
+    for length in (100, 1000, 9000):
+        s = one_logit([length], [n], lambda t: torch.where(t % 64 == 0, 0.0, -depth - (t * 37 % 64) / 256), Hq, Hkv, D, kind="chain")
+        t = torch.arange(length, device=DEV)
+        page, row = s.table[0].long()[t // s.P], t % s.P
+        s.v[page[::64], :, row[::64]] = 0
+        s.call()
+        torch.cuda.synchronize()
+        out, lse, _ = s.exact()
+        u, total = 2.0 ** -11, length + n
+        off = (2 * u + LOGIT + 2.3e-9 * total) * out + 2.0 ** -32 * 1000 * 64 * total / (total - 63) + 2.0 ** -24
+        worst = float(((s.out[:n].double() - out).abs() / off).max())
+        assert worst <= 1, (length, worst)
+        assert float((s.lse[:n].double() - lse).abs().max()) <= LOGIT
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("Hq,Hkv,n", SHAPES)
+def test_one_token_above_a_long_tail(dtype, Hq, Hkv, n):
+    """The first token, and 30 000 that are e^-14 of it together with it: a tenth of a percent of the weight"""
+    for b in range(2):
+        s = one_logit([30000], [n], lambda t: torch.where(t == 0, 0.0, -14.0 - (t % 64) / 64), Hq, Hkv, 64, dtype, kind="chain", P=64,
+                      host=(2,) * b)
+        s.check()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("rise", [5.4, 5.7, 11.0])                           # nats a tile; a reference follows from 2^8 (5.5) on
+@pytest.mark.parametrize("Hq,Hkv,n", SHAPES)
+def test_logits_that_climb(dtype, rise, Hq, Hkv, n):
+    s = one_logit([900], [n], lambda t: (t // 128) * rise - 30.0, Hq, Hkv, 128, dtype, kind="chain", host=(1,))
+    s.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,n", SHAPES)
+def test_host_partials_with_fp16(D, Hq, Hkv, n):
+    Step([400, 0, 2077], [n, 3, 1], Hq=Hq, Hkv=Hkv, D=D, host=(3, 1), kind="any").check()
+
+
 def test_many_short_sequences():
     r = np.random.RandomState(3)
     Step(r.randint(0, 200, 700).tolist(), r.randint(0, 5, 700).tolist(), Hq=4, Hkv=2, D=64).check()
