@@ -543,7 +543,7 @@ hg_status hg_kv_copy_pages(const int32_t* src, const int32_t* dst, const int32_t
  * alternatives behind the cache), prompts, or single tokens beside either.  The paper decodes one token a step; these
  * operators are one step over any number of them, in the order of their use:
  *     hg_kv_reserve        pages for the new tokens
- *     hg_kv_slots          which row of the packed tensors is which token, its position and its place in the pool, masks
+ *     hg_kv_slots_ready    which row of the packed tensors is which token, its position and its place in the pool, masks
  *     hg_kv_append_rope    (each layer) rotary positions; keys and values to their places
  *     hg_attn_decode_tree  (each layer) attention over the cache and, masked, over the new tokens
  *     hg_kv_accept         (each layer) the accepted tokens' rows move together behind the cache, the lengths grow
@@ -569,15 +569,33 @@ hg_status hg_kv_copy_pages(const int32_t* src, const int32_t* dst, const int32_t
  *             where the block table has no page (HG_DEV_BAD_PAGE) or ends (HG_DEV_RANGE)
  *   mask      dev uint32 [N][mask_words] out: bit j of row i (word j / 32, bit j % 32) says that token i sees token j of its
  *             sequence: itself and its ancestors
+ * Rows lie by n_new here and in every packed array of the step.  So n_new is what parent, q, k and v are packed by: to put n_ready of
+ * hg_kv_reserve in its place would move the rows behind a sequence that got fewer pages than it asked for; hg_kv_slots_ready
+ * takes both.
  * cu_new is needed, the other outputs may be NULL.  Rows at and beyond cu_new[B] get tok_seq = -1, tok_pos = 0, tok_slot = -1
  * and no mask bits, so that the step's other calls can run over all N rows.  Where the sequences have more than N tokens
  * together the last are cut, and with a parent or a mask each sequence is cut at HG_MAX_TREE_NODES and 32 * mask_words tokens
- * (HG_DEV_RANGE).  Outputs must not overlap each other or the inputs.  Of desc: batch, page_size, num_pages, the block table
+ * (HG_DEV_RANGE; the rows behind it move up, parent being read by the rows as they are then: pass no such n_new, or use
+ * hg_kv_slots_ready).  Outputs must not overlap each other or the inputs.  Of desc: batch, page_size, num_pages, the block table
  * and status (a description of the pool that hg_kv_append takes will do).
  */
 hg_status hg_kv_slots(const int32_t* seq_lens, const int32_t* n_new, const int32_t* parent, int32_t num_rows, int32_t* cu_new,
                       int32_t* tok_seq, int32_t* tok_pos, int64_t* tok_slot, uint32_t* mask, int32_t mask_words, void* stream,
                       const hg_attn_desc* desc);
+
+/*
+ * hg_kv_slots for a step of which some tokens may have got no page: as above, and
+ *   n_ready   dev int32 [B]    how many of a sequence's new tokens may be stored, from the first on (hg_kv_reserve's; 0 or less: none), or
+ *             NULL: all, which is hg_kv_slots
+ * No row moves on account of n_ready, nor of the limits on masks: a token from n_ready[b] on, and one behind HG_MAX_TREE_NODES or
+ * 32 * mask_words where there is a parent or a mask (HG_DEV_RANGE), keeps its row and gets tok_seq = b, tok_pos = seq_lens[b],
+ * tok_slot = -1 and no mask bits.  hg_kv_append_rope does not store it, hg_attn_decode_tree's result for it means nothing (and may
+ * report its missing page, HG_DEV_BAD_PAGE), and it must not be accepted; all other tokens are as they would be without it, since
+ * a token's ancestors come before it.
+ */
+hg_status hg_kv_slots_ready(const int32_t* seq_lens, const int32_t* n_new, const int32_t* n_ready, const int32_t* parent, int32_t num_rows,
+                            int32_t* cu_new, int32_t* tok_seq, int32_t* tok_pos, int64_t* tok_slot, uint32_t* mask, int32_t mask_words,
+                            void* stream, const hg_attn_desc* desc);
 
 /* Rotary position embeddings (host struct). */
 #define HG_ROPE_HALF 0        /* component i < rot_dim / 2 turns with component i + rot_dim / 2 */
@@ -698,7 +716,7 @@ size_t hg_attn_tree_workspace_bytes(const hg_attn_desc* desc, const hg_tree_desc
  * Keeps the accepted ones of the new tokens: the K and V rows at positions seq_lens[b] + path[b][j] go to seq_lens[b] + j, for
  * j < n_accept[b], and new_lens[b] = seq_lens[b] + n_accept[b].
  *   path      dev int32 [B][max_path], ascending (a token's ancestors come before it): the accepted tokens' numbers
- *   n_accept  dev int32 [B]  how many of the row count (clamped to [0, max_path])
+ *   n_accept  dev int32 [B]  how many of the row count (clamped to [0, max_path]); tokens whose tok_slot was -1 are not among them
  *   new_lens  dev int32 [B] (out): seq_lens itself, an array that does not overlap it, or NULL (in all but the last layer, say)
  * A path ends early where it does not ascend from 0 on or leaves the block-table row (HG_DEV_RANGE), or where a page is
  * missing (HG_DEV_BAD_PAGE); new_lens counts what was kept.  Pages that other rows use too are written like any (hg_kv_reserve

@@ -201,6 +201,8 @@ def lib():
         L.hg_kv_copy_pages.restype = C.c_int
         L.hg_kv_slots.argtypes = [vp] * 3 + [i32] + [vp] * 5 + [i32, vp, C.POINTER(HgAttnDesc)]
         L.hg_kv_slots.restype = C.c_int
+        L.hg_kv_slots_ready.argtypes = [vp] * 4 + [i32] + [vp] * 5 + [i32, vp, C.POINTER(HgAttnDesc)]
+        L.hg_kv_slots_ready.restype = C.c_int
         L.hg_rope.argtypes = [vp] * 3 + [i32] * 3 + [vp, C.POINTER(HgRopeDesc)]
         L.hg_rope.restype = C.c_int
         L.hg_kv_append_rope.argtypes = [vp] * 9 + [C.POINTER(HgAttnDesc), C.POINTER(HgRopeDesc)]
@@ -713,7 +715,7 @@ def _rows(t: Optional[torch.Tensor], name: str, desc_dtype: int, heads: int, hea
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0
 
 
-def _kv_slots_args(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, num_rows, desc: HgAttnDesc, stream):
+def _kv_slots_args(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, num_rows, desc: HgAttnDesc, stream, n_ready):
     B = desc.batch
     outputs = [t for t in (tok_seq, tok_pos, tok_slot, mask) if t is not None]
     if num_rows is None:
@@ -724,26 +726,27 @@ def _kv_slots_args(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, 
         raise ValueError(f"{num_rows} rows, a call takes 2^31 - 1")
     words = 0 if mask is None else mask.shape[1]
     return (_here(seq_lens, "seq_lens", torch.int32, B), _here(n_new, "n_new", torch.int32, B),
-            _here(parent, "parent", torch.int32, num_rows), num_rows, _here(cu_new, "cu_new", torch.int32, B + 1),
+            _here(n_ready, "n_ready", torch.int32, B), _here(parent, "parent", torch.int32, num_rows), num_rows, _here(cu_new, "cu_new", torch.int32, B + 1),
             _here(tok_seq, "tok_seq", torch.int32, num_rows), _here(tok_pos, "tok_pos", torch.int32, num_rows),
             _here(tok_slot, "tok_slot", torch.int64, num_rows), _here(mask, "mask", torch.int32, num_rows * words), words,
             _stream(stream), C.byref(desc))
 
 
 def hg_kv_slots(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, desc: HgAttnDesc, num_rows: Optional[int] = None,
-                stream=None) -> None:
+                stream=None, n_ready=None) -> None:
     """Rows, positions, places in the pool and masks of a step's new tokens, n_new[b] (None: one) of each sequence; ``parent``
-    (packed, None: chains) makes trees of them.  ``mask`` is int32 [N][words] (bits); rows behind the last token get -1 and 0."""
-    _check(lib().hg_kv_slots(*_kv_slots_args(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, num_rows, desc, stream)),
-           "hg_kv_slots")
+    (packed by n_new, None: chains) makes trees of them.  ``mask`` is int32 [N][words] (bits); rows behind the last token get -1 and 0.
+    ``n_ready`` (``hg_kv_reserve``'s): tokens from n_ready[b] on keep their rows, but get no place (``hg_kv_slots_ready``)."""
+    _check(lib().hg_kv_slots_ready(*_kv_slots_args(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, num_rows, desc, stream,
+                                                   n_ready)), "hg_kv_slots")
 
 
 def prepare_kv_slots(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, desc: HgAttnDesc, num_rows: Optional[int] = None,
-                     stream=None):
+                     stream=None, n_ready=None):
     """``hg_kv_slots`` with its arguments marshalled once (see ``prepare_partial``)."""
-    return _prepared(lib().hg_kv_slots,
-                     _kv_slots_args(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, num_rows, desc, stream),
-                     (seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, desc), "hg_kv_slots")
+    return _prepared(lib().hg_kv_slots_ready,
+                     _kv_slots_args(seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, num_rows, desc, stream, n_ready),
+                     (seq_lens, n_new, parent, cu_new, tok_seq, tok_pos, tok_slot, mask, n_ready, desc), "hg_kv_slots")
 
 
 _ROPE_LAYOUTS = {"half": HG_ROPE_HALF, "interleaved": HG_ROPE_INTERLEAVED}

@@ -76,6 +76,12 @@ extern "C" {
 hg_status hg_kv_slots(const int32_t* seq_lens, const int32_t* n_new, const int32_t* parent, int32_t num_rows, int32_t* cu_new,
                       int32_t* tok_seq, int32_t* tok_pos, int64_t* tok_slot, uint32_t* mask, int32_t mask_words, void* stream,
                       const hg_attn_desc* desc) {
+    return hg_kv_slots_ready(seq_lens, n_new, nullptr, parent, num_rows, cu_new, tok_seq, tok_pos, tok_slot, mask, mask_words, stream, desc);
+}
+
+hg_status hg_kv_slots_ready(const int32_t* seq_lens, const int32_t* n_new, const int32_t* n_ready, const int32_t* parent, int32_t num_rows,
+                            int32_t* cu_new, int32_t* tok_seq, int32_t* tok_pos, int64_t* tok_slot, uint32_t* mask, int32_t mask_words,
+                            void* stream, const hg_attn_desc* desc) {
     hg_status st = check_pool(desc);
     if (st != HG_OK) return st;
     if (!seq_lens || !cu_new || num_rows < 1 || (mask && mask_words < 1)) return HG_ERR_INVALID_ARG;
@@ -84,17 +90,18 @@ hg_status hg_kv_slots(const int32_t* seq_lens, const int32_t* n_new, const int32
     const size_t N = (size_t)num_rows, B = (size_t)desc->batch;
     const void* const out[5] = {cu_new, tok_seq, tok_pos, tok_slot, mask};
     const size_t out_bytes[5] = {(B + 1) * 4, N * 4, N * 4, N * 8, mask ? N * mask_words * 4 : 0};
-    const void* const in[4] = {seq_lens, n_new, parent, desc->block_table};
-    const size_t in_bytes[4] = {B * 4, B * 4, N * 4, B * desc->max_pages * 4};
+    const void* const in[5] = {seq_lens, n_new, n_ready, parent, desc->block_table};
+    const size_t in_bytes[5] = {B * 4, B * 4, B * 4, N * 4, B * desc->max_pages * 4};
     for (int i = 0; i < 5; ++i) {
         for (int j = 0; j < i; ++j) if (overlap(out[i], out_bytes[i], out[j], out_bytes[j])) return HG_ERR_INVALID_ARG;
-        for (int j = 0; j < 4; ++j) if (overlap(out[i], out_bytes[i], in[j], in_bytes[j])) return HG_ERR_INVALID_ARG;
+        for (int j = 0; j < 5; ++j) if (overlap(out[i], out_bytes[i], in[j], in_bytes[j])) return HG_ERR_INVALID_ARG;
     }
     SlotsParams p;
-    p.seq_lens = seq_lens; p.n_new = n_new; p.parent = parent; p.table = desc->block_table;
+    p.seq_lens = seq_lens; p.n_new = n_new; p.n_ready = n_ready; p.parent = parent; p.table = desc->block_table;
     p.cu = cu_new; p.seq = tok_seq; p.pos = tok_pos; p.slot = tok_slot; p.mask = mask; p.status = desc->status;
     p.B = desc->batch; p.N = num_rows; p.words = mask ? mask_words : 0;
-    p.cut = !parent && !mask ? 0x7fffffff : mask && mask_words * 32 < HG_MAX_TREE_NODES ? mask_words * 32 : HG_MAX_TREE_NODES;
+    p.limit = !parent && !mask ? 0x7fffffff : mask && mask_words * 32 < HG_MAX_TREE_NODES ? mask_words * 32 : HG_MAX_TREE_NODES;
+    p.cut = n_ready ? 0x7fffffff : p.limit;            // (with n_ready no sequence loses a row, and nothing behind it moves)
     p.page_shift = ilog2_exact(desc->page_size); p.max_pages = desc->max_pages; p.num_pages = desc->num_pages;
     if (desc->batch <= SLOTS_SCAN) {
         const bool quads = !parent && !mask && aligned16(tok_seq) && aligned16(tok_pos) && aligned16(tok_slot);

@@ -28,6 +28,7 @@ constexpr int SLOTS_SCAN = 2048;           // sequences that every CTA can scan
 struct SlotsParams {
     const int32_t* seq_lens;
     const int32_t* n_new;            // or NULL: one each
+    const int32_t* n_ready;          // or NULL: all of them
     const int32_t* parent;           // packed, or NULL: chains
     const int32_t* table;            // or NULL: identity paging
     int32_t* cu;
@@ -36,7 +37,8 @@ struct SlotsParams {
     int64_t* slot;
     uint32_t* mask;
     int32_t* status;
-    int B, N, words, cut;            // cut: the most tokens of a sequence
+    int B, N, words;
+    int cut, limit;                  // the most rows of a sequence; with n_ready, the most tokens that have a place
     int per;                         // sequences per CTA
     int page_shift, max_pages, num_pages;
 };
@@ -81,13 +83,19 @@ __device__ __forceinline__ int slots_ancestors(const SlotsParams& p, int first, 
     return depth;
 }
 
+// A token from the sequence's n_ready on (or behind the mask's bits) keeps its row, but has no place and no bits.
+__device__ __forceinline__ bool slots_unready(const SlotsParams& p, int b, int i) { return p.n_ready && i >= min(p.n_ready[b], p.limit); }
+
 // What a row gets: token i of sequence b, whose rows begin at `first` and whose cache has `len` tokens; `entry`: the block-table
 // entry of its page, -1 where the table ends.
 __device__ __forceinline__ void slots_row(const SlotsParams& p, int r, int b, int first, int len, int entry, int& trouble) {
     const int i = r - first;
     int depth = i;
     uint32_t* const bits = p.mask ? p.mask + (size_t)r * p.words : nullptr;
-    if (p.parent) depth = slots_ancestors(p, first, i, bits, trouble);
+    if (slots_unready(p, b, i)) {
+        depth = 0;
+        if (bits) for (int w = 0; w < p.words; ++w) bits[w] = 0;
+    } else if (p.parent) depth = slots_ancestors(p, first, i, bits, trouble);
     else if (bits)
         for (int w = 0; w < p.words; ++w) {
             const int last = i - w * 32;
@@ -101,8 +109,10 @@ __device__ __forceinline__ void slots_row(const SlotsParams& p, int r, int b, in
         p.slot[r] = entry < 0 ? -1ll : ((long long)entry << p.page_shift) + in_page;
     }
 }
-__device__ __forceinline__ int slots_entry(const SlotsParams& p, int b, long long t, int& trouble) {
-    const long long page = t >> p.page_shift;
+// Block-table entry of token i of a sequence with len cached ones; -1: none, -2: not in the pool.
+__device__ __forceinline__ int slots_entry(const SlotsParams& p, int b, int len, int i, int& trouble) {
+    if (slots_unready(p, b, i)) return -1;
+    const long long page = ((long long)len + i) >> p.page_shift;
     if (page >= p.max_pages) { trouble |= HG_DEV_RANGE; return -1; }
     const long long e = (long long)b * p.max_pages + page;
     const int entry = p.table ? p.table[e] : (int)e;
@@ -143,7 +153,7 @@ __global__ void __launch_bounds__(SLOTS_THREADS) kv_slots_kernel(SlotsParams p) 
         const int asked = start[b];
         const unsigned next = min(upto + (unsigned)min(asked, p.cut), N);
         start[b] = (int)upto;
-        if (next - upto < (unsigned)asked && blockIdx.x == 0) trouble |= HG_DEV_RANGE;
+        if ((next - upto < (unsigned)asked || asked > p.limit) && blockIdx.x == 0) trouble |= HG_DEV_RANGE;
         upto = next;
         if (b == p.B - 1) start[p.B] = (int)next;
     }
@@ -169,8 +179,8 @@ __global__ void __launch_bounds__(SLOTS_THREADS) kv_slots_kernel(SlotsParams p) 
                 const int r = (int)r0 + u;
                 while (start[k + 1] <= r) ++k;
                 seq[u] = k;
-                pos[u] = cached[k] + (r - start[k]);
-                if (p.slot) entry[u] = slots_entry(p, k, (long long)cached[k] + (r - start[k]), trouble);
+                pos[u] = cached[k] + (slots_unready(p, k, r - start[k]) ? 0 : r - start[k]);
+                if (p.slot) entry[u] = slots_entry(p, k, cached[k], r - start[k], trouble);
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
@@ -192,7 +202,7 @@ __global__ void __launch_bounds__(SLOTS_THREADS) kv_slots_kernel(SlotsParams p) 
                     if (p.slot) p.slot[r0 + u] = u == 0 ? slot[0] : u == 1 ? slot[1] : slot[2];
                 }
         } else if (r0 < total) {
-            const int r = (int)r0, entry = p.slot ? slots_entry(p, k, (long long)cached[k] + (r - start[k]), trouble) : -1;
+            const int r = (int)r0, entry = p.slot ? slots_entry(p, k, cached[k], r - start[k], trouble) : -1;
             slots_row(p, r, k, start[k], cached[k], entry, trouble);
         } else {                                                   // behind the last token
             if (p.seq) p.seq[r0] = -1;
@@ -246,7 +256,7 @@ __global__ void __launch_bounds__(SLOTS_THREADS) kv_slots_many_kernel(SlotsParam
         if (mine && blockIdx.y == 0) {
             p.cu[b] = lo;
             if (b == p.B - 1) p.cu[p.B] = hi;
-            if (hi - lo < asked) trouble |= HG_DEV_RANGE;
+            if (hi - lo < asked || asked > p.limit) trouble |= HG_DEV_RANGE;
         }
         __syncthreads();
         const int n_seqs = min(SLOTS_THREADS, s1 - q0);
@@ -257,7 +267,7 @@ __global__ void __launch_bounds__(SLOTS_THREADS) kv_slots_many_kernel(SlotsParam
                 const int mid = (k + above) >> 1;
                 if (first_row[mid] <= r) k = mid; else above = mid;
             }
-            const int entry = p.slot ? slots_entry(p, q0 + k, (long long)length[k] + (r - first_row[k]), trouble) : -1;
+            const int entry = p.slot ? slots_entry(p, q0 + k, length[k], r - first_row[k], trouble) : -1;
             slots_row(p, r, q0 + k, first_row[k], length[k], entry, trouble);
         }
     }

@@ -120,6 +120,25 @@ def test_slots_refuse_bad_arguments(lib):
     assert call(d=tabled(), pos=tabled().block_table) == INVALID
 
 
+def test_slots_with_ready_counts_refuse_bad_arguments(lib):
+    far = [FAKE + (i << 24) for i in range(9)]
+    names = ("lens", "n_new", "parent", "cu", "seq", "pos", "slot", "mask", "ready")
+
+    def call(d=None, rows=100, words=2, **over):
+        a = dict(zip(names, far))
+        a.update(over)
+        d = d or good_desc()
+        return lib.hg_kv_slots_ready(a["lens"], a["n_new"], a["ready"], a["parent"], rows, a["cu"], a["seq"], a["pos"], a["slot"], a["mask"],
+                                     words, None, C.byref(d))
+
+    assert call(lens=None) == INVALID and call(cu=None) == INVALID and call(rows=0) == INVALID and call(words=0) == INVALID
+    assert call(words=33) == UNSUPPORTED and call(slot=far[6] + 4) == INVALID and call(d=good_desc(page_size=24)) == UNSUPPORTED
+    # outputs in the counts' place
+    for name in ("cu", "seq", "pos", "slot", "mask"):
+        assert call(**{name: far[8]}) == INVALID, name
+    assert call(cu=far[8] + 4) == INVALID and call(d=tabled(), pos=tabled().block_table) == INVALID
+
+
 def test_rope_refuses_bad_arguments(lib):
     far = [FAKE + (i << 24) for i in range(4)]
 

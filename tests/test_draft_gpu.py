@@ -138,6 +138,78 @@ def test_slots_past_the_end_of_the_table():
     assert slot.tolist() == [-1] * 8
 
 
+def ready_plain(lens, n_new, n_ready, parent, N, table, P, num_pages, words):
+    """Row by row: packed by n_new, tokens without a place among them"""
+    limit = 1 << 31 if parent is None and not words else min(1024, 32 * words if words else 1024)
+    rows, cu, status = [], [0], 0
+    for b, n in enumerate(n_new):
+        first, L, sees = len(rows), max(lens[b], 0), []
+        if max(n, 0) > limit:
+            status |= hg.HG_DEV_RANGE
+        for i in range(max(n, 0)):
+            if len(rows) == N:
+                status |= hg.HG_DEV_RANGE
+                break
+            if i >= min(n_ready[b], limit):
+                rows.append((b, L, -1, [0] * words))
+                continue
+            p = i - 1 if parent is None else parent[first + i]
+            sees.append(([] if p < 0 else sees[p]) + [i])
+            e, t = -1, L + i
+            if t // P >= len(table[b]):
+                status |= hg.HG_DEV_RANGE
+            else:
+                e = table[b][t // P]
+            word = [sum(1 << j % 32 for j in sees[i] if j // 32 == w) for w in range(words)]
+            rows.append((b, L + len(sees[i]) - 1, -1 if e < 0 else e * P + t % P, [w - (1 << 32) if w >> 31 else w for w in word]))
+        cu.append(len(rows))
+    rows += [(-1, 0, -1, [0] * words)] * (N - len(rows))
+    return [cu] + [list(x) for x in zip(*rows)] + [status]
+
+
+@pytest.mark.parametrize("n_new,n_ready,words,N", [
+    ([5, 9, 3, 0, 7], [5, 4, 3, 0, 7], 1, 30), ([5, 9, 3, 0, 7], [0, 9, -2, 5, 3], 1, 24), ([5, 9, 3, 0, 7], [5, 9, 2, 0, 100], 1, 20),
+    ([40, 6, 33, 2], [40, 6, 33, 2], 1, 90), ([40, 6, 70, 2], [36, 6, 10, 0], 2, 118), ([1100, 8, 1030], [1100, 7, 1026], 32, 2200),
+    ([600, 1, 0, 900], [17, 1, 0, 899], 0, 1502), ([3] * 2500, [3, 1, 0, 2, 3] * 500, 1, 7510), ([50] + [2] * 2400, [50] + [1, 2] * 1200, 1, 4850)])
+@pytest.mark.parametrize("trees", [False, True])
+def test_slots_of_tokens_that_got_no_page(n_new, n_ready, words, N, trees):
+    """No row moves: with a mask and parents, without either (four rows a thread), in batches over and under 2048, and behind a
+    sequence with more tokens than mask bits"""
+    r = np.random.RandomState(len(n_new))
+    P, B, lens = 16, len(n_new), [int(x) for x in r.randint(0, 90, len(n_new))]
+    parent = random_parents(n_new, r) if trees else None
+    S = max(-(-(t + n) // P) for t, n in zip(lens, n_new))
+    num_pages = B * S + 1
+    table = r.permutation(num_pages)[:B * S].reshape(B, S).astype(np.int32)
+    cu, seq, pos = [torch.full((m,), 99, dtype=torch.int32, device=DEV) for m in (B + 1, N, N)]
+    slot, status = torch.full((N,), 99, dtype=torch.int64, device=DEV), ints([0])
+    mask = torch.full((N, words), 99, dtype=torch.int32, device=DEV) if words else None
+    par = ints((parent + [-1] * N)[:max(N, len(parent))]) if trees else None
+    hg.hg_kv_slots(ints(lens), ints(n_new), par, cu, seq, pos, slot, mask, pool_desc(torch.from_numpy(table).to(DEV), P, num_pages, status=status),
+                   n_ready=ints(n_ready))
+    torch.cuda.synchronize()
+    want = ready_plain(lens, n_new, n_ready, parent, N, table.tolist(), P, num_pages, words)
+    got = [x.tolist() for x in (cu, seq, pos, slot)] + [mask.tolist() if words else [[]] * N, int(status)]
+    for name, a, b in zip(("cu", "seq", "pos", "slot", "mask", "status"), got, want):
+        assert a == b, name
+
+
+def test_ready_counts_of_all_tokens_change_nothing():
+    lens, n = [5, 0, 31, 16], [7, 0, 20, 32]
+    r = np.random.RandomState(0)
+    parent, table = ints(random_parents(n, r) + [-1] * 3), ints(r.permutation(16).reshape(4, 4).tolist())
+    results = []
+    for ready in (None, ints(n), ints([99] * 4)):
+        cu, seq, pos = ints([0] * 5), ints([0] * 62), ints([0] * 62)
+        slot, mask = ints([0] * 62, torch.int64), torch.zeros((62, 1), dtype=torch.int32, device=DEV)
+        pkg.prepare_kv_slots(ints(lens), ints(n), parent, cu, seq, pos, slot, mask, pool_desc(table, 16, 16), n_ready=ready)()
+        torch.cuda.synchronize()
+        results.append((cu, seq, pos, slot, mask))
+    for other in results[1:]:
+        for a, b in zip(results[0], other):
+            assert torch.equal(a, b)
+
+
 def test_slots_with_identity_paging_and_without_outputs():
     cu, slot = ints([0] * 3), ints([0] * 5, torch.int64)
     desc = hg.attn_desc(batch=2, num_q_heads=1, num_kv_heads=1, head_dim=64, dtype=F16, page_size=16, num_pages=8, page_stride=1024, head_stride=1024,
@@ -477,3 +549,70 @@ def test_steps_of_speculative_decoding():
                 page = int(table[b, t // P])
                 assert torch.equal(pools[x][1][page, :, t % P].double(), vv)
                 assert near(pools[x][0][page, :, t % P], kk, kk.abs().max() * 1.5)
+
+
+@pytest.mark.parametrize("trees", [True, False])
+def test_a_step_whose_pool_runs_out_of_pages(trees):
+    """The second of three sequences gets one page of the three that it asked for, the third one of its own none, beside one that it
+    shares.  Every token that got a place has the result of the same step in a large pool, bit for bit, its keys and values
+    lie where they belong, and no other page changes."""
+    Hq, Hkv, D, P, S = 8, 2, 64, 16, 8
+    lens, n = [20, 16, 9], [5, 40, 10]
+    r = np.random.RandomState(2)
+    par = random_parents(n, r) if trees else [i - 1 for m in n for i in range(m)]
+    N, cu_want = sum(n) + 2, [0, 5, 45, 55]
+    rows = torch.randn((N, Hq + 2 * Hkv, D), device=DEV).half()
+    history = torch.randn((2, 3, Hkv, 32, D), device=DEV).half()
+    freq, _ = freqs(D)
+    rope = hg.rope_desc(rot_dim=D, freq=freq)
+    outs = []
+    for pages in (20, 6):
+        # pages 0 .. 4 hold the caches; sequence 2's only page is held by somebody else too
+        table = torch.full((3, S), -1, dtype=torch.int32, device=DEV)
+        table[0, :2], table[1, 0], table[2, 0] = ints([4, 1]), 3, 0
+        ref = ints([2, 1, 1, 1, 1] + [0] * (pages - 5))
+        pool = torch.full((2, pages, Hkv, P, D), 7.0, device=DEV).half()
+        for b, L in enumerate(lens):
+            for t in range(L):
+                pool[:, int(table[b, t // P]), :, t % P] = history[:, b, :, t]
+        before, status = pool.clone(), ints([0])
+        desc = pool_desc(table, P, pages, Hq, Hkv, D, F16, status)
+        seq_lens, n_new = ints(lens), ints(n)
+        copies, ready = [ints([-1] * 3) for _ in range(3)], ints([0] * 3)
+        cu, seq, pos = ints([0] * 4), ints([0] * N), ints([0] * N)
+        slot, mask = ints([0] * N, torch.int64), torch.zeros((N, 2), dtype=torch.int32, device=DEV)
+        parent = ints(par + [-1] * 2) if trees else None
+        hg.hg_kv_reserve(seq_lens, n_new, ref, *copies, ready, desc)
+        hg.hg_kv_copy_pages(copies[0], copies[1], copies[2], None, pool[0], pool[1], desc)
+        torch.cuda.synchronize()
+        counts, short = ready.tolist(), pages == 6
+        assert counts == ([5, 16, 0] if short else n) and bool(int(status) & hg.HG_DEV_NO_PAGE) == short
+        hg.hg_kv_slots(seq_lens, n_new, parent, cu, seq, pos, slot, mask if trees else None, desc, n_ready=ready)
+        q, k, v = rows.split([Hq, Hkv, Hkv], 1)
+        turned, out, lse = [torch.zeros((N, Hq, D), device=DEV).half() for _ in range(2)] + [torch.zeros((N, Hq), device=DEV)]
+        tree = hg.tree_desc(cu_nodes=cu, mask=mask if trees else None, num_rows=N, max_nodes=40)
+        ws = torch.empty(hg.hg_attn_tree_workspace_bytes(desc, tree), dtype=torch.uint8, device=DEV)
+        hg.hg_kv_append_rope(q, k, v, pos, slot, turned, pool[0], pool[1], desc, rope)
+        hg.hg_attn_decode_tree(turned, pool[0], pool[1], seq_lens, None, [], out, lse, ws, desc, tree)
+        torch.cuda.synchronize()
+        assert cu.tolist() == cu_want and int(status) & hg.HG_DEV_RANGE == 0
+        placed = [cu_want[b] + i for b in range(3) for i in range(counts[b])]
+        assert [x for x in range(N) if int(slot[x]) >= 0] == placed
+        changed = torch.zeros(pages, P, dtype=torch.bool)
+        for b in range(3):
+            for i in range(counts[b]):
+                page, row = int(table[b, (lens[b] + i) // P]), (lens[b] + i) % P
+                changed[page, row] = True
+                assert torch.equal(pool[1][page, :, row], v[cu_want[b] + i])
+        if short:
+            same = ~changed.to(DEV)
+            assert torch.equal(pool.transpose(2, 3)[:, same], before.transpose(2, 3)[:, same])
+        # a chain of accepted tokens where that is possible: nothing but what was placed
+        path = ints([list(range(40))] * 3)
+        hg.hg_kv_accept(path, torch.minimum(ready, ints([3, 30, 2])), seq_lens, seq_lens, pool[0], pool[1], desc)
+        torch.cuda.synchronize()
+        assert seq_lens.tolist() == [a + min(c, m) for a, c, m in zip(lens, counts, (3, 30, 2))]
+        outs.append((placed, out, lse, turned))
+    placed = outs[1][0]
+    for a, b in zip(outs[0][1:], outs[1][1:]):
+        assert torch.equal(a[placed], b[placed])
