@@ -410,6 +410,37 @@ def test_ranges_outside_are_cut():
         s.status.zero_()
 
 
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (8, 1)])                          # 32 and 64 rows a KV head
+@pytest.mark.parametrize("lens", [[76, -5], [80, 3], [100, 24]])
+def test_results_of_what_is_cut(Hq, Hkv, lens):
+    """Rows of the block table end at position 80: what lies behind is left out, whole rows that do not fit are left alone"""
+    s = Step([72, 72], [8, 8], kind="chain", P=16, Hq=Hq, Hkv=Hkv)
+    for x in (s.k, s.v):
+        x.nan_to_num_(0.5, 0.5, 0.5)
+    s.seq_lens, s.lens = ints(lens), [max(t, 0) for t in lens]
+    narrow = s.table
+    s.table = torch.cat([narrow, narrow], 1)                                # (any page behind the end: what it holds is dropped)
+    drop = [(b, t) for b in range(2) for t in range(80, s.lens[b] + 8)]
+    out, lse, off = s.exact(drop)
+    s.table = narrow
+    for cu, rows in ([0, 8, 16], range(16)), ([0, 8, 500], range(16)), ([-3, 8, 16], range(8, 16)), ([0, 9, 9], range(8)), ([3, 11, 11], range(3, 11)):
+        s.out.fill_(-77)
+        s.lse.fill_(-77)
+        s.status.zero_()
+        s.tree = hg.tree_desc(cu_nodes=ints(cu), num_rows=s.N, max_nodes=8)
+        s.call()
+        torch.cuda.synchronize()
+        rows = list(rows)
+        others = [r for r in range(s.N) if r not in rows]
+        assert (s.out[others] == -77).all() and (s.lse[others] == -77).all()
+        assert int(s.status) == hg.HG_DEV_RANGE                             # (sequence 0 passes the end, or cu is cut)
+        if cu[0] == 3:                                                      # other queries: only that they are results
+            assert torch.isfinite(s.out[rows]).all() and (s.lse[rows] != -77).all()
+            continue
+        assert float(((s.out[rows].double() - out[rows]).abs() / off[rows]).max()) <= 1
+        assert float((s.lse[rows].double() - lse[rows]).abs().max()) <= LOGIT
+
+
 def test_no_tokens_at_all():
     s = Step([10, 20], [0, 0], pad=4, max_nodes=5)
     s.check()
