@@ -867,10 +867,11 @@ def _decode_tree_args(q, k_cache, v_cache, seq_lens, tok_begin, partials, out, l
     pq, sq = _rows(q, "q", desc.dtype, desc.num_q_heads, desc.head_dim, N)
     if _DTYPES.get(out.dtype) != desc.dtype:
         raise ValueError(f"out has another type than the description: {out.dtype}")
-    for o, m, _ in partials:
+    for o, m, l in partials:
         if m.numel() < N * desc.num_q_heads * m.shape[-1] or o.shape[-1] != desc.head_dim:
             raise ValueError("partial source shapes must be o [N][Hq][nc][D], m and l [N][Hq][nc]")
-        _here(o, "partial o")
+        for name, t in (("o", o), ("m", m), ("l", l)):
+            _here(t, f"partial {name}")
     arr = _src_array(partials, host=False)
     d = HgTreeDesc.from_buffer_copy(tree)
     d.q_stride = sq

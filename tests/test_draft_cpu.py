@@ -4,6 +4,7 @@ import math
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2604_18529_b200 as pkg
 from paper_2604_18529_b200 import binding as hg
@@ -99,6 +100,38 @@ def test_tree_attention_refuses_what_it_cannot_run(lib):
         setattr(src[1], name, bad)
         assert decode(lib, d, x, src, 2) == INVALID, name
         setattr(src[1], name, was)
+
+
+class OnDevice:
+    """What the binding looks at of a CUDA tensor, on a device of the test's choice"""
+
+    def __init__(self, shape, dtype, device=0):
+        self.shape, self.dtype, self.device, self.is_cuda = torch.Size(shape), dtype, torch.device("cuda", device), True
+
+    numel = lambda self: math.prod(self.shape)
+    dim = lambda self: len(self.shape)
+    stride = lambda self, i=None: torch.empty(self.shape, device="meta").stride(i) if i is not None else torch.empty(self.shape, device="meta").stride()
+    is_contiguous = lambda self: True
+    data_ptr = lambda self: FAKE
+    element_size = lambda self: self.dtype.itemsize
+
+
+@pytest.mark.parametrize("which", ["q", "k", "v", "lens", "begin", "o", "m", "l", "out", "lse", "ws", "cu", "mask"])
+def test_tree_attention_refuses_tensors_of_another_device(lib, monkeypatch, which):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    f16, f32, i32, N, d = torch.float16, torch.float32, torch.int32, 64, good_desc()
+    shapes = dict(q=((N, 8, 128), f16), k=((64, 2, 16, 128), f16), v=((64, 2, 16, 128), f16), lens=((2,), i32), begin=((2,), i32),
+                  o=((N, 8, 1, 128), f32), m=((N, 8, 1), f32), l=((N, 8, 1), f32), out=((N, 8, 128), f16), lse=((N, 8), f32),
+                  ws=((1 << 26,), torch.uint8), cu=((3,), i32), mask=((N, 2), i32))
+
+    def marshal(away):
+        t = {n: OnDevice(*x, device=int(n == away)) for n, x in shapes.items()}
+        x = hg.tree_desc(cu_nodes=t["cu"], mask=t["mask"], num_rows=N, max_nodes=40)
+        return hg._decode_tree_args(t["q"], t["k"], t["v"], t["lens"], t["begin"], [(t["o"], t["m"], t["l"])], t["out"], t["lse"], t["ws"], d, x, 0)
+
+    marshal(None)
+    with pytest.raises(ValueError, match="cuda:1"):
+        marshal(which)
 
 
 def test_slots_refuse_bad_arguments(lib):
