@@ -107,14 +107,17 @@ hg_status hg_kv_slots_ready(const int32_t* seq_lens, const int32_t* n_new, const
         const bool quads = !parent && !mask && aligned16(tok_seq) && aligned16(tok_pos) && aligned16(tok_slot);
         const long long per_cta = SLOTS_THREADS * (quads ? 4 : 1), ctas = ((long long)num_rows + per_cta - 1) / per_cta;
         const dim3 grid((unsigned)(ctas < 888 ? ctas : 888));      // (what 148 SMs hold at a time)
-        return quads ? launch_draft(kv_slots_kernel<true>, grid, SLOTS_THREADS, 0, stream, p)
-                     : launch_draft(kv_slots_kernel<false>, grid, SLOTS_THREADS, 0, stream, p);
+        if (n_ready) return quads ? launch_draft(kv_slots_kernel<true, true>, grid, SLOTS_THREADS, 0, stream, p)
+                                  : launch_draft(kv_slots_kernel<false, true>, grid, SLOTS_THREADS, 0, stream, p);
+        return quads ? launch_draft(kv_slots_kernel<true, false>, grid, SLOTS_THREADS, 0, stream, p)
+                     : launch_draft(kv_slots_kernel<false, false>, grid, SLOTS_THREADS, 0, stream, p);
     }
     // ranges of sequences, and splits of their rows
     const int ranges = desc->batch < 592 ? desc->batch : 592;
     p.per = (desc->batch + ranges - 1) / ranges;
     const long long per_range = ((long long)num_rows + ranges - 1) / ranges, splits = (per_range + 511) / 512, most = 1184 / ranges;
-    return launch_draft(kv_slots_many_kernel, dim3((unsigned)ranges, (unsigned)(splits < most ? splits : most)), SLOTS_THREADS, 0, stream, p);
+    return launch_draft(n_ready ? kv_slots_many_kernel<true> : kv_slots_many_kernel<false>, dim3((unsigned)ranges, (unsigned)(splits < most ? splits : most)),
+                        SLOTS_THREADS, 0, stream, p);
 }
 
 hg_status hg_rope(const void* x, void* y, const int32_t* pos, int32_t num_heads, int32_t head_dim, int32_t dtype, void* stream,
