@@ -541,7 +541,8 @@ hg_status hg_kv_copy_pages(const int32_t* src, const int32_t* dst, const int32_t
 /*
  * Several new tokens of a sequence in one step: drafted tokens that the model verifies together (a chain or a tree of
  * alternatives behind the cache), prompts, or single tokens beside either.  The paper decodes one token a step; these
- * operators are one step over any number of them, in the order of their use:
+ * operators are one step over several, up to HG_MAX_TREE_NODES a sequence in hg_attn_decode_tree (a longer prompt goes in
+ * pieces, a step each), in the order of their use:
  *     hg_kv_reserve        pages for the new tokens
  *     hg_kv_slots_ready    which row of the packed tensors is which token, its position and its place in the pool, masks
  *     hg_kv_append_rope    (each layer) rotary positions; keys and values to their places
@@ -551,7 +552,7 @@ hg_status hg_kv_copy_pages(const int32_t* src, const int32_t* dst, const int32_t
  * the row cu[b] + i.  Token i lies at position seq_lens[b] + i of the block-table row, whatever its depth in a tree;
  * seq_lens counts the cached tokens only and grows in hg_kv_accept.
  */
-#define HG_MAX_TREE_NODES 1024 /* new tokens of a sequence that may have a mask */
+#define HG_MAX_TREE_NODES 1024 /* new tokens of a sequence that may have a mask, and that a call of hg_attn_decode_tree takes */
 
 /*
  * Rows, positions, places and masks of a step's new tokens.
@@ -681,7 +682,8 @@ typedef struct hg_tree_desc {
 /*
  * One step's attention for the new tokens of every sequence, each over the cached tokens [tok_begin, seq_len) and over those
  * of the sequence's new tokens that its mask shows, whose keys and values are in the pool already; joined with n_host_src (at
- * most HG_MAX_MERGE_SRC) sources of partials for tokens that the host holds.  (The paper's step has one new token per sequence
+ * most HG_MAX_MERGE_SRC) sources of partials for tokens that the host holds, one row per new token (the host's own operators
+ * take one query a sequence: the caller runs them for each and packs the rows).  (The paper's step has one new token per sequence
  * and needs no mask.)  The result is softmax attention over all of them.
  *
  *   q          dev 16-bit [N][Hq][D], 16-byte aligned
@@ -709,7 +711,8 @@ hg_status hg_attn_decode_tree(const void* q, const void* k_cache, const void* v_
                               void* workspace, size_t workspace_bytes, void* stream, const hg_attn_desc* desc,
                               const hg_tree_desc* tree);
 
-/* Bytes of device workspace hg_attn_decode_tree needs; 0 for an invalid description. */
+/* Bytes of device workspace hg_attn_decode_tree needs (43 MB with 128 components, 22 with 64, whatever the batch); 0 for an invalid
+ * description. */
 size_t hg_attn_tree_workspace_bytes(const hg_attn_desc* desc, const hg_tree_desc* tree);
 
 /*

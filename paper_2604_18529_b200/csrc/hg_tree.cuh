@@ -30,15 +30,16 @@
 // whole tokens); 12-15 (few rows) finish the pieces while the softmax warps are at the next.  Every wait is bounded.
 //
 // The roles share the instruction cache, so what runs once a piece or less often is kept small (rolled loops, estimates in place of
-// 64-bit quotients, one place that clears V rows): 107 KB of code became 88 (few rows) and 134 became 107, and with them 128 sequences, 8 heads of 64, 2 new and
-// up to 1500 tokens went from 62 to 83 us, by the run, to a steady 59, and 60 sequences, 40 heads, up to 48 and 873 from 217 to 190.
+// 64-bit quotients, one place that clears V rows).  Code of 107 KB became 88 (few rows) and 134 became 107: 128 sequences, 8 heads of
+// 64, 2 new and up to 1500 tokens went from 62 to 83 us, by the run, to a steady 59; the last step, V rows cleared in one place, took
+// 60 sequences, 40 heads, up to 48 new and 873 tokens from 207 to 190.
 //
 // Measured (K and V larger than the L2), us, in a loop / the floor at the measured rates: one new token, 8 sequences, 64/8 heads,
-// 32 768 tokens: 169 / 167; the same with 64 components and twice the tokens: 166 / 167; 8 new tokens: 172 / 167, 16: 183 / 168
-// (many rows); 32 and 131 072 tokens, one sequence: 140 / 84 (bound by the exponentials and products of a pair of tiles, 3400
-// cycles where the products take 2048, at 1.55 GHz under the power cap).  Short units cost more than their bytes (first tile, masked
+// 32 768 tokens: 169 / 167; the same with 64 components and twice the tokens: 166 / 167; 8 new tokens: 173 / 167, 16: 179 to 182 / 168
+// (many rows); 32 and 131 072 tokens, one sequence: 133 to 163 / 84, by the power cap's clock (bound by the exponentials and products of
+// a pair of tiles, some 3400 cycles where the products take 2048).  Short units cost more than their bytes (first tile, masked
 // last tile, join, some 5000 cycles in all with many rows): 60 sequences, 40/40 heads, up to 873 tokens, up to 32, 48 and 200 new
-// ones: 162 / 85, 192 / 88 and 330 / 115.
+// ones: 162 / 85, 187 to 190 / 88 and 329 / 115.
 #pragma once
 
 #include <cuda_runtime.h>
